@@ -37,6 +37,7 @@ extern "C" {
 #define LC_ERR_TIMEOUT (-6)   /* a bounded device-side wait gave up */
 #define LC_ERR_CUDA (-7)      /* a CUDA runtime call failed */
 #define LC_ERR_RANGE (-8)     /* lc_compress_async: some |delta| >= 2, which needs the live state after it was released */
+#define LC_ERR_INDEX (-9)     /* a slot or page number names a place that the cache does not have */
 
 #define LC_MAX_CHAIN 8 /* most streams one lc_recover call applies */
 
@@ -345,6 +346,96 @@ int lc_recover_host(const float* base_host, const void* const* streams_host,
 #define LC_NOALLOC_MAX_N 4194304ull
 int lc_compress_noalloc(const float* base, const float* cur, uint64_t n, int nbits, void* stream,
                         uint64_t stream_capacity, lc_cuda_stream_t cs);
+
+/*
+ * State in few bits, to work with. What lc_recover gives back is a model's fp32 state; a program that serves it keeps the
+ * weights in 4 bits and what it remembers of its sequences (keys and values) in 8 or 4. Both are groups of 32, 64 or 128
+ * consecutive values, held as whole numbers with one scale for the group (docs/QUANT.md):
+ *   scale = bf16(max |w| / Q), Q = 7 (4 bits) or 127 (8 bits), rounded once to nearest even; 0 if below 2^-126
+ *   code  = the whole number nearest to w / scale, ties to even; 0 if the scale is 0
+ * and a code stands for code * scale, which fp32 holds exactly. The last group of a row may be shorter. A group with an Inf or
+ * a NaN has a scale of NaN: all of it reads as NaN.
+ * The calls below return without waiting; their buffers must not overlap except where that is said.
+ */
+#define LC_TYPE_F32 0
+#define LC_TYPE_BF16 1
+#define LC_TYPE_F16 2
+
+/*
+ * 4-bit weights. A matrix of rows x cols values, grouped along its rows, in one buffer of lc_q4_bytes (0 if rows or cols is 0,
+ * or an argument is out of range), DEVICE, 256-byte aligned, in the order in which lc_q4_matvec reads it (docs/QUANT.md, section 2).
+ * rows, cols, group   of every call: those the buffer was made with. rows < 2^31, cols < 2^31 - 128, and at most 2^32 groups.
+ * lc_q4_quantize: w   DEVICE, `type` LC_TYPE_*, row r at w + r * row_stride values, row_stride >= cols; aligned like its type.
+ *                     workspace as for lc_recover (lc_workspace_bytes(0)): an Inf or NaN sets LC_ERR_NONFINITE in its status word.
+ * lc_recover_q4:      lc_recover of a chain of streams of rows * cols < 2^32 elements (a layer's, see lc_compress_segments) into
+ *                     `scratch` (DEVICE, rows * cols fp32, 16-byte aligned; may be base), then lc_q4_quantize of that. Status
+ *                     word: the first error of the two; the weights mean nothing if it is set.
+ * lc_q4_read:         out[r, c] = code * scale, rounded to `type`; strides and alignment as for lc_q4_quantize.
+ */
+uint64_t lc_q4_bytes(uint64_t rows, uint64_t cols, int group);
+int lc_q4_quantize(const void* w, int type, uint64_t rows, uint64_t cols, uint64_t row_stride, int group, void* q4,
+                   uint64_t q4_bytes, void* workspace, uint64_t workspace_bytes, lc_cuda_stream_t cs);
+int lc_recover_q4(const float* base, const void* const* streams, const uint64_t* stream_bytes, int k, uint64_t rows,
+                  uint64_t cols, int group, void* q4, uint64_t q4_bytes, float* scratch, void* workspace,
+                  uint64_t workspace_bytes, lc_cuda_stream_t cs);
+int lc_q4_read(const void* q4, uint64_t q4_bytes, uint64_t rows, uint64_t cols, int group, void* out, int type,
+               uint64_t row_stride, lc_cuda_stream_t cs);
+
+/*
+ * Products with 4-bit weights, for the vectors of one or a few tokens:
+ *   out[t, r] = sum over the groups G of row r of scale[r, G] * (sum over c in G of code[r, c] * x[t, c]),
+ * sums in fp32, one rounding to the output's type. The weights are read once for up to 64 tokens (21 if x is fp32); more are
+ * taken in several parts. For long prompts lc_q4_read and a matrix product are the better way.
+ * x          DEVICE, `type` LC_TYPE_*, vector t at x + t * x_stride values, x_stride >= cols or 0 (one vector for all); aligned like
+ *            its type. All of its bits count, also in fp32 (but what lies below 2^-133). A group's sum is formed before its
+ *            scale is applied: it has to stay in fp32's range (|x| below 2^117 is always enough).
+ * out        DEVICE, `out_type` = type or LC_TYPE_F32, row t at out + t * out_stride, out_stride >= rows; aligned like its type.
+ * tokens     0 ... LC_Q4_MAX_TOKENS. With cols = 0 the products are 0.
+ * The same inputs give the same bits.
+ */
+#define LC_Q4_MAX_TOKENS 1048576u
+int lc_q4_matvec(const void* q4, uint64_t q4_bytes, uint64_t rows, uint64_t cols, int group, const void* x, int type,
+                 uint64_t tokens, uint64_t x_stride, void* out, int out_type, uint64_t out_stride, lc_cuda_stream_t cs);
+
+/*
+ * A cache of rows of heads x dim values, quantised as they are written, grouped along dim. It has `slots` places; with
+ * planes = 2 every place holds two rows, a key and a value. The memory is the caller's, laid out row by row (docs/QUANT.md,
+ * section 3): codes lc_cache_code_bytes, 16-byte aligned, scales (bf16) lc_cache_scale_bytes. What was never written reads as
+ * what its bytes say; zeroed scales read as zeros.
+ * bits 4 or 8; group 32, 64 or 128; 1 <= heads, dim <= 65536; slots < 2^40. The size functions return 0 on bad arguments.
+ *
+ * rows       of the call; rows * heads * groups per row of dim < 2^31.
+ * src, out   HOST array with an entry per plane: row i's head h at data + i * row_stride + h * head_stride values of `type`, dim
+ *            consecutive ones; DEVICE, aligned like its type, row_stride < 2^33, head_stride < 2^40. Rows of src may share memory, those of out must not (LC_ERR_ARG).
+ * slots      DEVICE, a slot for each row. -1: the row has none (it fills a batch up): nothing is written, neither to the cache
+ *            nor to out. The slots of one lc_cache_write must differ: what a slot named twice holds afterwards is unspecified.
+ * lc_cache_read_pages: the rows of `sequences` sequences one behind the other. Sequence s takes the rows begin[s] ...
+ *            begin[s + 1] - 1 (begin: DEVICE, sequences + 1 entries, not decreasing); its row j is position first[s] + j of the
+ *            sequence (first: DEVICE or NULL for 0), which lies in slot table[s * table_stride + p / page] * page + p % page
+ *            (table: DEVICE, `width` pages a sequence, table_stride >= width and < 2^32). Rows ahead of begin[0] and from
+ *            begin[sequences] on are left as they are.
+ * status     DEVICE or NULL: a word that receives LC_ERR_INDEX, if it is 0, when a slot or page is none of the cache's or a position lies
+ *            beyond the table; such a row is passed over like one without a slot. No call clears it; lc_last_status reads it.
+ */
+typedef struct lc_cache {
+  void* codes;
+  void* scales;
+  uint64_t slots;
+  uint32_t planes, heads, dim, bits, group;
+} lc_cache;
+typedef struct lc_rows {
+  void* data;
+  uint64_t row_stride, head_stride;
+} lc_rows;
+uint64_t lc_cache_code_bytes(const lc_cache* cache);
+uint64_t lc_cache_scale_bytes(const lc_cache* cache);
+int lc_cache_write(const lc_cache* cache, const lc_rows* src, int type, uint64_t rows, const int64_t* slots,
+                   int32_t* status, lc_cuda_stream_t cs);
+int lc_cache_read(const lc_cache* cache, const lc_rows* out, int type, uint64_t rows, const int64_t* slots,
+                  int32_t* status, lc_cuda_stream_t cs);
+int lc_cache_read_pages(const lc_cache* cache, const lc_rows* out, int type, uint64_t rows, const int32_t* table,
+                        uint64_t table_stride, uint32_t width, uint32_t page, const int32_t* begin, const int32_t* first,
+                        uint32_t sequences, int32_t* status, lc_cuda_stream_t cs);
 
 #ifdef __cplusplus
 }

@@ -9,12 +9,13 @@ from __future__ import annotations
 import ctypes as C
 import os
 import threading
+from typing import NamedTuple
 
 import torch
 
 from . import build as _build
 
-OK, ERR_ARG, ERR_CAPACITY, ERR_NONFINITE, ERR_FORMAT, ERR_MISMATCH, ERR_TIMEOUT, ERR_CUDA, ERR_RANGE = 0, -1, -2, -3, -4, -5, -6, -7, -8
+OK, ERR_ARG, ERR_CAPACITY, ERR_NONFINITE, ERR_FORMAT, ERR_MISMATCH, ERR_TIMEOUT, ERR_CUDA, ERR_RANGE, ERR_INDEX = 0, -1, -2, -3, -4, -5, -6, -7, -8, -9
 MAX_CHAIN = 8
 WAIT_PAGE_BYTES = 128
 
@@ -25,6 +26,8 @@ SYMBOLS = (
     "lc_stream_info", "lc_last_status", "lc_wait", "lc_host_arena_bytes", "lc_compress_host", "lc_recover_host",
     "lc_debug_bins", "lc_debug_codes", "lc_debug_split_segments", "lc_debug_decode_warps",
     "lc_compress_noalloc",
+    "lc_q4_bytes", "lc_q4_quantize", "lc_recover_q4", "lc_q4_read", "lc_q4_matvec",
+    "lc_cache_code_bytes", "lc_cache_scale_bytes", "lc_cache_write", "lc_cache_read", "lc_cache_read_pages",
 )
 NOALLOC_MAX_N = 4194304
 
@@ -36,6 +39,15 @@ class LCInfo(C.Structure):
         ("max_len", C.c_uint32), ("nchunks", C.c_uint32), ("valid", C.c_int32), ("fixed_width", C.c_uint32), ("shard", C.c_uint32),
         ("cached_lengths", C.c_uint32), ("mean_rep", C.c_uint32),
     ]
+
+
+class LCCache(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("slots", C.c_uint64), ("planes", C.c_uint32), ("heads", C.c_uint32),
+                ("dim", C.c_uint32), ("bits", C.c_uint32), ("group", C.c_uint32)]
+
+
+class LCRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_uint64), ("head_stride", C.c_uint64)]
 
 
 class LCError(RuntimeError):
@@ -97,6 +109,17 @@ def lib():
     L.lc_debug_split_segments.restype = C.c_uint32
     L.lc_debug_decode_warps.argtypes = [i32, u64, C.c_uint32]
     L.lc_debug_decode_warps.restype = C.c_uint32
+    L.lc_q4_bytes.argtypes = [u64, u64, i32]
+    L.lc_q4_bytes.restype = u64
+    L.lc_q4_quantize.argtypes = [vp, i32, u64, u64, u64, i32, vp, u64, vp, u64, vp]
+    L.lc_recover_q4.argtypes = [vp, C.POINTER(vp), C.POINTER(u64), i32, u64, u64, i32, vp, u64, vp, vp, u64, vp]
+    L.lc_q4_read.argtypes = [vp, u64, u64, u64, i32, vp, i32, u64, vp]
+    L.lc_q4_matvec.argtypes = [vp, u64, u64, u64, i32, vp, i32, u64, u64, vp, i32, u64, vp]
+    cache, rows = C.POINTER(LCCache), C.POINTER(LCRows)
+    for f in (L.lc_cache_code_bytes, L.lc_cache_scale_bytes):
+        f.argtypes, f.restype = [cache], u64
+    L.lc_cache_write.argtypes = L.lc_cache_read.argtypes = [cache, rows, i32, u64, vp, vp, vp]
+    L.lc_cache_read_pages.argtypes = [cache, rows, i32, u64, vp, u64, C.c_uint32, C.c_uint32, vp, vp, C.c_uint32, vp, vp]
     _lib = L
     return L
 
@@ -500,3 +523,247 @@ def compress_noalloc(base, cur, nbits, stream):
                                    stream.numel(), _cs(base.device))
     _check(rc, "lc_compress_noalloc")
     return stream[: stream_info(stream).total_bytes]
+
+
+# ---- state in few bits: 4-bit weights and a quantised cache ------------------------------------------------------
+
+TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+Q4_MAX_TOKENS = 1048576
+
+
+def _call(fn, what, device, *args):
+    """fn(*args, the current stream of ``device``), with that device current; raises on a host-side error."""
+    index = device.index
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    if rc != OK:
+        raise LCError(rc, what)
+
+
+def _numbers(t, name, dims, device=None):
+    """The LC_TYPE_* of a CUDA tensor of numbers whose last axis is contiguous."""
+    kind = TYPES.get(t.dtype)
+    if kind is None or not t.is_cuda or t.dim() != dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError("%s must be a %d-dimensional CUDA tensor of float32, bfloat16 or float16, contiguous along its last axis" % (name, dims))
+    if device is not None and t.device != device:
+        raise ValueError("%s is on another device" % name)
+    return kind
+
+
+class Q4(NamedTuple):
+    """A matrix of 4-bit weights: what lc_q4_quantize wrote into ``data`` (uint8), and its shape."""
+
+    data: torch.Tensor
+    rows: int
+    cols: int
+    group: int
+
+
+def q4_bytes(rows, cols, group) -> int:
+    return int(lib().lc_q4_bytes(rows, cols, group))
+
+
+def alloc_q4(rows, cols, group, device) -> Q4:
+    """Room for rows x cols weights, not written yet."""
+    size = q4_bytes(rows, cols, group)
+    if size == 0 and rows and cols:
+        raise LCError(ERR_ARG, "lc_q4_bytes")
+    return Q4(torch.empty(size, dtype=torch.uint8, device=device), rows, cols, group)
+
+
+def _q4(q4):
+    return q4.data.data_ptr(), q4.data.numel(), q4.rows, q4.cols, q4.group
+
+
+def q4_quantize_async(w, q4, workspace):
+    """lc_q4_quantize of the matrix ``w`` into ``q4`` on the current stream; an Inf or NaN shows in last_status(workspace)."""
+    kind = _numbers(w, "w", 2, q4.data.device)
+    if w.shape[0] != q4.rows or w.shape[1] != q4.cols:
+        raise ValueError("w has another shape than the weights")
+    if workspace.device != w.device:
+        raise ValueError("workspace is on another device")
+    data, size, rows, cols, group = _q4(q4)
+    _call(lib().lc_q4_quantize, "lc_q4_quantize", w.device, w.data_ptr(), kind, rows, cols, w.stride(0), group, data, size, workspace.data_ptr(),
+          workspace.numel())
+
+
+def q4_quantize(w, group=128, q4=None, workspace=None) -> Q4:
+    """The matrix ``w`` (float32, bfloat16 or float16) as 4-bit weights; raises if it holds an Inf or NaN."""
+    _numbers(w, "w", 2)
+    if q4 is None:
+        q4 = alloc_q4(w.shape[0], w.shape[1], group, w.device)
+    if workspace is None:
+        workspace = alloc_workspace(0, w.device)
+    q4_quantize_async(w, q4, workspace)
+    with torch.cuda.device(w.device):
+        _wait(workspace, "lc_q4_quantize (device)")
+    return q4
+
+
+def recover_q4_async(base, streams, q4, scratch, workspace):
+    """lc_recover_q4 on the current stream: the state that ``streams`` lead to from ``base`` (q4.rows x q4.cols values), as 4-bit
+    weights. ``scratch`` receives the recovered state."""
+    _f32_cuda(base, "base"), _f32_cuda(scratch, "scratch")
+    if base.numel() != q4.rows * q4.cols or scratch.numel() != base.numel():
+        raise ValueError("base, scratch and the weights differ in size")
+    k = len(streams)
+    ptrs = (C.c_void_p * k)(*[s.data_ptr() for s in streams])
+    sizes = (C.c_uint64 * k)(*[s.numel() for s in streams])
+    data, size, rows, cols, group = _q4(q4)
+    _call(lib().lc_recover_q4, "lc_recover_q4", base.device, base.data_ptr(), ptrs, sizes, k, rows, cols, group, data, size, scratch.data_ptr(),
+          workspace.data_ptr(), workspace.numel())
+
+
+def recover_q4(base, streams, rows, group=128, q4=None, scratch=None, workspace=None) -> Q4:
+    """Recovers a layer of ``rows`` rows from a base and a chain of streams, as 4-bit weights."""
+    if q4 is None:
+        if rows < 1 or base.numel() % rows:
+            raise ValueError("base does not divide into that many rows")
+        q4 = alloc_q4(rows, base.numel() // rows, group, base.device)
+    if scratch is None:
+        scratch = torch.empty_like(base)
+    if workspace is None:
+        workspace = alloc_workspace(0, base.device)
+    recover_q4_async(base, streams, q4, scratch, workspace)
+    with torch.cuda.device(base.device):
+        _wait(workspace, "lc_recover_q4 (device)")
+    return q4
+
+
+def q4_read(q4, out=None, dtype=torch.float32):
+    """The numbers that the weights stand for, [rows, cols], on the current stream."""
+    if out is None:
+        out = torch.empty(q4.rows, q4.cols, dtype=dtype, device=q4.data.device)
+    kind = _numbers(out, "out", 2, q4.data.device)
+    if out.shape[0] != q4.rows or out.shape[1] != q4.cols:
+        raise ValueError("out has another shape than the weights")
+    _call(lib().lc_q4_read, "lc_q4_read", out.device, *_q4(q4), out.data_ptr(), kind, out.stride(0))
+    return out
+
+
+def q4_matvec(q4, x, out=None):
+    """Products of the weights with the vectors ``x`` [tokens, cols] (or one vector [cols]), on the current stream: [tokens, rows]
+    in x's type, or in that of ``out`` (x's or float32). No gradient is kept."""
+    if x.dim() == 1:
+        return q4_matvec(q4, x.unsqueeze(0), None if out is None else out.unsqueeze(0)).squeeze(0)
+    kind = _numbers(x, "x", 2, q4.data.device)
+    tokens, cols = x.shape
+    if cols != q4.cols:
+        raise ValueError("x has %d columns, the weights have %d" % (cols, q4.cols))
+    if x.requires_grad and torch.is_grad_enabled():
+        raise ValueError("q4_matvec has no gradient: detach x, or call it under torch.no_grad()")
+    if out is None:
+        out = torch.empty(tokens, q4.rows, dtype=x.dtype, device=x.device)
+        out_kind = kind
+    else:
+        out_kind = _numbers(out, "out", 2, x.device)
+        if out.shape[0] != tokens or out.shape[1] != q4.rows:
+            raise ValueError("out must be [tokens, rows]")
+    _call(lib().lc_q4_matvec, "lc_q4_matvec", x.device, *_q4(q4), x.data_ptr(), kind, tokens, x.stride(0), out.data_ptr(), out_kind, out.stride(0))
+    return out
+
+
+class Cache:
+    """A quantised cache (lc_cache): ``codes`` [planes, slots, heads, bytes of a row] uint8 and ``scales`` [planes, slots, heads,
+    groups] bfloat16, both contiguous. planes = 2: keys and values."""
+
+    def __init__(self, codes, scales, dim, bits, group):
+        if not (codes.is_cuda and codes.dtype == torch.uint8 and codes.dim() == 4 and codes.is_contiguous()):
+            raise ValueError("codes must be a contiguous 4-dimensional uint8 CUDA tensor")
+        if not (scales.dtype == torch.bfloat16 and scales.is_contiguous() and scales.device == codes.device):
+            raise ValueError("scales must be a contiguous bfloat16 tensor beside codes")
+        self.codes, self.scales, self.device = codes, scales, codes.device
+        self.planes, self.slots, self.heads = codes.shape[:3]
+        self.dim, self.bits, self.group = dim, bits, group
+        self._c = LCCache(codes.data_ptr(), scales.data_ptr(), self.slots, self.planes, self.heads, dim, bits, group)
+        if lib().lc_cache_code_bytes(self._c) != codes.numel() or lib().lc_cache_scale_bytes(self._c) != 2 * scales.numel():
+            raise ValueError("codes and scales do not have the sizes of such a cache")
+
+
+def alloc_cache(slots, heads, dim, bits, group, device, planes=2) -> Cache:
+    """A cache of zeros."""
+    shape = LCCache(None, None, 1, 1, 1, dim, bits, group)
+    row, scale = int(lib().lc_cache_code_bytes(shape)), int(lib().lc_cache_scale_bytes(shape)) // 2
+    if row == 0:
+        raise LCError(ERR_ARG, "lc_cache_code_bytes")
+    return Cache(torch.zeros(planes, slots, heads, row, dtype=torch.uint8, device=device),
+                 torch.zeros(planes, slots, heads, scale, dtype=torch.bfloat16, device=device), dim, bits, group)
+
+
+def _rows(cache, tensors, what):
+    """The lc_rows of one tensor [rows, heads, dim] per plane, their type and their number."""
+    if len(tensors) != cache.planes:
+        raise ValueError("%s: the cache has %d planes" % (what, cache.planes))
+    first = tensors[0]
+    kind = _numbers(first, what, 3, cache.device)
+    rows, heads, dim = first.shape
+    if heads != cache.heads or dim != cache.dim:
+        raise ValueError("%s must be [rows, heads, dim] of the cache" % what)
+    if cache.planes == 1:
+        return (LCRows * 1)((first.data_ptr(), first.stride(0), first.stride(1))), kind, rows
+    second = tensors[1]
+    if _numbers(second, what, 3, cache.device) != kind or second.shape != first.shape:
+        raise ValueError("%s: keys and values differ in shape or type" % what)
+    return (LCRows * 2)((first.data_ptr(), first.stride(0), first.stride(1)), (second.data_ptr(), second.stride(0), second.stride(1))), kind, rows
+
+
+def _whole(t, name, dtype, device):
+    if t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor on the cache's device" % (name, dtype))
+    return t.data_ptr()
+
+
+def _status(status, device):
+    return None if status is None else _whole(status, "status", torch.int32, device)
+
+
+def alloc_status(device):
+    """A status word for the cache calls, clear; last_status reads it."""
+    return torch.zeros(1, dtype=torch.int32, device=device)
+
+
+def cache_write(cache, k, v, slots, status=None):
+    """Rows [rows, heads, dim] of keys and values (``v`` None if the cache has one plane) into the cache's ``slots`` (int64; -1: none),
+    on the current stream."""
+    src, kind, rows = _rows(cache, (k,) if v is None else (k, v), "keys and values")
+    at = _whole(slots, "slots", torch.int64, cache.device)
+    if slots.numel() != rows:
+        raise ValueError("a slot for each row is needed")
+    _call(lib().lc_cache_write, "lc_cache_write", cache.device, cache._c, src, kind, rows, at, _status(status, cache.device))
+
+
+def _outs(cache, outs, rows, dtype):
+    """The tensors that a read writes; new ones are zeroed, for rows without a slot stay as they are."""
+    if outs is not None:
+        return outs
+    return [torch.zeros(rows, cache.heads, cache.dim, dtype=dtype, device=cache.device) for _ in range(cache.planes)]
+
+
+def cache_read(cache, slots, outs=None, dtype=torch.bfloat16, status=None):
+    """The rows in ``slots``, on the current stream: a tensor [rows, heads, dim] per plane (``outs``, or new ones of ``dtype``)."""
+    outs = _outs(cache, outs, slots.numel(), dtype)
+    out, kind, rows = _rows(cache, outs, "outs")
+    at = _whole(slots, "slots", torch.int64, cache.device)
+    if slots.numel() != rows:
+        raise ValueError("a slot for each row is needed")
+    _call(lib().lc_cache_read, "lc_cache_read", cache.device, cache._c, out, kind, rows, at, _status(status, cache.device))
+    return outs
+
+
+def cache_read_pages(cache, table, page, begin, outs, first=None, status=None):
+    """Sequences out of pages of ``page`` slots, one behind the other, into ``outs`` (a tensor [rows, heads, dim] per plane), on the
+    current stream. ``table`` [sequences, width] int32: pages; ``begin`` [sequences + 1] int32: where each sequence's rows begin in
+    ``outs``; ``first`` [sequences] int32: the position of each one's first row (0 if None)."""
+    out, kind, rows = _rows(cache, outs, "outs")
+    if table.dim() != 2 or table.dtype != torch.int32 or table.device != cache.device or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError("table must be [sequences, width] int32 on the cache's device, contiguous along its last axis")
+    sequences, width = table.shape
+    at = _whole(begin, "begin", torch.int32, cache.device)
+    if begin.numel() != sequences + 1 or (first is not None and first.numel() != sequences):
+        raise ValueError("begin has an entry per sequence and one more, first one per sequence")
+    _call(lib().lc_cache_read_pages, "lc_cache_read_pages", cache.device, cache._c, out, kind, rows, table.data_ptr(), table.stride(0), width, page, at,
+          None if first is None else _whole(first, "first", torch.int32, cache.device), sequences, _status(status, cache.device))
+    return outs

@@ -148,6 +148,7 @@ const char* lc_strerror(int code) {
     case LC_ERR_TIMEOUT: return "device-side wait timed out";
     case LC_ERR_CUDA: return "CUDA runtime error";
     case LC_ERR_RANGE: return "a delta of magnitude 2 or more needs the state that the call has released";
+    case LC_ERR_INDEX: return "a slot or page that the cache does not have";
     default: return "unknown status";
   }
 }
