@@ -1,18 +1,32 @@
 // Products of 4-bit weights with the vectors of a few tokens:
 //   out[t, r] = sum over groups G of scale[r, G] * (sum over c in G of code[r, c] * x[t, c]).
 //
-// The weights are read once and bound the product up to some 16 tokens; the multiplications go to the tensor cores (m16n8k16:
-// 16 rows, 8 tokens, 16 columns), which take the codes as exact 16-bit numbers and add up in fp32. A group's scale meets the group's
-// sum in fp32, not the codes: code * scale needs 11 bits, more than bf16 has. An fp32 vector takes three columns of the product: its
-// values cut into three bf16 numbers, 8 bits each, whose sum they are, so that nothing of them is lost (but what lies below 2^-133).
+// The weights are read once. The multiplications go to the tensor cores (m16n8k16: 16 rows, 8 tokens, 16 columns), which multiply
+// 16-bit numbers exactly and add up in fp32. A group's scale meets the group's sum in fp32, not the codes: code * scale needs 11
+// bits, more than bf16 has. An fp32 vector takes three columns of the product: its values cut into three bf16 numbers, 8 bits
+// each, whose sum they are, so that nothing of them is lost.
+//
+// What bounds it, once enough is in flight, is the work of making 16-bit operands of 4-bit codes, so that is as little as can be:
+// the codes are used as the low bits of a 16-bit float. In a float's lowest 8 (bf16) or 11 (fp16) bits a whole number N stands for
+// N * 2^-133 or N * 2^-24 (subnormal numbers, and the first binade above them, which goes on in the same steps): with n = code + 8,
+// a mask takes two n's out of a word for a row r, and the same mask four bits up two 16 n's for row r + 8. One shift and four masks for eight codes;
+// what is too much by it is taken off in fp32: the accumulators start at -8 times the group's sum of x. To keep the products with
+// bf16 vectors (and parts of fp32 ones) in fp32's normal range, x is multiplied by 2^80 when it is staged. Vectors with values of
+// 2^40 and more, Inf or NaN among them, take plain multiplications instead (slow_tile), a CTA for itself.
+#include <stdlib.h>
+#include <type_traits>
+
 #include "lc_q4.cuh"
 
 namespace lc {
 namespace {
 
 constexpr uint32_t kWarps = 8;
-constexpr uint32_t kAhead = 4;       // steps of weights that a warp has in flight: 4 KB
-constexpr uint32_t kRedStride = 20;  // floats from one column of a tile's sums to the next: the lanes of a store meet in no bank
+constexpr uint32_t kStepScales = 128;   // bytes kept for the scales of a step: 16 rows, up to 4 groups
+constexpr uint32_t kSlot = kQ4StepBytes + kStepScales;
+constexpr uint32_t kRingSlots = 6;      // steps of 16 rows in the ring of a warp
+constexpr uint32_t kMaxSplit = 8;       // CTAs of a cluster that share a tile's columns
+constexpr uint32_t kSharedPerSM = 227 * 1024;
 
 struct MatvecArgs {
   const uint8_t* q4;
@@ -22,14 +36,12 @@ struct MatvecArgs {
   Q4Layout L;
   uint32_t tokens, per_pass;  // vectors in all, and of one pass (blockIdx.y)
   int out_type;
-  uint32_t chunk_steps;       // steps whose part of x is in shared memory at a time
+  uint32_t ways;              // warps of a CTA that share a tile's columns
+  uint32_t slice;             // steps of a CTA: all of them, or its share in the cluster
+  uint32_t chunk;             // steps whose part of x is in shared memory at a time
+  uint32_t rounds;            // blocks of rows that a group of warps goes through, at most
+  FastDiv by_count;           // vectors of a whole pass
 };
-
-__device__ __forceinline__ uint4 load_weights(const uint8_t* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
-}
 
 template <class M>
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
@@ -46,220 +58,512 @@ __device__ __forceinline__ void mma<__half>(float (&d)[4], const uint32_t (&a)[4
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// The eight codes of a word as four pairs of 16-bit numbers. A code n + 8 in the low bits of 128 (bf16) or 1024 (fp16), less 136 or
-// 1032; the fp16 mantissa also holds a code four bits up, which a multiplication by 1/16 brings down.
+// The eight codes of a word, plus 8, as four pairs of tiny numbers: of row r, of row r + 8 (times 16), and so for two more columns.
+__device__ __forceinline__ void operands(uint32_t w, uint32_t (&a)[4]) {
+  a[0] = w & 0x000F000Fu;
+  a[1] = w & 0x00F000F0u;
+  w >>= 8;
+  a[2] = w & 0x000F000Fu;
+  a[3] = w & 0x00F000F0u;
+}
+// kUp: what x is multiplied by; kUnit: what the sums of products of row r are then to be multiplied by.
 template <class M>
-__device__ __forceinline__ void operands(uint32_t w, uint32_t (&a)[4]);
+struct Unit;
 template <>
-__device__ __forceinline__ void operands<__nv_bfloat16>(uint32_t w, uint32_t (&a)[4]) {
+struct Unit<__nv_bfloat16> {
+  static constexpr float kUp = 0x1p80f, kUnit = 0x1p53f;
+};
+template <>
+struct Unit<__half> {
+  static constexpr float kUp = 1.0f, kUnit = 0x1p24f;
+};
+
+// Whether one of the values behind a piece's bits is none for the products above.
+template <class X>
+__device__ __forceinline__ bool too_large(const uint32_t (&raw)[2 * sizeof(X)]) {
+  bool any = false;
 #pragma unroll
-  for (int p = 0; p < 4; ++p) {
-    const uint32_t u = ((w >> (4 * p)) & 0x000F000Fu) | 0x43004300u;
-    const __nv_bfloat162 d = __hsub2(reinterpret_cast<const __nv_bfloat162&>(u), __nv_bfloat162(__ushort_as_bfloat16(0x4308), __ushort_as_bfloat16(0x4308)));
-    a[p] = reinterpret_cast<const uint32_t&>(d);
+  for (int k = 0; k < (int)(2 * sizeof(X)); ++k) {
+    if constexpr (sizeof(X) == 4) any |= (raw[k] & 0x7F800000u) >= ((127u + 40u) << 23);
+    else if constexpr (std::is_same<X, __half>::value) any |= (raw[k] & 0x7C00u) == 0x7C00u || (raw[k] & 0x7C000000u) == 0x7C000000u;
+    else any |= (raw[k] & 0x7F80u) >= ((127u + 40u) << 7) || (raw[k] & 0x7F800000u) >= ((127u + 40u) << 23);
   }
+  return any;
 }
-template <>
-__device__ __forceinline__ void operands<__half>(uint32_t w, uint32_t (&a)[4]) {
+
+// Eight values of a vector from column `col` on, as they are in memory; zeros behind the last column.
+template <class X>
+__device__ __forceinline__ void load_piece(const MatvecArgs& A, uint32_t token, uint32_t col, bool there, uint32_t (&raw)[2 * sizeof(X)]) {
+  const int valid = !there || col >= A.L.cols ? 0 : (int)min(8u, A.L.cols - col);
+  const X* p = static_cast<const X*>(A.x) + (uint64_t)token * A.x_stride + col;
+  if (valid == 8 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
 #pragma unroll
-  for (int p = 0; p < 4; ++p) {
-    const uint32_t v = p < 2 ? w : w >> 8;
-    const uint32_t u = (v & (p & 1 ? 0x00F000F0u : 0x000F000Fu)) | 0x64006400u;
-    const __half2 h = reinterpret_cast<const __half2&>(u);
-    const __half2 d = p & 1 ? __hfma2(h, __half2(__ushort_as_half(0x2C00), __ushort_as_half(0x2C00)), __half2(__ushort_as_half(0xD480), __ushort_as_half(0xD480)))
-                            : __hsub2(h, __half2(__ushort_as_half(0x6408), __ushort_as_half(0x6408)));
-    a[p] = reinterpret_cast<const uint32_t&>(d);
+    for (int k = 0; k < (int)sizeof(X) / 2; ++k) {
+      const uint4 v = __ldg(reinterpret_cast<const uint4*>(p) + k);
+      raw[4 * k] = v.x, raw[4 * k + 1] = v.y, raw[4 * k + 2] = v.z, raw[4 * k + 3] = v.w;
+    }
+  } else if constexpr (sizeof(X) == 4) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) raw[k] = k < valid ? __ldg(reinterpret_cast<const uint32_t*>(p) + k) : 0u;
+  } else {
+    const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) raw[k] = (2 * k < valid ? __ldg(h + 2 * k) : 0u) | (uint32_t)(2 * k + 1 < valid ? __ldg(h + 2 * k + 1) : 0u) << 16;
   }
 }
 
+// A piece into shared memory as columns of the product (one, or the three parts of fp32, `stride` apart), and the sum of each.
 // The three bf16 numbers of an fp32: the upper half of its bits, that of the exact rest, and what is then left (8 bits at most).
-// Inf and NaN are their own first part (a NaN stays one: its lower bits may be all that tells it from Inf).
-__device__ __forceinline__ void three_parts(float x, uint32_t (&part)[3]) {
-  const uint32_t u = __float_as_uint(x);
-  if ((u & 0x7F800000u) == 0x7F800000u) {
-    part[0] = (u >> 16) | ((u & 0x007FFFFFu) ? 0x40u : 0u);
-    part[1] = part[2] = 0;
-    return;
-  }
-  part[0] = u >> 16;
-  const float r1 = x - __uint_as_float(u & 0xFFFF0000u);
-  part[1] = __float_as_uint(r1) >> 16;
-  const float r2 = r1 - __uint_as_float(__float_as_uint(r1) & 0xFFFF0000u);
-  part[2] = __float_as_uint(r2) >> 16;
-}
-
-// x of the steps [begin, end) into shared memory: 16 bytes (8 columns of one token) at ((unit * columns + column) * 4 + t) * 16,
-// unit: 32 columns of the matrix, t: the quarter of them that lanes 4 r + t multiply. Zeros behind the matrix's last column.
 template <class X, class M>
-__device__ __forceinline__ void stage_x(const MatvecArgs& A, uint32_t first, uint32_t count, uint32_t columns, uint32_t begin, uint32_t end, uint4* xs) {
-  const uint32_t units = (end - begin) * 4;
-  for (uint32_t i = threadIdx.x; i < units * count * 4; i += kWarps * 32) {
-    const uint32_t t = i & 3u, token = (i >> 2) % count, unit = (i >> 2) / count;
-    const uint32_t col = begin * kQ4StepCols + unit * 32 + 8 * t;
-    const int valid = col >= A.L.cols ? 0 : (int)min(8u, A.L.cols - col);
-    const X* p = static_cast<const X*>(A.x) + (uint64_t)(first + token) * A.x_stride + col;
-    if constexpr (sizeof(X) == 4) {
-      float v[8];
-      load8(p, valid, v);
-      uint32_t part[8][3];
+__device__ __forceinline__ void store_piece(const uint32_t (&raw)[2 * sizeof(X)], uint4* to, uint32_t stride, float (&sum)[sizeof(X) == 4 ? 3 : 1]) {
+  if constexpr (sizeof(X) == 4) {
+    uint32_t part[3][8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) three_parts(v[e], part[e]);
+    for (int k = 0; k < 3; ++k) sum[k] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float v = __uint_as_float(raw[e]) * Unit<M>::kUp;
 #pragma unroll
       for (int k = 0; k < 3; ++k) {
-        uint4 o;
-        o.x = part[0][k] | part[1][k] << 16;
-        o.y = part[2][k] | part[3][k] << 16;
-        o.z = part[4][k] | part[5][k] << 16;
-        o.w = part[6][k] | part[7][k] << 16;
-        xs[(unit * columns + 3 * token + k) * 4 + t] = o;
+        const uint32_t u = __float_as_uint(v) & 0xFFFF0000u;
+        part[k][e] = u;
+        sum[k] += __uint_as_float(u);
+        v -= __uint_as_float(u);
       }
-    } else {
-      uint4 o = make_uint4(0, 0, 0, 0);
-      if (valid == 8 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
-        o = __ldg(reinterpret_cast<const uint4*>(p));
-      } else {
-        const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
-        uint32_t e[8];
+    }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) e[k] = k < valid ? h[k] : 0u;
-        o = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+    for (int k = 0; k < 3; ++k) {
+      uint32_t w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = __byte_perm(part[k][2 * e], part[k][2 * e + 1], 0x7632);
+      to[k * stride] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  } else {
+    uint32_t w[4];
+    float s = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (std::is_same<X, __half>::value) {
+        const float2 f = __half22float2(reinterpret_cast<const __half2&>(raw[e]));
+        s += f.x + f.y;
+        w[e] = raw[e];
+      } else {
+        const float lo = __uint_as_float(raw[e] << 16) * Unit<M>::kUp, hi = __uint_as_float(raw[e] & 0xFFFF0000u) * Unit<M>::kUp;
+        s += lo + hi;
+        w[e] = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
       }
-      xs[(unit * columns + token) * 4 + t] = o;
+    }
+    to[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    sum[0] = s;
+  }
+}
+
+// x of the steps [begin, end) into shared memory, one column of the product behind the other: `stride` 16-byte pieces, an odd
+// number of units (32 columns of the matrix, four pieces) of which lanes 4 r + t multiply piece t, so that eight columns lie in
+// eight different parts of the banks. Beside it, where the accumulators start: per group (at its first unit) and column of the
+// product. A thread asks for four pieces before it stores the first. Returns, in every thread, whether some value is too large.
+template <class X, class M, int NT, int G>
+__device__ __forceinline__ bool stage_x(const MatvecArgs& A, uint32_t first, uint32_t count, uint32_t begin, uint32_t end, uint32_t stride, uint4* xs, float* starts) {
+  constexpr int kBatch = 4, kParts = sizeof(X) == 4 ? 3 : 1;
+  const uint32_t pieces = (end - begin) * 4 * count, t = threadIdx.x & 3u, step = kWarps * 8, quad = 15u << (threadIdx.x & 28u);
+  bool large = false;
+  for (uint32_t i0 = threadIdx.x >> 2; i0 < pieces; i0 += kBatch * step) {
+    uint32_t raw[kBatch][2 * sizeof(X)], unit[kBatch], token[kBatch];
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      const uint32_t i = i0 + b * step;
+      unit[b] = count == A.by_count.d ? A.by_count.div(i) : i / count;
+      token[b] = i - unit[b] * count;
+      load_piece<X>(A, first + token[b], (begin * 4 + unit[b]) * 32 + 8 * t, i < pieces, raw[b]);
+    }
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      if (i0 + b * step >= pieces) break;  // the same for the four threads of a unit
+      large |= too_large<X>(raw[b]);
+      float sum[kParts];
+      store_piece<X, M>(raw[b], xs + token[b] * kParts * stride + unit[b] * 4 + t, stride, sum);
+#pragma unroll
+      for (int k = 0; k < kParts; ++k) {
+        sum[k] += __shfl_xor_sync(quad, sum[k], 1);
+        sum[k] += __shfl_xor_sync(quad, sum[k], 2);
+        if (t == 0) starts[unit[b] * 8 * NT + token[b] * kParts + k] = sum[k] * (-8.0f / Unit<M>::kUp / Unit<M>::kUnit);
+      }
+    }
+  }
+  large = __syncthreads_or(large);
+  if (G > 32) {
+    constexpr uint32_t kUnits = G / 32;
+    for (uint32_t i = threadIdx.x; i < (end - begin) * (4 / kUnits) * count * kParts; i += kWarps * 32) {
+      const uint32_t g = i / (count * kParts);
+      float* p = starts + g * kUnits * 8 * NT + (i - g * count * kParts);
+      float s = p[0];
+#pragma unroll
+      for (uint32_t u = 1; u < kUnits; ++u) s += p[u * 8 * NT];
+      p[0] = s;
+    }
+    __syncthreads();
+  }
+  return large;
+}
+
+// Whether a value of the vectors in the steps [begin, end) is too large, for when they are not staged all at once.
+template <class X>
+__device__ __forceinline__ bool find_large(const MatvecArgs& A, uint32_t first, uint32_t count, uint32_t begin, uint32_t end) {
+  bool large = false;
+  for (uint32_t i = threadIdx.x; i < (end - begin) * 16 * count; i += kWarps * 32) {
+    const uint32_t token = i / ((end - begin) * 16);
+    uint32_t raw[2 * sizeof(X)];
+    load_piece<X>(A, first + token, (begin * 16 + (i - token * (end - begin) * 16)) * 8, true, raw);
+    large |= too_large<X>(raw);
+  }
+  return __syncthreads_or(large);
+}
+
+// A warp's sums for 16 rows by plain multiplications: what the definition says for Inf, NaN and large values.
+template <class X>
+__device__ __noinline__ void slow_tile(const MatvecArgs& A, uint32_t tile, uint32_t first, uint32_t count, uint32_t begin, uint32_t end, float* red, uint32_t red_stride) {
+  constexpr uint32_t kParts = sizeof(X) == 4 ? 3 : 1;
+  const uint32_t lane = threadIdx.x & 31, r = lane >> 2, t = lane & 3;
+  for (uint32_t token = 0; token < count; ++token) {
+    const X* x = static_cast<const X*>(A.x) + (uint64_t)(first + token) * A.x_stride;
+    float y[2] = {0.0f, 0.0f};
+    for (uint32_t step = begin; step < end; step += A.ways) {
+      for (uint32_t h = 0; h < 4; ++h) {
+        const uint2 w = __ldg(reinterpret_cast<const uint2*>(A.q4 + ((uint64_t)tile * A.L.steps + step) * kQ4StepBytes + (h / 2) * 512 + lane * 16 + (h & 1) * 8));
+        const uint32_t col = step * kQ4StepCols + h * 32 + 8 * t;
+        const uint32_t s = __ldg(reinterpret_cast<const uint32_t*>(A.q4 + A.L.scales_off) + ((uint64_t)tile * A.L.groups + col / A.L.group) * 8 + r);
+        float p[2] = {0.0f, 0.0f};
+        for (uint32_t e = 0; e < 8; ++e) {
+          if (col + e >= A.L.cols) break;
+          const float v = to_float(x[col + e]);
+          const uint32_t n = (e < 4 ? w.x : w.y) >> (16 * (e & 1) + 8 * ((e >> 1) & 1));
+          p[0] += (float)((int)(n & 15u) - 8) * v;
+          p[1] += (float)((int)((n >> 4) & 15u) - 8) * v;
+        }
+        y[0] += __uint_as_float(s << 16) * p[0];
+        y[1] += __uint_as_float(s & 0xFFFF0000u) * p[1];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      y[i] += __shfl_xor_sync(0xFFFFFFFFu, y[i], 1);
+      y[i] += __shfl_xor_sync(0xFFFFFFFFu, y[i], 2);
+      if (t < kParts) red[(token * kParts + t) * red_stride + r + 8 * i] = t == 0 ? y[i] : 0.0f;
     }
   }
 }
 
-template <int G>
-struct Step {  // a warp's part of 16 rows and 128 columns
-  uint4 w[2];
-  uint32_t s[kQ4StepCols / G];
+__device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void store_in_cluster(float* mine, uint32_t rank, float v) {
+  asm volatile("{ .reg .u32 a; mapa.shared::cluster.u32 a, %0, %1; st.shared::cluster.f32 [a], %2; }" ::"r"(shared_address(mine)), "r"(rank), "f"(v) : "memory");
+}
+
+// Shared memory: the warps' rings, their sums, what the cluster's CTAs send each other, where accumulators start, x.
+template <int NT, int MT>
+struct Shared {
+  static constexpr uint32_t kRows = MT * kQ4TileRows, kRedStride = kRows + 4;  // floats from column to column: the lanes of a store meet in no bank
+  static constexpr uint32_t kRing = kRingSlots * kSlot, kRed = 8 * NT * kRedStride * 4, kFixed = kWarps * (kRing + kRed);
+  static __host__ __device__ __forceinline__ uint32_t part_tokens(uint32_t per_pass, uint32_t split) { return split > 1 ? (per_pass + split - 1) / split : 0; }
+  static __host__ __device__ __forceinline__ uint32_t part(uint32_t ways, uint32_t split, uint32_t per_pass) {  // [2][groups][split][part_tokens][kRows] floats
+    return 2 * (kWarps / ways) * split * part_tokens(per_pass, split) * kRows * 4;
+  }
+  static __host__ __device__ __forceinline__ uint32_t starts(uint32_t steps) { return steps * 4 * 8 * NT * 4; }
+  // a column of zeros behind the others, if the product has more columns than they are
+  static __host__ __device__ __forceinline__ uint64_t x(uint32_t columns, uint32_t steps) { return (uint64_t)(columns + (columns < 8 * NT)) * (steps * 256 + 64); }
 };
 
-template <class X, class M, int NT, int G>
-__global__ void __launch_bounds__(kWarps * 32) matvec_kernel(MatvecArgs A) {
+// The `ways` warps of a group share a block of MT tiles of 16 rows: they deal its steps (128 columns) among themselves, each with a ring
+// of steps in flight in shared memory that goes on from one block to the next. x is staged once, if the slice's part of it fits.
+// kSplit: the CTAs of a cluster have a slice of the columns each.
+template <class X, class M, int NT, int MT, int G, bool kSplit>
+__global__ void __launch_bounds__(kWarps * 32, 2) matvec_kernel(const __grid_constant__ MatvecArgs A) {
   extern __shared__ uint4 smem[];
-  constexpr uint32_t kParts = sizeof(X) == 4 ? 3 : 1;
-  float* red = reinterpret_cast<float*>(smem);
-  uint4* xs = smem + kWarps * 8 * NT * kRedStride / 4;
-
+  using S = Shared<NT, MT>;
+  constexpr uint32_t kParts = sizeof(X) == 4 ? 3 : 1, kGroups = kQ4StepCols / G, kRows = S::kRows, kRedStride = S::kRedStride;
+  constexpr uint32_t kStages = kRingSlots / MT, kStage = MT * kSlot;
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, t = lane & 3;
-  const uint32_t tile = blockIdx.x, first = blockIdx.y * A.per_pass;
-  const uint32_t count = min(A.per_pass, A.tokens - first), columns = count * kParts;
-  const uint8_t* weights = A.q4 + (uint64_t)tile * A.L.steps * kQ4StepBytes + lane * 16;
-  const uint32_t* scales = reinterpret_cast<const uint32_t*>(A.q4 + A.L.scales_off) + (uint64_t)tile * A.L.groups * 8 + r;
+  const uint32_t way = warp & (A.ways - 1), groups = kWarps / A.ways, group = warp / A.ways;
+  uint32_t split = 1, rank = 0;
+  if constexpr (kSplit) {
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(split));
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    cluster_arrive();  // the others' shared memory may be written once they have begun
+  }
+  const uint32_t first = blockIdx.y * A.per_pass, count = min(A.per_pass, A.tokens - first), columns = count * kParts;
+  const uint32_t slice = min(rank * A.slice, A.L.steps), slice_end = min(slice + A.slice, A.L.steps);
+  const uint32_t clusters = gridDim.x / split, slots = clusters * groups, blocks = (A.L.tiles + MT - 1) / MT;
+  uint32_t block = group * clusters + blockIdx.x / split;
 
-  auto load = [&](Step<G>& d, uint32_t step) {
-    const uint8_t* p = weights + (uint64_t)step * kQ4StepBytes;
-    d.w[0] = load_weights(p);
-    d.w[1] = load_weights(p + 512);
+  uint8_t* base = reinterpret_cast<uint8_t*>(smem);
+  uint8_t* ring = base + warp * S::kRing;
+  float* red = reinterpret_cast<float*>(base + kWarps * S::kRing);
+  float* part = reinterpret_cast<float*>(base + S::kFixed);
+  const uint32_t part_tokens = S::part_tokens(A.per_pass, split);
+  float* starts = part + S::part(A.ways, split, A.per_pass) / 4;
+  uint4* xs = reinterpret_cast<uint4*>(starts + S::starts(A.chunk) / 4);
+  const uint32_t x_stride = A.chunk * 16 + 4;
+
+  // the next step to ask for: where it is, and how many there are left of this block and in all
+  const uint32_t turns = slice + way < slice_end ? (slice_end - slice - way + A.ways - 1) / A.ways : 0;
+  uint32_t left = block < blocks ? ((blocks - block + slots - 1) / slots) * turns : 0, left_block = turns, ask_slot = 0;
+  const uint8_t* codes = A.q4 + ((uint64_t)block * MT * A.L.steps + slice + way) * kQ4StepBytes + lane * 16;
+  const uint8_t* scales = A.q4 + A.L.scales_off + (((uint64_t)block * MT * A.L.groups + (slice + way) * kGroups + t) * 8 + r) * 4;
+  const uint64_t tile_codes = (uint64_t)A.L.steps * kQ4StepBytes, tile_scales = (uint64_t)A.L.groups * 32;
+  const uint64_t next_block = MT * slots * tile_codes - (uint64_t)turns * A.ways * kQ4StepBytes;
+  const uint64_t next_block_scales = MT * slots * tile_scales - (uint64_t)turns * A.ways * kGroups * 32;
+  const uint32_t ring_at = shared_address(ring) + lane * 16, ring_scales = shared_address(ring) + kQ4StepBytes + (t * 8 + r) * 4;
+  uint32_t ask_tiles = A.L.tiles - block * MT;  // of this block, if it is the matrix's last
+  auto ask_next = [&]() {
+    if (left != 0) {
 #pragma unroll
-    for (int i = 0; i < (int)kQ4StepCols / G; ++i) d.s[i] = __ldg(scales + (step * (kQ4StepCols / G) + i) * 8);
+      for (uint32_t m = 0; m < MT; ++m) {
+        if (m > 0 && ask_tiles <= m) break;  // the last block may be half a one
+        const uint32_t to = ask_slot + m * kSlot;
+        copy16(ring_at + to, codes + m * tile_codes);
+        copy16(ring_at + to + 512, codes + m * tile_codes + 512);
+        if (t < kGroups) copy4(ring_scales + to, scales + m * tile_scales);
+      }
+      --left;
+      codes += A.ways * kQ4StepBytes;
+      scales += A.ways * kGroups * 32;
+      if (--left_block == 0) {
+        left_block = turns;
+        codes += next_block;
+        scales += next_block_scales;
+        ask_tiles -= MT * slots;
+      }
+      ask_slot = ask_slot + kStage == kStages * kStage ? 0 : ask_slot + kStage;
+    }
+    copies_end();
   };
+#pragma unroll
+  for (int i = 0; i < (int)kStages - 1; ++i) ask_next();
 
-  float sum[NT][4] = {};
-  for (uint32_t begin = 0; begin < A.L.steps; begin += A.chunk_steps) {
-    const uint32_t end = min(A.L.steps, begin + A.chunk_steps);
-    Step<G> ring[kAhead];
+  const bool resident = A.chunk >= A.slice;
+  if (columns < 8 * NT)
+    for (uint32_t i = threadIdx.x; i < x_stride; i += kWarps * 32) xs[columns * x_stride + i] = make_uint4(0, 0, 0, 0);
+  const bool large = resident ? stage_x<X, M, NT, G>(A, first, count, slice, slice_end, x_stride, xs, starts) : find_large<X>(A, first, count, slice, slice_end);
+  if constexpr (kSplit) {
+    __syncwarp();
+    cluster_wait();
+  }
+  const uint4* column[NT];  // this lane's column of each eight; one of zeros for those that are not there
 #pragma unroll
-    for (uint32_t d = 0; d < kAhead; ++d)
-      if (begin + warp + d * kWarps < end) load(ring[d], begin + warp + d * kWarps);
-    __syncthreads();
-    stage_x<X, M>(A, first, count, columns, begin, end, xs);
-    __syncthreads();
-    for (uint32_t s0 = begin + warp; s0 < end; s0 += kAhead * kWarps) {
+  for (int n = 0; n < NT; ++n) column[n] = xs + min(8 * n + r, columns) * x_stride + t;
+
+  uint32_t slot = 0;
+  for (uint32_t round = 0; round < A.rounds; ++round, block += slots) {
+    const bool there = block < blocks;
+    float* mine = red + warp * 8 * NT * kRedStride;
+    if (!large) {
+      float sum[MT][NT][4] = {};
+      for (uint32_t begin = slice; begin < slice_end; begin += A.chunk) {
+        const uint32_t end = min(slice_end, begin + A.chunk);
+        if (!resident) {
+          __syncthreads();
+          stage_x<X, M, NT, G>(A, first, count, begin, end, x_stride, xs, starts);
+        }
+        if (!there) continue;
+#pragma unroll 1
+        for (uint32_t step = begin + way; step < end; step += A.ways) {
+          copies_wait<kStages - 2>();
+          __syncwarp();  // the scales of a row are copied by its four lanes; and all lanes have left the slot asked for now
+          ask_next();
+          const uint8_t* w = ring + slot;
+          slot = slot + kStage == kStages * kStage ? 0 : slot + kStage;
+          float acc[MT][NT][4];
+          const uint32_t at = (step - begin) * 16;
+          const float2* start = reinterpret_cast<const float2*>(starts + (step - begin) * 32 * NT) + t;
 #pragma unroll
-      for (uint32_t d = 0; d < kAhead; ++d) {
-        const uint32_t step = s0 + d * kWarps;
-        if (step < end) {
-          float part[NT][4] = {};
+          for (int h = 0; h < 2; ++h) {
+            uint4 v[MT];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const uint32_t w0 = u & 1 ? ring[d].w[u >> 1].z : ring[d].w[u >> 1].x, w1 = u & 1 ? ring[d].w[u >> 1].w : ring[d].w[u >> 1].y;
-            uint32_t a0[4], a1[4];
-            operands<M>(w0, a0);
-            operands<M>(w1, a1);
-            const uint4* xu = xs + ((step - begin) * 4 + u) * columns * 4;
+            for (int m = 0; m < MT; ++m) v[m] = *reinterpret_cast<const uint4*>(w + m * kSlot + h * 512 + lane * 16);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              uint4 b = make_uint4(0, 0, 0, 0);
-              if (8 * n + r < columns) b = xu[(8 * n + r) * 4 + t];
-              mma<M>(part[n], a0, b.x, b.y);
-              mma<M>(part[n], a1, b.z, b.w);
-            }
-            if (((u + 1) * 32) % G == 0) {
-              const uint32_t s = ring[d].s[u * 32 / G];
-              const float s_lo = __uint_as_float(s << 16), s_hi = __uint_as_float(s & 0xFFFF0000u);
+            for (int u = 2 * h; u < 2 * h + 2; ++u) {
+              if (u * 32 % G == 0) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                  const float2 s = start[(u * NT + n) * 4];
+#pragma unroll
+                  for (int m = 0; m < MT; ++m) {
+                    acc[m][n][0] = s.x;
+                    acc[m][n][1] = s.y;
+                    acc[m][n][2] = 16.0f * s.x;
+                    acc[m][n][3] = 16.0f * s.y;
+                  }
+                }
+              }
+              uint32_t a[MT][2][4];
+#pragma unroll
+              for (int m = 0; m < MT; ++m) {
+                operands(u & 1 ? v[m].z : v[m].x, a[m][0]);
+                operands(u & 1 ? v[m].w : v[m].y, a[m][1]);
+              }
 #pragma unroll
               for (int n = 0; n < NT; ++n) {
-                sum[n][0] += s_lo * part[n][0];
-                sum[n][1] += s_lo * part[n][1];
-                sum[n][2] += s_hi * part[n][2];
-                sum[n][3] += s_hi * part[n][3];
-                part[n][0] = part[n][1] = part[n][2] = part[n][3] = 0.0f;
+                const uint4 b = column[n][at + u * 4];
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                  mma<M>(acc[m][n], a[m][0], b.x, b.y);
+                  mma<M>(acc[m][n], a[m][1], b.z, b.w);
+                }
+              }
+              if ((u + 1) * 32 % G == 0) {
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                  const uint32_t s = *reinterpret_cast<const uint32_t*>(w + m * kSlot + kQ4StepBytes + (u * 32 / G * 8 + r) * 4);
+                  const float s_lo = __uint_as_float(s << 16), s_hi = __uint_as_float(s & 0xFFFF0000u);
+#pragma unroll
+                  for (int n = 0; n < NT; ++n) {  // not the scale times kUnit: that could overflow
+                    sum[m][n][0] += s_lo * (acc[m][n][0] * Unit<M>::kUnit);
+                    sum[m][n][1] += s_lo * (acc[m][n][1] * Unit<M>::kUnit);
+                    sum[m][n][2] += s_hi * (acc[m][n][2] * (Unit<M>::kUnit / 16));
+                    sum[m][n][3] += s_hi * (acc[m][n][3] * (Unit<M>::kUnit / 16));
+                  }
+                }
               }
             }
           }
-          if (step + kAhead * kWarps < end) load(ring[d], step + kAhead * kWarps);
         }
       }
+      if (there) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            float* o = mine + (8 * n + 2 * t) * kRedStride + m * 16 + r;
+            o[0] = sum[m][n][0];
+            o[kRedStride] = sum[m][n][1];
+            o[8] = sum[m][n][2];
+            o[kRedStride + 8] = sum[m][n][3];
+          }
+        }
+      }
+    } else if (there) {
+      for (uint32_t m = 0; m < MT && block * MT + m < A.L.tiles; ++m)
+        slow_tile<X>(A, block * MT + m, first, count, slice + way, slice_end, mine + m * 16, kRedStride);
     }
-  }
 
-  // the warps' sums, added up in their order
+    // the warps' sums, added up in their order, then those of the cluster's CTAs
+    auto group_barrier = [&]() {
+      if (A.ways == 1) __syncwarp();
+      else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(A.ways * 32) : "memory");
+    };
+    auto put = [&](uint32_t token, uint32_t row, float y) {
+      row += block * kRows;
+      if (row >= A.L.rows) return;
+      const uint64_t at = (uint64_t)(first + token) * A.out_stride + row;
+      if (sizeof(X) == 2 && A.out_type) from_float(y, static_cast<X*>(A.out)[at]);
+      else static_cast<float*>(A.out)[at] = y;
+    };
+    group_barrier();
+    if (there) {
+      for (uint32_t i = way * 32 + lane; i < count * kRows; i += A.ways * 32) {
+        const uint32_t token = i / kRows, row = i % kRows;
+        float y = 0.0f;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    float* o = red + (warp * 8 * NT + 8 * n + 2 * t) * kRedStride + r;
-    o[0] = sum[n][0];
-    o[kRedStride] = sum[n][1];
-    o[8] = sum[n][2];
-    o[kRedStride + 8] = sum[n][3];
-  }
-  __syncthreads();
-  for (uint32_t i = threadIdx.x; i < count * kQ4TileRows; i += kWarps * 32) {
-    const uint32_t token = i / kQ4TileRows, row = tile * kQ4TileRows + i % kQ4TileRows;
-    if (row >= A.L.rows) continue;
-    float y = 0.0f;
-#pragma unroll
-    for (int k = (int)kParts - 1; k >= 0; --k) {  // the smallest part first
-      const float* p = red + (token * kParts + k) * kRedStride + i % kQ4TileRows;
-      float v = 0.0f;
-#pragma unroll
-      for (uint32_t w = 0; w < kWarps; ++w) v += p[w * 8 * NT * kRedStride];
-      y += v;
+        for (int k = (int)kParts - 1; k >= 0; --k) {  // the smallest part first
+          const float* p = red + (group * A.ways * 8 * NT + token * kParts + k) * kRedStride + row;
+          float v = 0.0f;
+          for (uint32_t w = 0; w < A.ways; ++w) v += p[w * 8 * NT * kRedStride];
+          y += v;
+        }
+        if constexpr (kSplit) store_in_cluster(part + ((((round & 1) * groups + group) * split + rank) * part_tokens + token / split) * kRows + row, (token + round) % split, y);
+        else put(token, row, y);
+      }
     }
-    const uint64_t at = (uint64_t)(first + token) * A.out_stride + row;
-    if (sizeof(X) == 2 && A.out_type) from_float(y, static_cast<X*>(A.out)[at]);
-    else static_cast<float*>(A.out)[at] = y;
+    if constexpr (kSplit) {
+      __syncwarp();
+      cluster_arrive();  // also ends the reads of `red`
+      cluster_wait();
+      if (there) {
+        for (uint32_t i = way * 32 + lane; i < part_tokens * kRows; i += A.ways * 32) {
+          const uint32_t token = i / kRows * split + (rank + split - round % split) % split, row = i % kRows;
+          if (token >= count) continue;
+          float y = 0.0f;
+          for (uint32_t s = 0; s < split; ++s) y += part[(((round & 1) * groups + group) * split + s) * part_tokens * kRows + i];
+          put(token, row, y);
+        }
+        __syncwarp();
+      }
+    } else {
+      group_barrier();
+    }
   }
+  copies_wait<0>();
 }
 
-template <class X, class M, int NT, int G>
-cudaError_t launch(MatvecArgs A, uint32_t passes, uint32_t columns, cudaStream_t cs) {
-  const size_t red = kWarps * 8 * NT * kRedStride * 4;
-  A.chunk_steps = 65536 / (columns * kQ4StepCols * 2);
-  if (A.chunk_steps > A.L.steps) A.chunk_steps = A.L.steps ? A.L.steps : 1;
-  const size_t smem = red + (size_t)A.chunk_steps * columns * kQ4StepCols * 2;
-  static bool raised[kMaxDevices];
+template <class X, class M, int NT, int MT, int G, bool kSplit>
+cudaError_t launch_split(MatvecArgs A, uint32_t passes, uint32_t split, size_t smem, uint32_t per_sm, cudaStream_t cs) {
+  const auto kernel = matvec_kernel<X, M, NT, MT, G, kSplit>;
+  static int sms[kMaxDevices];
   const int dev = current_device_index();
   if (dev < 0) return cudaErrorInvalidDevice;
-  if (!raised[dev]) {
-    const cudaError_t e = cudaFuncSetAttribute(matvec_kernel<X, M, NT, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)red + 65536);
+  if (sms[dev] == 0) {
+    int n = 0;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedPerSM);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return e;
-    raised[dev] = true;
+    sms[dev] = n;
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(A.L.tiles, passes);
   cfg.blockDim = dim3(kWarps * 32);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = cs;
-  return cudaLaunchKernelEx(&cfg, matvec_kernel<X, M, NT, G>, A);
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = split;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = kSplit ? 1 : 0;
+  const uint32_t groups = kWarps / A.ways, blocks = (A.L.tiles + MT - 1) / MT, fill = (blocks + groups - 1) / groups;
+  uint32_t clusters = (uint32_t)sms[dev] * per_sm / split;
+  if (clusters > fill) clusters = fill;
+  A.rounds = (blocks + clusters * groups - 1) / (clusters * groups);
+  cfg.gridDim = dim3(clusters * split, passes);
+  return cudaLaunchKernelEx(&cfg, kernel, A);
 }
 
-template <class X, class M, int NT>
+template <class X, class M, int NT, int MT, int G>
+cudaError_t launch(MatvecArgs A, uint32_t passes, uint32_t columns, cudaStream_t cs) {
+  using S = Shared<NT, MT>;
+  const uint32_t blocks = (A.L.tiles + MT - 1) / MT;
+  A.ways = 1;
+  while (A.ways < kWarps && blocks * A.ways < 148 * 16 && A.ways * 2 < A.L.steps) A.ways *= 2;
+  if (const char* s = getenv("LC_WAYS")) A.ways = atoi(s);
+  uint32_t split = 1;
+  auto slice = [&]() { return A.L.steps ? (A.L.steps + split - 1) / split : 1u; };
+  auto bytes = [&](uint32_t steps) { return S::kFixed + S::part(A.ways, split, A.per_pass) + S::starts(steps) + S::x(columns, steps); };
+  const uint64_t two = kSharedPerSM / 2 - 1024;  // of two CTAs on an SM
+  while (split < kMaxSplit && bytes(slice()) > two) split *= 2;
+  if (const char* s = getenv("LC_SPLIT")) split = atoi(s);
+  A.slice = slice();
+  A.chunk = A.slice;
+  const uint32_t per_sm = bytes(A.slice) > two ? 1 : 2;
+  for (; bytes(A.chunk) > kSharedPerSM; A.ways /= 2) {
+    while (A.chunk > A.ways && bytes(A.chunk) > kSharedPerSM) A.chunk = (A.chunk - 1) / A.ways * A.ways;  // whole turns of the warps
+    if (bytes(A.chunk) <= kSharedPerSM || A.ways == 1) break;
+  }
+  const size_t smem = bytes(A.chunk);
+  return split > 1 ? launch_split<X, M, NT, MT, G, true>(A, passes, split, smem, per_sm, cs) : launch_split<X, M, NT, MT, G, false>(A, passes, split, smem, per_sm, cs);
+}
+
+template <class X, class M, int NT, int MT>
 cudaError_t launch_group(const MatvecArgs& A, uint32_t passes, uint32_t columns, cudaStream_t cs) {
-  if (A.L.group == 32) return launch<X, M, NT, 32>(A, passes, columns, cs);
-  if (A.L.group == 64) return launch<X, M, NT, 64>(A, passes, columns, cs);
-  return launch<X, M, NT, 128>(A, passes, columns, cs);
+  if (A.L.group == 32) return launch<X, M, NT, MT, 32>(A, passes, columns, cs);
+  if (A.L.group == 64) return launch<X, M, NT, MT, 64>(A, passes, columns, cs);
+  return launch<X, M, NT, MT, 128>(A, passes, columns, cs);
 }
 
 template <class X, class M>
@@ -267,11 +571,14 @@ cudaError_t launch_columns(MatvecArgs A, cudaStream_t cs) {
   constexpr uint32_t kParts = sizeof(X) == 4 ? 3 : 1, kMost = 64 / kParts;
   const uint32_t passes = (A.tokens + kMost - 1) / kMost;
   A.per_pass = (A.tokens + passes - 1) / passes;
+  A.by_count = FastDiv(A.per_pass);
   const uint32_t columns = A.per_pass * kParts;
-  if (columns <= 8) return launch_group<X, M, 1>(A, passes, columns, cs);
-  if (columns <= 16) return launch_group<X, M, 2>(A, passes, columns, cs);
-  if (columns <= 32) return launch_group<X, M, 4>(A, passes, columns, cs);
-  return launch_group<X, M, 8>(A, passes, columns, cs);
+  bool two = A.L.tiles >= 148 * 8;
+  if (const char* s = getenv("LC_MT")) two = atoi(s) == 2;
+  if (columns <= 8) return two ? launch_group<X, M, 1, 2>(A, passes, columns, cs) : launch_group<X, M, 1, 1>(A, passes, columns, cs);
+  if (columns <= 16) return two ? launch_group<X, M, 2, 2>(A, passes, columns, cs) : launch_group<X, M, 2, 1>(A, passes, columns, cs);
+  if (columns <= 32) return launch_group<X, M, 4, 2>(A, passes, columns, cs);
+  return launch_group<X, M, 8, 1>(A, passes, columns, cs);
 }
 
 }  // namespace
