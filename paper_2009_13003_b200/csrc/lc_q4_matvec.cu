@@ -13,6 +13,7 @@
 // what is too much by it is taken off in fp32: the accumulators start at -8 times the group's sum of x. To keep the products with
 // bf16 vectors (and parts of fp32 ones) in fp32's normal range, x is multiplied by 2^80 when it is staged. Vectors with values of
 // 2^40 and more, Inf or NaN among them, take plain multiplications instead (slow_tile), a CTA for itself.
+#include <stdio.h>
 #include <stdlib.h>
 #include <type_traits>
 
@@ -21,10 +22,6 @@
 namespace lc {
 namespace {
 
-constexpr uint32_t kWarps = 8;
-constexpr uint32_t kStepScales = 128;   // bytes kept for the scales of a step: 16 rows, up to 4 groups
-constexpr uint32_t kSlot = kQ4StepBytes + kStepScales;
-constexpr uint32_t kRingSlots = 6;      // steps of 16 rows in the ring of a warp
 constexpr uint32_t kMaxSplit = 8;       // CTAs of a cluster that share a tile's columns
 constexpr uint32_t kSharedPerSM = 227 * 1024;
 
@@ -36,7 +33,10 @@ struct MatvecArgs {
   Q4Layout L;
   uint32_t tokens, per_pass;  // vectors in all, and of one pass (blockIdx.y)
   int out_type;
-  uint32_t ways;              // warps of a CTA that share a tile's columns
+  uint32_t ways;              // warps of a CTA that share a block of rows
+  uint32_t direct;            // 1 if a warp's sums are the results: nothing to add up
+  uint32_t stages;            // steps in the ring of a warp
+  uint32_t aligned;           // 1 if every vector begins on a 16-byte boundary
   uint32_t slice;             // steps of a CTA: all of them, or its share in the cluster
   uint32_t chunk;             // steps whose part of x is in shared memory at a time
   uint32_t rounds;            // blocks of rows that a group of warps goes through, at most
@@ -47,13 +47,13 @@ template <class M>
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
 template <>
 __device__ __forceinline__ void mma<__nv_bfloat16>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 template <>
 __device__ __forceinline__ void mma<__half>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -158,101 +158,6 @@ __device__ __forceinline__ void store_piece(const uint32_t (&raw)[2 * sizeof(X)]
   }
 }
 
-// x of the steps [begin, end) into shared memory, one column of the product behind the other: `stride` 16-byte pieces, an odd
-// number of units (32 columns of the matrix, four pieces) of which lanes 4 r + t multiply piece t, so that eight columns lie in
-// eight different parts of the banks. Beside it, where the accumulators start: per group (at its first unit) and column of the
-// product. A thread asks for four pieces before it stores the first. Returns, in every thread, whether some value is too large.
-template <class X, class M, int NT, int G>
-__device__ __forceinline__ bool stage_x(const MatvecArgs& A, uint32_t first, uint32_t count, uint32_t begin, uint32_t end, uint32_t stride, uint4* xs, float* starts) {
-  constexpr int kBatch = 4, kParts = sizeof(X) == 4 ? 3 : 1;
-  const uint32_t pieces = (end - begin) * 4 * count, t = threadIdx.x & 3u, step = kWarps * 8, quad = 15u << (threadIdx.x & 28u);
-  bool large = false;
-  for (uint32_t i0 = threadIdx.x >> 2; i0 < pieces; i0 += kBatch * step) {
-    uint32_t raw[kBatch][2 * sizeof(X)], unit[kBatch], token[kBatch];
-#pragma unroll
-    for (int b = 0; b < kBatch; ++b) {
-      const uint32_t i = i0 + b * step;
-      unit[b] = count == A.by_count.d ? A.by_count.div(i) : i / count;
-      token[b] = i - unit[b] * count;
-      load_piece<X>(A, first + token[b], (begin * 4 + unit[b]) * 32 + 8 * t, i < pieces, raw[b]);
-    }
-#pragma unroll
-    for (int b = 0; b < kBatch; ++b) {
-      if (i0 + b * step >= pieces) break;  // the same for the four threads of a unit
-      large |= too_large<X>(raw[b]);
-      float sum[kParts];
-      store_piece<X, M>(raw[b], xs + token[b] * kParts * stride + unit[b] * 4 + t, stride, sum);
-#pragma unroll
-      for (int k = 0; k < kParts; ++k) {
-        sum[k] += __shfl_xor_sync(quad, sum[k], 1);
-        sum[k] += __shfl_xor_sync(quad, sum[k], 2);
-        if (t == 0) starts[unit[b] * 8 * NT + token[b] * kParts + k] = sum[k] * (-8.0f / Unit<M>::kUp / Unit<M>::kUnit);
-      }
-    }
-  }
-  large = __syncthreads_or(large);
-  if (G > 32) {
-    constexpr uint32_t kUnits = G / 32;
-    for (uint32_t i = threadIdx.x; i < (end - begin) * (4 / kUnits) * count * kParts; i += kWarps * 32) {
-      const uint32_t g = i / (count * kParts);
-      float* p = starts + g * kUnits * 8 * NT + (i - g * count * kParts);
-      float s = p[0];
-#pragma unroll
-      for (uint32_t u = 1; u < kUnits; ++u) s += p[u * 8 * NT];
-      p[0] = s;
-    }
-    __syncthreads();
-  }
-  return large;
-}
-
-// Whether a value of the vectors in the steps [begin, end) is too large, for when they are not staged all at once.
-template <class X>
-__device__ __forceinline__ bool find_large(const MatvecArgs& A, uint32_t first, uint32_t count, uint32_t begin, uint32_t end) {
-  bool large = false;
-  for (uint32_t i = threadIdx.x; i < (end - begin) * 16 * count; i += kWarps * 32) {
-    const uint32_t token = i / ((end - begin) * 16);
-    uint32_t raw[2 * sizeof(X)];
-    load_piece<X>(A, first + token, (begin * 16 + (i - token * (end - begin) * 16)) * 8, true, raw);
-    large |= too_large<X>(raw);
-  }
-  return __syncthreads_or(large);
-}
-
-// A warp's sums for 16 rows by plain multiplications: what the definition says for Inf, NaN and large values.
-template <class X>
-__device__ __noinline__ void slow_tile(const MatvecArgs& A, uint32_t tile, uint32_t first, uint32_t count, uint32_t begin, uint32_t end, float* red, uint32_t red_stride) {
-  constexpr uint32_t kParts = sizeof(X) == 4 ? 3 : 1;
-  const uint32_t lane = threadIdx.x & 31, r = lane >> 2, t = lane & 3;
-  for (uint32_t token = 0; token < count; ++token) {
-    const X* x = static_cast<const X*>(A.x) + (uint64_t)(first + token) * A.x_stride;
-    float y[2] = {0.0f, 0.0f};
-    for (uint32_t step = begin; step < end; step += A.ways) {
-      for (uint32_t h = 0; h < 4; ++h) {
-        const uint2 w = __ldg(reinterpret_cast<const uint2*>(A.q4 + ((uint64_t)tile * A.L.steps + step) * kQ4StepBytes + (h / 2) * 512 + lane * 16 + (h & 1) * 8));
-        const uint32_t col = step * kQ4StepCols + h * 32 + 8 * t;
-        const uint32_t s = __ldg(reinterpret_cast<const uint32_t*>(A.q4 + A.L.scales_off) + ((uint64_t)tile * A.L.groups + col / A.L.group) * 8 + r);
-        float p[2] = {0.0f, 0.0f};
-        for (uint32_t e = 0; e < 8; ++e) {
-          if (col + e >= A.L.cols) break;
-          const float v = to_float(x[col + e]);
-          const uint32_t n = (e < 4 ? w.x : w.y) >> (16 * (e & 1) + 8 * ((e >> 1) & 1));
-          p[0] += (float)((int)(n & 15u) - 8) * v;
-          p[1] += (float)((int)((n >> 4) & 15u) - 8) * v;
-        }
-        y[0] += __uint_as_float(s << 16) * p[0];
-        y[1] += __uint_as_float(s & 0xFFFF0000u) * p[1];
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      y[i] += __shfl_xor_sync(0xFFFFFFFFu, y[i], 1);
-      y[i] += __shfl_xor_sync(0xFFFFFFFFu, y[i], 2);
-      if (t < kParts) red[(token * kParts + t) * red_stride + r + 8 * i] = t == 0 ? y[i] : 0.0f;
-    }
-  }
-}
-
 __device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void copy16(uint32_t to, const void* from) {
   asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
@@ -261,6 +166,141 @@ __device__ __forceinline__ void copy4(uint32_t to, const void* from) { asm volat
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int kLeft>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
+// Waits for all but the latest `left` (at most 4) groups of copies.
+__device__ __forceinline__ void copies_wait(uint32_t left) {
+  if (left >= 4) copies_wait<4>();
+  else if (left == 3) copies_wait<3>();
+  else if (left == 2) copies_wait<2>();
+  else if (left == 1) copies_wait<1>();
+  else copies_wait<0>();
+}
+
+
+// x of the steps [begin, end) into shared memory, one column of the product behind the other: `stride` 16-byte pieces, an odd
+// number of units (32 columns of the matrix, four pieces) of which lanes 4 r + t multiply piece t, so that eight columns lie in
+// eight different parts of the banks. The pieces of a group of columns are its neighbouring threads'.
+template <int G>
+struct Pieces {  // how a thread's pieces follow each other
+  static constexpr uint32_t kUnits = G / 32;
+  uint32_t i, count, unit, token;
+  __device__ __forceinline__ void at(const MatvecArgs& A, uint32_t i_) {
+    i = i_;
+    const uint32_t rest = i / kUnits, g = count == A.by_count.d ? A.by_count.div(rest) : rest / count;
+    unit = g * kUnits + (i & (kUnits - 1));
+    token = rest - g * count;
+  }
+};
+
+// Begins to copy them as they are (an fp32 piece to where its first two parts will be), if the vectors are aligned.
+template <class X, int G>
+__device__ __forceinline__ void copy_x(const MatvecArgs& A, uint32_t first, uint32_t count, uint32_t begin, uint32_t end, uint32_t stride, uint4* xs) {
+  constexpr int kParts = sizeof(X) == 4 ? 3 : 1;
+  if (A.aligned) {
+    Pieces<G> p;
+    p.count = count;
+    for (uint32_t i = threadIdx.x >> 2; i < (end - begin) * 4 * count; i += blockDim.x / 4) {
+      p.at(A, i);
+      const uint32_t t = threadIdx.x & 3u, col = (begin * 4 + p.unit) * 32 + 8 * t;
+      const X* from = static_cast<const X*>(A.x) + (uint64_t)(first + p.token) * A.x_stride + col;
+      if (col + 8 <= A.L.cols) {
+        const uint32_t to = shared_address(xs + p.token * kParts * stride + p.unit * 4 + t);
+#pragma unroll
+        for (int k = 0; k < (int)sizeof(X) / 2; ++k) copy16(to + k * stride * 16, reinterpret_cast<const uint4*>(from) + k);
+      }
+    }
+  }
+  copies_end();
+}
+
+// Makes columns of the product of them, in place or (not aligned) from memory, several at a time. Beside them, per group and column, where the accumulators
+// start. Returns, in every thread, whether some value is too large. The copies of the calling thread have arrived.
+template <class X, class M, int NT, int G>
+__device__ __forceinline__ bool stage_x(const MatvecArgs& A, uint32_t first, uint32_t count, uint32_t begin, uint32_t end, uint32_t stride, uint4* xs, float* starts) {
+  constexpr int kBatch = 1, kParts = sizeof(X) == 4 ? 3 : 1;
+  constexpr uint32_t kLanes = G / 8;  // that have a group's pieces
+  const uint32_t pieces = (end - begin) * 4 * count, lane = threadIdx.x & 31, t = lane & 3u, step = blockDim.x / 4;
+  const uint32_t mine = (uint32_t)((1ull << kLanes) - 1) << (lane & ~(kLanes - 1));
+  bool large = false;
+  for (uint32_t i0 = threadIdx.x >> 2; i0 < pieces; i0 += kBatch * step) {
+    uint32_t raw[kBatch][2 * sizeof(X)];
+    Pieces<G> p[kBatch];
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      p[b].count = count;
+      p[b].at(A, i0 + b * step);
+      const uint32_t col = (begin * 4 + p[b].unit) * 32 + 8 * t;
+      if (A.aligned && p[b].i < pieces && col + 8 <= A.L.cols) {
+#pragma unroll
+        for (int k = 0; k < (int)sizeof(X) / 2; ++k) {
+          const uint4 v = xs[(p[b].token * kParts + k) * stride + p[b].unit * 4 + t];
+          raw[b][4 * k] = v.x, raw[b][4 * k + 1] = v.y, raw[b][4 * k + 2] = v.z, raw[b][4 * k + 3] = v.w;
+        }
+      } else {
+        load_piece<X>(A, first + p[b].token, col, p[b].i < pieces, raw[b]);
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      if (p[b].i >= pieces) break;  // the same for the threads of a group
+      large |= too_large<X>(raw[b]);
+      float sum[kParts];
+      store_piece<X, M>(raw[b], xs + p[b].token * kParts * stride + p[b].unit * 4 + t, stride, sum);
+#pragma unroll
+      for (int k = 0; k < kParts; ++k) {
+#pragma unroll
+        for (uint32_t d = 1; d < kLanes; d *= 2) sum[k] += __shfl_xor_sync(mine, sum[k], d);
+        if ((lane & (kLanes - 1)) == 0) starts[p[b].unit / (G / 32) * 8 * NT + p[b].token * kParts + k] = sum[k] * (-8.0f / Unit<M>::kUp / Unit<M>::kUnit);
+      }
+    }
+  }
+  return __syncthreads_or(large);
+}
+
+// Whether a value of the vectors in the steps [begin, end) is too large, for when they are not staged all at once.
+template <class X>
+__device__ __forceinline__ bool find_large(const MatvecArgs& A, uint32_t first, uint32_t count, uint32_t begin, uint32_t end) {
+  bool large = false;
+  for (uint32_t i = threadIdx.x; i < (end - begin) * 16 * count; i += blockDim.x) {
+    const uint32_t token = i / ((end - begin) * 16);
+    uint32_t raw[2 * sizeof(X)];
+    load_piece<X>(A, first + token, (begin * 16 + (i - token * (end - begin) * 16)) * 8, true, raw);
+    large |= too_large<X>(raw);
+  }
+  return __syncthreads_or(large);
+}
+
+// A warp's sums for one vector and rows r and r + 8 of a tile by plain multiplications, in all four lanes of r: what the definition
+// says for Inf, NaN and large values.
+template <class X>
+__device__ __noinline__ float2 slow_sums(const MatvecArgs& A, uint32_t tile, uint32_t token, uint32_t begin, uint32_t end) {
+  const uint32_t lane = threadIdx.x & 31, r = lane >> 2, t = lane & 3;
+  const X* x = static_cast<const X*>(A.x) + (uint64_t)token * A.x_stride;
+  float2 y = make_float2(0.0f, 0.0f);
+  for (uint32_t step = begin; step < end; step += A.ways) {
+    for (uint32_t h = 0; h < 4; ++h) {
+      const uint2 w = __ldg(reinterpret_cast<const uint2*>(A.q4 + ((uint64_t)tile * A.L.steps + step) * kQ4StepBytes + (h / 2) * 512 + lane * 16 + (h & 1) * 8));
+      const uint32_t col = step * kQ4StepCols + h * 32 + 8 * t;
+      const uint32_t s = __ldg(reinterpret_cast<const uint32_t*>(A.q4 + A.L.scales_off) + ((uint64_t)tile * A.L.groups + col / A.L.group) * 8 + r);
+      float2 p = make_float2(0.0f, 0.0f);
+      for (uint32_t e = 0; e < 8; ++e) {
+        if (col + e >= A.L.cols) break;
+        const float v = to_float(x[col + e]);
+        const uint32_t n = (e < 4 ? w.x : w.y) >> (16 * (e & 1) + 8 * ((e >> 1) & 1));
+        p.x += (float)((int)(n & 15u) - 8) * v;
+        p.y += (float)((int)((n >> 4) & 15u) - 8) * v;
+      }
+      y.x += __uint_as_float(s << 16) * p.x;
+      y.y += __uint_as_float(s & 0xFFFF0000u) * p.y;
+    }
+  }
+  __syncwarp();
+#pragma unroll
+  for (int d = 1; d < 4; d *= 2) {
+    y.x += __shfl_xor_sync(0xFFFFFFFFu, y.x, d);
+    y.y += __shfl_xor_sync(0xFFFFFFFFu, y.y, d);
+  }
+  return y;
+}
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -269,30 +309,31 @@ __device__ __forceinline__ void store_in_cluster(float* mine, uint32_t rank, flo
 }
 
 // Shared memory: the warps' rings, their sums, what the cluster's CTAs send each other, where accumulators start, x.
-template <int NT, int MT>
+template <int NT, int MT, int G>
 struct Shared {
+  static constexpr uint32_t kGroups = kQ4StepCols / G, kSlot = kQ4StepBytes + kGroups * 32, kStage = MT * kSlot;  // codes and scales of a step
   static constexpr uint32_t kRows = MT * kQ4TileRows, kRedStride = kRows + 4;  // floats from column to column: the lanes of a store meet in no bank
-  static constexpr uint32_t kRing = kRingSlots * kSlot, kRed = 8 * NT * kRedStride * 4, kFixed = kWarps * (kRing + kRed);
   static __host__ __device__ __forceinline__ uint32_t part_tokens(uint32_t per_pass, uint32_t split) { return split > 1 ? (per_pass + split - 1) / split : 0; }
-  static __host__ __device__ __forceinline__ uint32_t part(uint32_t ways, uint32_t split, uint32_t per_pass) {  // [2][groups][split][part_tokens][kRows] floats
-    return 2 * (kWarps / ways) * split * part_tokens(per_pass, split) * kRows * 4;
+  static __host__ __device__ __forceinline__ uint32_t red(bool direct, uint32_t warps, uint32_t columns) { return direct ? 0 : warps * columns * kRedStride * 4; }
+  static __host__ __device__ __forceinline__ uint32_t part(uint32_t groups, uint32_t split, uint32_t per_pass) {  // [2][groups][split][part_tokens][kRows] floats
+    return 2 * groups * split * part_tokens(per_pass, split) * kRows * 4;
   }
-  static __host__ __device__ __forceinline__ uint32_t starts(uint32_t steps) { return steps * 4 * 8 * NT * 4; }
-  // a column of zeros behind the others, if the product has more columns than they are
-  static __host__ __device__ __forceinline__ uint64_t x(uint32_t columns, uint32_t steps) { return (uint64_t)(columns + (columns < 8 * NT)) * (steps * 256 + 64); }
+  static __host__ __device__ __forceinline__ uint32_t starts(uint32_t steps) { return steps * kGroups * 8 * NT * 4; }
+  static __host__ __device__ __forceinline__ uint64_t x(uint32_t columns, uint32_t steps) { return (uint64_t)columns * (steps * 256 + 64); }
 };
+constexpr uint32_t kMostWarps = 16;  // on an SM, by their registers
 
 // The `ways` warps of a group share a block of MT tiles of 16 rows: they deal its steps (128 columns) among themselves, each with a ring
 // of steps in flight in shared memory that goes on from one block to the next. x is staged once, if the slice's part of it fits.
 // kSplit: the CTAs of a cluster have a slice of the columns each.
 template <class X, class M, int NT, int MT, int G, bool kSplit>
-__global__ void __launch_bounds__(kWarps * 32, 2) matvec_kernel(const __grid_constant__ MatvecArgs A) {
+__global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid_constant__ MatvecArgs A) {
   extern __shared__ uint4 smem[];
-  using S = Shared<NT, MT>;
-  constexpr uint32_t kParts = sizeof(X) == 4 ? 3 : 1, kGroups = kQ4StepCols / G, kRows = S::kRows, kRedStride = S::kRedStride;
-  constexpr uint32_t kStages = kRingSlots / MT, kStage = MT * kSlot;
-  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, t = lane & 3;
-  const uint32_t way = warp & (A.ways - 1), groups = kWarps / A.ways, group = warp / A.ways;
+  using S = Shared<NT, MT, G>;
+  constexpr uint32_t kParts = sizeof(X) == 4 ? 3 : 1, kGroups = S::kGroups, kRows = S::kRows, kRedStride = S::kRedStride;
+  constexpr uint32_t kSlot = S::kSlot, kStage = S::kStage;
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, r = lane >> 2, t = lane & 3;
+  const uint32_t way = warp & (A.ways - 1), groups = warps / A.ways, group = warp / A.ways;
   uint32_t split = 1, rank = 0;
   if constexpr (kSplit) {
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(split));
@@ -305,13 +346,16 @@ __global__ void __launch_bounds__(kWarps * 32, 2) matvec_kernel(const __grid_con
   uint32_t block = group * clusters + blockIdx.x / split;
 
   uint8_t* base = reinterpret_cast<uint8_t*>(smem);
-  uint8_t* ring = base + warp * S::kRing;
-  float* red = reinterpret_cast<float*>(base + kWarps * S::kRing);
-  float* part = reinterpret_cast<float*>(base + S::kFixed);
-  const uint32_t part_tokens = S::part_tokens(A.per_pass, split);
-  float* starts = part + S::part(A.ways, split, A.per_pass) / 4;
+  const uint32_t ring_bytes = A.stages * kStage;
+  uint8_t* ring = base + warp * ring_bytes;
+  float* red = reinterpret_cast<float*>(base + warps * ring_bytes);
+  const uint32_t part_tokens = S::part_tokens(A.per_pass, split), red_columns = A.per_pass * kParts;
+  float* part = red + S::red(A.direct, warps, red_columns) / 4;
+  float* starts = part + S::part(groups, split, A.per_pass) / 4;
   uint4* xs = reinterpret_cast<uint4*>(starts + S::starts(A.chunk) / 4);
   const uint32_t x_stride = A.chunk * 16 + 4;
+  const bool resident = A.chunk >= A.slice;
+  if (resident) copy_x<X, G>(A, first, count, slice, slice_end, x_stride, xs);
 
   // the next step to ask for: where it is, and how many there are left of this block and in all
   const uint32_t turns = slice + way < slice_end ? (slice_end - slice - way + A.ways - 1) / A.ways : 0;
@@ -342,48 +386,57 @@ __global__ void __launch_bounds__(kWarps * 32, 2) matvec_kernel(const __grid_con
         scales += next_block_scales;
         ask_tiles -= MT * slots;
       }
-      ask_slot = ask_slot + kStage == kStages * kStage ? 0 : ask_slot + kStage;
+      ask_slot = ask_slot + kStage == ring_bytes ? 0 : ask_slot + kStage;
     }
     copies_end();
   };
-#pragma unroll
-  for (int i = 0; i < (int)kStages - 1; ++i) ask_next();
+  for (uint32_t i = 1; i < A.stages; ++i) ask_next();
 
-  const bool resident = A.chunk >= A.slice;
-  if (columns < 8 * NT)
-    for (uint32_t i = threadIdx.x; i < x_stride; i += kWarps * 32) xs[columns * x_stride + i] = make_uint4(0, 0, 0, 0);
-  const bool large = resident ? stage_x<X, M, NT, G>(A, first, count, slice, slice_end, x_stride, xs, starts) : find_large<X>(A, first, count, slice, slice_end);
+  bool large = resident ? false : find_large<X>(A, first, count, slice, slice_end);
   if constexpr (kSplit) {
     __syncwarp();
     cluster_wait();
   }
   const uint4* column[NT];  // this lane's column of each eight; one of zeros for those that are not there
 #pragma unroll
-  for (int n = 0; n < NT; ++n) column[n] = xs + min(8 * n + r, columns) * x_stride + t;
+  for (int n = 0; n < NT; ++n) column[n] = xs + (8 * n + r < columns ? 8 * n + r : 0) * x_stride + t;
 
   uint32_t slot = 0;
   for (uint32_t round = 0; round < A.rounds; ++round, block += slots) {
     const bool there = block < blocks;
-    float* mine = red + warp * 8 * NT * kRedStride;
-    if (!large) {
+    float* mine = red + warp * red_columns * kRedStride;
+    auto put = [&](uint32_t token, uint32_t row, float y) {
+      row += block * kRows;
+      if (row >= A.L.rows) return;
+      const uint64_t at = (uint64_t)(first + token) * A.out_stride + row;
+      if (sizeof(X) == 2 && A.out_type) from_float(y, static_cast<X*>(A.out)[at]);
+      else static_cast<float*>(A.out)[at] = y;
+    };
+    if (!large || round == 0) {
       float sum[MT][NT][4] = {};
       for (uint32_t begin = slice; begin < slice_end; begin += A.chunk) {
         const uint32_t end = min(slice_end, begin + A.chunk);
-        if (!resident) {
-          __syncthreads();
-          stage_x<X, M, NT, G>(A, first, count, begin, end, x_stride, xs, starts);
+        if (!resident || round == 0) {
+          if (!resident) {
+            __syncthreads();
+            copy_x<X, G>(A, first, count, begin, end, x_stride, xs);
+            copies_wait<0>();
+          } else {
+            copies_wait(A.stages - 1);
+          }
+          large |= stage_x<X, M, NT, G>(A, first, count, begin, end, x_stride, xs, starts);
         }
-        if (!there) continue;
+        if (!there || large) continue;
 #pragma unroll 1
         for (uint32_t step = begin + way; step < end; step += A.ways) {
-          copies_wait<kStages - 2>();
+          copies_wait(A.stages - 2);
           __syncwarp();  // the scales of a row are copied by its four lanes; and all lanes have left the slot asked for now
           ask_next();
           const uint8_t* w = ring + slot;
-          slot = slot + kStage == kStages * kStage ? 0 : slot + kStage;
+          slot = slot + kStage == ring_bytes ? 0 : slot + kStage;
           float acc[MT][NT][4];
           const uint32_t at = (step - begin) * 16;
-          const float2* start = reinterpret_cast<const float2*>(starts + (step - begin) * 32 * NT) + t;
+          const float2* start = reinterpret_cast<const float2*>(starts + (step - begin) * kGroups * 8 * NT) + t;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             uint4 v[MT];
@@ -394,7 +447,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) matvec_kernel(const __grid_con
               if (u * 32 % G == 0) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                  const float2 s = start[(u * NT + n) * 4];
+                  const float2 s = start[(u * 32 / G * NT + n) * 4];
 #pragma unroll
                   for (int m = 0; m < MT; ++m) {
                     acc[m][n][0] = s.x;
@@ -425,11 +478,11 @@ __global__ void __launch_bounds__(kWarps * 32, 2) matvec_kernel(const __grid_con
                   const uint32_t s = *reinterpret_cast<const uint32_t*>(w + m * kSlot + kQ4StepBytes + (u * 32 / G * 8 + r) * 4);
                   const float s_lo = __uint_as_float(s << 16), s_hi = __uint_as_float(s & 0xFFFF0000u);
 #pragma unroll
-                  for (int n = 0; n < NT; ++n) {  // not the scale times kUnit: that could overflow
-                    sum[m][n][0] += s_lo * (acc[m][n][0] * Unit<M>::kUnit);
-                    sum[m][n][1] += s_lo * (acc[m][n][1] * Unit<M>::kUnit);
-                    sum[m][n][2] += s_hi * (acc[m][n][2] * (Unit<M>::kUnit / 16));
-                    sum[m][n][3] += s_hi * (acc[m][n][3] * (Unit<M>::kUnit / 16));
+                  for (int n = 0; n < NT; ++n) {
+                    sum[m][n][0] += s_lo * acc[m][n][0];
+                    sum[m][n][1] += s_lo * acc[m][n][1];
+                    sum[m][n][2] += s_hi * acc[m][n][2];
+                    sum[m][n][3] += s_hi * acc[m][n][3];
                   }
                 }
               }
@@ -437,35 +490,43 @@ __global__ void __launch_bounds__(kWarps * 32, 2) matvec_kernel(const __grid_con
           }
         }
       }
-      if (there) {
+      if (there && !large) {
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            float* o = mine + (8 * n + 2 * t) * kRedStride + m * 16 + r;
-            o[0] = sum[m][n][0];
-            o[kRedStride] = sum[m][n][1];
-            o[8] = sum[m][n][2];
-            o[kRedStride + 8] = sum[m][n][3];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t col = 8 * n + 2 * t + (i & 1), row = m * 16 + r + 8 * (i >> 1);
+              const float y = sum[m][n][i] * (i < 2 ? Unit<M>::kUnit : Unit<M>::kUnit / 16);
+              if (col >= columns) continue;
+              if (kParts == 1 && A.direct) put(col, row, y);
+              else mine[col * kRedStride + row] = y;
+            }
           }
         }
       }
-    } else if (there) {
-      for (uint32_t m = 0; m < MT && block * MT + m < A.L.tiles; ++m)
-        slow_tile<X>(A, block * MT + m, first, count, slice + way, slice_end, mine + m * 16, kRedStride);
+    }
+    if (there && large) {
+      for (uint32_t m = 0; m < MT && block * MT + m < A.L.tiles; ++m) {
+        for (uint32_t token = 0; token < count; ++token) {
+          const float2 y = slow_sums<X>(A, block * MT + m, first + token, slice + way, slice_end);
+          const uint32_t row = m * 16 + r;
+          if (kParts == 1 && A.direct) {
+            if (t == 0) put(token, row, y.x), put(token, row + 8, y.y);
+          } else if (t < kParts) {
+            mine[(token * kParts + t) * kRedStride + row] = t == 0 ? y.x : 0.0f;
+            mine[(token * kParts + t) * kRedStride + row + 8] = t == 0 ? y.y : 0.0f;
+          }
+        }
+      }
     }
 
     // the warps' sums, added up in their order, then those of the cluster's CTAs
+    if (kParts == 1 && A.direct) continue;
     auto group_barrier = [&]() {
       if (A.ways == 1) __syncwarp();
       else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(A.ways * 32) : "memory");
-    };
-    auto put = [&](uint32_t token, uint32_t row, float y) {
-      row += block * kRows;
-      if (row >= A.L.rows) return;
-      const uint64_t at = (uint64_t)(first + token) * A.out_stride + row;
-      if (sizeof(X) == 2 && A.out_type) from_float(y, static_cast<X*>(A.out)[at]);
-      else static_cast<float*>(A.out)[at] = y;
     };
     group_barrier();
     if (there) {
@@ -474,9 +535,9 @@ __global__ void __launch_bounds__(kWarps * 32, 2) matvec_kernel(const __grid_con
         float y = 0.0f;
 #pragma unroll
         for (int k = (int)kParts - 1; k >= 0; --k) {  // the smallest part first
-          const float* p = red + (group * A.ways * 8 * NT + token * kParts + k) * kRedStride + row;
+          const float* p = red + (group * A.ways * red_columns + token * kParts + k) * kRedStride + row;
           float v = 0.0f;
-          for (uint32_t w = 0; w < A.ways; ++w) v += p[w * 8 * NT * kRedStride];
+          for (uint32_t w = 0; w < A.ways; ++w) v += p[w * red_columns * kRedStride];
           y += v;
         }
         if constexpr (kSplit) store_in_cluster(part + ((((round & 1) * groups + group) * split + rank) * part_tokens + token / split) * kRows + row, (token + round) % split, y);
@@ -505,20 +566,19 @@ __global__ void __launch_bounds__(kWarps * 32, 2) matvec_kernel(const __grid_con
 }
 
 template <class X, class M, int NT, int MT, int G, bool kSplit>
-cudaError_t launch_split(MatvecArgs A, uint32_t passes, uint32_t split, size_t smem, uint32_t per_sm, cudaStream_t cs) {
+cudaError_t launch_split(MatvecArgs A, uint32_t blocks, uint32_t passes, uint32_t split, uint32_t warps, size_t smem, cudaStream_t cs) {
   const auto kernel = matvec_kernel<X, M, NT, MT, G, kSplit>;
-  static int sms[kMaxDevices];
+  static bool raised[kMaxDevices];
   const int dev = current_device_index();
   if (dev < 0) return cudaErrorInvalidDevice;
-  if (sms[dev] == 0) {
-    int n = 0;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedPerSM);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
-    if (e != cudaSuccess) return e;
-    sms[dev] = n;
+  cudaError_t e;
+  if (!raised[dev]) {
+    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedPerSM)) != cudaSuccess) return e;
+    raised[dev] = true;
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.blockDim = dim3(kWarps * 32);
+  cfg.gridDim = dim3(split, passes);
+  cfg.blockDim = dim3(warps * 32);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = cs;
   cudaLaunchAttribute at[1];
@@ -526,44 +586,57 @@ cudaError_t launch_split(MatvecArgs A, uint32_t passes, uint32_t split, size_t s
   at[0].val.clusterDim.x = split;
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
-  cfg.numAttrs = kSplit ? 1 : 0;
-  const uint32_t groups = kWarps / A.ways, blocks = (A.L.tiles + MT - 1) / MT, fill = (blocks + groups - 1) / groups;
-  uint32_t clusters = (uint32_t)sms[dev] * per_sm / split;
-  if (clusters > fill) clusters = fill;
+  cfg.numAttrs = 1;
+  int fit = 0;  // clusters that the device holds at once; a query takes 0.2 us
+  if ((e = cudaOccupancyMaxActiveClusters(&fit, kernel, &cfg)) != cudaSuccess) return e;
+  if (fit < 1) return cudaErrorInvalidConfiguration;
+  const uint32_t groups = warps / A.ways, fill = (blocks + groups - 1) / groups;
+  const uint32_t clusters = (uint32_t)fit < fill ? (uint32_t)fit : fill;
   A.rounds = (blocks + clusters * groups - 1) / (clusters * groups);
-  cfg.gridDim = dim3(clusters * split, passes);
+  cfg.gridDim.x = clusters * split;
+  cfg.numAttrs = kSplit ? 1 : 0;
+  if (getenv("LC_SHOW")) fprintf(stderr, "NT %d MT %d G %d ways %u split %u warps %u stages %u slice %u chunk %u smem %zu fit %u clusters %u rounds %u direct %u\n", NT, MT, G, A.ways, split, warps, A.stages, A.slice, A.chunk, smem, fit, clusters, A.rounds, A.direct);
   return cudaLaunchKernelEx(&cfg, kernel, A);
 }
 
+int env(const char* name, int otherwise) {
+  const char* s = getenv(name);
+  return s && *s ? atoi(s) : otherwise;
+}
+
 template <class X, class M, int NT, int MT, int G>
-cudaError_t launch(MatvecArgs A, uint32_t passes, uint32_t columns, cudaStream_t cs) {
-  using S = Shared<NT, MT>;
+cudaError_t launch(MatvecArgs A, uint32_t sms, uint32_t passes, uint32_t columns, cudaStream_t cs) {
+  using S = Shared<NT, MT, G>;
   const uint32_t blocks = (A.L.tiles + MT - 1) / MT;
   A.ways = 1;
-  while (A.ways < kWarps && blocks * A.ways < 148 * 16 && A.ways * 2 < A.L.steps) A.ways *= 2;
-  if (const char* s = getenv("LC_WAYS")) A.ways = atoi(s);
-  uint32_t split = 1;
+  while (A.ways < 8 && blocks * A.ways < sms * kMostWarps && A.ways * 2 < A.L.steps) A.ways *= 2;
+  A.ways = env("LC_WAYS", A.ways);
+  uint32_t split = env("LC_SPLIT", 1), warps = env("LC_WARPS", 8);
+  A.stages = env("LC_STAGES", MT == 1 ? 6 : 3);
   auto slice = [&]() { return A.L.steps ? (A.L.steps + split - 1) / split : 1u; };
-  auto bytes = [&](uint32_t steps) { return S::kFixed + S::part(A.ways, split, A.per_pass) + S::starts(steps) + S::x(columns, steps); };
-  const uint64_t two = kSharedPerSM / 2 - 1024;  // of two CTAs on an SM
-  while (split < kMaxSplit && bytes(slice()) > two) split *= 2;
-  if (const char* s = getenv("LC_SPLIT")) split = atoi(s);
+  auto bytes = [&](uint32_t steps) {
+    A.direct = A.ways == 1 && split == 1 && sizeof(X) == 2;
+    return warps * A.stages * S::kStage + S::red(A.direct, warps, columns) + S::part(warps / A.ways, split, A.per_pass) + S::starts(steps) + S::x(columns, steps);
+  };
+  if (bytes(slice()) > kSharedPerSM && warps > 8) warps = 8;
+  if (bytes(slice()) > kSharedPerSM && MT == 1) A.stages = 4;
+  while (split < kMaxSplit && bytes(slice()) > kSharedPerSM) split *= 2;
   A.slice = slice();
   A.chunk = A.slice;
-  const uint32_t per_sm = bytes(A.slice) > two ? 1 : 2;
   for (; bytes(A.chunk) > kSharedPerSM; A.ways /= 2) {
     while (A.chunk > A.ways && bytes(A.chunk) > kSharedPerSM) A.chunk = (A.chunk - 1) / A.ways * A.ways;  // whole turns of the warps
     if (bytes(A.chunk) <= kSharedPerSM || A.ways == 1) break;
   }
   const size_t smem = bytes(A.chunk);
-  return split > 1 ? launch_split<X, M, NT, MT, G, true>(A, passes, split, smem, per_sm, cs) : launch_split<X, M, NT, MT, G, false>(A, passes, split, smem, per_sm, cs);
+  return split > 1 ? launch_split<X, M, NT, MT, G, true>(A, blocks, passes, split, warps, smem, cs)
+                   : launch_split<X, M, NT, MT, G, false>(A, blocks, passes, 1, warps, smem, cs);
 }
 
 template <class X, class M, int NT, int MT>
-cudaError_t launch_group(const MatvecArgs& A, uint32_t passes, uint32_t columns, cudaStream_t cs) {
-  if (A.L.group == 32) return launch<X, M, NT, MT, 32>(A, passes, columns, cs);
-  if (A.L.group == 64) return launch<X, M, NT, MT, 64>(A, passes, columns, cs);
-  return launch<X, M, NT, MT, 128>(A, passes, columns, cs);
+cudaError_t launch_group(const MatvecArgs& A, uint32_t sms, uint32_t passes, uint32_t columns, cudaStream_t cs) {
+  if (A.L.group == 32) return launch<X, M, NT, MT, 32>(A, sms, passes, columns, cs);
+  if (A.L.group == 64) return launch<X, M, NT, MT, 64>(A, sms, passes, columns, cs);
+  return launch<X, M, NT, MT, 128>(A, sms, passes, columns, cs);
 }
 
 template <class X, class M>
@@ -573,12 +646,22 @@ cudaError_t launch_columns(MatvecArgs A, cudaStream_t cs) {
   A.per_pass = (A.tokens + passes - 1) / passes;
   A.by_count = FastDiv(A.per_pass);
   const uint32_t columns = A.per_pass * kParts;
-  bool two = A.L.tiles >= 148 * 8;
-  if (const char* s = getenv("LC_MT")) two = atoi(s) == 2;
-  if (columns <= 8) return two ? launch_group<X, M, 1, 2>(A, passes, columns, cs) : launch_group<X, M, 1, 1>(A, passes, columns, cs);
-  if (columns <= 16) return two ? launch_group<X, M, 2, 2>(A, passes, columns, cs) : launch_group<X, M, 2, 1>(A, passes, columns, cs);
-  if (columns <= 32) return launch_group<X, M, 4, 2>(A, passes, columns, cs);
-  return launch_group<X, M, 8, 1>(A, passes, columns, cs);
+  A.aligned = (reinterpret_cast<uintptr_t>(A.x) & 15) == 0 && (A.tokens == 1 || A.x_stride % (16 / sizeof(X)) == 0);
+  static int count[kMaxDevices];  // SMs
+  const int dev = current_device_index();
+  if (dev < 0) return cudaErrorInvalidDevice;
+  if (count[dev] == 0) {
+    int n = 0;
+    const cudaError_t e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return e;
+    count[dev] = n;
+  }
+  const uint32_t sms = (uint32_t)count[dev];
+  const bool two = env("LC_MT", A.L.tiles >= sms * 8 ? 2 : 1) == 2;
+  if (columns <= 8) return two ? launch_group<X, M, 1, 2>(A, sms, passes, columns, cs) : launch_group<X, M, 1, 1>(A, sms, passes, columns, cs);
+  if (columns <= 16) return two ? launch_group<X, M, 2, 2>(A, sms, passes, columns, cs) : launch_group<X, M, 2, 1>(A, sms, passes, columns, cs);
+  if (columns <= 32) return launch_group<X, M, 4, 2>(A, sms, passes, columns, cs);
+  return launch_group<X, M, 8, 1>(A, sms, passes, columns, cs);
 }
 
 }  // namespace
