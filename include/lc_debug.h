@@ -65,6 +65,12 @@ uint32_t lc_debug_split_segments(const uint64_t* seg_begin, int nseg, uint32_t w
  */
 uint32_t lc_debug_decode_warps(int k, uint64_t chunk_bytes, uint32_t regs);
 
+/* How lc_q4_matvec lays a product out on a device of `sms` SMs (no GPU needed): vectors of a pass, eights of columns of the product,
+ * tiles of a block, warps that share a block, CTAs of a cluster, warps of a CTA, steps in a warp's ring, steps of a CTA, of x
+ * staged at a time, whether sums go out directly, bytes of shared memory (0: none fits). */
+#define LC_Q4_PLAN_WORDS 11
+int lc_debug_q4_plan(uint64_t rows, uint64_t cols, int group, int type, uint32_t tokens, uint32_t sms, uint32_t* plan);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,7 +26,7 @@ SYMBOLS = (
     "lc_stream_info", "lc_last_status", "lc_wait", "lc_host_arena_bytes", "lc_compress_host", "lc_recover_host",
     "lc_debug_bins", "lc_debug_codes", "lc_debug_split_segments", "lc_debug_decode_warps",
     "lc_compress_noalloc",
-    "lc_q4_bytes", "lc_q4_quantize", "lc_recover_q4", "lc_q4_read", "lc_q4_matvec",
+    "lc_q4_bytes", "lc_q4_quantize", "lc_recover_q4", "lc_q4_read", "lc_q4_matvec", "lc_debug_q4_plan",
     "lc_cache_code_bytes", "lc_cache_scale_bytes", "lc_cache_write", "lc_cache_read", "lc_cache_read_pages",
 )
 NOALLOC_MAX_N = 4194304
@@ -115,6 +115,7 @@ def lib():
     L.lc_recover_q4.argtypes = [vp, C.POINTER(vp), C.POINTER(u64), i32, u64, u64, i32, vp, u64, vp, vp, u64, vp]
     L.lc_q4_read.argtypes = [vp, u64, u64, u64, i32, vp, i32, u64, vp]
     L.lc_q4_matvec.argtypes = [vp, u64, u64, u64, i32, vp, i32, u64, u64, vp, i32, u64, vp]
+    L.lc_debug_q4_plan.argtypes = [u64, u64, i32, i32, C.c_uint32, C.c_uint32, C.POINTER(C.c_uint32)]
     cache, rows = C.POINTER(LCCache), C.POINTER(LCRows)
     for f in (L.lc_cache_code_bytes, L.lc_cache_scale_bytes):
         f.argtypes, f.restype = [cache], u64

@@ -9,15 +9,17 @@
 // What bounds it, once enough is in flight, is the work of making 16-bit operands of 4-bit codes, so that is as little as can be:
 // the codes are used as the low bits of a 16-bit float. In a float's lowest 8 (bf16) or 11 (fp16) bits a whole number N stands for
 // N * 2^-133 or N * 2^-24 (subnormal numbers, and the first binade above them, which goes on in the same steps): with n = code + 8,
-// a mask takes two n's out of a word for a row r, and the same mask four bits up two 16 n's for row r + 8. One shift and four masks for eight codes;
-// what is too much by it is taken off in fp32: the accumulators start at -8 times the group's sum of x. To keep the products with
-// bf16 vectors (and parts of fp32 ones) in fp32's normal range, x is multiplied by 2^80 when it is staged. Vectors with values of
-// 2^40 and more, Inf or NaN among them, take plain multiplications instead (slow_tile), a CTA for itself.
+// a mask takes two n's out of a word for a row r, and the same mask four bits up two 16 n's for row r + 8. One shift and four masks
+// for eight codes. What is too much by it, 8 times the group's sum of x, is taken off the group's sum in fp32; it comes from products
+// with a constant, once a CTA. To keep the products with bf16 vectors (and parts of fp32 ones) in fp32's normal range, x is
+// multiplied by 2^80 when it is staged. Where a sum comes out as Inf or NaN (x holds one, or values of 2^48 and more), the warp takes
+// that tile again by plain multiplications (slow_sums).
 #include <stdio.h>
 #include <stdlib.h>
 #include <type_traits>
 
 #include "lc_q4.cuh"
+#include "../../include/lc_debug.h"
 
 namespace lc {
 namespace {
@@ -58,6 +60,22 @@ __device__ __forceinline__ void mma<__half>(float (&d)[4], const uint32_t (&a)[4
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// The same, from zero.
+template <class M>
+__device__ __forceinline__ void mma_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma_first<__nv_bfloat16>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
+}
+template <>
+__device__ __forceinline__ void mma_first<__half>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
+}
+
 // The eight codes of a word, plus 8, as four pairs of tiny numbers: of row r, of row r + 8 (times 16), and so for two more columns.
 __device__ __forceinline__ void operands(uint32_t w, uint32_t (&a)[4]) {
   a[0] = w & 0x000F000Fu;
@@ -66,6 +84,9 @@ __device__ __forceinline__ void operands(uint32_t w, uint32_t (&a)[4]) {
   a[2] = w & 0x000F000Fu;
   a[3] = w & 0x00F000F0u;
 }
+// -8 as such a number, in both halves.
+constexpr uint32_t kMinus8 = 0x80088008u;
+
 // kUp: what x is multiplied by; kUnit: what the sums of products of row r are then to be multiplied by.
 template <class M>
 struct Unit;
@@ -77,19 +98,6 @@ template <>
 struct Unit<__half> {
   static constexpr float kUp = 1.0f, kUnit = 0x1p24f;
 };
-
-// Whether one of the values behind a piece's bits is none for the products above.
-template <class X>
-__device__ __forceinline__ bool too_large(const uint32_t (&raw)[2 * sizeof(X)]) {
-  bool any = false;
-#pragma unroll
-  for (int k = 0; k < (int)(2 * sizeof(X)); ++k) {
-    if constexpr (sizeof(X) == 4) any |= (raw[k] & 0x7F800000u) >= ((127u + 40u) << 23);
-    else if constexpr (std::is_same<X, __half>::value) any |= (raw[k] & 0x7C00u) == 0x7C00u || (raw[k] & 0x7C000000u) == 0x7C000000u;
-    else any |= (raw[k] & 0x7F80u) >= ((127u + 40u) << 7) || (raw[k] & 0x7F800000u) >= ((127u + 40u) << 23);
-  }
-  return any;
-}
 
 // Eight values of a vector from column `col` on, as they are in memory; zeros behind the last column.
 template <class X>
@@ -112,23 +120,19 @@ __device__ __forceinline__ void load_piece(const MatvecArgs& A, uint32_t token, 
   }
 }
 
-// A piece into shared memory as columns of the product (one, or the three parts of fp32, `stride` apart), and the sum of each.
-// The three bf16 numbers of an fp32: the upper half of its bits, that of the exact rest, and what is then left (8 bits at most).
-template <class X, class M>
-__device__ __forceinline__ void store_piece(const uint32_t (&raw)[2 * sizeof(X)], uint4* to, uint32_t stride, float (&sum)[sizeof(X) == 4 ? 3 : 1]) {
+// A piece into shared memory as columns of the product: one, or `stride` apart the three parts of fp32, which are the upper half of its
+// bits, that of the exact rest, and what is then left (8 bits at most).
+template <class X>
+__device__ __forceinline__ void store_piece(const uint32_t (&raw)[2 * sizeof(X)], uint4* to, uint32_t stride) {
   if constexpr (sizeof(X) == 4) {
     uint32_t part[3][8];
 #pragma unroll
-    for (int k = 0; k < 3; ++k) sum[k] = 0.0f;
-#pragma unroll
     for (int e = 0; e < 8; ++e) {
-      float v = __uint_as_float(raw[e]) * Unit<M>::kUp;
+      float v = __uint_as_float(raw[e]) * Unit<__nv_bfloat16>::kUp;
 #pragma unroll
       for (int k = 0; k < 3; ++k) {
-        const uint32_t u = __float_as_uint(v) & 0xFFFF0000u;
-        part[k][e] = u;
-        sum[k] += __uint_as_float(u);
-        v -= __uint_as_float(u);
+        part[k][e] = __float_as_uint(v);
+        v -= __uint_as_float(part[k][e] & 0xFFFF0000u);
       }
     }
 #pragma unroll
@@ -138,23 +142,17 @@ __device__ __forceinline__ void store_piece(const uint32_t (&raw)[2 * sizeof(X)]
       for (int e = 0; e < 4; ++e) w[e] = __byte_perm(part[k][2 * e], part[k][2 * e + 1], 0x7632);
       to[k * stride] = make_uint4(w[0], w[1], w[2], w[3]);
     }
+  } else if constexpr (std::is_same<X, __half>::value) {
+    to[0] = make_uint4(raw[0], raw[1], raw[2], raw[3]);
   } else {
     uint32_t w[4];
-    float s = 0.0f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      if constexpr (std::is_same<X, __half>::value) {
-        const float2 f = __half22float2(reinterpret_cast<const __half2&>(raw[e]));
-        s += f.x + f.y;
-        w[e] = raw[e];
-      } else {
-        const float lo = __uint_as_float(raw[e] << 16) * Unit<M>::kUp, hi = __uint_as_float(raw[e] & 0xFFFF0000u) * Unit<M>::kUp;
-        s += lo + hi;
-        w[e] = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
-      }
+      const __nv_bfloat162 up(__ushort_as_bfloat16(0x6780), __ushort_as_bfloat16(0x6780));  // 2^80
+      const __nv_bfloat162 v = __hmul2(reinterpret_cast<const __nv_bfloat162&>(raw[e]), up);
+      w[e] = reinterpret_cast<const uint32_t&>(v);
     }
     to[0] = make_uint4(w[0], w[1], w[2], w[3]);
-    sum[0] = s;
   }
 }
 
@@ -178,95 +176,61 @@ __device__ __forceinline__ void copies_wait(uint32_t left) {
 
 // x of the steps [begin, end) into shared memory, one column of the product behind the other: `stride` 16-byte pieces, an odd
 // number of units (32 columns of the matrix, four pieces) of which lanes 4 r + t multiply piece t, so that eight columns lie in
-// eight different parts of the banks. The pieces of a group of columns are its neighbouring threads'.
-template <int G>
-struct Pieces {  // how a thread's pieces follow each other
-  static constexpr uint32_t kUnits = G / 32;
-  uint32_t i, count, unit, token;
-  __device__ __forceinline__ void at(const MatvecArgs& A, uint32_t i_) {
-    i = i_;
-    const uint32_t rest = i / kUnits, g = count == A.by_count.d ? A.by_count.div(rest) : rest / count;
-    unit = g * kUnits + (i & (kUnits - 1));
-    token = rest - g * count;
-  }
-};
-
-// Begins to copy them as they are (an fp32 piece to where its first two parts will be), if the vectors are aligned.
-template <class X, int G>
-__device__ __forceinline__ void copy_x(const MatvecArgs& A, uint32_t first, uint32_t count, uint32_t begin, uint32_t end, uint32_t stride, uint4* xs) {
-  constexpr int kParts = sizeof(X) == 4 ? 3 : 1;
-  if (A.aligned) {
-    Pieces<G> p;
-    p.count = count;
-    for (uint32_t i = threadIdx.x >> 2; i < (end - begin) * 4 * count; i += blockDim.x / 4) {
-      p.at(A, i);
-      const uint32_t t = threadIdx.x & 3u, col = (begin * 4 + p.unit) * 32 + 8 * t;
-      const X* from = static_cast<const X*>(A.x) + (uint64_t)(first + p.token) * A.x_stride + col;
-      if (col + 8 <= A.L.cols) {
-        const uint32_t to = shared_address(xs + p.token * kParts * stride + p.unit * 4 + t);
-#pragma unroll
-        for (int k = 0; k < (int)sizeof(X) / 2; ++k) copy16(to + k * stride * 16, reinterpret_cast<const uint4*>(from) + k);
-      }
-    }
-  }
-  copies_end();
-}
-
-// Makes columns of the product of them, in place or (not aligned) from memory, several at a time. Beside them, per group and column, where the accumulators
-// start. Returns, in every thread, whether some value is too large. The copies of the calling thread have arrived.
-template <class X, class M, int NT, int G>
-__device__ __forceinline__ bool stage_x(const MatvecArgs& A, uint32_t first, uint32_t count, uint32_t begin, uint32_t end, uint32_t stride, uint4* xs, float* starts) {
-  constexpr int kBatch = 1, kParts = sizeof(X) == 4 ? 3 : 1;
-  constexpr uint32_t kLanes = G / 8;  // that have a group's pieces
-  const uint32_t pieces = (end - begin) * 4 * count, lane = threadIdx.x & 31, t = lane & 3u, step = blockDim.x / 4;
-  const uint32_t mine = (uint32_t)((1ull << kLanes) - 1) << (lane & ~(kLanes - 1));
-  bool large = false;
-  for (uint32_t i0 = threadIdx.x >> 2; i0 < pieces; i0 += kBatch * step) {
-    uint32_t raw[kBatch][2 * sizeof(X)];
-    Pieces<G> p[kBatch];
-#pragma unroll
-    for (int b = 0; b < kBatch; ++b) {
-      p[b].count = count;
-      p[b].at(A, i0 + b * step);
-      const uint32_t col = (begin * 4 + p[b].unit) * 32 + 8 * t;
-      if (A.aligned && p[b].i < pieces && col + 8 <= A.L.cols) {
-#pragma unroll
-        for (int k = 0; k < (int)sizeof(X) / 2; ++k) {
-          const uint4 v = xs[(p[b].token * kParts + k) * stride + p[b].unit * 4 + t];
-          raw[b][4 * k] = v.x, raw[b][4 * k + 1] = v.y, raw[b][4 * k + 2] = v.z, raw[b][4 * k + 3] = v.w;
-        }
-      } else {
-        load_piece<X>(A, first + p[b].token, col, p[b].i < pieces, raw[b]);
-      }
-    }
-#pragma unroll
-    for (int b = 0; b < kBatch; ++b) {
-      if (p[b].i >= pieces) break;  // the same for the threads of a group
-      large |= too_large<X>(raw[b]);
-      float sum[kParts];
-      store_piece<X, M>(raw[b], xs + p[b].token * kParts * stride + p[b].unit * 4 + t, stride, sum);
-#pragma unroll
-      for (int k = 0; k < kParts; ++k) {
-#pragma unroll
-        for (uint32_t d = 1; d < kLanes; d *= 2) sum[k] += __shfl_xor_sync(mine, sum[k], d);
-        if ((lane & (kLanes - 1)) == 0) starts[p[b].unit / (G / 32) * 8 * NT + p[b].token * kParts + k] = sum[k] * (-8.0f / Unit<M>::kUp / Unit<M>::kUnit);
-      }
-    }
-  }
-  return __syncthreads_or(large);
-}
-
-// Whether a value of the vectors in the steps [begin, end) is too large, for when they are not staged all at once.
+// eight different parts of the banks. Zeros behind the matrix's last column. Where the vectors are aligned, a thread first copies its
+// pieces as they are (an fp32 piece to where its first two parts will be), all of them on their way at once, and then changes
+// them in place; fp16 has nothing to change. (The code is short rather than unrolled: in a small product it runs once, and reading it
+// from memory takes as long as the loads; with four pieces a turn 2048 x 2048 took 4.9 us, with one 4.1.)
 template <class X>
-__device__ __forceinline__ bool find_large(const MatvecArgs& A, uint32_t first, uint32_t count, uint32_t begin, uint32_t end) {
-  bool large = false;
-  for (uint32_t i = threadIdx.x; i < (end - begin) * 16 * count; i += blockDim.x) {
-    const uint32_t token = i / ((end - begin) * 16);
+__device__ __forceinline__ void stage_x(const MatvecArgs& A, uint32_t first, uint32_t count, uint32_t begin, uint32_t end, uint32_t stride, uint4* xs, bool copy) {
+  constexpr int kParts = sizeof(X) == 4 ? 3 : 1;
+  const uint32_t t = threadIdx.x & 3u, step = blockDim.x / 4;
+#pragma unroll 1
+  for (uint32_t i = threadIdx.x >> 2; i < (end - begin) * 4 * count; i += step) {
+    const uint32_t unit = count == A.by_count.d ? A.by_count.div(i) : i / count, token = i - unit * count, col = (begin * 4 + unit) * 32 + 8 * t;
+    uint4* to = xs + token * kParts * stride + unit * 4 + t;
+    const bool whole = A.aligned && col + 8 <= A.L.cols;
+    if (copy) {
+      if (!whole) continue;
+      const X* from = static_cast<const X*>(A.x) + (uint64_t)(first + token) * A.x_stride + col;
+#pragma unroll
+      for (int k = 0; k < (int)sizeof(X) / 2; ++k) copy16(shared_address(to + k * stride), reinterpret_cast<const uint4*>(from) + k);
+      continue;
+    }
+    if (whole && std::is_same<X, __half>::value) continue;
     uint32_t raw[2 * sizeof(X)];
-    load_piece<X>(A, first + token, (begin * 16 + (i - token * (end - begin) * 16)) * 8, true, raw);
-    large |= too_large<X>(raw);
+    if (whole) {
+#pragma unroll
+      for (int k = 0; k < (int)sizeof(X) / 2; ++k) {
+        const uint4 v = to[k * stride];
+        raw[4 * k] = v.x, raw[4 * k + 1] = v.y, raw[4 * k + 2] = v.z, raw[4 * k + 3] = v.w;
+      }
+    } else {
+      load_piece<X>(A, first + token, col, true, raw);
+    }
+    store_piece<X>(raw, to, stride);
   }
-  return __syncthreads_or(large);
+}
+
+// What is to be added to the sums of row r (16 times it to those of row r + 8), per group of the staged steps and column of the product.
+template <class M, int NT, int G>
+__device__ __forceinline__ void sum_groups(const uint4* const (&column)[NT], uint32_t steps, float* starts) {
+  const uint32_t lane = threadIdx.x & 31;
+  constexpr uint32_t kUnits = G / 32;
+  const uint32_t minus[4] = {kMinus8, kMinus8, kMinus8, kMinus8};
+#pragma unroll 1
+  for (uint32_t g = threadIdx.x >> 5; g < steps * 4 / kUnits; g += blockDim.x >> 5) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (uint32_t u = 0; u < kUnits; ++u) {
+        const uint4 b = column[n][(g * kUnits + u) * 4];
+        mma<M>(acc, minus, b.x, b.y);
+        mma<M>(acc, minus, b.z, b.w);
+      }
+      if (lane < 4) *reinterpret_cast<float2*>(starts + g * 8 * NT + 8 * n + 2 * lane) = make_float2(acc[0], acc[1]);
+    }
+  }
 }
 
 // A warp's sums for one vector and rows r and r + 8 of a tile by plain multiplications, in all four lanes of r: what the definition
@@ -308,7 +272,7 @@ __device__ __forceinline__ void store_in_cluster(float* mine, uint32_t rank, flo
   asm volatile("{ .reg .u32 a; mapa.shared::cluster.u32 a, %0, %1; st.shared::cluster.f32 [a], %2; }" ::"r"(shared_address(mine)), "r"(rank), "f"(v) : "memory");
 }
 
-// Shared memory: the warps' rings, their sums, what the cluster's CTAs send each other, where accumulators start, x.
+// Shared memory: the warps' rings, their sums, what the cluster's CTAs send each other, what is added to the sums of groups, x.
 template <int NT, int MT, int G>
 struct Shared {
   static constexpr uint32_t kGroups = kQ4StepCols / G, kSlot = kQ4StepBytes + kGroups * 32, kStage = MT * kSlot;  // codes and scales of a step
@@ -355,7 +319,8 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid
   uint4* xs = reinterpret_cast<uint4*>(starts + S::starts(A.chunk) / 4);
   const uint32_t x_stride = A.chunk * 16 + 4;
   const bool resident = A.chunk >= A.slice;
-  if (resident) copy_x<X, G>(A, first, count, slice, slice_end, x_stride, xs);
+  if (resident && A.aligned) stage_x<X>(A, first, count, slice, slice_end, x_stride, xs, true);
+  copies_end();
 
   // the next step to ask for: where it is, and how many there are left of this block and in all
   const uint32_t turns = slice + way < slice_end ? (slice_end - slice - way + A.ways - 1) / A.ways : 0;
@@ -392,7 +357,6 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid
   };
   for (uint32_t i = 1; i < A.stages; ++i) ask_next();
 
-  bool large = resident ? false : find_large<X>(A, first, count, slice, slice_end);
   if constexpr (kSplit) {
     __syncwarp();
     cluster_wait();
@@ -412,21 +376,24 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid
       if (sizeof(X) == 2 && A.out_type) from_float(y, static_cast<X*>(A.out)[at]);
       else static_cast<float*>(A.out)[at] = y;
     };
-    if (!large || round == 0) {
-      float sum[MT][NT][4] = {};
-      for (uint32_t begin = slice; begin < slice_end; begin += A.chunk) {
-        const uint32_t end = min(slice_end, begin + A.chunk);
-        if (!resident || round == 0) {
-          if (!resident) {
-            __syncthreads();
-            copy_x<X, G>(A, first, count, begin, end, x_stride, xs);
-            copies_wait<0>();
-          } else {
-            copies_wait(A.stages - 1);
-          }
-          large |= stage_x<X, M, NT, G>(A, first, count, begin, end, x_stride, xs, starts);
+    float sum[MT][NT][4] = {};
+    for (uint32_t begin = slice; begin < slice_end; begin += A.chunk) {
+      const uint32_t end = min(slice_end, begin + A.chunk);
+      if (!resident || round == 0) {
+        if (!resident) {
+          __syncthreads();
+          if (A.aligned) stage_x<X>(A, first, count, begin, end, x_stride, xs, true);
+          copies_end();
+          copies_wait<0>();
+        } else {
+          copies_wait(A.stages - 1);
         }
-        if (!there || large) continue;
+        if (!std::is_same<X, __half>::value || !A.aligned || A.L.cols % kQ4StepCols != 0) stage_x<X>(A, first, count, begin, end, x_stride, xs, false);
+        __syncthreads();
+        sum_groups<M, NT, G>(column, end - begin, starts);
+        __syncthreads();
+      }
+      if (!there) continue;
 #pragma unroll 1
         for (uint32_t step = begin + way; step < end; step += A.ways) {
           copies_wait(A.stages - 2);
@@ -444,19 +411,7 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid
             for (int m = 0; m < MT; ++m) v[m] = *reinterpret_cast<const uint4*>(w + m * kSlot + h * 512 + lane * 16);
 #pragma unroll
             for (int u = 2 * h; u < 2 * h + 2; ++u) {
-              if (u * 32 % G == 0) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                  const float2 s = start[(u * 32 / G * NT + n) * 4];
-#pragma unroll
-                  for (int m = 0; m < MT; ++m) {
-                    acc[m][n][0] = s.x;
-                    acc[m][n][1] = s.y;
-                    acc[m][n][2] = 16.0f * s.x;
-                    acc[m][n][3] = 16.0f * s.y;
-                  }
-                }
-              }
+              const bool begins = u * 32 % G == 0, ends = (u + 1) * 32 % G == 0;  // a group
               uint32_t a[MT][2][4];
 #pragma unroll
               for (int m = 0; m < MT; ++m) {
@@ -468,55 +423,64 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid
                 const uint4 b = column[n][at + u * 4];
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
-                  mma<M>(acc[m][n], a[m][0], b.x, b.y);
+                  if (begins) mma_first<M>(acc[m][n], a[m][0], b.x, b.y);
+                  else mma<M>(acc[m][n], a[m][0], b.x, b.y);
                   mma<M>(acc[m][n], a[m][1], b.z, b.w);
                 }
               }
-              if ((u + 1) * 32 % G == 0) {
+              if (ends) {
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                   const uint32_t s = *reinterpret_cast<const uint32_t*>(w + m * kSlot + kQ4StepBytes + (u * 32 / G * 8 + r) * 4);
                   const float s_lo = __uint_as_float(s << 16), s_hi = __uint_as_float(s & 0xFFFF0000u);
 #pragma unroll
                   for (int n = 0; n < NT; ++n) {
-                    sum[m][n][0] += s_lo * acc[m][n][0];
-                    sum[m][n][1] += s_lo * acc[m][n][1];
-                    sum[m][n][2] += s_hi * acc[m][n][2];
-                    sum[m][n][3] += s_hi * acc[m][n][3];
+                    const float2 f = start[(u * 32 / G * NT + n) * 4];
+                    sum[m][n][0] += s_lo * (acc[m][n][0] + f.x);
+                    sum[m][n][1] += s_lo * (acc[m][n][1] + f.y);
+                    sum[m][n][2] += s_hi * __fmaf_rn(16.0f, f.x, acc[m][n][2]);
+                    sum[m][n][3] += s_hi * __fmaf_rn(16.0f, f.y, acc[m][n][3]);
                   }
                 }
               }
             }
           }
         }
-      }
-      if (there && !large) {
+    }
+    if (there) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
+      for (int m = 0; m < MT; ++m) {
+        if (m > 0 && block * MT + m >= A.L.tiles) break;
+        bool fine = true;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            sum[m][n][i] *= i < 2 ? Unit<M>::kUnit : Unit<M>::kUnit / 16;
+            fine &= fabsf(sum[m][n][i]) < __uint_as_float(0x7F800000u);
+          }
+        }
+        if (__all_sync(0xFFFFFFFFu, fine)) {
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const uint32_t col = 8 * n + 2 * t + (i & 1), row = m * 16 + r + 8 * (i >> 1);
-              const float y = sum[m][n][i] * (i < 2 ? Unit<M>::kUnit : Unit<M>::kUnit / 16);
               if (col >= columns) continue;
-              if (kParts == 1 && A.direct) put(col, row, y);
-              else mine[col * kRedStride + row] = y;
+              if (kParts == 1 && A.direct) put(col, row, sum[m][n][i]);
+              else mine[col * kRedStride + row] = sum[m][n][i];
             }
           }
-        }
-      }
-    }
-    if (there && large) {
-      for (uint32_t m = 0; m < MT && block * MT + m < A.L.tiles; ++m) {
-        for (uint32_t token = 0; token < count; ++token) {
-          const float2 y = slow_sums<X>(A, block * MT + m, first + token, slice + way, slice_end);
-          const uint32_t row = m * 16 + r;
-          if (kParts == 1 && A.direct) {
-            if (t == 0) put(token, row, y.x), put(token, row + 8, y.y);
-          } else if (t < kParts) {
-            mine[(token * kParts + t) * kRedStride + row] = t == 0 ? y.x : 0.0f;
-            mine[(token * kParts + t) * kRedStride + row + 8] = t == 0 ? y.y : 0.0f;
+        } else {
+          for (uint32_t token = 0; token < count; ++token) {
+            const float2 y = slow_sums<X>(A, block * MT + m, first + token, slice + way, slice_end);
+            const uint32_t row = m * 16 + r;
+            if (kParts == 1 && A.direct) {
+              if (t == 0) put(token, row, y.x), put(token, row + 8, y.y);
+            } else if (t < kParts) {
+              mine[(token * kParts + t) * kRedStride + row] = t == 0 ? y.x : 0.0f;
+              mine[(token * kParts + t) * kRedStride + row + 8] = t == 0 ? y.y : 0.0f;
+            }
           }
         }
       }
@@ -530,14 +494,14 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid
     };
     group_barrier();
     if (there) {
-      for (uint32_t i = way * 32 + lane; i < count * kRows; i += A.ways * 32) {
-        const uint32_t token = i / kRows, row = i % kRows;
+      const uint32_t row = lane % kRows;  // the lanes of a warp take as many vectors side by side as they are times the rows
+      for (uint32_t token = (way * 32 + lane) / kRows; token < count; token += A.ways * 32 / kRows) {
         float y = 0.0f;
 #pragma unroll
         for (int k = (int)kParts - 1; k >= 0; --k) {  // the smallest part first
           const float* p = red + (group * A.ways * red_columns + token * kParts + k) * kRedStride + row;
           float v = 0.0f;
-          for (uint32_t w = 0; w < A.ways; ++w) v += p[w * red_columns * kRedStride];
+          for (uint32_t w = 0; w < A.ways; ++w, p += red_columns * kRedStride) v += *p;
           y += v;
         }
         if constexpr (kSplit) store_in_cluster(part + ((((round & 1) * groups + group) * split + rank) * part_tokens + token / split) * kRows + row, (token + round) % split, y);
@@ -599,51 +563,98 @@ cudaError_t launch_split(MatvecArgs A, uint32_t blocks, uint32_t passes, uint32_
   return cudaLaunchKernelEx(&cfg, kernel, A);
 }
 
-int env(const char* name, int otherwise) {
-  const char* s = getenv(name);
-  return s && *s ? atoi(s) : otherwise;
+// How a product is laid out over the device.
+struct Plan {
+  uint32_t mt, ways, split, warps, stages, slice, chunk, direct, smem;
+};
+
+uint64_t plan_bytes(const Plan& p, uint32_t nt, uint32_t group, uint32_t per_pass, uint32_t parts, uint32_t steps) {
+  const uint32_t columns = per_pass * parts, rows = p.mt * kQ4TileRows, groups = kQ4StepCols / group;
+  const uint32_t stage = p.mt * (kQ4StepBytes + groups * 32), part_tokens = p.split > 1 ? (per_pass + p.split - 1) / p.split : 0;
+  return (uint64_t)p.warps * p.stages * stage + (p.direct ? 0 : (uint64_t)p.warps * columns * (rows + 4) * 4) +
+         (uint64_t)2 * (p.warps / p.ways) * p.split * part_tokens * rows * 4 + (uint64_t)steps * groups * 8 * nt * 4 + (uint64_t)columns * (steps * 256 + 64);
+}
+
+// About how many cycles a layout takes, from measured products: a step takes a warp `alone` cycles and an SM `work` instructions, 2.2
+// a cycle with all its warps; x is staged by every CTA; the sums of a round of blocks are added up behind it.
+constexpr uint32_t kStepAlone[2][4] = {{830, 1100, 1700, 3500}, {1400, 1800, 3000, 7000}}, kStepWork[2][4] = {{130, 240, 440, 900}, {250, 430, 800, 1800}};
+uint32_t plan_cycles(const Plan& p, uint32_t nt_log, uint32_t tiles, uint32_t per_pass, uint32_t parts, uint32_t sms) {
+  const uint32_t per_sm = p.warps <= 8 && p.smem <= kSharedPerSM / 2 - 1024 ? 2 : 1;
+  // clusters of 2, 4 and 8 on 148 SMs with one CTA each: 74, 33 and 15
+  const uint32_t clusters = p.split == 1 ? sms * per_sm : p.split == 2 ? sms * per_sm / 2 : p.split == 4 ? sms * per_sm * 33 / 148 : sms * per_sm * 15 / 148;
+  const uint32_t groups = p.warps / p.ways, blocks = (tiles + p.mt - 1) / p.mt, slots = (clusters ? clusters : 1) * groups;
+  const uint32_t steps = (p.slice + p.ways - 1) / p.ways, alone = kStepAlone[p.mt - 1][nt_log], work = kStepWork[p.mt - 1][nt_log];
+  const uint32_t rows = p.mt * kQ4TileRows;
+  const uint32_t sums = 300 + per_pass * rows * (20 + 6 * p.ways * parts) / (32 * p.ways) + (p.split > 1 ? 1200 : 0);
+  auto round = [&](uint32_t used) {  // blocks of a round
+    const uint32_t warps = (used * p.ways * p.split + sms - 1) / sms, all = p.warps * per_sm;
+    const uint32_t busy = (warps < all ? warps : all) * work * 10 / 22;
+    return steps * (busy > alone ? busy : alone) + sums;
+  };
+  const uint32_t pieces = p.slice * 16 * per_pass, staged = p.chunk >= p.slice ? 1 : blocks / slots + 1;
+  return staged * pieces / 32 * (parts == 3 ? 60 : 20) + (p.split > 1 ? 1000 : 0) + blocks / slots * round(slots) + (blocks % slots ? round(blocks % slots) : 0);
+}
+
+Plan make_plan(uint32_t nt_log, const Q4Layout& L, uint32_t per_pass, uint32_t parts, uint32_t sms) {
+  const uint32_t nt = 1u << nt_log;
+  Plan best = {};
+  uint32_t least = ~0u;
+  for (uint32_t mt = nt_log == 2 ? 2 : 1; mt <= (nt_log == 3 ? 1 : 2); ++mt) {
+    const uint32_t blocks = (L.tiles + mt - 1) / mt;
+    for (uint32_t split = 1; split <= kMaxSplit; split *= 2) {
+      if (split > 1 && L.steps < 2 * split) break;
+      for (uint32_t ways = 1; ways <= 8; ways *= 2) {
+        const uint32_t slice = L.steps ? (L.steps + split - 1) / split : 1, shared = blocks * ways * split;  // warps that there is work for
+        if (ways > 1 && (slice < ways || shared / 2 > sms * kMostWarps * 2)) break;  // nothing to share, or no need to
+        if (shared < sms && ways < 8 && slice >= 2 * ways) continue;
+        Plan p = {mt, ways, split, shared > sms * 8 ? 16u : 8u, mt == 1 ? 6u : 3u, slice, 0, ways == 1 && split == 1 && parts == 1, 0};
+        p.chunk = p.slice;
+        uint64_t bytes = plan_bytes(p, nt, L.group, per_pass, parts, p.chunk);
+        if (bytes > kSharedPerSM) {
+          p.warps = 8;
+          if (mt == 1) p.stages = 4;
+          if ((bytes = plan_bytes(p, nt, L.group, per_pass, parts, p.chunk)) > kSharedPerSM) {  // x in parts: whole turns of the warps
+            const uint64_t fixed = plan_bytes(p, nt, L.group, per_pass, parts, 0), step = plan_bytes(p, nt, L.group, per_pass, parts, 1) - fixed;
+            p.chunk = fixed >= kSharedPerSM ? 0 : (uint32_t)((kSharedPerSM - fixed) / step) / ways * ways;
+            if (p.chunk == 0) continue;
+            bytes = plan_bytes(p, nt, L.group, per_pass, parts, p.chunk);
+          }
+        }
+        p.smem = (uint32_t)bytes;
+        const uint32_t cycles = plan_cycles(p, nt_log, L.tiles, per_pass, parts, sms);
+        if (cycles < least) least = cycles, best = p;
+      }
+    }
+  }
+  return best;
 }
 
 template <class X, class M, int NT, int MT, int G>
-cudaError_t launch(MatvecArgs A, uint32_t sms, uint32_t passes, uint32_t columns, cudaStream_t cs) {
-  using S = Shared<NT, MT, G>;
+cudaError_t launch(const MatvecArgs& A, const Plan& p, uint32_t passes, cudaStream_t cs) {
   const uint32_t blocks = (A.L.tiles + MT - 1) / MT;
-  A.ways = 1;
-  while (A.ways < 8 && blocks * A.ways < sms * kMostWarps && A.ways * 2 < A.L.steps) A.ways *= 2;
-  A.ways = env("LC_WAYS", A.ways);
-  uint32_t split = env("LC_SPLIT", 1), warps = env("LC_WARPS", 8);
-  A.stages = env("LC_STAGES", MT == 1 ? 6 : 3);
-  auto slice = [&]() { return A.L.steps ? (A.L.steps + split - 1) / split : 1u; };
-  auto bytes = [&](uint32_t steps) {
-    A.direct = A.ways == 1 && split == 1 && sizeof(X) == 2;
-    return warps * A.stages * S::kStage + S::red(A.direct, warps, columns) + S::part(warps / A.ways, split, A.per_pass) + S::starts(steps) + S::x(columns, steps);
-  };
-  if (bytes(slice()) > kSharedPerSM && warps > 8) warps = 8;
-  if (bytes(slice()) > kSharedPerSM && MT == 1) A.stages = 4;
-  while (split < kMaxSplit && bytes(slice()) > kSharedPerSM) split *= 2;
-  A.slice = slice();
-  A.chunk = A.slice;
-  for (; bytes(A.chunk) > kSharedPerSM; A.ways /= 2) {
-    while (A.chunk > A.ways && bytes(A.chunk) > kSharedPerSM) A.chunk = (A.chunk - 1) / A.ways * A.ways;  // whole turns of the warps
-    if (bytes(A.chunk) <= kSharedPerSM || A.ways == 1) break;
-  }
-  const size_t smem = bytes(A.chunk);
-  return split > 1 ? launch_split<X, M, NT, MT, G, true>(A, blocks, passes, split, warps, smem, cs)
-                   : launch_split<X, M, NT, MT, G, false>(A, blocks, passes, 1, warps, smem, cs);
+  return p.split > 1 ? launch_split<X, M, NT, MT, G, true>(A, blocks, passes, p.split, p.warps, p.smem, cs)
+                     : launch_split<X, M, NT, MT, G, false>(A, blocks, passes, 1, p.warps, p.smem, cs);
 }
 
 template <class X, class M, int NT, int MT>
-cudaError_t launch_group(const MatvecArgs& A, uint32_t sms, uint32_t passes, uint32_t columns, cudaStream_t cs) {
-  if (A.L.group == 32) return launch<X, M, NT, MT, 32>(A, sms, passes, columns, cs);
-  if (A.L.group == 64) return launch<X, M, NT, MT, 64>(A, sms, passes, columns, cs);
-  return launch<X, M, NT, MT, 128>(A, sms, passes, columns, cs);
+cudaError_t launch_group(const MatvecArgs& A, const Plan& p, uint32_t passes, cudaStream_t cs) {
+  if (A.L.group == 32) return launch<X, M, NT, MT, 32>(A, p, passes, cs);
+  if (A.L.group == 64) return launch<X, M, NT, MT, 64>(A, p, passes, cs);
+  return launch<X, M, NT, MT, 128>(A, p, passes, cs);
 }
+
+// The tokens of a pass, and the logarithm of the eights of columns that the product then has.
+uint32_t tokens_per_pass(uint32_t tokens, uint32_t parts) {
+  const uint32_t most = 64 / parts, passes = (tokens + most - 1) / most;
+  return (tokens + passes - 1) / passes;
+}
+uint32_t eights_log(uint32_t columns) { return columns <= 8 ? 0 : columns <= 16 ? 1 : columns <= 32 ? 2 : 3; }
 
 template <class X, class M>
 cudaError_t launch_columns(MatvecArgs A, cudaStream_t cs) {
-  constexpr uint32_t kParts = sizeof(X) == 4 ? 3 : 1, kMost = 64 / kParts;
-  const uint32_t passes = (A.tokens + kMost - 1) / kMost;
-  A.per_pass = (A.tokens + passes - 1) / passes;
+  constexpr uint32_t kParts = sizeof(X) == 4 ? 3 : 1;
+  A.per_pass = tokens_per_pass(A.tokens, kParts);
+  const uint32_t passes = (A.tokens + A.per_pass - 1) / A.per_pass;
   A.by_count = FastDiv(A.per_pass);
   const uint32_t columns = A.per_pass * kParts;
   A.aligned = (reinterpret_cast<uintptr_t>(A.x) & 15) == 0 && (A.tokens == 1 || A.x_stride % (16 / sizeof(X)) == 0);
@@ -657,11 +668,24 @@ cudaError_t launch_columns(MatvecArgs A, cudaStream_t cs) {
     count[dev] = n;
   }
   const uint32_t sms = (uint32_t)count[dev];
-  const bool two = env("LC_MT", A.L.tiles >= sms * 8 ? 2 : 1) == 2;
-  if (columns <= 8) return two ? launch_group<X, M, 1, 2>(A, sms, passes, columns, cs) : launch_group<X, M, 1, 1>(A, sms, passes, columns, cs);
-  if (columns <= 16) return two ? launch_group<X, M, 2, 2>(A, sms, passes, columns, cs) : launch_group<X, M, 2, 1>(A, sms, passes, columns, cs);
-  if (columns <= 32) return launch_group<X, M, 4, 2>(A, sms, passes, columns, cs);
-  return launch_group<X, M, 8, 1>(A, sms, passes, columns, cs);
+  const uint32_t nt_log = eights_log(columns);
+  Plan p = make_plan(nt_log, A.L, A.per_pass, kParts, sms);
+  if (getenv("LC_WAYS")) {
+    p.ways = atoi(getenv("LC_WAYS")), p.split = atoi(getenv("LC_SPLIT")), p.mt = atoi(getenv("LC_MT")), p.warps = atoi(getenv("LC_WARPS")), p.stages = atoi(getenv("LC_STAGES"));
+    p.slice = A.L.steps ? (A.L.steps + p.split - 1) / p.split : 1, p.chunk = p.slice, p.direct = p.ways == 1 && p.split == 1 && kParts == 1;
+    p.smem = plan_bytes(p, 1 << nt_log, A.L.group, A.per_pass, kParts, p.chunk);
+    if (p.smem > kSharedPerSM) return cudaErrorInvalidValue;
+  }
+  if (p.smem == 0) return cudaErrorInvalidConfiguration;
+  A.ways = p.ways;
+  A.direct = p.direct;
+  A.stages = p.stages;
+  A.slice = p.slice;
+  A.chunk = p.chunk;
+  if (nt_log == 0) return p.mt == 2 ? launch_group<X, M, 1, 2>(A, p, passes, cs) : launch_group<X, M, 1, 1>(A, p, passes, cs);
+  if (nt_log == 1) return p.mt == 2 ? launch_group<X, M, 2, 2>(A, p, passes, cs) : launch_group<X, M, 2, 1>(A, p, passes, cs);
+  if (nt_log == 2) return launch_group<X, M, 4, 2>(A, p, passes, cs);
+  return launch_group<X, M, 8, 1>(A, p, passes, cs);
 }
 
 }  // namespace
@@ -683,3 +707,15 @@ cudaError_t launch_q4_matvec(const Q4Layout& L, const uint8_t* q4, const void* x
 }
 
 }  // namespace lc
+
+// Declared in include/lc_debug.h: how a product is laid out, for the test of its bounds.
+extern "C" int lc_debug_q4_plan(uint64_t rows, uint64_t cols, int group, int type, uint32_t tokens, uint32_t sms, uint32_t* plan) {
+  using namespace lc;
+  if (!plan || !group_ok(group) || !type_ok(type) || tokens == 0 || sms == 0 || rows == 0 || rows >= (1ull << 31) || cols >= (1ull << 31) - kQ4StepCols)
+    return LC_ERR_ARG;
+  const uint32_t parts = type == LC_TYPE_F32 ? 3 : 1, per_pass = tokens_per_pass(tokens, parts), nt_log = eights_log(per_pass * parts);
+  const Plan p = make_plan(nt_log, q4_layout(rows, cols, group), per_pass, parts, sms);
+  const uint32_t values[LC_Q4_PLAN_WORDS] = {per_pass, 1u << nt_log, p.mt, p.ways, p.split, p.warps, p.stages, p.slice, p.chunk, p.direct, p.smem};
+  for (int i = 0; i < LC_Q4_PLAN_WORDS; ++i) plan[i] = values[i];
+  return LC_OK;
+}
