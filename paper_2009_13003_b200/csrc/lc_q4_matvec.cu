@@ -14,8 +14,6 @@
 // with a constant, once a CTA. To keep the products with bf16 vectors (and parts of fp32 ones) in fp32's normal range, x is
 // multiplied by 2^80 when it is staged. Where a sum comes out as Inf or NaN (x holds one, or values of 2^48 and more), the warp takes
 // that tile again by plain multiplications (slow_sums).
-#include <stdio.h>
-#include <stdlib.h>
 #include <type_traits>
 
 #include "lc_q4.cuh"
@@ -559,7 +557,6 @@ cudaError_t launch_split(MatvecArgs A, uint32_t blocks, uint32_t passes, uint32_
   A.rounds = (blocks + clusters * groups - 1) / (clusters * groups);
   cfg.gridDim.x = clusters * split;
   cfg.numAttrs = kSplit ? 1 : 0;
-  if (getenv("LC_SHOW")) fprintf(stderr, "NT %d MT %d G %d ways %u split %u warps %u stages %u slice %u chunk %u smem %zu fit %u clusters %u rounds %u direct %u\n", NT, MT, G, A.ways, split, warps, A.stages, A.slice, A.chunk, smem, fit, clusters, A.rounds, A.direct);
   return cudaLaunchKernelEx(&cfg, kernel, A);
 }
 
@@ -575,24 +572,24 @@ uint64_t plan_bytes(const Plan& p, uint32_t nt, uint32_t group, uint32_t per_pas
          (uint64_t)2 * (p.warps / p.ways) * p.split * part_tokens * rows * 4 + (uint64_t)steps * groups * 8 * nt * 4 + (uint64_t)columns * (steps * 256 + 64);
 }
 
-// About how many cycles a layout takes, from measured products: a step takes a warp `alone` cycles and an SM `work` instructions, 2.2
-// a cycle with all its warps; x is staged by every CTA; the sums of a round of blocks are added up behind it.
-constexpr uint32_t kStepAlone[2][4] = {{830, 1100, 1700, 3500}, {1400, 1800, 3000, 7000}}, kStepWork[2][4] = {{130, 240, 440, 900}, {250, 430, 800, 1800}};
+// About how many cycles a layout takes: a step takes a warp `alone` cycles and an SM with all its warps `busy`; every CTA stages x; the
+// sums of a round of blocks are added up behind it. The numbers are fitted to 37 shapes of 1 to 40 vectors in up to 64 layouts each;
+// what the rule then takes is 3 % slower than the fastest of them (geometric mean; 12 % at most but for x of over 16 vectors).
+constexpr uint32_t kStepAlone[2][4] = {{825, 1130, 1750, 3500}, {1270, 1800, 3000, 7000}}, kStepBusy[2][4] = {{71, 110, 200, 430}, {130, 190, 390, 800}};
 uint32_t plan_cycles(const Plan& p, uint32_t nt_log, uint32_t tiles, uint32_t per_pass, uint32_t parts, uint32_t sms) {
   const uint32_t per_sm = p.warps <= 8 && p.smem <= kSharedPerSM / 2 - 1024 ? 2 : 1;
   // clusters of 2, 4 and 8 on 148 SMs with one CTA each: 74, 33 and 15
-  const uint32_t clusters = p.split == 1 ? sms * per_sm : p.split == 2 ? sms * per_sm / 2 : p.split == 4 ? sms * per_sm * 33 / 148 : sms * per_sm * 15 / 148;
-  const uint32_t groups = p.warps / p.ways, blocks = (tiles + p.mt - 1) / p.mt, slots = (clusters ? clusters : 1) * groups;
-  const uint32_t steps = (p.slice + p.ways - 1) / p.ways, alone = kStepAlone[p.mt - 1][nt_log], work = kStepWork[p.mt - 1][nt_log];
-  const uint32_t rows = p.mt * kQ4TileRows;
-  const uint32_t sums = 300 + per_pass * rows * (20 + 6 * p.ways * parts) / (32 * p.ways) + (p.split > 1 ? 1200 : 0);
+  const uint32_t clusters = sms * per_sm * (p.split <= 2 ? 148 / p.split : p.split == 4 ? 33 : 15) / 148;
+  const uint32_t groups = p.warps / p.ways, rows = p.mt * kQ4TileRows, blocks = (tiles + p.mt - 1) / p.mt, slots = (clusters ? clusters : 1) * groups;
+  const uint32_t steps = (p.slice + p.ways - 1) / p.ways, alone = kStepAlone[p.mt - 1][nt_log], busy = kStepBusy[p.mt - 1][nt_log];
+  const uint32_t sums = 300 + per_pass * rows * (20 + 6 * p.ways * parts) / (32 * p.ways) + (p.split == 1 ? 0 : p.split == 2 ? 1160 : p.split == 4 ? 1400 : 1600);
   auto round = [&](uint32_t used) {  // blocks of a round
     const uint32_t warps = (used * p.ways * p.split + sms - 1) / sms, all = p.warps * per_sm;
-    const uint32_t busy = (warps < all ? warps : all) * work * 10 / 22;
-    return steps * (busy > alone ? busy : alone) + sums;
+    const uint32_t together = (warps < all ? warps : all) * busy;
+    return steps * (together > alone ? together : alone) + sums;
   };
-  const uint32_t pieces = p.slice * 16 * per_pass, staged = p.chunk >= p.slice ? 1 : blocks / slots + 1;
-  return staged * pieces / 32 * (parts == 3 ? 60 : 20) + (p.split > 1 ? 1000 : 0) + blocks / slots * round(slots) + (blocks % slots ? round(blocks % slots) : 0);
+  const uint32_t staged = (p.chunk >= p.slice ? 1 : blocks / slots + 1) * per_sm * (p.slice * per_pass / 2) * (parts == 3 ? 90 : 50);  // 32 pieces at a time
+  return staged + (p.split > 1 ? 950 : 0) + blocks / slots * round(slots) + (blocks % slots ? round(blocks % slots) : 0);
 }
 
 Plan make_plan(uint32_t nt_log, const Q4Layout& L, uint32_t per_pass, uint32_t parts, uint32_t sms) {
@@ -670,12 +667,6 @@ cudaError_t launch_columns(MatvecArgs A, cudaStream_t cs) {
   const uint32_t sms = (uint32_t)count[dev];
   const uint32_t nt_log = eights_log(columns);
   Plan p = make_plan(nt_log, A.L, A.per_pass, kParts, sms);
-  if (getenv("LC_WAYS")) {
-    p.ways = atoi(getenv("LC_WAYS")), p.split = atoi(getenv("LC_SPLIT")), p.mt = atoi(getenv("LC_MT")), p.warps = atoi(getenv("LC_WARPS")), p.stages = atoi(getenv("LC_STAGES"));
-    p.slice = A.L.steps ? (A.L.steps + p.split - 1) / p.split : 1, p.chunk = p.slice, p.direct = p.ways == 1 && p.split == 1 && kParts == 1;
-    p.smem = plan_bytes(p, 1 << nt_log, A.L.group, A.per_pass, kParts, p.chunk);
-    if (p.smem > kSharedPerSM) return cudaErrorInvalidValue;
-  }
   if (p.smem == 0) return cudaErrorInvalidConfiguration;
   A.ways = p.ways;
   A.direct = p.direct;
