@@ -10,8 +10,9 @@ struct CacheArgs {
   uint8_t* codes;
   unsigned short* scales;
   uint64_t slots;
-  uint32_t heads, dim, groups, lanes, row_bytes, bits;  // groups per row of dim values; lanes: of 8 values, per group
-  FastDiv by_row, by_groups;                            // items (head, group) per row; groups per head
+  uint32_t heads, dim, groups, row_bytes;  // groups per row of dim values
+  uint32_t per_plane, per_row;                        // lanes: of a plane's row, of all planes'
+  FastDiv by_head, by_warps;                          // lanes of a head, warps that share a row
 };
 
 struct Rows {  // the caller's rows of one plane
@@ -70,83 +71,145 @@ __device__ __forceinline__ int64_t slot_of(const Places& P, uint32_t row, uint64
   return slot;
 }
 
-// group / 8 lanes hold a group, eight values each; one pass over the rows, bound by memory.
-template <class T>
-__global__ void __launch_bounds__(kThreads) cache_write_kernel(CacheArgs C, Planes src, Places P, uint32_t items, int32_t* status) {
-  const uint32_t item = (uint32_t)(((uint64_t)blockIdx.x * kThreads + threadIdx.x) / C.lanes);
-  const uint32_t lane = threadIdx.x & (C.lanes - 1);
-  const bool inside = item < items;
-  const uint32_t row = inside ? C.by_row.div(item) : 0, hg = inside ? item - row * C.by_row.d : 0;
-  const uint32_t head = C.by_groups.div(hg), g = hg - head * C.groups;
-  bool bad = false;
-  const int64_t slot = inside ? slot_of<false>(P, row, C.slots, bad) : -1;
-  if (bad && status) set_status(status, LC_ERR_INDEX);
-  const uint32_t at = (g * C.lanes + lane) * 8;
-  const int valid = slot < 0 || at >= C.dim ? 0 : (int)min(8u, C.dim - at);
-  const Rows& R = src.plane[blockIdx.y];
-  float v[8];
-  load8(reinterpret_cast<const T*>(R.data) + row * R.row_stride + head * R.head_stride + at, valid, v);
-  const uint32_t scale = group_scale(max_over_lanes(max_bits8(v), (int)C.lanes), C.bits == 4 ? 7.0f : 127.0f);
-  if (valid == 0) return;
-  int q[8];
-  codes8(v, scale, q);
-  const uint64_t place = (blockIdx.y * C.slots + (uint64_t)slot) * C.heads + head;
-  uint8_t* o = C.codes + place * C.row_bytes + at * C.bits / 8;
-  if (C.bits == 4) *reinterpret_cast<uint32_t*>(o) = pack4(q);
-  else *reinterpret_cast<uint2*>(o) = pack8(q);
-  if (lane == 0) C.scales[place * C.groups + g] = (unsigned short)(scale >> 16);
+// A warp takes a row (or, with few rows, several share one): its place is looked up once for all planes and heads. group / 16 lanes hold
+// a group, 16 values each: neighbouring ones where they are quantised; where they are read, runs of 16 bytes of the output, so that
+// the lanes' runs follow each other. One pass over the rows; from and to 16 bits the instructions of the codes weigh as much as the bytes
+// (reading 131072 rows of 8 x 128 from 4 bits to bf16, twice: 119 us; with one run of 8 values a lane, and so twice the index arithmetic, 177).
+struct Lane {
+  uint32_t plane, head, part;  // part: which of the head's lanes
+};
+__device__ __forceinline__ Lane lane_of(const CacheArgs& C, uint32_t j) {
+  Lane l;
+  l.plane = j >= C.per_plane;
+  const uint32_t v = j - (l.plane ? C.per_plane : 0);
+  l.head = C.by_head.div(v);
+  l.part = v - l.head * C.by_head.d;
+  return l;
 }
 
-template <class T, bool kPages>
-__global__ void __launch_bounds__(kThreads) cache_read_kernel(CacheArgs C, Planes out, Places P, uint32_t items, int32_t* status) {
-  const uint32_t item = (uint32_t)(((uint64_t)blockIdx.x * kThreads + threadIdx.x) / C.lanes);
-  if (item >= items) return;
-  const uint32_t lane = threadIdx.x & (C.lanes - 1);
-  const uint32_t row = C.by_row.div(item), hg = item - row * C.by_row.d;
-  const uint32_t head = C.by_groups.div(hg), g = hg - head * C.groups;
+template <class T, int G, int kBits>
+__global__ void __launch_bounds__(kThreads) cache_write_kernel(CacheArgs C, Planes src, Places P, uint32_t rows, int32_t* status) {
+  constexpr int kLanes = G / 16;
+  const uint32_t lane = threadIdx.x & 31, warp = (uint32_t)(((uint64_t)blockIdx.x * kThreads + threadIdx.x) >> 5);
+  const uint32_t row = C.by_warps.div(warp);
+  if (row >= rows) return;  // whole warps
+  bool bad = false;
+  const int64_t slot = slot_of<false>(P, row, C.slots, bad);
+  if (bad && status && lane == 0) set_status(status, LC_ERR_INDEX);
+  if (slot < 0) return;
+  for (uint32_t j0 = (warp - row * C.by_warps.d) * 32; j0 < C.per_row; j0 += C.by_warps.d * 32) {
+    const bool inside = j0 + lane < C.per_row;
+    const Lane l = lane_of(C, inside ? j0 + lane : 0);
+    const uint32_t at = l.part * 16;
+    const Rows R = l.plane ? src.plane[1] : src.plane[0];
+    const T* p = reinterpret_cast<const T*>(R.data) + row * R.row_stride + l.head * R.head_stride + at;
+    const int valid = inside ? (int)C.dim - (int)at : 0;
+    float v[16], m = 0.0f;
+    load8(p, valid, v);
+    load8(p + 8, valid - 8, v + 8);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) m = max_magnitude(m, v[i]);
+    const uint32_t scale = group_scale<kBits>(max_over_lanes(m, kLanes));
+    if (valid <= 0) continue;
+    float t[16];
+    codes<T, kBits>(v, scale, t);
+    const uint64_t place = (l.plane * C.slots + (uint64_t)slot) * C.heads + l.head;
+    uint8_t* o = C.codes + place * C.row_bytes + at * kBits / 8;
+    if constexpr (kBits == 4) {
+      const uint32_t a = pack4(t), b = pack4(t + 8);
+      if (valid > 8 && (reinterpret_cast<uintptr_t>(o) & 7) == 0) {
+        *reinterpret_cast<uint2*>(o) = make_uint2(a, b);
+      } else {
+        *reinterpret_cast<uint32_t*>(o) = a;
+        if (valid > 8) *reinterpret_cast<uint32_t*>(o + 4) = b;
+      }
+    } else {
+      const uint2 a = pack8(t), b = pack8(t + 8);
+      if (valid > 8 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+        *reinterpret_cast<uint4*>(o) = make_uint4(a.x, a.y, b.x, b.y);
+      } else {
+        *reinterpret_cast<uint2*>(o) = a;
+        if (valid > 8) *reinterpret_cast<uint2*>(o + 8) = b;
+      }
+    }
+    if ((lane & (kLanes - 1)) == 0) C.scales[place * C.groups + at / G] = (unsigned short)(scale >> 16);
+  }
+}
+
+// Four values' codes of 4 bits, of a word that holds eight: the first four are in its bytes 0 and 2, the others in 1 and 3.
+__device__ __forceinline__ uint32_t half_word(const uint8_t* p, uint32_t at) {
+  return *reinterpret_cast<const uint32_t*>(p - (at & 4) / 2) >> ((at & 4) * 2);
+}
+
+template <class T, int G, int kBits, bool kPages>
+__global__ void __launch_bounds__(kThreads) cache_read_kernel(CacheArgs C, Planes out, Places P, uint32_t rows, int32_t* status) {
+  constexpr uint32_t kLanes = G / 16, n = kRun<T>, kRuns = 16 / n;
+  const uint32_t lane = threadIdx.x & 31, warp = (uint32_t)(((uint64_t)blockIdx.x * kThreads + threadIdx.x) >> 5);
+  const uint32_t row = C.by_warps.div(warp);
+  if (row >= rows) return;
   bool bad = false;
   const int64_t slot = slot_of<kPages>(P, row, C.slots, bad);
-  if (bad && status) set_status(status, LC_ERR_INDEX);
-  const uint32_t at = (g * C.lanes + lane) * 8;
-  if (slot < 0 || at >= C.dim) return;
-  const uint64_t place = (blockIdx.y * C.slots + (uint64_t)slot) * C.heads + head;
-  const uint8_t* p = C.codes + place * C.row_bytes + at * C.bits / 8;
-  const float scale = __uint_as_float((uint32_t)C.scales[place * C.groups + g] << 16);
-  float v[8];
-  if (C.bits == 4) values_of4(*reinterpret_cast<const uint32_t*>(p), scale, v);
-  else values_of8(*reinterpret_cast<const uint2*>(p), scale, v);
-  const Rows& R = out.plane[blockIdx.y];
-  store8(reinterpret_cast<T*>(R.data) + row * R.row_stride + head * R.head_stride + at, (int)min(8u, C.dim - at), v);
+  if (bad && status && lane == 0) set_status(status, LC_ERR_INDEX);
+  if (slot < 0) return;
+  for (uint32_t j = (warp - row * C.by_warps.d) * 32 + lane; j < C.per_row; j += C.by_warps.d * 32) {
+    const Lane l = lane_of(C, j);
+    const uint32_t group = l.part / kLanes, at = group * G + (l.part & (kLanes - 1)) * n;  // of the first run
+    const uint64_t place = (l.plane * C.slots + (uint64_t)slot) * C.heads + l.head;
+    const uint8_t* p = C.codes + place * C.row_bytes + at * kBits / 8;
+    uint2 w[kRuns];
+#pragma unroll
+    for (uint32_t k = 0; k < kRuns; ++k) {
+      constexpr uint32_t kStep = kLanes * n * kBits / 8;
+      w[k] = make_uint2(0, 0);
+      if (at + k * kLanes * n >= C.dim) continue;
+      if constexpr (n * kBits == 16) w[k].x = half_word(p + k * kStep, at);
+      else if constexpr (n * kBits == 32) w[k].x = *reinterpret_cast<const uint32_t*>(p + k * kStep);
+      else w[k] = *reinterpret_cast<const uint2*>(p + k * kStep);
+    }
+    const float scale = __uint_as_float((uint32_t)C.scales[place * C.groups + group] << 16);
+    const Rows R = l.plane ? out.plane[1] : out.plane[0];
+    T* o = reinterpret_cast<T*>(R.data) + row * R.row_stride + l.head * R.head_stride + at;
+#pragma unroll
+    for (uint32_t k = 0; k < kRuns; ++k) {
+      const uint32_t first = at + k * kLanes * n;
+      if (first >= C.dim) continue;
+      float v[n];
+      values_of<kBits, n>(w[k], scale, v);
+      store_run(o + k * kLanes * n, (int)min(n, C.dim - first), v);
+    }
+  }
 }
 
 bool cache_ok(const lc_cache* c) {
   return c && (c->bits == 4 || c->bits == 8) && group_ok((int)c->group) && (c->planes == 1 || c->planes == 2) && c->heads >= 1 && c->heads <= 65536 &&
-         c->dim >= 1 && c->dim <= 65536 && c->slots < (1ull << 40);
+         c->dim >= 1 && c->dim <= 65536 && (uint64_t)c->heads * c->dim < (1ull << 31) && c->slots < (1ull << 40);
 }
 
 uint32_t row_bytes(const lc_cache* c) { return (c->dim + 7) / 8 * c->bits; }
 uint32_t row_groups(const lc_cache* c) { return (c->dim + c->group - 1) / c->group; }
 
-CacheArgs cache_args(const lc_cache* c) {
+CacheArgs cache_args(const lc_cache* c, uint64_t rows) {
+  const uint32_t lanes = row_groups(c) * (c->group / 16);  // of a head
   CacheArgs a = {};
   a.codes = static_cast<uint8_t*>(c->codes);
   a.scales = static_cast<unsigned short*>(c->scales);
   a.slots = c->slots;
   a.heads = c->heads;
   a.dim = c->dim;
-  a.bits = c->bits;
   a.row_bytes = row_bytes(c);
   a.groups = row_groups(c);
-  a.lanes = c->group / 8;
-  a.by_row = FastDiv(a.heads * a.groups);
-  a.by_groups = FastDiv(a.groups);
+  a.per_plane = c->heads * lanes;
+  a.per_row = a.per_plane * c->planes;
+  a.by_head = FastDiv(lanes);
+  // with few rows several warps share one, so that some thousands of them have work
+  const uint64_t turns = ((uint64_t)a.per_row + 31) / 32, wanted = (4096 + rows - 1) / rows;
+  a.by_warps = FastDiv((uint32_t)(wanted < turns ? wanted : turns));
   return a;
 }
 
 // The rows of a call: every plane's pointer and strides. written: no two rows may share memory.
 int check_rows(const lc_cache* c, const lc_rows* rows, int type, uint64_t n, bool written) {
   if (!cache_ok(c) || !type_ok(type) || !rows) return LC_ERR_ARG;
-  if ((uint64_t)c->heads * row_groups(c) >= (1ull << 31)) return LC_ERR_ARG;
   if (n == 0) return LC_OK;
   if (n >= (1ull << 31) || n * c->heads * row_groups(c) >= (1ull << 31)) return LC_ERR_ARG;
   if (c->slots > 0 && (!c->codes || !c->scales || !aligned_to(c->codes, 16) || !aligned_to(c->scales, 2))) return LC_ERR_ARG;
@@ -166,22 +229,31 @@ Planes planes_of(const lc_cache* c, const lc_rows* rows) {
   return p;
 }
 
-int launch_rows(void (*kernel)(CacheArgs, Planes, Places, uint32_t, int32_t*), const lc_cache* c, const lc_rows* rows, const Places& places, uint64_t n,
-                int32_t* status, cudaStream_t cs) {
-  const CacheArgs a = cache_args(c);
-  const uint32_t items = (uint32_t)n * a.by_row.d;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(((uint64_t)items * a.lanes + kThreads - 1) / kThreads), c->planes);
-  cfg.blockDim = dim3(kThreads);
-  cfg.stream = cs;
-  return cudaLaunchKernelEx(&cfg, kernel, a, planes_of(c, rows), places, items, status) == cudaSuccess ? LC_OK : LC_ERR_CUDA;
+using Kernel = void (*)(CacheArgs, Planes, Places, uint32_t, int32_t*);
+
+int launch_rows(Kernel kernel, const lc_cache* c, const lc_rows* rows, const Places& places, uint64_t n, int32_t* status, cudaStream_t cs) {
+  const CacheArgs a = cache_args(c, n);
+  const unsigned grid = (unsigned)((n * a.by_warps.d * 32 + kThreads - 1) / kThreads);
+  return launch_kernel(false, kernel, grid, kThreads, 0, cs, a, planes_of(c, rows), places, (uint32_t)n, status) == cudaSuccess ? LC_OK : LC_ERR_CUDA;
+}
+
+template <class T, int G>
+Kernel write_kernel(int bits) { return bits == 4 ? cache_write_kernel<T, G, 4> : cache_write_kernel<T, G, 8>; }
+template <class T>
+Kernel write_kernel(int group, int bits) { return group == 32 ? write_kernel<T, 32>(bits) : group == 64 ? write_kernel<T, 64>(bits) : write_kernel<T, 128>(bits); }
+template <class T, int G, bool kPages>
+Kernel read_kernel(int bits) { return bits == 4 ? cache_read_kernel<T, G, 4, kPages> : cache_read_kernel<T, G, 8, kPages>; }
+template <class T, bool kPages>
+Kernel read_kernel(int group, int bits) {
+  return group == 32 ? read_kernel<T, 32, kPages>(bits) : group == 64 ? read_kernel<T, 64, kPages>(bits) : read_kernel<T, 128, kPages>(bits);
 }
 
 template <bool kPages>
 int read_impl(const lc_cache* c, const lc_rows* out, int type, const Places& places, uint64_t n, int32_t* status, cudaStream_t cs) {
-  auto kernel = type == LC_TYPE_F32    ? cache_read_kernel<float, kPages>
-                : type == LC_TYPE_BF16 ? cache_read_kernel<__nv_bfloat16, kPages>
-                                       : cache_read_kernel<__half, kPages>;
+  const int group = (int)c->group, bits = (int)c->bits;
+  const Kernel kernel = type == LC_TYPE_F32    ? read_kernel<float, kPages>(group, bits)
+                        : type == LC_TYPE_BF16 ? read_kernel<__nv_bfloat16, kPages>(group, bits)
+                                               : read_kernel<__half, kPages>(group, bits);
   return launch_rows(kernel, c, out, places, n, status, cs);
 }
 
@@ -202,7 +274,10 @@ int lc_cache_write(const lc_cache* cache, const lc_rows* src, int type, uint64_t
   Places places = {};
   places.slots = slots;
   places.by_page = FastDiv(1);
-  auto kernel = type == LC_TYPE_F32 ? cache_write_kernel<float> : type == LC_TYPE_BF16 ? cache_write_kernel<__nv_bfloat16> : cache_write_kernel<__half>;
+  const int group = (int)cache->group, bits = (int)cache->bits;
+  const Kernel kernel = type == LC_TYPE_F32    ? write_kernel<float>(group, bits)
+                        : type == LC_TYPE_BF16 ? write_kernel<__nv_bfloat16>(group, bits)
+                                               : write_kernel<__half>(group, bits);
   return launch_rows(kernel, cache, src, places, rows, status, cs);
 }
 

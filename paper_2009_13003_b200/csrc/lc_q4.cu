@@ -6,110 +6,128 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// A thread takes eight columns of rows r and r + 8 of a tile, which is where the two words that hold them meet; the group / 8 lanes
-// of a group sit side by side, so that a group's maximum is a few shuffles and a row is read in whole lines. The next lanes take the
-// next r: together they write whole blocks. One pass, bound by memory: 4.5 (fp32) or 2.5 bytes a weight.
-template <class T>
+// A thread takes columns 8 t ... 8 t + 7 of both halves of a block of 64, of rows r and r + 8 of a tile: what 16 bytes of a lane's words
+// hold. The 4 lanes t (with groups of 128, those of two blocks) have a group's maximum by a few shuffles; the next lanes take the next
+// r, so that a warp writes whole blocks. One pass, bound by memory: 4.5 bytes a weight from fp32 (4096 x 25088: 70 us, the copy rate),
+// 2.5 from 16 bits, where the instructions of the codes weigh as much.
+template <class T, int G>
 __global__ void __launch_bounds__(kThreads) q4_quantize_kernel(const T* __restrict__ w, uint64_t row_stride, Q4Layout L, uint8_t* __restrict__ q4,
-                                                               int32_t* status, FastDiv by_groups) {
-  const uint32_t lanes = L.group / 8;
-  const uint64_t item = ((uint64_t)blockIdx.x * kThreads + threadIdx.x) / lanes;  // (tile, group, r)
-  const uint32_t lane = threadIdx.x & (lanes - 1);
-  const uint32_t r = (uint32_t)item & 7u;
-  const uint32_t tg = (uint32_t)(item >> 3);
-  const bool inside = (item >> 3) < (uint64_t)L.tiles * L.groups;  // all lanes stay for the shuffles
-  const uint32_t tile = inside ? by_groups.div(tg) : 0, g = tg - tile * L.groups;
-  const uint32_t col = g * L.group + 8 * lane;
-  const int valid = !inside || col >= L.cols ? 0 : (int)min(8u, L.cols - col);
-  uint32_t scale[2];
-  float v[2][8];
+                                                               int32_t* status, FastDiv by_spans) {
+  constexpr uint32_t kSpan = G == 128 ? 128 : 64, kLanes = kSpan / 16, kScales = G == 32 ? 2 : 1;  // columns, lanes and scales a row has here
+  const uint64_t item = ((uint64_t)blockIdx.x * kThreads + threadIdx.x) / kLanes;                  // (tile, span, r)
+  const uint32_t lane = threadIdx.x & (kLanes - 1), r = (uint32_t)item & 7u;
+  const bool inside = (item >> 3) < (uint64_t)L.tiles * by_spans.d;  // all lanes stay for the shuffles
+  const uint32_t tile = inside ? by_spans.div((uint32_t)(item >> 3)) : 0, span = inside ? (uint32_t)(item >> 3) - tile * by_spans.d : 0;
+  const uint32_t col = span * kSpan + (lane >> 2) * 64 + (lane & 3) * 8;
+  float v[2][2][8];  // row, half
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const uint64_t row = (uint64_t)tile * kQ4TileRows + r + 8 * h;
-    load8(w + row * row_stride + col, row < L.rows ? valid : 0, v[h]);
-  }
 #pragma unroll
-  for (int h = 0; h < 2; ++h) scale[h] = group_scale(max_over_lanes(max_bits8(v[h]), (int)lanes), 7.0f);
-  if (!inside) return;
-  int q[2][8];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) codes8(v[h], scale[h], q[h]);
-  uint32_t word[2];
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    uint32_t x = 0;
-#pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      const int* s = &q[p & 1][4 * j + 2 * (p >> 1)];
-      x |= ((uint32_t)(s[0] + 8) & 15u) << (4 * p) | ((uint32_t)(s[1] + 8) & 15u) << (16 + 4 * p);
+    for (int u = 0; u < 2; ++u) {
+      const uint32_t c = col + 32 * u;
+      load8(w + row * row_stride + c, !inside || row >= L.rows || c >= L.cols ? 0 : (int)min(8u, L.cols - c), v[h][u]);
     }
-    word[j] = x;
   }
-  const uint32_t block = col / 64, half = (col / 32) & 1, t = (col / 8) & 3;
-  uint8_t* at = q4 + ((uint64_t)tile * L.steps * 2 + block) * 512 + (r * 4 + t) * 16 + half * 8;
-  *reinterpret_cast<uint2*>(at) = make_uint2(word[0], word[1]);
+  uint32_t scale[2][kScales];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float m[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m[u % kScales] = max_magnitude(m[u % kScales], v[h][u][i]);
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < kScales; ++k) scale[h][k] = group_scale<4>(max_over_lanes(m[k], kLanes));
+  }
+  if (!inside) return;
+  uint32_t word[2][2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    float t[2][8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) codes<T, 4>(v[h][u], scale[h][u % kScales], t[h]);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float *a = t[0] + 4 * j, *b = t[1] + 4 * j;
+      word[u][j] = pack_pairs(pair_of(a[0], a[1]), pair_of(b[0], b[1]), pair_of(a[2], a[3]), pair_of(b[2], b[3]));
+    }
+  }
+  *reinterpret_cast<uint4*>(q4 + ((uint64_t)tile * L.steps * 2 + col / 64) * 512 + (r * 4 + (lane & 3)) * 16) = make_uint4(word[0][0], word[0][1], word[1][0], word[1][1]);
   if (lane == 0) {
-    reinterpret_cast<uint32_t*>(q4 + L.scales_off)[((uint64_t)tile * L.groups + g) * 8 + r] = (scale[0] >> 16) | (scale[1] & 0xFFFF0000u);
-    if (scale[0] == kScaleNaN || scale[1] == kScaleNaN) set_status(status, LC_ERR_NONFINITE);
+#pragma unroll
+    for (uint32_t k = 0; k < kScales; ++k) {
+      reinterpret_cast<uint32_t*>(q4 + L.scales_off)[((uint64_t)tile * L.groups + span * kScales + k) * 8 + r] = (scale[0][k] >> 16) | (scale[1][k] & 0xFFFF0000u);
+      if (scale[0][k] == kScaleNaN || scale[1][k] == kScaleNaN) set_status(status, LC_ERR_NONFINITE);
+    }
   }
 }
 
-// The same threads the other way round.
+// The other way round: rows r and r + 8 of a block of 64 columns, in both halves of it 16 bytes of the output a lane, so that the lanes of
+// a row write whole runs: 4 lanes for a 16-bit output, 8 for fp32 (half the words each).
 template <class T>
 __global__ void __launch_bounds__(kThreads) q4_read_kernel(const uint8_t* __restrict__ q4, Q4Layout L, T* __restrict__ out, uint64_t row_stride,
-                                                           FastDiv by_groups) {
-  const uint32_t lanes = L.group / 8;
-  const uint64_t item = ((uint64_t)blockIdx.x * kThreads + threadIdx.x) / lanes;
-  const uint32_t r = (uint32_t)item & 7u;
-  const uint32_t tg = (uint32_t)(item >> 3);
-  if ((item >> 3) >= (uint64_t)L.tiles * L.groups) return;
-  const uint32_t tile = by_groups.div(tg), g = tg - tile * L.groups;
-  const uint32_t col = g * L.group + 8 * (threadIdx.x & (lanes - 1));
-  if (col >= L.cols) return;
-  const int valid = (int)min(8u, L.cols - col);
-  const uint32_t block = col / 64, half = (col / 32) & 1, t = (col / 8) & 3;
-  const uint8_t* at = q4 + ((uint64_t)tile * L.steps * 2 + block) * 512 + (r * 4 + t) * 16 + half * 8;
-  const uint2 w = __ldg(reinterpret_cast<const uint2*>(at));
-  const uint32_t s = __ldg(reinterpret_cast<const uint32_t*>(q4 + L.scales_off) + ((uint64_t)tile * L.groups + g) * 8 + r);
+                                                           FastDiv by_blocks) {
+  constexpr uint32_t n = kRun<T>, kLanes = 32 / n;
+  const uint64_t item = ((uint64_t)blockIdx.x * kThreads + threadIdx.x) / kLanes;  // (tile, block, r)
+  if ((item >> 3) >= (uint64_t)L.tiles * by_blocks.d) return;
+  const uint32_t lane = threadIdx.x & (kLanes - 1), r = (uint32_t)item & 7u, tile = by_blocks.div((uint32_t)(item >> 3)), block = (uint32_t)(item >> 3) - tile * by_blocks.d;
+  const uint8_t* at = q4 + ((uint64_t)tile * L.steps * 2 + block) * 512 + r * 64;
+  uint2 w[2];  // of a half: the words of n columns
+  if constexpr (n == 8) {
+    const uint4 x = __ldg(reinterpret_cast<const uint4*>(at) + lane);
+    w[0] = make_uint2(x.x, x.y);
+    w[1] = make_uint2(x.z, x.w);
+  } else {
+    const uint32_t* x = reinterpret_cast<const uint32_t*>(at) + (lane >> 1) * 4 + (lane & 1);
+    w[0].x = __ldg(x);
+    w[1].x = __ldg(x + 2);
+  }
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const uint64_t row = (uint64_t)tile * kQ4TileRows + r + 8 * h;
-    const float scale = __uint_as_float(h ? s & 0xFFFF0000u : s << 16);
-    float v[8];
+  for (int u = 0; u < 2; ++u) {
+    const uint32_t c = block * 64 + 32 * u, s = __ldg(reinterpret_cast<const uint32_t*>(q4 + L.scales_off) + ((uint64_t)tile * L.groups + c / L.group) * 8 + r);
+    const uint32_t col = c + lane * n;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int bit = 16 * (e & 1) + 4 * (h + 2 * ((e >> 1) & 1));
-      v[e] = (__uint_as_float((((e < 4 ? w.x : w.y) >> bit) & 15u) | 0x4B000000u) - 8388616.0f) * scale;
+    for (int h = 0; h < 2; ++h) {
+      const uint64_t row = (uint64_t)tile * kQ4TileRows + r + 8 * h;
+      const float scale = __uint_as_float(h ? s & 0xFFFF0000u : s << 16);
+      float v[n];
+#pragma unroll
+      for (uint32_t e = 0; e < n; ++e) v[e] = code_of<4>(((e < 4 ? w[u].x : w[u].y) >> (16 * (e & 1) + 4 * (h + 2 * ((e >> 1) & 1)))) & 15u) * scale;
+      if (row < L.rows && col < L.cols) store_run(out + row * row_stride + col, (int)min(n, L.cols - col), v);
     }
-    if (row < L.rows) store8(out + row * row_stride + col, valid, v);
   }
 }
 
-uint64_t blocks_for(const Q4Layout& L) { return ((uint64_t)L.tiles * L.groups * L.group + kThreads - 1) / kThreads; }  // 8 r, group / 8 lanes
+// Threads for a tile's spans of `columns`, eight rows r each
+unsigned grid_of(const Q4Layout& L, uint32_t spans, uint32_t lanes) { return (unsigned)(((uint64_t)L.tiles * spans * 8 * lanes + kThreads - 1) / kThreads); }
+
+template <class T>
+cudaError_t quantize(const Q4Layout& L, const void* w, uint64_t row_stride, uint8_t* q4, int32_t* status, cudaStream_t cs) {
+  const auto kernel = L.group == 32 ? q4_quantize_kernel<T, 32> : L.group == 64 ? q4_quantize_kernel<T, 64> : q4_quantize_kernel<T, 128>;
+  const uint32_t spans = L.group == 128 ? L.steps : 2 * L.steps, lanes = L.group == 128 ? 8 : 4;
+  return launch_kernel(false, kernel, grid_of(L, spans, lanes), kThreads, 0, cs, static_cast<const T*>(w), row_stride, L, q4, status, FastDiv(spans));
+}
+template <class T>
+cudaError_t read(const Q4Layout& L, const uint8_t* q4, void* out, uint64_t row_stride, cudaStream_t cs) {
+  return launch_kernel(false, q4_read_kernel<T>, grid_of(L, 2 * L.steps, 32 / kRun<T>), kThreads, 0, cs, q4, L, static_cast<T*>(out), row_stride, FastDiv(2 * L.steps));
+}
 
 }  // namespace
 
 cudaError_t launch_q4_quantize(const Q4Layout& L, const void* w, int type, uint64_t row_stride, uint8_t* q4, int32_t* status, cudaStream_t cs) {
-  const uint64_t blocks = blocks_for(L);
-  if (blocks == 0) return cudaSuccess;
-  const FastDiv by_groups(L.groups);
-  if (type == LC_TYPE_F32)
-    return launch_kernel(false, q4_quantize_kernel<float>, (unsigned)blocks, kThreads, 0, cs, static_cast<const float*>(w), row_stride, L, q4, status, by_groups);
-  if (type == LC_TYPE_BF16)
-    return launch_kernel(false, q4_quantize_kernel<__nv_bfloat16>, (unsigned)blocks, kThreads, 0, cs, static_cast<const __nv_bfloat16*>(w), row_stride, L, q4,
-                         status, by_groups);
-  return launch_kernel(false, q4_quantize_kernel<__half>, (unsigned)blocks, kThreads, 0, cs, static_cast<const __half*>(w), row_stride, L, q4, status, by_groups);
+  if (L.tiles == 0 || L.steps == 0) return cudaSuccess;
+  if (type == LC_TYPE_F32) return quantize<float>(L, w, row_stride, q4, status, cs);
+  if (type == LC_TYPE_BF16) return quantize<__nv_bfloat16>(L, w, row_stride, q4, status, cs);
+  return quantize<__half>(L, w, row_stride, q4, status, cs);
 }
 
 cudaError_t launch_q4_read(const Q4Layout& L, const uint8_t* q4, void* out, int type, uint64_t row_stride, cudaStream_t cs) {
-  const uint64_t blocks = blocks_for(L);
-  if (blocks == 0) return cudaSuccess;
-  const FastDiv by_groups(L.groups);
-  if (type == LC_TYPE_F32)
-    return launch_kernel(false, q4_read_kernel<float>, (unsigned)blocks, kThreads, 0, cs, q4, L, static_cast<float*>(out), row_stride, by_groups);
-  if (type == LC_TYPE_BF16)
-    return launch_kernel(false, q4_read_kernel<__nv_bfloat16>, (unsigned)blocks, kThreads, 0, cs, q4, L, static_cast<__nv_bfloat16*>(out), row_stride, by_groups);
-  return launch_kernel(false, q4_read_kernel<__half>, (unsigned)blocks, kThreads, 0, cs, q4, L, static_cast<__half*>(out), row_stride, by_groups);
+  if (L.tiles == 0 || L.steps == 0) return cudaSuccess;
+  if (type == LC_TYPE_F32) return read<float>(L, q4, out, row_stride, cs);
+  if (type == LC_TYPE_BF16) return read<__nv_bfloat16>(L, q4, out, row_stride, cs);
+  return read<__half>(L, q4, out, row_stride, cs);
 }
 
 }  // namespace lc

@@ -6,7 +6,7 @@
 //
 // The scale has 8 significant bits because the codes are chosen against the rounded scale (so its rounding costs nothing) and
 // because w - code * scale and scale / 2 are then exact in fp32: whether a code is the nearest one is decided exactly, by a
-// compare, although the first guess comes from a product with a rounded reciprocal. max / scale is at most Q / (1 - 2^-8), i.e.
+// compare, although the first guess comes from a product with a reciprocal. max / scale is at most Q / (1 - 2^-8), i.e.
 // 7.03 and 127.4981, so codes stay within +-Q without a clamp. A group that holds Inf or NaN gets a scale of NaN (and codes of 0).
 #pragma once
 
@@ -40,121 +40,152 @@ __device__ __forceinline__ void from_float(float v, float& x) { x = v; }
 __device__ __forceinline__ void from_float(float v, __nv_bfloat16& x) { x = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void from_float(float v, __half& x) { x = __float2half_rn(v); }
 
-// Eight neighbouring values of a row as fp32, zeros from `valid` on. Where all are there and the address allows it, by loads of 16 bytes.
+// Eight neighbouring values of a row as fp32, zeros from `valid` on: by the widest loads that the address allows (rows of heads of 100
+// values in 16 bits begin on 8 bytes).
 template <class T>
-__device__ __forceinline__ void load8(const T* p, int valid, float (&v)[8]) {
-  if (valid >= 8 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+__device__ __forceinline__ void load8(const T* p, int valid, float* v) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+  if (valid >= 8 && (at & 15) == 0) {
     uint4 raw[sizeof(T) / 2];
 #pragma unroll
     for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
     const T* e = reinterpret_cast<const T*>(raw);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = to_float(e[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < valid ? to_float(p[i]) : 0.0f;
-  }
-}
-
-template <class T>
-__device__ __forceinline__ void store8(T* p, int valid, const float (&v)[8]) {
-  if (valid >= 8 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
-    uint4 raw[sizeof(T) / 2];
-    T* e = reinterpret_cast<T*>(raw);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) from_float(v[i], e[i]);
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(p)[i] = raw[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < valid) from_float(v[i], p[i]);
-  }
-}
-
-// The largest magnitude of eight values as fp32 bits: as whole numbers these order like the magnitudes, with Inf and NaN above.
-__device__ __forceinline__ uint32_t max_bits8(const float (&v)[8]) {
-  uint32_t m = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-  return m;
-}
-
-// The maximum over the `lanes` neighbouring lanes (a power of two, aligned) that hold a group. All 32 lanes take part.
-__device__ __forceinline__ uint32_t max_over_lanes(uint32_t m, int lanes) {
-  for (int d = 1; d < lanes; d <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-  return m;
-}
-
-// bf16(max / top), as fp32 bits, from the maximum's bits. The fp32 quotient rounds a second time only if it lies exactly between
-// two bf16 numbers; the sign of its remainder (exact, by one multiply-add) then tells on which side the true quotient is.
-__device__ __forceinline__ uint32_t group_scale(uint32_t max_bits, float top) {
-  if (max_bits >= 0x7F800000u) return kScaleNaN;
-  const float most = __uint_as_float(max_bits), q = __fdiv_rn(most, top);
-  const uint32_t u = __float_as_uint(q);
-  uint32_t s = u + 0x7FFFu + ((u >> 16) & 1u);
-  if ((u & 0xFFFFu) == 0x8000u) {
-    const float rest = __fmaf_rn(-q, top, most);
-    if (rest != 0.0f) s = rest > 0.0f ? u + 0x8000u : u;
-  }
-  s &= 0xFFFF0000u;
-  return s < 0x00800000u ? 0u : s;
-}
-
-// The codes of eight values, as two's complement whole numbers. (x + 1.5 * 2^23 rounds x to a whole number, ties to even, and
-// holds it in its low bits.)
-__device__ __forceinline__ void codes8(const float (&v)[8], uint32_t scale_bits, int (&q)[8]) {
-  if (scale_bits == 0u || scale_bits == kScaleNaN) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = 0;
     return;
   }
-  const float s = __uint_as_float(scale_bits), inv = __frcp_rn(s), half = 0.5f * s, magic = 12582912.0f;
-  float far = 0.0f, rest[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float t = __fmaf_rn(v[i], inv, magic);
-    q[i] = (int)(__float_as_uint(t) - __float_as_uint(magic));
-    rest[i] = __fmaf_rn(-(t - magic), s, v[i]);
-    far = fmaxf(far, fabsf(rest[i]));
-  }
-  if (far >= half) {  // a guess on the wrong side of a border, or a value on one
+  for (int h = 0; h < 8; h += 4) {
+    if (sizeof(T) == 2 && valid >= h + 4 && (at & 7) == 0) {
+      const uint2 raw = __ldg(reinterpret_cast<const uint2*>(p + h));
+      const T* e = reinterpret_cast<const T*>(&raw);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float r = fabsf(rest[i]);
-      if (r > half || (r == half && (q[i] & 1))) q[i] += rest[i] > 0.0f ? 1 : -1;
+      for (int i = 0; i < 4; ++i) v[h + i] = to_float(e[i]);
+    } else {
+#pragma unroll
+      for (int i = h; i < h + 4; ++i) v[i] = i < valid ? to_float(p[i]) : 0.0f;
     }
   }
 }
 
-// Eight codes in a row of 4 bits: value e at bit 4 * (e / 2) + 16 * (e % 2), offset by 8, so that a mask takes two neighbours out
-// as the two halves of a word. In 8 bits: one byte after the other, offset by 128.
-__device__ __forceinline__ uint32_t pack4(const int (&q)[8]) {
-  uint32_t w = 0;
+// `n` neighbouring values the other way, 16 bytes of them where all are there. The lanes of a warp hold neighbouring runs, so that a store
+// of theirs is one run of bytes: with 32 bytes a lane and two stores of every other 16, memory pays for both halves of each 32 (0.4 GB of
+// fp32 from 4 bits: 98 us; so 72).
+template <class T>
+constexpr int kRun = 16 / sizeof(T);
+template <class T>
+__device__ __forceinline__ void store_run(T* p, int valid, const float* v) {
+  constexpr int n = kRun<T>;
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+  if (valid >= n && (at & 15) == 0) {
+    uint4 raw;
+    T* e = reinterpret_cast<T*>(&raw);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) w |= ((uint32_t)(q[e] + 8) & 15u) << (4 * (e / 2) + 16 * (e % 2));
-  return w;
-}
-__device__ __forceinline__ uint2 pack8(const int (&q)[8]) {
-  uint2 w = make_uint2(0, 0);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    w.x |= ((uint32_t)(q[e] + 128) & 255u) << (8 * e);
-    w.y |= ((uint32_t)(q[e + 4] + 128) & 255u) << (8 * e);
+    for (int i = 0; i < n; ++i) from_float(v[i], e[i]);
+    *reinterpret_cast<uint4*>(p) = raw;
+    return;
   }
-  return w;
+#pragma unroll
+  for (int h = 0; h < n; h += 4) {
+    if (sizeof(T) == 2 && valid >= h + 4 && (at & 7) == 0) {
+      uint2 raw;
+      T* e = reinterpret_cast<T*>(&raw);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) from_float(v[h + i], e[i]);
+      *reinterpret_cast<uint2*>(p + h) = raw;
+    } else {
+#pragma unroll
+      for (int i = h; i < h + 4; ++i)
+        if (i < valid) from_float(v[i], p[i]);
+    }
+  }
 }
 
-// code * scale, exact in fp32. 2^23 + n holds n in its low bits.
-__device__ __forceinline__ void values_of4(uint32_t w, float s, float (&v)[8]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e)
-    v[e] = (__uint_as_float(((w >> (4 * (e / 2) + 16 * (e % 2))) & 15u) | 0x4B000000u) - 8388616.0f) * s;
+// The larger of two magnitudes; NaN if one is.
+__device__ __forceinline__ float max_magnitude(float a, float b) {
+  float m;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(fabsf(a)), "f"(fabsf(b)));
+  return m;
 }
-__device__ __forceinline__ void values_of8(uint2 w, float s, float (&v)[8]) {
+
+// The largest magnitude over the `lanes` neighbouring lanes (a power of two, aligned) that hold a group. All 32 lanes take part.
+__device__ __forceinline__ float max_over_lanes(float m, int lanes) {
+  for (int d = 1; d < lanes; d <<= 1) m = max_magnitude(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+  return m;
+}
+
+// bf16(most / Q), as fp32 bits. From a quotient that is right to a few units in fp32's last place, cut to bf16: the next bf16 number is the
+// nearer one if most lies beyond Q times the middle between the two, or on it and the lower one is odd. That product has 16 bits, so
+// the compare is exact (and it holds also where the cut is one number off).
+template <int kBits>
+__device__ __forceinline__ uint32_t group_scale(float most) {
+  constexpr float kTop = (1 << (kBits - 1)) - 1;
+  if (!(most < __uint_as_float(0x7F800000u))) return kScaleNaN;
+  const uint32_t low = __float_as_uint(most * (1.0f / kTop)) & 0xFFFF0000u;
+  const float beyond = __fmaf_rn(-__uint_as_float(low | 0x8000u), kTop, most);
+  const uint32_t s = beyond > 0.0f || (beyond == 0.0f && (low & 0x10000u)) ? low + 0x10000u : low;
+  return s < 0x00800000u ? 0u : s;
+}
+
+// The codes of `n` values of type T, each plus 2^(bits - 1) in the low bits of a float's pattern (x + 1.5 * 2^23 rounds x to a whole number,
+// ties to even, and holds it there). With at most 11 bits in a value and 8 in the scale, a quotient is a tie or far from one, and one
+// step of refinement makes it the nearest fp32 number, which a tie is itself. An fp32 value can be anywhere: its code is a guess
+// that the exact remainder confirms, or, hardly ever, moves by one.
+template <class T, int kBits, int n>
+__device__ __forceinline__ void codes(const float (&v)[n], uint32_t scale_bits, float (&t)[n]) {
+  constexpr float kMagic = 12582912.0f + (1 << (kBits - 1));
+  if (scale_bits == 0u || scale_bits == kScaleNaN) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-    v[e] = (__uint_as_float(__byte_perm(e < 4 ? w.x : w.y, 0x4B000000u, 0x7540 | (e & 3))) - 8388736.0f) * s;
+    for (int i = 0; i < n; ++i) t[i] = kMagic;
+    return;
+  }
+  const float s = __uint_as_float(scale_bits), half = 0.5f * s;
+  float inv, far = 0.0f;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(s));
+#pragma unroll
+  for (int i = 0; i < n; ++i) {
+    if constexpr (sizeof(T) == 2) {
+      const float q = v[i] * inv;
+      t[i] = __fadd_rn(__fmaf_rn(__fmaf_rn(-q, s, v[i]), inv, q), kMagic);
+    } else {
+      t[i] = __fmaf_rn(v[i], inv, kMagic);
+      far = fmaxf(far, fabsf(__fmaf_rn(kMagic - t[i], s, v[i])));
+    }
+  }
+  if (sizeof(T) == 4 && far >= half) {
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const float rest = __fmaf_rn(kMagic - t[i], s, v[i]), r = fabsf(rest);
+      if (r > half || (r == half && (__float_as_uint(t[i]) & 1u))) t[i] += rest > 0.0f ? 1.0f : -1.0f;
+    }
+  }
+}
+
+// Two neighbouring codes as the halves of a word, and four pairs of 4 bits as one: a mask takes a pair out again. Pair p of eight values
+// in a row is values 2 p and 2 p + 1.
+__device__ __forceinline__ uint32_t pair_of(float a, float b) { return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x5410); }
+__device__ __forceinline__ uint32_t pack_pairs(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return a + (b << 4) + (c << 8) + (d << 12); }
+__device__ __forceinline__ uint32_t pack4(const float* t) {
+  return pack_pairs(pair_of(t[0], t[1]), pair_of(t[2], t[3]), pair_of(t[4], t[5]), pair_of(t[6], t[7]));
+}
+// Four codes of 8 bits, one byte after the other.
+__device__ __forceinline__ uint32_t pack_bytes(const float* t) {
+  const uint32_t a = __byte_perm(__float_as_uint(t[0]), __float_as_uint(t[1]), 0x0040), b = __byte_perm(__float_as_uint(t[2]), __float_as_uint(t[3]), 0x0040);
+  return __byte_perm(a, b, 0x5410);
+}
+__device__ __forceinline__ uint2 pack8(const float* t) { return make_uint2(pack_bytes(t), pack_bytes(t + 4)); }
+
+// The number in the low bits of 2^23 + n, less what was added to it: n - offset.
+template <int kBits>
+__device__ __forceinline__ float code_of(uint32_t n) { return __uint_as_float(n | 0x4B000000u) - (8388608.0f + (1 << (kBits - 1))); }
+// Values `first` ... `first` + n - 1 of eight in a row of a cache: code * scale, exact in fp32. first: a multiple of 4.
+template <int kBits, int n>
+__device__ __forceinline__ void values_of(uint2 w, float s, float* v) {
+#pragma unroll
+  for (int e = 0; e < n; ++e) {
+    const uint32_t code = kBits == 4 ? (w.x >> (4 * (e / 2) + 16 * (e % 2))) & 15u : __byte_perm(e < 4 ? w.x : w.y, 0, 0x4440 | (e & 3));
+    v[e] = code_of<kBits>(code) * s;
+  }
 }
 
 // n / d by a multiplication, for n < 2^31 and 1 <= d < 2^31 (a division by a number known only at run time takes some twenty
