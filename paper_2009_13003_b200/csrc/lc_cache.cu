@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(CacheArgs C, Plane
       const uint32_t first = at + k * kLanes * n;
       if (first >= C.dim) continue;
       float v[n];
-      values_of<kBits, n>(w[k], scale, v);
+      values_in_row<kBits, n>(w[k], scale, v);
       store_run(o + k * kLanes * n, (int)min(n, C.dim - first), v);
     }
   }

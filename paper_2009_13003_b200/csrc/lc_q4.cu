@@ -92,9 +92,11 @@ __global__ void __launch_bounds__(kThreads) q4_read_kernel(const uint8_t* __rest
     for (int h = 0; h < 2; ++h) {
       const uint64_t row = (uint64_t)tile * kQ4TileRows + r + 8 * h;
       const float scale = __uint_as_float(h ? s & 0xFFFF0000u : s << 16);
-      float v[n];
+      uint32_t codes[n];
 #pragma unroll
-      for (uint32_t e = 0; e < n; ++e) v[e] = code_of<4>(((e < 4 ? w[u].x : w[u].y) >> (16 * (e & 1) + 4 * (h + 2 * ((e >> 1) & 1)))) & 15u) * scale;
+      for (uint32_t e = 0; e < n; ++e) codes[e] = ((e < 4 ? w[u].x : w[u].y) >> (16 * (e & 1) + 4 * (h + 2 * ((e >> 1) & 1)))) & 15u;
+      float v[n];
+      values_of<4>(codes, scale, v);
       if (row < L.rows && col < L.cols) store_run(out + row * row_stride + col, (int)min(n, L.cols - col), v);
     }
   }

@@ -127,6 +127,30 @@ __device__ __forceinline__ uint32_t group_scale(float most) {
   return s < 0x00800000u ? 0u : s;
 }
 
+// Two fp32 numbers in one instruction.
+using Two = unsigned long long;
+__device__ __forceinline__ Two two(float a, float b) {
+  Two r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void split_two(Two r, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r)); }
+__device__ __forceinline__ Two fma_two(Two a, Two b, Two c) {
+  Two r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ Two add_two(Two a, Two b) {
+  Two r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ Two mul_two(Two a, Two b) {
+  Two r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 // The codes of `n` values of type T, each plus 2^(bits - 1) in the low bits of a float's pattern (x + 1.5 * 2^23 rounds x to a whole number,
 // ties to even, and holds it there). With at most 11 bits in a value and 8 in the scale, a quotient is a tie or far from one, and one
 // step of refinement makes it the nearest fp32 number, which a tie is itself. An fp32 value can be anywhere: its code is a guess
@@ -142,14 +166,19 @@ __device__ __forceinline__ void codes(const float (&v)[n], uint32_t scale_bits, 
   const float s = __uint_as_float(scale_bits), half = 0.5f * s;
   float inv, far = 0.0f;
   asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(s));
+  const Two inv2 = two(inv, inv), minus_s = two(-s, -s), magic = two(kMagic, kMagic);
 #pragma unroll
-  for (int i = 0; i < n; ++i) {
+  for (int i = 0; i < n; i += 2) {
+    const Two x = two(v[i], v[i + 1]);
     if constexpr (sizeof(T) == 2) {
-      const float q = v[i] * inv;
-      t[i] = __fadd_rn(__fmaf_rn(__fmaf_rn(-q, s, v[i]), inv, q), kMagic);
+      const Two q = mul_two(x, inv2);
+      split_two(add_two(fma_two(fma_two(q, minus_s, x), inv2, q), magic), t[i], t[i + 1]);
     } else {
-      t[i] = __fmaf_rn(v[i], inv, kMagic);
-      far = fmaxf(far, fabsf(__fmaf_rn(kMagic - t[i], s, v[i])));
+      const Two c = fma_two(x, inv2, magic);
+      float a, b;
+      split_two(fma_two(add_two(c, two(-kMagic, -kMagic)), minus_s, x), a, b);
+      far = fmaxf(far, fmaxf(fabsf(a), fabsf(b)));
+      split_two(c, t[i], t[i + 1]);
     }
   }
   if (sizeof(T) == 4 && far >= half) {
@@ -175,17 +204,23 @@ __device__ __forceinline__ uint32_t pack_bytes(const float* t) {
 }
 __device__ __forceinline__ uint2 pack8(const float* t) { return make_uint2(pack_bytes(t), pack_bytes(t + 4)); }
 
-// The number in the low bits of 2^23 + n, less what was added to it: n - offset.
-template <int kBits>
-__device__ __forceinline__ float code_of(uint32_t n) { return __uint_as_float(n | 0x4B000000u) - (8388608.0f + (1 << (kBits - 1))); }
-// Values `first` ... `first` + n - 1 of eight in a row of a cache: code * scale, exact in fp32. first: a multiple of 4.
-template <int kBits, int n>
-__device__ __forceinline__ void values_of(uint2 w, float s, float* v) {
+// What the codes in the low bits of n[] stand for, in fp32: exact. (2^23 + n holds n in its low bits.)
+template <int kBits, int count>
+__device__ __forceinline__ void values_of(const uint32_t (&n)[count], float scale, float* v) {
+  constexpr float kOffset = -(8388608.0f + (1 << (kBits - 1)));
 #pragma unroll
-  for (int e = 0; e < n; ++e) {
-    const uint32_t code = kBits == 4 ? (w.x >> (4 * (e / 2) + 16 * (e % 2))) & 15u : __byte_perm(e < 4 ? w.x : w.y, 0, 0x4440 | (e & 3));
-    v[e] = code_of<kBits>(code) * s;
+  for (int e = 0; e < count; e += 2) {
+    const Two x = two(__uint_as_float(n[e] | 0x4B000000u), __uint_as_float(n[e + 1] | 0x4B000000u));
+    split_two(mul_two(add_two(x, two(kOffset, kOffset)), two(scale, scale)), v[e], v[e + 1]);
   }
+}
+// The first `count` values of eight in a row of a cache.
+template <int kBits, int count>
+__device__ __forceinline__ void values_in_row(uint2 w, float scale, float* v) {
+  uint32_t n[count];
+#pragma unroll
+  for (int e = 0; e < count; ++e) n[e] = kBits == 4 ? (w.x >> (4 * (e / 2) + 16 * (e % 2))) & 15u : __byte_perm(e < 4 ? w.x : w.y, 0, 0x4440 | (e & 3));
+  values_of<kBits>(n, scale, v);
 }
 
 // n / d by a multiplication, for n < 2^31 and 1 <= d < 2^31 (a division by a number known only at run time takes some twenty
