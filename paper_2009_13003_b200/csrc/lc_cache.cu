@@ -12,6 +12,7 @@ struct CacheArgs {
   uint64_t slots;
   uint32_t heads, dim, groups, row_bytes;  // groups per row of dim values
   uint32_t per_plane, per_row;                        // lanes: of a plane's row, of all planes'
+  uint32_t width_log;                                 // of the lanes of a warp that a row gets: less than all, if they are enough
   FastDiv by_head, by_warps;                          // lanes of a head, warps that share a row
 };
 
@@ -71,7 +72,7 @@ __device__ __forceinline__ int64_t slot_of(const Places& P, uint32_t row, uint64
   return slot;
 }
 
-// A warp takes a row (or, with few rows, several share one): its place is looked up once for all planes and heads. group / 16 lanes hold
+// A warp takes a row (with few rows several share one; short rows share a warp): its place is looked up once for all planes and heads. group / 16 lanes hold
 // a group, 16 values each: neighbouring ones where they are quantised; where they are read, runs of 16 bytes of the output, so that
 // the lanes' runs follow each other. One pass over the rows; from and to 16 bits the instructions of the codes weigh as much as the bytes
 // (reading 131072 rows of 8 x 128 from 4 bits to bf16, twice: 119 us; with one run of 8 values a lane, and so twice the index arithmetic, 177).
@@ -87,26 +88,29 @@ __device__ __forceinline__ Lane lane_of(const CacheArgs& C, uint32_t j) {
   return l;
 }
 
-template <class T, int G, int kBits>
+// kWhole: dim is a multiple of 16, and so are the addresses of all heads' rows (in bytes): nothing is cut off and nothing to be looked at a lane.
+template <class T, int G, int kBits, bool kWhole>
 __global__ void __launch_bounds__(kThreads) cache_write_kernel(CacheArgs C, Planes src, Places P, uint32_t rows, int32_t* status) {
   constexpr int kLanes = G / 16;
-  const uint32_t lane = threadIdx.x & 31, warp = (uint32_t)(((uint64_t)blockIdx.x * kThreads + threadIdx.x) >> 5);
-  const uint32_t row = C.by_warps.div(warp);
-  if (row >= rows) return;  // whole warps
+  const uint32_t warp = (uint32_t)(((uint64_t)blockIdx.x * kThreads + threadIdx.x) >> 5), width = 1u << C.width_log;
+  const uint32_t lane = threadIdx.x & (width - 1), share = C.by_warps.div(warp), row = (share << (5 - C.width_log)) + ((threadIdx.x & 31) >> C.width_log);
+  if (row >= rows) return;  // a row's lanes together
   bool bad = false;
   const int64_t slot = slot_of<false>(P, row, C.slots, bad);
   if (bad && status && lane == 0) set_status(status, LC_ERR_INDEX);
   if (slot < 0) return;
-  for (uint32_t j0 = (warp - row * C.by_warps.d) * 32; j0 < C.per_row; j0 += C.by_warps.d * 32) {
+  for (uint32_t j0 = (warp - share * C.by_warps.d) * 32; j0 < C.per_row; j0 += C.by_warps.d * 32) {
     const bool inside = j0 + lane < C.per_row;
     const Lane l = lane_of(C, inside ? j0 + lane : 0);
     const uint32_t at = l.part * 16;
     const Rows R = l.plane ? src.plane[1] : src.plane[0];
     const T* p = reinterpret_cast<const T*>(R.data) + row * R.row_stride + l.head * R.head_stride + at;
     const int valid = inside ? (int)C.dim - (int)at : 0;
-    float v[16], m = 0.0f;
-    load8(p, valid, v);
-    load8(p + 8, valid - 8, v + 8);
+    float v[16] = {}, m = 0.0f;
+    if (!kWhole || valid > 0) {
+      load8<kWhole>(p, valid, v);
+      load8<kWhole>(p + 8, valid - 8, v + 8);
+    }
 #pragma unroll
     for (int i = 0; i < 16; ++i) m = max_magnitude(m, v[i]);
     const uint32_t scale = group_scale<kBits>(max_over_lanes(m, kLanes));
@@ -117,7 +121,7 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(CacheArgs C, Plan
     uint8_t* o = C.codes + place * C.row_bytes + at * kBits / 8;
     if constexpr (kBits == 4) {
       const uint32_t a = pack4(t), b = pack4(t + 8);
-      if (valid > 8 && (reinterpret_cast<uintptr_t>(o) & 7) == 0) {
+      if (kWhole || (valid > 8 && (reinterpret_cast<uintptr_t>(o) & 7) == 0)) {
         *reinterpret_cast<uint2*>(o) = make_uint2(a, b);
       } else {
         *reinterpret_cast<uint32_t*>(o) = a;
@@ -125,7 +129,7 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(CacheArgs C, Plan
       }
     } else {
       const uint2 a = pack8(t), b = pack8(t + 8);
-      if (valid > 8 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+      if (kWhole || (valid > 8 && (reinterpret_cast<uintptr_t>(o) & 15) == 0)) {
         *reinterpret_cast<uint4*>(o) = make_uint4(a.x, a.y, b.x, b.y);
       } else {
         *reinterpret_cast<uint2*>(o) = a;
@@ -141,27 +145,28 @@ __device__ __forceinline__ uint32_t half_word(const uint8_t* p, uint32_t at) {
   return *reinterpret_cast<const uint32_t*>(p - (at & 4) / 2) >> ((at & 4) * 2);
 }
 
-template <class T, int G, int kBits, bool kPages>
+template <class T, int G, int kBits, bool kPages, bool kWhole>
 __global__ void __launch_bounds__(kThreads) cache_read_kernel(CacheArgs C, Planes out, Places P, uint32_t rows, int32_t* status) {
   constexpr uint32_t kLanes = G / 16, n = kRun<T>, kRuns = 16 / n;
-  const uint32_t lane = threadIdx.x & 31, warp = (uint32_t)(((uint64_t)blockIdx.x * kThreads + threadIdx.x) >> 5);
-  const uint32_t row = C.by_warps.div(warp);
+  const uint32_t warp = (uint32_t)(((uint64_t)blockIdx.x * kThreads + threadIdx.x) >> 5), width = 1u << C.width_log;
+  const uint32_t lane = threadIdx.x & (width - 1), share = C.by_warps.div(warp), row = (share << (5 - C.width_log)) + ((threadIdx.x & 31) >> C.width_log);
   if (row >= rows) return;
   bool bad = false;
   const int64_t slot = slot_of<kPages>(P, row, C.slots, bad);
   if (bad && status && lane == 0) set_status(status, LC_ERR_INDEX);
   if (slot < 0) return;
-  for (uint32_t j = (warp - row * C.by_warps.d) * 32 + lane; j < C.per_row; j += C.by_warps.d * 32) {
+  for (uint32_t j = (warp - share * C.by_warps.d) * 32 + lane; j < C.per_row; j += C.by_warps.d * 32) {
     const Lane l = lane_of(C, j);
     const uint32_t group = l.part / kLanes, at = group * G + (l.part & (kLanes - 1)) * n;  // of the first run
     const uint64_t place = (l.plane * C.slots + (uint64_t)slot) * C.heads + l.head;
     const uint8_t* p = C.codes + place * C.row_bytes + at * kBits / 8;
+    const bool whole = kWhole && (group + 1) * G <= C.dim;  // the row's last group may be short
     uint2 w[kRuns];
 #pragma unroll
     for (uint32_t k = 0; k < kRuns; ++k) {
       constexpr uint32_t kStep = kLanes * n * kBits / 8;
       w[k] = make_uint2(0, 0);
-      if (at + k * kLanes * n >= C.dim) continue;
+      if (!whole && at + k * kLanes * n >= C.dim) continue;
       if constexpr (n * kBits == 16) w[k].x = half_word(p + k * kStep, at);
       else if constexpr (n * kBits == 32) w[k].x = *reinterpret_cast<const uint32_t*>(p + k * kStep);
       else w[k] = *reinterpret_cast<const uint2*>(p + k * kStep);
@@ -172,10 +177,10 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(CacheArgs C, Plane
 #pragma unroll
     for (uint32_t k = 0; k < kRuns; ++k) {
       const uint32_t first = at + k * kLanes * n;
-      if (first >= C.dim) continue;
+      if (!whole && first >= C.dim) continue;
       float v[n];
       values_in_row<kBits, n>(w[k], scale, v);
-      store_run(o + k * kLanes * n, (int)min(n, C.dim - first), v);
+      store_run<kWhole>(o + k * kLanes * n, (int)min(n, C.dim - first), v);
     }
   }
 }
@@ -204,6 +209,7 @@ CacheArgs cache_args(const lc_cache* c, uint64_t rows) {
   // with few rows several warps share one, so that some thousands of them have work
   const uint64_t turns = ((uint64_t)a.per_row + 31) / 32, wanted = (4096 + rows - 1) / rows;
   a.by_warps = FastDiv((uint32_t)(wanted < turns ? wanted : turns));
+  while ((1u << a.width_log) < a.per_row && a.width_log < 5) ++a.width_log;
   return a;
 }
 
@@ -233,27 +239,44 @@ using Kernel = void (*)(CacheArgs, Planes, Places, uint32_t, int32_t*);
 
 int launch_rows(Kernel kernel, const lc_cache* c, const lc_rows* rows, const Places& places, uint64_t n, int32_t* status, cudaStream_t cs) {
   const CacheArgs a = cache_args(c, n);
-  const unsigned grid = (unsigned)((n * a.by_warps.d * 32 + kThreads - 1) / kThreads);
+  const uint64_t shares = (n + (32 >> a.width_log) - 1) >> (5 - a.width_log);
+  const unsigned grid = (unsigned)((shares * a.by_warps.d * 32 + kThreads - 1) / kThreads);
   return launch_kernel(false, kernel, grid, kThreads, 0, cs, a, planes_of(c, rows), places, (uint32_t)n, status) == cudaSuccess ? LC_OK : LC_ERR_CUDA;
 }
 
-template <class T, int G>
-Kernel write_kernel(int bits) { return bits == 4 ? cache_write_kernel<T, G, 4> : cache_write_kernel<T, G, 8>; }
-template <class T>
-Kernel write_kernel(int group, int bits) { return group == 32 ? write_kernel<T, 32>(bits) : group == 64 ? write_kernel<T, 64>(bits) : write_kernel<T, 128>(bits); }
-template <class T, int G, bool kPages>
-Kernel read_kernel(int bits) { return bits == 4 ? cache_read_kernel<T, G, 4, kPages> : cache_read_kernel<T, G, 8, kPages>; }
-template <class T, bool kPages>
+template <class T, int G, bool kWhole>
+Kernel write_kernel(int bits) { return bits == 4 ? cache_write_kernel<T, G, 4, kWhole> : cache_write_kernel<T, G, 8, kWhole>; }
+template <class T, bool kWhole>
+Kernel write_kernel(int group, int bits) {
+  return group == 32 ? write_kernel<T, 32, kWhole>(bits) : group == 64 ? write_kernel<T, 64, kWhole>(bits) : write_kernel<T, 128, kWhole>(bits);
+}
+template <class T, int G, bool kPages, bool kWhole>
+Kernel read_kernel(int bits) { return bits == 4 ? cache_read_kernel<T, G, 4, kPages, kWhole> : cache_read_kernel<T, G, 8, kPages, kWhole>; }
+template <class T, bool kPages, bool kWhole>
 Kernel read_kernel(int group, int bits) {
-  return group == 32 ? read_kernel<T, 32, kPages>(bits) : group == 64 ? read_kernel<T, 64, kPages>(bits) : read_kernel<T, 128, kPages>(bits);
+  return group == 32 ? read_kernel<T, 32, kPages, kWhole>(bits) : group == 64 ? read_kernel<T, 64, kPages, kWhole>(bits) : read_kernel<T, 128, kPages, kWhole>(bits);
+}
+
+// Whether all rows of a call are whole runs of 16 values on 16 bytes.
+bool whole_rows(const lc_cache* c, const lc_rows* rows, int type) {
+  const uint64_t run = 16 / type_bytes(type);
+  bool whole = c->dim % 16 == 0;
+  for (uint32_t i = 0; i < c->planes; ++i) whole &= aligned_to(rows[i].data, 16) && rows[i].row_stride % run == 0 && rows[i].head_stride % run == 0;
+  return whole;
 }
 
 template <bool kPages>
 int read_impl(const lc_cache* c, const lc_rows* out, int type, const Places& places, uint64_t n, int32_t* status, cudaStream_t cs) {
   const int group = (int)c->group, bits = (int)c->bits;
-  const Kernel kernel = type == LC_TYPE_F32    ? read_kernel<float, kPages>(group, bits)
-                        : type == LC_TYPE_BF16 ? read_kernel<__nv_bfloat16, kPages>(group, bits)
-                                               : read_kernel<__half, kPages>(group, bits);
+  Kernel kernel;
+  if (whole_rows(c, out, type))
+    kernel = type == LC_TYPE_F32    ? read_kernel<float, kPages, true>(group, bits)
+             : type == LC_TYPE_BF16 ? read_kernel<__nv_bfloat16, kPages, true>(group, bits)
+                                    : read_kernel<__half, kPages, true>(group, bits);
+  else
+    kernel = type == LC_TYPE_F32    ? read_kernel<float, kPages, false>(group, bits)
+             : type == LC_TYPE_BF16 ? read_kernel<__nv_bfloat16, kPages, false>(group, bits)
+                                    : read_kernel<__half, kPages, false>(group, bits);
   return launch_rows(kernel, c, out, places, n, status, cs);
 }
 
@@ -275,9 +298,15 @@ int lc_cache_write(const lc_cache* cache, const lc_rows* src, int type, uint64_t
   places.slots = slots;
   places.by_page = FastDiv(1);
   const int group = (int)cache->group, bits = (int)cache->bits;
-  const Kernel kernel = type == LC_TYPE_F32    ? write_kernel<float>(group, bits)
-                        : type == LC_TYPE_BF16 ? write_kernel<__nv_bfloat16>(group, bits)
-                                               : write_kernel<__half>(group, bits);
+  Kernel kernel;
+  if (whole_rows(cache, src, type))
+    kernel = type == LC_TYPE_F32    ? write_kernel<float, true>(group, bits)
+             : type == LC_TYPE_BF16 ? write_kernel<__nv_bfloat16, true>(group, bits)
+                                    : write_kernel<__half, true>(group, bits);
+  else
+    kernel = type == LC_TYPE_F32    ? write_kernel<float, false>(group, bits)
+             : type == LC_TYPE_BF16 ? write_kernel<__nv_bfloat16, false>(group, bits)
+                                    : write_kernel<__half, false>(group, bits);
   return launch_rows(kernel, cache, src, places, rows, status, cs);
 }
 

@@ -30,6 +30,7 @@ __global__ void __launch_bounds__(kThreads) q4_quantize_kernel(const T* __restri
     }
   }
   uint32_t scale[2][kScales];
+  float most[2][kScales];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     float m[2] = {0.0f, 0.0f};
@@ -39,7 +40,15 @@ __global__ void __launch_bounds__(kThreads) q4_quantize_kernel(const T* __restri
       for (int i = 0; i < 8; ++i) m[u % kScales] = max_magnitude(m[u % kScales], v[h][u][i]);
     }
 #pragma unroll
-    for (uint32_t k = 0; k < kScales; ++k) scale[h][k] = group_scale<4>(max_over_lanes(m[k], kLanes));
+    for (uint32_t k = 0; k < kScales; ++k) most[h][k] = max_over_lanes(m[k], kLanes);
+  }
+  if constexpr (kScales == 2) {  // four scales and four lanes: one each
+    const uint32_t mine = group_scale<4>(lane & 2 ? (lane & 1 ? most[1][1] : most[1][0]) : (lane & 1 ? most[0][1] : most[0][0]));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) scale[i >> 1][i & 1] = __shfl_sync(0xFFFFFFFFu, mine, i, 4);
+  } else {
+    scale[0][0] = group_scale<4>(most[0][0]);
+    scale[1][0] = group_scale<4>(most[1][0]);
   }
   if (!inside) return;
   uint32_t word[2][2];

@@ -42,10 +42,11 @@ __device__ __forceinline__ void from_float(float v, __half& x) { x = __float2hal
 
 // Eight neighbouring values of a row as fp32, zeros from `valid` on: by the widest loads that the address allows (rows of heads of 100
 // values in 16 bits begin on 8 bytes).
-template <class T>
+// kWhole: the caller knows that all are there, on 16 bytes.
+template <bool kWhole = false, class T>
 __device__ __forceinline__ void load8(const T* p, int valid, float* v) {
   const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-  if (valid >= 8 && (at & 15) == 0) {
+  if (kWhole || (valid >= 8 && (at & 15) == 0)) {
     uint4 raw[sizeof(T) / 2];
 #pragma unroll
     for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
@@ -73,11 +74,11 @@ __device__ __forceinline__ void load8(const T* p, int valid, float* v) {
 // fp32 from 4 bits: 98 us; so 72).
 template <class T>
 constexpr int kRun = 16 / sizeof(T);
-template <class T>
+template <bool kWhole = false, class T>
 __device__ __forceinline__ void store_run(T* p, int valid, const float* v) {
   constexpr int n = kRun<T>;
   const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-  if (valid >= n && (at & 15) == 0) {
+  if (kWhole || (valid >= n && (at & 15) == 0)) {
     uint4 raw;
     T* e = reinterpret_cast<T*>(&raw);
 #pragma unroll
