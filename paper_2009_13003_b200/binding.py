@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 import threading
 from typing import NamedTuple
 
@@ -116,11 +117,11 @@ def lib():
     L.lc_q4_read.argtypes = [vp, u64, u64, u64, i32, vp, i32, u64, vp]
     L.lc_q4_matvec.argtypes = [vp, u64, u64, u64, i32, vp, i32, u64, u64, vp, i32, u64, vp]
     L.lc_debug_q4_plan.argtypes = [u64, u64, i32, i32, C.c_uint32, C.c_uint32, C.POINTER(C.c_uint32)]
-    cache, rows = C.POINTER(LCCache), C.POINTER(LCRows)
+    cache = C.POINTER(LCCache)
     for f in (L.lc_cache_code_bytes, L.lc_cache_scale_bytes):
         f.argtypes, f.restype = [cache], u64
-    L.lc_cache_write.argtypes = L.lc_cache_read.argtypes = [cache, rows, i32, u64, vp, vp, vp]
-    L.lc_cache_read_pages.argtypes = [cache, rows, i32, u64, vp, u64, C.c_uint32, C.c_uint32, vp, vp, C.c_uint32, vp, vp]
+    L.lc_cache_write.argtypes = L.lc_cache_read.argtypes = [vp, vp, i32, u64, vp, vp, vp]
+    L.lc_cache_read_pages.argtypes = [vp, vp, i32, u64, vp, u64, C.c_uint32, C.c_uint32, vp, vp, C.c_uint32, vp, vp]
     _lib = L
     return L
 
@@ -532,26 +533,32 @@ TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 Q4_MAX_TOKENS = 1048576
 
 
-def _call(fn, what, device, *args):
-    """fn(*args, the current stream of ``device``), with that device current; raises on a host-side error."""
-    index = device.index
-    if index != torch.cuda.current_device():
-        with torch.cuda.device(index):
-            rc = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_functions = {}  # of the library, by name
+
+
+def _call(name, index, *args):
+    """The library's ``name``(*args, the current stream of device ``index``), with that device current; raises on a host-side error.
+    Small calls last as long as the interpreter takes to make them, so this does no more than that."""
+    fn = _functions.get(name)
+    if fn is None:
+        fn = _functions[name] = getattr(lib(), name)
+    if index == torch._C._cuda_getDevice():
+        rc = fn(*args, _raw_stream(index))
     else:
-        rc = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+        with torch.cuda.device(index):
+            rc = fn(*args, _raw_stream(index))
     if rc != OK:
-        raise LCError(rc, what)
+        raise LCError(rc, name)
 
 
-def _numbers(t, name, dims, device=None):
-    """The LC_TYPE_* of a CUDA tensor of numbers whose last axis is contiguous."""
-    kind = TYPES.get(t.dtype)
-    if kind is None or not t.is_cuda or t.dim() != dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
-        raise ValueError("%s must be a %d-dimensional CUDA tensor of float32, bfloat16 or float16, contiguous along its last axis" % (name, dims))
-    if device is not None and t.device != device:
-        raise ValueError("%s is on another device" % name)
-    return kind
+def _numbers(t, name, dims, index):
+    """(LC_TYPE_*, shape, strides) of a tensor of numbers on CUDA device ``index`` whose last axis is contiguous."""
+    kind, shape, strides = TYPES.get(t.dtype), t.shape, t.stride()
+    if kind is None or t.get_device() != index or index < 0 or len(shape) != dims or (strides[-1] != 1 and shape[-1] > 1):
+        raise ValueError("%s must be a %d-dimensional tensor of float32, bfloat16 or float16 on the CUDA device of the call, contiguous along its last axis"
+                         % (name, dims))
+    return kind, shape, strides
 
 
 class Q4(NamedTuple):
@@ -575,25 +582,21 @@ def alloc_q4(rows, cols, group, device) -> Q4:
     return Q4(torch.empty(size, dtype=torch.uint8, device=device), rows, cols, group)
 
 
-def _q4(q4):
-    return q4.data.data_ptr(), q4.data.numel(), q4.rows, q4.cols, q4.group
-
-
 def q4_quantize_async(w, q4, workspace):
     """lc_q4_quantize of the matrix ``w`` into ``q4`` on the current stream; an Inf or NaN shows in last_status(workspace)."""
-    kind = _numbers(w, "w", 2, q4.data.device)
-    if w.shape[0] != q4.rows or w.shape[1] != q4.cols:
+    data, rows, cols, group = q4
+    index = data.get_device()
+    kind, shape, strides = _numbers(w, "w", 2, index)
+    if shape[0] != rows or shape[1] != cols:
         raise ValueError("w has another shape than the weights")
-    if workspace.device != w.device:
+    if workspace.get_device() != index:
         raise ValueError("workspace is on another device")
-    data, size, rows, cols, group = _q4(q4)
-    _call(lib().lc_q4_quantize, "lc_q4_quantize", w.device, w.data_ptr(), kind, rows, cols, w.stride(0), group, data, size, workspace.data_ptr(),
-          workspace.numel())
+    _call("lc_q4_quantize", index, w.data_ptr(), kind, rows, cols, strides[0], group, data.data_ptr(), data.numel(), workspace.data_ptr(), workspace.numel())
 
 
 def q4_quantize(w, group=128, q4=None, workspace=None) -> Q4:
     """The matrix ``w`` (float32, bfloat16 or float16) as 4-bit weights; raises if it holds an Inf or NaN."""
-    _numbers(w, "w", 2)
+    _numbers(w, "w", 2, w.get_device())
     if q4 is None:
         q4 = alloc_q4(w.shape[0], w.shape[1], group, w.device)
     if workspace is None:
@@ -613,8 +616,10 @@ def recover_q4_async(base, streams, q4, scratch, workspace):
     k = len(streams)
     ptrs = (C.c_void_p * k)(*[s.data_ptr() for s in streams])
     sizes = (C.c_uint64 * k)(*[s.numel() for s in streams])
-    data, size, rows, cols, group = _q4(q4)
-    _call(lib().lc_recover_q4, "lc_recover_q4", base.device, base.data_ptr(), ptrs, sizes, k, rows, cols, group, data, size, scratch.data_ptr(),
+    data, rows, cols, group = q4
+    if not data.get_device() == base.get_device() == scratch.get_device() == workspace.get_device():
+        raise ValueError("base, scratch, workspace and the weights are not on one device")
+    _call("lc_recover_q4", base.get_device(), base.data_ptr(), ptrs, sizes, k, rows, cols, group, data.data_ptr(), data.numel(), scratch.data_ptr(),
           workspace.data_ptr(), workspace.numel())
 
 
@@ -636,12 +641,14 @@ def recover_q4(base, streams, rows, group=128, q4=None, scratch=None, workspace=
 
 def q4_read(q4, out=None, dtype=torch.float32):
     """The numbers that the weights stand for, [rows, cols], on the current stream."""
+    data, rows, cols, group = q4
     if out is None:
-        out = torch.empty(q4.rows, q4.cols, dtype=dtype, device=q4.data.device)
-    kind = _numbers(out, "out", 2, q4.data.device)
-    if out.shape[0] != q4.rows or out.shape[1] != q4.cols:
+        out = torch.empty(rows, cols, dtype=dtype, device=data.device)
+    index = data.get_device()
+    kind, shape, strides = _numbers(out, "out", 2, index)
+    if shape[0] != rows or shape[1] != cols:
         raise ValueError("out has another shape than the weights")
-    _call(lib().lc_q4_read, "lc_q4_read", out.device, *_q4(q4), out.data_ptr(), kind, out.stride(0))
+    _call("lc_q4_read", index, data.data_ptr(), data.numel(), rows, cols, group, out.data_ptr(), kind, strides[0])
     return out
 
 
@@ -650,20 +657,20 @@ def q4_matvec(q4, x, out=None):
     in x's type, or in that of ``out`` (x's or float32). No gradient is kept."""
     if x.dim() == 1:
         return q4_matvec(q4, x.unsqueeze(0), None if out is None else out.unsqueeze(0)).squeeze(0)
-    kind = _numbers(x, "x", 2, q4.data.device)
-    tokens, cols = x.shape
-    if cols != q4.cols:
-        raise ValueError("x has %d columns, the weights have %d" % (cols, q4.cols))
+    data, rows, cols, group = q4
+    index = data.get_device()
+    kind, shape, strides = _numbers(x, "x", 2, index)
+    tokens = shape[0]
+    if shape[1] != cols:
+        raise ValueError("x has %d columns, the weights have %d" % (shape[1], cols))
     if x.requires_grad and torch.is_grad_enabled():
         raise ValueError("q4_matvec has no gradient: detach x, or call it under torch.no_grad()")
     if out is None:
-        out = torch.empty(tokens, q4.rows, dtype=x.dtype, device=x.device)
-        out_kind = kind
-    else:
-        out_kind = _numbers(out, "out", 2, x.device)
-        if out.shape[0] != tokens or out.shape[1] != q4.rows:
-            raise ValueError("out must be [tokens, rows]")
-    _call(lib().lc_q4_matvec, "lc_q4_matvec", x.device, *_q4(q4), x.data_ptr(), kind, tokens, x.stride(0), out.data_ptr(), out_kind, out.stride(0))
+        out = torch.empty(tokens, rows, dtype=x.dtype, device=x.device)
+    out_kind, out_shape, out_strides = _numbers(out, "out", 2, index)
+    if out_shape[0] != tokens or out_shape[1] != rows:
+        raise ValueError("out must be [tokens, rows]")
+    _call("lc_q4_matvec", index, data.data_ptr(), data.numel(), rows, cols, group, x.data_ptr(), kind, tokens, strides[0], out.data_ptr(), out_kind, out_strides[0])
     return out
 
 
@@ -680,6 +687,7 @@ class Cache:
         self.planes, self.slots, self.heads = codes.shape[:3]
         self.dim, self.bits, self.group = dim, bits, group
         self._c = LCCache(codes.data_ptr(), scales.data_ptr(), self.slots, self.planes, self.heads, dim, bits, group)
+        self._at, self._index, self._row = C.addressof(self._c), codes.get_device(), (self.heads, dim)
         if lib().lc_cache_code_bytes(self._c) != codes.numel() or lib().lc_cache_scale_bytes(self._c) != 2 * scales.numel():
             raise ValueError("codes and scales do not have the sizes of such a cache")
 
@@ -694,31 +702,32 @@ def alloc_cache(slots, heads, dim, bits, group, device, planes=2) -> Cache:
                  torch.zeros(planes, slots, heads, scale, dtype=torch.bfloat16, device=device), dim, bits, group)
 
 
+_one_plane, _two_planes = struct.Struct("=QQQ").pack, struct.Struct("=QQQQQQ").pack  # an lc_rows, or two: faster than through ctypes
+
+
 def _rows(cache, tensors, what):
     """The lc_rows of one tensor [rows, heads, dim] per plane, their type and their number."""
     if len(tensors) != cache.planes:
         raise ValueError("%s: the cache has %d planes" % (what, cache.planes))
-    first = tensors[0]
-    kind = _numbers(first, what, 3, cache.device)
-    rows, heads, dim = first.shape
-    if heads != cache.heads or dim != cache.dim:
+    kind, shape, strides = _numbers(tensors[0], what, 3, cache._index)
+    if shape[1:] != cache._row:
         raise ValueError("%s must be [rows, heads, dim] of the cache" % what)
     if cache.planes == 1:
-        return (LCRows * 1)((first.data_ptr(), first.stride(0), first.stride(1))), kind, rows
-    second = tensors[1]
-    if _numbers(second, what, 3, cache.device) != kind or second.shape != first.shape:
+        return _one_plane(tensors[0].data_ptr(), strides[0], strides[1]), kind, shape[0]
+    kind2, shape2, strides2 = _numbers(tensors[1], what, 3, cache._index)
+    if kind2 != kind or shape2 != shape:
         raise ValueError("%s: keys and values differ in shape or type" % what)
-    return (LCRows * 2)((first.data_ptr(), first.stride(0), first.stride(1)), (second.data_ptr(), second.stride(0), second.stride(1))), kind, rows
+    return _two_planes(tensors[0].data_ptr(), strides[0], strides[1], tensors[1].data_ptr(), strides2[0], strides2[1]), kind, shape[0]
 
 
-def _whole(t, name, dtype, device):
-    if t.dtype != dtype or t.device != device or not t.is_contiguous():
+def _whole(t, name, dtype, index):
+    if t.dtype != dtype or t.get_device() != index or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor on the cache's device" % (name, dtype))
     return t.data_ptr()
 
 
-def _status(status, device):
-    return None if status is None else _whole(status, "status", torch.int32, device)
+def _status(status, index):
+    return None if status is None else _whole(status, "status", torch.int32, index)
 
 
 def alloc_status(device):
@@ -730,10 +739,10 @@ def cache_write(cache, k, v, slots, status=None):
     """Rows [rows, heads, dim] of keys and values (``v`` None if the cache has one plane) into the cache's ``slots`` (int64; -1: none),
     on the current stream."""
     src, kind, rows = _rows(cache, (k,) if v is None else (k, v), "keys and values")
-    at = _whole(slots, "slots", torch.int64, cache.device)
+    at = _whole(slots, "slots", torch.int64, cache._index)
     if slots.numel() != rows:
         raise ValueError("a slot for each row is needed")
-    _call(lib().lc_cache_write, "lc_cache_write", cache.device, cache._c, src, kind, rows, at, _status(status, cache.device))
+    _call("lc_cache_write", cache._index, cache._at, src, kind, rows, at, _status(status, cache._index))
 
 
 def _outs(cache, outs, rows, dtype):
@@ -747,10 +756,10 @@ def cache_read(cache, slots, outs=None, dtype=torch.bfloat16, status=None):
     """The rows in ``slots``, on the current stream: a tensor [rows, heads, dim] per plane (``outs``, or new ones of ``dtype``)."""
     outs = _outs(cache, outs, slots.numel(), dtype)
     out, kind, rows = _rows(cache, outs, "outs")
-    at = _whole(slots, "slots", torch.int64, cache.device)
+    at = _whole(slots, "slots", torch.int64, cache._index)
     if slots.numel() != rows:
         raise ValueError("a slot for each row is needed")
-    _call(lib().lc_cache_read, "lc_cache_read", cache.device, cache._c, out, kind, rows, at, _status(status, cache.device))
+    _call("lc_cache_read", cache._index, cache._at, out, kind, rows, at, _status(status, cache._index))
     return outs
 
 
@@ -758,13 +767,14 @@ def cache_read_pages(cache, table, page, begin, outs, first=None, status=None):
     """Sequences out of pages of ``page`` slots, one behind the other, into ``outs`` (a tensor [rows, heads, dim] per plane), on the
     current stream. ``table`` [sequences, width] int32: pages; ``begin`` [sequences + 1] int32: where each sequence's rows begin in
     ``outs``; ``first`` [sequences] int32: the position of each one's first row (0 if None)."""
+    index = cache._index
     out, kind, rows = _rows(cache, outs, "outs")
-    if table.dim() != 2 or table.dtype != torch.int32 or table.device != cache.device or (table.shape[1] > 1 and table.stride(1) != 1):
+    if table.dim() != 2 or table.dtype != torch.int32 or table.get_device() != index or (table.shape[1] > 1 and table.stride(1) != 1):
         raise ValueError("table must be [sequences, width] int32 on the cache's device, contiguous along its last axis")
     sequences, width = table.shape
-    at = _whole(begin, "begin", torch.int32, cache.device)
+    at = _whole(begin, "begin", torch.int32, index)
     if begin.numel() != sequences + 1 or (first is not None and first.numel() != sequences):
         raise ValueError("begin has an entry per sequence and one more, first one per sequence")
-    _call(lib().lc_cache_read_pages, "lc_cache_read_pages", cache.device, cache._c, out, kind, rows, table.data_ptr(), table.stride(0), width, page, at,
-          None if first is None else _whole(first, "first", torch.int32, cache.device), sequences, _status(status, cache.device))
+    _call("lc_cache_read_pages", index, cache._at, out, kind, rows, table.data_ptr(), table.stride(0), width, page, at,
+          None if first is None else _whole(first, "first", torch.int32, index), sequences, _status(status, index))
     return outs

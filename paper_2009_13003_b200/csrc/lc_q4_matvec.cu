@@ -94,7 +94,7 @@ struct Unit<__nv_bfloat16> {
 };
 template <>
 struct Unit<__half> {
-  static constexpr float kUp = 1.0f, kUnit = 0x1p24f;
+  static constexpr float kUnit = 0x1p24f;
 };
 
 // Eight values of a vector from column `col` on, as they are in memory; zeros behind the last column.
@@ -527,8 +527,10 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid
   copies_wait<0>();
 }
 
+uint32_t ctas_per_sm(uint32_t warps, uint32_t smem) { return warps * 2 <= kMostWarps && smem <= kSharedPerSM / 2 - 1024 ? 2 : 1; }
+
 template <class X, class M, int NT, int MT, int G, bool kSplit>
-cudaError_t launch_split(MatvecArgs A, uint32_t blocks, uint32_t passes, uint32_t split, uint32_t warps, size_t smem, cudaStream_t cs) {
+cudaError_t launch_split(MatvecArgs A, uint32_t blocks, uint32_t passes, uint32_t split, uint32_t warps, uint32_t smem, uint32_t sms, cudaStream_t cs) {
   const auto kernel = matvec_kernel<X, M, NT, MT, G, kSplit>;
   static bool raised[kMaxDevices];
   const int dev = current_device_index();
@@ -548,15 +550,16 @@ cudaError_t launch_split(MatvecArgs A, uint32_t blocks, uint32_t passes, uint32_
   at[0].val.clusterDim.x = split;
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
-  cfg.numAttrs = 1;
-  int fit = 0;  // clusters that the device holds at once; a query takes 0.2 us
-  if ((e = cudaOccupancyMaxActiveClusters(&fit, kernel, &cfg)) != cudaSuccess) return e;
-  if (fit < 1) return cudaErrorInvalidConfiguration;
+  int fit = (int)(sms * ctas_per_sm(warps, smem));  // clusters that the device holds at once
+  if (kSplit) {
+    cfg.numAttrs = 1;
+    if ((e = cudaOccupancyMaxActiveClusters(&fit, kernel, &cfg)) != cudaSuccess) return e;  // 0.2 us
+    if (fit < 1) return cudaErrorInvalidConfiguration;
+  }
   const uint32_t groups = warps / A.ways, fill = (blocks + groups - 1) / groups;
   const uint32_t clusters = (uint32_t)fit < fill ? (uint32_t)fit : fill;
   A.rounds = (blocks + clusters * groups - 1) / (clusters * groups);
   cfg.gridDim.x = clusters * split;
-  cfg.numAttrs = kSplit ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, kernel, A);
 }
 
@@ -577,7 +580,7 @@ uint64_t plan_bytes(const Plan& p, uint32_t nt, uint32_t group, uint32_t per_pas
 // what the rule then takes is 3 % slower than the fastest of them (geometric mean; 12 % at most but for x of over 16 vectors).
 constexpr uint32_t kStepAlone[2][4] = {{825, 1130, 1750, 3500}, {1270, 1800, 3000, 7000}}, kStepBusy[2][4] = {{71, 110, 200, 430}, {130, 190, 390, 800}};
 uint32_t plan_cycles(const Plan& p, uint32_t nt_log, uint32_t tiles, uint32_t per_pass, uint32_t parts, uint32_t sms) {
-  const uint32_t per_sm = p.warps <= 8 && p.smem <= kSharedPerSM / 2 - 1024 ? 2 : 1;
+  const uint32_t per_sm = ctas_per_sm(p.warps, p.smem);
   // clusters of 2, 4 and 8 on 148 SMs with one CTA each: 74, 33 and 15
   const uint32_t clusters = sms * per_sm * (p.split <= 2 ? 148 / p.split : p.split == 4 ? 33 : 15) / 148;
   const uint32_t groups = p.warps / p.ways, rows = p.mt * kQ4TileRows, blocks = (tiles + p.mt - 1) / p.mt, slots = (clusters ? clusters : 1) * groups;
@@ -627,17 +630,17 @@ Plan make_plan(uint32_t nt_log, const Q4Layout& L, uint32_t per_pass, uint32_t p
 }
 
 template <class X, class M, int NT, int MT, int G>
-cudaError_t launch(const MatvecArgs& A, const Plan& p, uint32_t passes, cudaStream_t cs) {
+cudaError_t launch(const MatvecArgs& A, const Plan& p, uint32_t passes, uint32_t sms, cudaStream_t cs) {
   const uint32_t blocks = (A.L.tiles + MT - 1) / MT;
-  return p.split > 1 ? launch_split<X, M, NT, MT, G, true>(A, blocks, passes, p.split, p.warps, p.smem, cs)
-                     : launch_split<X, M, NT, MT, G, false>(A, blocks, passes, 1, p.warps, p.smem, cs);
+  return p.split > 1 ? launch_split<X, M, NT, MT, G, true>(A, blocks, passes, p.split, p.warps, p.smem, sms, cs)
+                     : launch_split<X, M, NT, MT, G, false>(A, blocks, passes, 1, p.warps, p.smem, sms, cs);
 }
 
 template <class X, class M, int NT, int MT>
-cudaError_t launch_group(const MatvecArgs& A, const Plan& p, uint32_t passes, cudaStream_t cs) {
-  if (A.L.group == 32) return launch<X, M, NT, MT, 32>(A, p, passes, cs);
-  if (A.L.group == 64) return launch<X, M, NT, MT, 64>(A, p, passes, cs);
-  return launch<X, M, NT, MT, 128>(A, p, passes, cs);
+cudaError_t launch_group(const MatvecArgs& A, const Plan& p, uint32_t passes, uint32_t sms, cudaStream_t cs) {
+  if (A.L.group == 32) return launch<X, M, NT, MT, 32>(A, p, passes, sms, cs);
+  if (A.L.group == 64) return launch<X, M, NT, MT, 64>(A, p, passes, sms, cs);
+  return launch<X, M, NT, MT, 128>(A, p, passes, sms, cs);
 }
 
 // The tokens of a pass, and the logarithm of the eights of columns that the product then has.
@@ -673,10 +676,10 @@ cudaError_t launch_columns(MatvecArgs A, cudaStream_t cs) {
   A.stages = p.stages;
   A.slice = p.slice;
   A.chunk = p.chunk;
-  if (nt_log == 0) return p.mt == 2 ? launch_group<X, M, 1, 2>(A, p, passes, cs) : launch_group<X, M, 1, 1>(A, p, passes, cs);
-  if (nt_log == 1) return p.mt == 2 ? launch_group<X, M, 2, 2>(A, p, passes, cs) : launch_group<X, M, 2, 1>(A, p, passes, cs);
-  if (nt_log == 2) return launch_group<X, M, 4, 2>(A, p, passes, cs);
-  return launch_group<X, M, 8, 1>(A, p, passes, cs);
+  if (nt_log == 0) return p.mt == 2 ? launch_group<X, M, 1, 2>(A, p, passes, sms, cs) : launch_group<X, M, 1, 1>(A, p, passes, sms, cs);
+  if (nt_log == 1) return p.mt == 2 ? launch_group<X, M, 2, 2>(A, p, passes, sms, cs) : launch_group<X, M, 2, 1>(A, p, passes, sms, cs);
+  if (nt_log == 2) return launch_group<X, M, 4, 2>(A, p, passes, sms, cs);
+  return launch_group<X, M, 8, 1>(A, p, passes, sms, cs);
 }
 
 }  // namespace

@@ -1,5 +1,6 @@
 """State in few bits, without a GPU: the reference against exact fractions, sizes against the text, and what the entry points refuse
 (made-up addresses: the checks come before anything is touched)."""
+import ctypes as C
 from fractions import Fraction
 
 import numpy as np
@@ -102,8 +103,8 @@ def test_the_cache_refuses():
                               for k in ("codes", "scales", "slots", "planes", "heads", "dim", "bits", "group")])
         rows = (binding.LCRows * 2)(*(planes or [(0x30000, 120, 40), (0x40000, 120, 40)]))
         if fn == "pages":
-            return L.lc_cache_read_pages(c, rows, kind, n, 0x50000, 4, 4, 16, at, None, 2, status, None)
-        return (L.lc_cache_write if fn == "write" else L.lc_cache_read)(c, rows, kind, n, at, status, None)
+            return L.lc_cache_read_pages(C.byref(c), rows, kind, n, 0x50000, 4, 4, 16, at, None, 2, status, None)
+        return (L.lc_cache_write if fn == "write" else L.lc_cache_read)(C.byref(c), rows, kind, n, at, status, None)
 
     for fn in ("write", "read", "pages"):
         for bad in (dict(kind=3), dict(at=None), dict(at=slots + 2), dict(status=2), dict(n=1 << 31), dict(n=1 << 30), dict(cache=dict(codes=None)),
@@ -118,7 +119,7 @@ def test_the_cache_refuses():
     c = binding.LCCache(0x10000, 0x20000, 64, 2, 3, 40, 4, 32)
     rows = (binding.LCRows * 2)((0x30000, 120, 40), (0x40000, 120, 40))
     pages = lambda table=0x50000, stride=4, width=4, page=16, begin=0x60000, first=None, n=2: L.lc_cache_read_pages(
-        c, rows, 1, 5, table, stride, width, page, begin, first, n, None, None)
+        C.byref(c), rows, 1, 5, table, stride, width, page, begin, first, n, None, None)
     for bad in (dict(table=None), dict(table=0x50002), dict(stride=3), dict(page=0), dict(page=1 << 31), dict(begin=None), dict(begin=0x60002), dict(first=2),
                 dict(stride=1 << 32)):
         assert pages(**bad) == A, bad
