@@ -384,11 +384,12 @@ int lc_q4_read(const void* q4, uint64_t q4_bytes, uint64_t rows, uint64_t cols, 
 /*
  * Products with 4-bit weights, for the vectors of one or a few tokens:
  *   out[t, r] = sum over the groups G of row r of scale[r, G] * (sum over c in G of code[r, c] * x[t, c]),
- * sums in fp32, one rounding to the output's type. The weights are read once for up to 64 tokens (21 if x is fp32); more are
- * taken in several parts. For long prompts lc_q4_read and a matrix product are the better way.
+ * sums in fp32, one rounding to the output's type. The weights are read once for up to 32 tokens (10 if x is fp32); more are
+ * taken in several parts. From some 30 on, lc_q4_read and a matrix product are the better way.
  * x          DEVICE, `type` LC_TYPE_*, vector t at x + t * x_stride values, x_stride >= cols or 0 (one vector for all); aligned like
- *            its type. All of its bits count, also in fp32 (but what lies below 2^-133). A group's sum is formed before its
- *            scale is applied: it has to stay in fp32's range (|x| below 2^117 is always enough).
+ *            its type. All of its bits count, also in fp32 (of a group's sum, what lies below 2^-96 may be lost). A group's sum is formed
+ *            before its scale is applied: it has to stay in fp32's range (|x| below 2^117 is always enough). Vectors with values of
+ *            2^48 and more, Inf and NaN among them, take many times as long.
  * out        DEVICE, `out_type` = type or LC_TYPE_F32, row t at out + t * out_stride, out_stride >= rows; aligned like its type.
  * tokens     0 ... LC_Q4_MAX_TOKENS. With cols = 0 the products are 0.
  * The same inputs give the same bits.

@@ -12,8 +12,9 @@
 // a mask takes two n's out of a word for a row r, and the same mask four bits up two 16 n's for row r + 8. One shift and four masks
 // for eight codes. What is too much by it, 8 times the group's sum of x, is taken off the group's sum in fp32; it comes from products
 // with a constant, once a CTA. To keep the products with bf16 vectors (and parts of fp32 ones) in fp32's normal range, x is
-// multiplied by 2^80 when it is staged. Where a sum comes out as Inf or NaN (x holds one, or values of 2^48 and more), the warp takes
-// that tile again by plain multiplications (slow_sums).
+// multiplied by 2^80 when it is staged, so that sums keep all bits of an x down to 2^-72 and are exact to 2^-96 below. Where a sum comes
+// out as Inf or NaN (x holds one, or values of 2^48 and more, or a scale is beyond 2^74), the warp takes that tile again by plain
+// multiplications (slow_sums).
 #include <type_traits>
 
 #include "lc_q4.cuh"
@@ -85,7 +86,7 @@ __device__ __forceinline__ void operands(uint32_t w, uint32_t (&a)[4]) {
 // -8 as such a number, in both halves.
 constexpr uint32_t kMinus8 = 0x80088008u;
 
-// kUp: what x is multiplied by; kUnit: what the sums of products of row r are then to be multiplied by.
+// kUp: what x is multiplied by; kUnit: what the scale of row r is then to be multiplied by (row r + 8: a sixteenth of it).
 template <class M>
 struct Unit;
 template <>
@@ -430,7 +431,7 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                   const uint32_t s = *reinterpret_cast<const uint32_t*>(w + m * kSlot + kQ4StepBytes + (u * 32 / G * 8 + r) * 4);
-                  const float s_lo = __uint_as_float(s << 16), s_hi = __uint_as_float(s & 0xFFFF0000u);
+                  const float s_lo = __uint_as_float(s << 16) * Unit<M>::kUnit, s_hi = __uint_as_float(s & 0xFFFF0000u) * (Unit<M>::kUnit / 16);
 #pragma unroll
                   for (int n = 0; n < NT; ++n) {
                     const float2 f = start[(u * 32 / G * NT + n) * 4];
@@ -453,10 +454,7 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            sum[m][n][i] *= i < 2 ? Unit<M>::kUnit : Unit<M>::kUnit / 16;
-            fine &= fabsf(sum[m][n][i]) < __uint_as_float(0x7F800000u);
-          }
+          for (int i = 0; i < 4; ++i) fine &= fabsf(sum[m][n][i]) < __uint_as_float(0x7F800000u);
         }
         if (__all_sync(0xFFFFFFFFu, fine)) {
 #pragma unroll
@@ -578,31 +576,34 @@ uint64_t plan_bytes(const Plan& p, uint32_t nt, uint32_t group, uint32_t per_pas
 // About how many cycles a layout takes: a step takes a warp `alone` cycles and an SM with all its warps `busy`; every CTA stages x; the
 // sums of a round of blocks are added up behind it. The numbers are fitted to 37 shapes of 1 to 40 vectors in up to 64 layouts each;
 // what the rule then takes is 3 % slower than the fastest of them (geometric mean; 12 % at most but for x of over 16 vectors).
-constexpr uint32_t kStepAlone[2][4] = {{825, 1130, 1750, 3500}, {1270, 1800, 3000, 7000}}, kStepBusy[2][4] = {{71, 110, 200, 430}, {130, 190, 390, 800}};
-uint32_t plan_cycles(const Plan& p, uint32_t nt_log, uint32_t tiles, uint32_t per_pass, uint32_t parts, uint32_t sms) {
+constexpr uint32_t kStepAlone[2][3] = {{825, 1130, 1750}, {1270, 1800, 3000}}, kStepBusy[2][3] = {{71, 110, 200}, {130, 190, 390}};
+uint64_t plan_cycles(const Plan& p, uint32_t nt_log, uint32_t tiles, uint32_t per_pass, uint32_t parts, uint32_t sms) {
   const uint32_t per_sm = ctas_per_sm(p.warps, p.smem);
   // clusters of 2, 4 and 8 on 148 SMs with one CTA each: 74, 33 and 15
   const uint32_t clusters = sms * per_sm * (p.split <= 2 ? 148 / p.split : p.split == 4 ? 33 : 15) / 148;
   const uint32_t groups = p.warps / p.ways, rows = p.mt * kQ4TileRows, blocks = (tiles + p.mt - 1) / p.mt, slots = (clusters ? clusters : 1) * groups;
   const uint32_t steps = (p.slice + p.ways - 1) / p.ways, alone = kStepAlone[p.mt - 1][nt_log], busy = kStepBusy[p.mt - 1][nt_log];
-  const uint32_t sums = 300 + per_pass * rows * (20 + 6 * p.ways * parts) / (32 * p.ways) + (p.split == 1 ? 0 : p.split == 2 ? 1160 : p.split == 4 ? 1400 : 1600);
+  const uint32_t sums = 300 + per_pass * rows * (20 + 6 * p.ways * parts) / (32 * p.ways) + (p.split == 1 ? 0 : p.split == 2 ? 1160 : p.split == 4 ? 1400 : 2000);
   auto round = [&](uint32_t used) {  // blocks of a round
-    const uint32_t warps = (used * p.ways * p.split + sms - 1) / sms, all = p.warps * per_sm;
+    const uint32_t warps = (uint32_t)(((uint64_t)used * p.ways * p.split + sms - 1) / sms), all = p.warps * per_sm;
     const uint32_t together = (warps < all ? warps : all) * busy;
-    return steps * (together > alone ? together : alone) + sums;
+    return (uint64_t)steps * (together > alone ? together : alone) + sums;
   };
-  const uint32_t staged = (p.chunk >= p.slice ? 1 : blocks / slots + 1) * per_sm * (p.slice * per_pass / 2) * (parts == 3 ? 90 : 50);  // 32 pieces at a time
+  // 32 pieces of x at a time; what does not fit comes again with every round, but then enough of it is on its way
+  const bool resident = p.chunk >= p.slice;
+  const uint64_t staged = (uint64_t)(resident ? per_sm : blocks / slots + 1) * (p.slice * (uint64_t)per_pass / 2) * (parts == 3 ? 90 : resident ? 50 : 20);
   return staged + (p.split > 1 ? 950 : 0) + blocks / slots * round(slots) + (blocks % slots ? round(blocks % slots) : 0);
 }
 
 Plan make_plan(uint32_t nt_log, const Q4Layout& L, uint32_t per_pass, uint32_t parts, uint32_t sms) {
   const uint32_t nt = 1u << nt_log;
   Plan best = {};
-  uint32_t least = ~0u;
-  for (uint32_t mt = nt_log == 2 ? 2 : 1; mt <= (nt_log == 3 ? 1 : 2); ++mt) {
+  uint64_t least = ~0ull;
+  for (uint32_t mt = nt_log == 2 ? 2 : 1; mt <= 2; ++mt) {
     const uint32_t blocks = (L.tiles + mt - 1) / mt;
+    if (mt == 2 && L.tiles <= sms && best.smem) break;  // too few tiles to put two together
     for (uint32_t split = 1; split <= kMaxSplit; split *= 2) {
-      if (split > 1 && L.steps < 2 * split) break;
+      if (split > 1 && L.steps < 8 * split && best.smem && best.chunk >= best.slice) break;  // too few columns to share
       for (uint32_t ways = 1; ways <= 8; ways *= 2) {
         const uint32_t slice = L.steps ? (L.steps + split - 1) / split : 1, shared = blocks * ways * split;  // warps that there is work for
         if (ways > 1 && (slice < ways || shared / 2 > sms * kMostWarps * 2)) break;  // nothing to share, or no need to
@@ -621,7 +622,7 @@ Plan make_plan(uint32_t nt_log, const Q4Layout& L, uint32_t per_pass, uint32_t p
           }
         }
         p.smem = (uint32_t)bytes;
-        const uint32_t cycles = plan_cycles(p, nt_log, L.tiles, per_pass, parts, sms);
+        const uint64_t cycles = plan_cycles(p, nt_log, L.tiles, per_pass, parts, sms);
         if (cycles < least) least = cycles, best = p;
       }
     }
@@ -643,12 +644,14 @@ cudaError_t launch_group(const MatvecArgs& A, const Plan& p, uint32_t passes, ui
   return launch<X, M, NT, MT, 128>(A, p, passes, sms, cs);
 }
 
-// The tokens of a pass, and the logarithm of the eights of columns that the product then has.
+// The tokens of a pass, and the logarithm of the eights of columns that the product then has. 64 columns in one pass hold twice the sums in
+// registers and x in shared memory, for fewer warps: 28672 x 8192, 64 vectors 321 us, in two passes 210.
+constexpr uint32_t kMostColumns = 32;
 uint32_t tokens_per_pass(uint32_t tokens, uint32_t parts) {
-  const uint32_t most = 64 / parts, passes = (tokens + most - 1) / most;
+  const uint32_t most = kMostColumns / parts, passes = (tokens + most - 1) / most;
   return (tokens + passes - 1) / passes;
 }
-uint32_t eights_log(uint32_t columns) { return columns <= 8 ? 0 : columns <= 16 ? 1 : columns <= 32 ? 2 : 3; }
+uint32_t eights_log(uint32_t columns) { return columns <= 8 ? 0 : columns <= 16 ? 1 : 2; }
 
 template <class X, class M>
 cudaError_t launch_columns(MatvecArgs A, cudaStream_t cs) {
@@ -678,8 +681,7 @@ cudaError_t launch_columns(MatvecArgs A, cudaStream_t cs) {
   A.chunk = p.chunk;
   if (nt_log == 0) return p.mt == 2 ? launch_group<X, M, 1, 2>(A, p, passes, sms, cs) : launch_group<X, M, 1, 1>(A, p, passes, sms, cs);
   if (nt_log == 1) return p.mt == 2 ? launch_group<X, M, 2, 2>(A, p, passes, sms, cs) : launch_group<X, M, 2, 1>(A, p, passes, sms, cs);
-  if (nt_log == 2) return launch_group<X, M, 4, 2>(A, p, passes, sms, cs);
-  return launch_group<X, M, 8, 1>(A, p, passes, sms, cs);
+  return launch_group<X, M, 4, 2>(A, p, passes, sms, cs);
 }
 
 }  // namespace

@@ -55,16 +55,18 @@ __device__ __forceinline__ void load8(const T* p, int valid, float* v) {
     for (int i = 0; i < 8; ++i) v[i] = to_float(e[i]);
     return;
   }
+  if constexpr (!kWhole) {
 #pragma unroll
-  for (int h = 0; h < 8; h += 4) {
-    if (sizeof(T) == 2 && valid >= h + 4 && (at & 7) == 0) {
-      const uint2 raw = __ldg(reinterpret_cast<const uint2*>(p + h));
-      const T* e = reinterpret_cast<const T*>(&raw);
+    for (int h = 0; h < 8; h += 4) {
+      if (sizeof(T) == 2 && valid >= h + 4 && (at & 7) == 0) {
+        const uint2 raw = __ldg(reinterpret_cast<const uint2*>(p + h));
+        const T* e = reinterpret_cast<const T*>(&raw);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[h + i] = to_float(e[i]);
-    } else {
+        for (int i = 0; i < 4; ++i) v[h + i] = to_float(e[i]);
+      } else {
 #pragma unroll
-      for (int i = h; i < h + 4; ++i) v[i] = i < valid ? to_float(p[i]) : 0.0f;
+        for (int i = h; i < h + 4; ++i) v[i] = i < valid ? to_float(p[i]) : 0.0f;
+      }
     }
   }
 }
@@ -86,18 +88,20 @@ __device__ __forceinline__ void store_run(T* p, int valid, const float* v) {
     *reinterpret_cast<uint4*>(p) = raw;
     return;
   }
+  if constexpr (!kWhole) {
 #pragma unroll
-  for (int h = 0; h < n; h += 4) {
-    if (sizeof(T) == 2 && valid >= h + 4 && (at & 7) == 0) {
-      uint2 raw;
-      T* e = reinterpret_cast<T*>(&raw);
+    for (int h = 0; h < n; h += 4) {
+      if (sizeof(T) == 2 && valid >= h + 4 && (at & 7) == 0) {
+        uint2 raw;
+        T* e = reinterpret_cast<T*>(&raw);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) from_float(v[h + i], e[i]);
-      *reinterpret_cast<uint2*>(p + h) = raw;
-    } else {
+        for (int i = 0; i < 4; ++i) from_float(v[h + i], e[i]);
+        *reinterpret_cast<uint2*>(p + h) = raw;
+      } else {
 #pragma unroll
-      for (int i = h; i < h + 4; ++i)
-        if (i < valid) from_float(v[i], p[i]);
+        for (int i = h; i < h + 4; ++i)
+          if (i < valid) from_float(v[i], p[i]);
+      }
     }
   }
 }

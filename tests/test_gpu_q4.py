@@ -185,6 +185,23 @@ def test_all_bits_of_an_fp32_vector_count(lc):
     assert np.all(np.abs(got.astype(np.float64) - want) <= 2.0 ** -22 * np.abs(want))
 
 
+@pytest.mark.parametrize("tokens", [1, 3, 20])
+@pytest.mark.parametrize("kind", ["fp32", "bf16"])
+def test_small_and_large_weights_and_vectors(lc, kind, tokens):
+    rows, cols, group = 70, 900, 64
+    bound = 17 * group / 16 * 2.0 ** -23 + (cols / group + 16) * 2.0 ** -24
+    for w_exp, x_exp in ((-100, 0), (-100, 60), (90, 0), (90, -60), (0, 46), (0, 50), (0, 100), (-60, 100), (0, -70), (100, -70)):
+        w = random_weights(rows, cols, 21) * 2.0 ** w_exp
+        x = (torch.randn(tokens, cols, device=DEV) * 2.0 ** x_exp).to(TYPES[kind])
+        x[0, 5] *= 16.0
+        got = lc.q4_matvec(lc.q4_quantize(w, group), x, torch.empty(tokens, rows, device=DEV)).double().cpu()
+        codes, scales = ref.quantize(w.double().cpu().numpy(), 4, group)
+        v, xd = torch.from_numpy(ref.values(codes, scales, group)), x.double().cpu()
+        # a sum of codes and x may lose what lies below 2^-96, a group's scale times that
+        lost = 2.0 ** -95 * 16 * torch.from_numpy(ref.bf16_values(scales)).sum(-1)
+        assert bool(((got - xd @ v.T).abs() <= (xd.abs() @ v.abs().T) * bound + lost + 2.0 ** -149).all()), (w_exp, x_exp)
+
+
 @pytest.mark.parametrize("kind", list(TYPES))
 def test_inf_and_nan_in_a_vector(lc, kind):
     w = torch.ones(40, 200, device=DEV)

@@ -22,7 +22,7 @@ def check(rows, cols, group, kind, tokens, sms=148):
     parts, steps = 3 if kind == 0 else 1, -(-cols // 128)
     columns = p["per_pass"] * parts
     assert 0 < p["smem"] <= MOST, case
-    assert columns <= 8 * p["nt"] <= 64 and p["mt"] in (1, 2) and p["mt"] * p["nt"] <= 8, case
+    assert columns <= 8 * p["nt"] <= 32 and p["mt"] in (1, 2) and p["mt"] * p["nt"] <= 8, case
     assert p["ways"] in (1, 2, 4, 8) and p["split"] in (1, 2, 4, 8) and p["warps"] in (8, 16), case
     groups = p["warps"] // p["ways"]
     assert p["ways"] == 1 or groups <= 15, case  # a named barrier for each
