@@ -533,17 +533,15 @@ TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 Q4_MAX_TOKENS = 1048576
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 _functions = {}  # of the library, by name
 
 
 def _call(name, index, *args):
     """The library's ``name``(*args, the current stream of device ``index``), with that device current; raises on a host-side error.
     Small calls last as long as the interpreter takes to make them, so this does no more than that."""
-    fn = _functions.get(name)
-    if fn is None:
-        fn = _functions[name] = getattr(lib(), name)
-    if index == torch._C._cuda_getDevice():
+    fn = _functions.get(name) or _functions.setdefault(name, getattr(lib(), name))
+    if index == _current_device():
         rc = fn(*args, _raw_stream(index))
     else:
         with torch.cuda.device(index):
@@ -660,17 +658,19 @@ def q4_matvec(q4, x, out=None):
     data, rows, cols, group = q4
     index = data.get_device()
     kind, shape, strides = _numbers(x, "x", 2, index)
-    tokens = shape[0]
-    if shape[1] != cols:
-        raise ValueError("x has %d columns, the weights have %d" % (shape[1], cols))
+    tokens, width = shape
+    if width != cols:
+        raise ValueError("x has %d columns, the weights have %d" % (width, cols))
     if x.requires_grad and torch.is_grad_enabled():
         raise ValueError("q4_matvec has no gradient: detach x, or call it under torch.no_grad()")
     if out is None:
-        out = torch.empty(tokens, rows, dtype=x.dtype, device=x.device)
-    out_kind, out_shape, out_strides = _numbers(out, "out", 2, index)
-    if out_shape[0] != tokens or out_shape[1] != rows:
-        raise ValueError("out must be [tokens, rows]")
-    _call("lc_q4_matvec", index, data.data_ptr(), data.numel(), rows, cols, group, x.data_ptr(), kind, tokens, strides[0], out.data_ptr(), out_kind, out_strides[0])
+        out, out_kind, out_stride = torch.empty(tokens, rows, dtype=x.dtype, device=x.device), kind, rows
+    else:
+        out_kind, out_shape, out_strides = _numbers(out, "out", 2, index)
+        out_stride = out_strides[0]
+        if out_shape != (tokens, rows):
+            raise ValueError("out must be [tokens, rows]")
+    _call("lc_q4_matvec", index, data.data_ptr(), data.numel(), rows, cols, group, x.data_ptr(), kind, tokens, strides[0], out.data_ptr(), out_kind, out_stride)
     return out
 
 

@@ -9,7 +9,7 @@ LIB = os.path.join(HERE, "liblc.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
-    "-O3", "-lineinfo", "-std=c++17",
+    "-O3", "-lineinfo", "-std=c++17", "-t", "0",
     "-Xcompiler", "-fPIC", "-shared",
 ]
 
