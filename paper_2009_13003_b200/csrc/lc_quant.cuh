@@ -12,6 +12,7 @@
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+#include <string.h>
 
 #include "lc_common.cuh"
 
@@ -63,6 +64,23 @@ __device__ __forceinline__ void load8(const T* p, int valid, float* v) {
         const T* e = reinterpret_cast<const T*>(&raw);
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[h + i] = to_float(e[i]);
+      } else if (sizeof(T) == 2 && valid >= h + 4) {  // pairs on 4 bytes, and what is left at the ends
+        const int odd = (at & 2) / 2;
+        const uint32_t a = __ldg(reinterpret_cast<const uint32_t*>(p + h + odd));
+        const T* e = reinterpret_cast<const T*>(&a);
+        if (odd) {
+          v[h] = to_float(p[h]);
+          v[h + 1] = to_float(e[0]);
+          v[h + 2] = to_float(e[1]);
+          v[h + 3] = to_float(p[h + 3]);
+        } else {
+          const uint32_t b = __ldg(reinterpret_cast<const uint32_t*>(p + h + 2));
+          const T* f = reinterpret_cast<const T*>(&b);
+          v[h] = to_float(e[0]);
+          v[h + 1] = to_float(e[1]);
+          v[h + 2] = to_float(f[0]);
+          v[h + 3] = to_float(f[1]);
+        }
       } else {
 #pragma unroll
         for (int i = h; i < h + 4; ++i) v[i] = i < valid ? to_float(p[i]) : 0.0f;
@@ -97,6 +115,20 @@ __device__ __forceinline__ void store_run(T* p, int valid, const float* v) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) from_float(v[h + i], e[i]);
         *reinterpret_cast<uint2*>(p + h) = raw;
+      } else if (sizeof(T) == 2 && valid >= h + 4) {
+        T e[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) from_float(v[h + i], e[i]);
+        uint32_t w[2];
+        memcpy(w, e, sizeof w);
+        if (at & 2) {
+          p[h] = e[0];
+          *reinterpret_cast<uint32_t*>(p + h + 1) = __byte_perm(w[0], w[1], 0x5432);
+          p[h + 3] = e[3];
+        } else {
+          reinterpret_cast<uint32_t*>(p + h)[0] = w[0];
+          reinterpret_cast<uint32_t*>(p + h)[1] = w[1];
+        }
       } else {
 #pragma unroll
         for (int i = h; i < h + 4; ++i)
