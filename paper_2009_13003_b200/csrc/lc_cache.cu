@@ -107,12 +107,14 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(CacheArgs C, Plan
     const T* p = reinterpret_cast<const T*>(R.data) + row * R.row_stride + l.head * R.head_stride + at;
     const int valid = inside ? (int)C.dim - (int)at : 0;
     float v[16] = {}, m = 0.0f;
-    if (!kWhole || valid > 0) {
-      load8<kWhole>(p, valid, v);
-      load8<kWhole>(p + 8, valid - 8, v + 8);
-    }
+    if constexpr (kWhole) {
+      if (valid > 0) m = load16(p, v);
+    } else {
+      load8(p, valid, v);
+      load8(p + 8, valid - 8, v + 8);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) m = max_magnitude(m, v[i]);
+      for (int i = 0; i < 16; ++i) m = max_magnitude(m, v[i]);
+    }
     const uint32_t scale = group_scale<kBits>(max_over_lanes(m, kLanes));
     if (valid <= 0) continue;
     float t[16];

@@ -375,7 +375,7 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid
       if (sizeof(X) == 2 && A.out_type) from_float(y, static_cast<X*>(A.out)[at]);
       else static_cast<float*>(A.out)[at] = y;
     };
-    float sum[MT][NT][4] = {};
+    Two sum[MT][NT][2] = {};  // of rows r and r + 8, two columns each
     for (uint32_t begin = slice; begin < slice_end; begin += A.chunk) {
       const uint32_t end = min(slice_end, begin + A.chunk);
       if (!resident || round == 0) {
@@ -394,67 +394,79 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid
       }
       if (!there) continue;
 #pragma unroll 1
-        for (uint32_t step = begin + way; step < end; step += A.ways) {
-          copies_wait(A.stages - 2);
-          __syncwarp();  // the scales of a row are copied by its four lanes; and all lanes have left the slot asked for now
-          ask_next();
-          const uint8_t* w = ring + slot;
-          slot = slot + kStage == ring_bytes ? 0 : slot + kStage;
-          float acc[MT][NT][4];
-          const uint32_t at = (step - begin) * 16;
-          const float2* start = reinterpret_cast<const float2*>(starts + (step - begin) * kGroups * 8 * NT) + t;
+      for (uint32_t step = begin + way; step < end; step += A.ways) {
+        copies_wait(A.stages - 2);
+        __syncwarp();  // the scales of a row are copied by its four lanes; and all lanes have left the slot asked for now
+        ask_next();
+        const uint8_t* w = ring + slot;
+        slot = slot + kStage == ring_bytes ? 0 : slot + kStage;
+        float acc[MT][NT][4];
+        const uint32_t at = (step - begin) * 16;
+        const Two* start = reinterpret_cast<const Two*>(starts + (step - begin) * kGroups * 8 * NT) + t;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint4 v[MT];
+        for (int h = 0; h < 2; ++h) {
+          uint4 v[MT];
 #pragma unroll
-            for (int m = 0; m < MT; ++m) v[m] = *reinterpret_cast<const uint4*>(w + m * kSlot + h * 512 + lane * 16);
+          for (int m = 0; m < MT; ++m) v[m] = *reinterpret_cast<const uint4*>(w + m * kSlot + h * 512 + lane * 16);
 #pragma unroll
-            for (int u = 2 * h; u < 2 * h + 2; ++u) {
-              const bool begins = u * 32 % G == 0, ends = (u + 1) * 32 % G == 0;  // a group
-              uint32_t a[MT][2][4];
+          for (int u = 2 * h; u < 2 * h + 2; ++u) {
+            const bool begins = u * 32 % G == 0, ends = (u + 1) * 32 % G == 0;  // a group
+            uint32_t a[MT][2][4];
 #pragma unroll
-              for (int m = 0; m < MT; ++m) {
-                operands(u & 1 ? v[m].z : v[m].x, a[m][0]);
-                operands(u & 1 ? v[m].w : v[m].y, a[m][1]);
-              }
+            for (int m = 0; m < MT; ++m) {
+              operands(u & 1 ? v[m].z : v[m].x, a[m][0]);
+              operands(u & 1 ? v[m].w : v[m].y, a[m][1]);
+            }
+            constexpr int kSide = NT < 2 ? 1 : 2;  // eights of columns at a time: products that do not wait for each other
 #pragma unroll
-              for (int n = 0; n < NT; ++n) {
-                const uint4 b = column[n][at + u * 4];
+            for (int n0 = 0; n0 < NT; n0 += kSide) {
+              uint4 b[kSide];
+#pragma unroll
+              for (int i = 0; i < kSide; ++i) b[i] = column[n0 + i][at + u * 4];
+#pragma unroll
+              for (int i = 0; i < kSide; ++i) {
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
-                  if (begins) mma_first<M>(acc[m][n], a[m][0], b.x, b.y);
-                  else mma<M>(acc[m][n], a[m][0], b.x, b.y);
-                  mma<M>(acc[m][n], a[m][1], b.z, b.w);
+                  if (begins) mma_first<M>(acc[m][n0 + i], a[m][0], b[i].x, b[i].y);
+                  else mma<M>(acc[m][n0 + i], a[m][0], b[i].x, b[i].y);
                 }
               }
-              if (ends) {
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                  const uint32_t s = *reinterpret_cast<const uint32_t*>(w + m * kSlot + kQ4StepBytes + (u * 32 / G * 8 + r) * 4);
-                  const float s_lo = __uint_as_float(s << 16) * Unit<M>::kUnit, s_hi = __uint_as_float(s & 0xFFFF0000u) * (Unit<M>::kUnit / 16);
+              for (int i = 0; i < kSide; ++i) {
 #pragma unroll
-                  for (int n = 0; n < NT; ++n) {
-                    const float2 f = start[(u * 32 / G * NT + n) * 4];
-                    sum[m][n][0] += s_lo * (acc[m][n][0] + f.x);
-                    sum[m][n][1] += s_lo * (acc[m][n][1] + f.y);
-                    sum[m][n][2] += s_hi * __fmaf_rn(16.0f, f.x, acc[m][n][2]);
-                    sum[m][n][3] += s_hi * __fmaf_rn(16.0f, f.y, acc[m][n][3]);
-                  }
+                for (int m = 0; m < MT; ++m) mma<M>(acc[m][n0 + i], a[m][1], b[i].z, b[i].w);
+              }
+            }
+            if (ends) {
+#pragma unroll
+              for (int m = 0; m < MT; ++m) {
+                const uint32_t s = *reinterpret_cast<const uint32_t*>(w + m * kSlot + kQ4StepBytes + (u * 32 / G * 8 + r) * 4);
+                const float s_lo = __uint_as_float(s << 16) * Unit<M>::kUnit, s_hi = __uint_as_float(s & 0xFFFF0000u) * (Unit<M>::kUnit / 16);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                  const Two f = start[(u * 32 / G * NT + n) * 4];
+                  sum[m][n][0] = fma_two(two(s_lo, s_lo), add_two(two(acc[m][n][0], acc[m][n][1]), f), sum[m][n][0]);
+                  sum[m][n][1] = fma_two(two(s_hi, s_hi), fma_two(two(16.0f, 16.0f), f, two(acc[m][n][2], acc[m][n][3])), sum[m][n][1]);
                 }
               }
             }
           }
         }
+      }
     }
     if (there) {
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         if (m > 0 && block * MT + m >= A.L.tiles) break;
+        float y[NT][4];
         bool fine = true;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) fine &= fabsf(sum[m][n][i]) < __uint_as_float(0x7F800000u);
+          for (int i = 0; i < 4; i += 2) {
+            split_two(sum[m][n][i / 2], y[n][i], y[n][i + 1]);
+            fine &= fabsf(y[n][i]) < __uint_as_float(0x7F800000u) && fabsf(y[n][i + 1]) < __uint_as_float(0x7F800000u);
+          }
         }
         if (__all_sync(0xFFFFFFFFu, fine)) {
 #pragma unroll
@@ -463,8 +475,8 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid
             for (int i = 0; i < 4; ++i) {
               const uint32_t col = 8 * n + 2 * t + (i & 1), row = m * 16 + r + 8 * (i >> 1);
               if (col >= columns) continue;
-              if (kParts == 1 && A.direct) put(col, row, sum[m][n][i]);
-              else mine[col * kRedStride + row] = sum[m][n][i];
+              if (kParts == 1 && A.direct) put(col, row, y[n][i]);
+              else mine[col * kRedStride + row] = y[n][i];
             }
           }
         } else {

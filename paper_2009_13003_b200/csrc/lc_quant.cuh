@@ -145,6 +145,36 @@ __device__ __forceinline__ float max_magnitude(float a, float b) {
   return m;
 }
 
+// 16 whole values on 16 bytes as fp32, and the largest magnitude of them. Of 16-bit values, two at a time: without their signs their
+// patterns order like the magnitudes, Inf and NaN last.
+template <class T>
+__device__ __forceinline__ float load16(const T* p, float (&v)[16]) {
+  if constexpr (sizeof(T) == 2) {
+    uint32_t w[8], most = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint4 x = __ldg(reinterpret_cast<const uint4*>(p) + i);
+      w[4 * i] = x.x, w[4 * i + 1] = x.y, w[4 * i + 2] = x.z, w[4 * i + 3] = x.w;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      most = __vmaxu2(most, w[i] & 0x7FFF7FFFu);
+      const T* e = reinterpret_cast<const T*>(&w[i]);
+      v[2 * i] = to_float(e[0]);
+      v[2 * i + 1] = to_float(e[1]);
+    }
+    const unsigned short m = (unsigned short)max(most & 0xFFFFu, most >> 16);
+    return to_float(reinterpret_cast<const T&>(m));
+  } else {
+    load8<true>(p, 8, v);
+    load8<true>(p + 8, 8, v + 8);
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) m = max_magnitude(m, v[i]);
+    return m;
+  }
+}
+
 // The largest magnitude over the `lanes` neighbouring lanes (a power of two, aligned) that hold a group. All 32 lanes take part.
 __device__ __forceinline__ float max_over_lanes(float m, int lanes) {
   for (int d = 1; d < lanes; d <<= 1) m = max_magnitude(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
