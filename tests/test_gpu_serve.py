@@ -59,3 +59,57 @@ def test_recover_multiply_write_read(oracle, bits, group):
         seq = torch.cat([given[:n, s, plane] for s, n in enumerate(lengths)])
         codes, scales = ref.quantize(seq.double().cpu().numpy(), bits, group)
         assert torch.equal(outs[plane].cpu(), torch.from_numpy(ref.values(codes, scales, group)).float().to(torch.bfloat16))
+
+
+def test_two_streams_and_two_graphs_at_once():
+    """Products, writes and reads of two states on two streams, eagerly and as graphs replayed side by side, give what they give alone."""
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_2009_13003_b200 import binding as lc
+
+    g = torch.Generator(device=DEV).manual_seed(3)
+    sides = []
+    for rows, cols, tokens, bits in ((3000, 2100, 2, 8), (500, 9000, 5, 4)):
+        w = torch.randn(rows, cols, generator=g, device=DEV)
+        q4, ws = lc.alloc_q4(rows, cols, 64, DEV), lc.alloc_workspace(0, DEV)
+        x, y = torch.randn(tokens, cols, generator=g, device=DEV), torch.empty(tokens, rows, device=DEV)
+        cache, status = lc.alloc_cache(96, 2, 80, bits, 32, DEV), lc.alloc_status(DEV)
+        kv = torch.randn(48, 2, 2, 80, generator=g, device=DEV)
+        at, outs = torch.randperm(96, generator=g, device=DEV)[:48], [torch.empty(48, 2, 80, device=DEV) for _ in range(2)]
+
+        def run(w=w, q4=q4, ws=ws, x=x, y=y, cache=cache, status=status, kv=kv, at=at, outs=outs):
+            lc.q4_quantize_async(w, q4, ws)
+            lc.q4_matvec(q4, x, y)
+            lc.cache_write(cache, kv[:, 0], kv[:, 1], at, status)
+            lc.cache_read(cache, at, outs, status=status)
+
+        run()
+        torch.cuda.synchronize()
+        sides.append((run, [y, *outs], [t.clone() for t in (y, *outs)], (ws, status)))
+
+    streams = [torch.cuda.Stream(DEV) for _ in sides]
+
+    def compare():
+        torch.cuda.synchronize()
+        for _, got, want, words in sides:
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+            assert all(lc.last_status(word) == lc.OK for word in words)
+            for t in got:
+                t.zero_()
+        torch.cuda.synchronize()
+
+    compare()
+    for _ in range(20):
+        for (run, *_), s in zip(sides, streams):
+            with torch.cuda.stream(s):
+                run()
+    compare()
+    graphs = [torch.cuda.CUDAGraph() for _ in sides]
+    for (run, *_), s, graph in zip(sides, streams, graphs):
+        with torch.cuda.graph(graph, stream=s):
+            run()
+    for _ in range(20):
+        for graph, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                graph.replay()
+    compare()
