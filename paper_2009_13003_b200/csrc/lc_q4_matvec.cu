@@ -663,6 +663,7 @@ uint32_t tokens_per_pass(uint32_t tokens, uint32_t parts) {
   const uint32_t most = kMostColumns / parts, passes = (tokens + most - 1) / most;
   return (tokens + passes - 1) / passes;
 }
+constexpr uint32_t kMostTokens = 1u << 19;  // of a launch: 52429 passes of 10 fp32 vectors, where a grid has 65535 rows
 uint32_t eights_log(uint32_t columns) { return columns <= 8 ? 0 : columns <= 16 ? 1 : 2; }
 
 template <class X, class M>
@@ -702,16 +703,20 @@ cudaError_t launch_q4_matvec(const Q4Layout& L, const uint8_t* q4, const void* x
                              uint64_t out_stride, cudaStream_t cs) {
   MatvecArgs A = {};
   A.q4 = q4;
-  A.x = x;
-  A.out = out;
   A.x_stride = x_stride;
   A.out_stride = out_stride;
   A.L = L;
-  A.tokens = tokens;
   A.out_type = out_type;
-  if (type == LC_TYPE_F32) return launch_columns<float, __nv_bfloat16>(A, cs);
-  if (type == LC_TYPE_BF16) return launch_columns<__nv_bfloat16, __nv_bfloat16>(A, cs);
-  return launch_columns<__half, __half>(A, cs);
+  for (uint32_t first = 0; first < tokens; first += kMostTokens) {
+    A.x = static_cast<const uint8_t*>(x) + first * x_stride * type_bytes(type);
+    A.out = static_cast<uint8_t*>(out) + first * out_stride * type_bytes(out_type);
+    A.tokens = tokens - first < kMostTokens ? tokens - first : kMostTokens;
+    const cudaError_t e = type == LC_TYPE_F32    ? launch_columns<float, __nv_bfloat16>(A, cs)
+                          : type == LC_TYPE_BF16 ? launch_columns<__nv_bfloat16, __nv_bfloat16>(A, cs)
+                                                 : launch_columns<__half, __half>(A, cs);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
 }
 
 }  // namespace lc

@@ -232,6 +232,16 @@ def test_one_vector_for_all_tokens_and_nothing_to_do(lc):
     assert torch.equal(lc.q4_matvec(none, torch.empty(3, 0, device=DEV)), torch.zeros(3, 50, device=DEV)) and lc.q4_read(none).shape == (50, 0)
 
 
+@pytest.mark.parametrize("kind,tokens", [("fp32", 655351), ("fp32", 1048576), ("bf16", 1048576)])
+def test_as_many_vectors_as_allowed(lc, kind, tokens):
+    """Up to LC_Q4_MAX_TOKENS vectors, more passes than a grid has rows; whole numbers, so that every sum is exact."""
+    w = whole_weights(2, 32, 32, 5)
+    x = (torch.arange(tokens * 32, device=DEV).view(tokens, 32) % 9 - 4).to(TYPES[kind])
+    got = lc.q4_matvec(lc.q4_quantize(torch.from_numpy(w).to(DEV), 32), x, torch.empty(tokens, 2, device=DEV))
+    want = (x.double() @ torch.from_numpy(w.astype(np.float64)).to(DEV).T).float()
+    assert torch.equal(got, want)
+
+
 def test_on_another_stream_and_in_a_graph(lc):
     w, x = random_weights(200, 700, 11), torch.randn(3, 700, device=DEV)
     q4, ws = lc.alloc_q4(200, 700, 64, DEV), lc.alloc_workspace(0, DEV)
