@@ -403,7 +403,8 @@ int lc_q4_matvec(const void* q4, uint64_t q4_bytes, uint64_t rows, uint64_t cols
  * planes = 2 every place holds two rows, a key and a value. The memory is the caller's, laid out row by row (docs/QUANT.md,
  * section 3): codes lc_cache_code_bytes, 16-byte aligned, scales (bf16) lc_cache_scale_bytes. What was never written reads as
  * what its bytes say; zeroed scales read as zeros.
- * bits 4 or 8; group 32, 64 or 128; 1 <= heads, dim <= 65536, heads * dim < 2^31; slots < 2^40. The size functions return 0 on bad arguments.
+ * bits 4 or 8; group 32, 64 or 128; 1 <= heads, dim <= 65536, heads * dim < 2^31; slots < 2^40; codes of
+ * less than 2^62 bytes. The size functions return 0 on bad arguments.
  *
  * rows       of the call; rows * heads * groups per row of dim < 2^31.
  * src, out   HOST array with an entry per plane: row i's head h at data + i * row_stride + h * head_stride values of `type`, dim

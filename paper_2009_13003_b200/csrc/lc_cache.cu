@@ -187,12 +187,14 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(CacheArgs C, Plane
   }
 }
 
+uint32_t row_bytes(const lc_cache* c) { return (c->dim + 7) / 8 * c->bits; }
+// Codes of less than 2^62 bytes (scales take no more): every size and offset fits 64 bits.
 bool cache_ok(const lc_cache* c) {
   return c && (c->bits == 4 || c->bits == 8) && group_ok((int)c->group) && (c->planes == 1 || c->planes == 2) && c->heads >= 1 && c->heads <= 65536 &&
-         c->dim >= 1 && c->dim <= 65536 && (uint64_t)c->heads * c->dim < (1ull << 31) && c->slots < (1ull << 40);
+         c->dim >= 1 && c->dim <= 65536 && (uint64_t)c->heads * c->dim < (1ull << 31) && c->slots < (1ull << 40) &&
+         c->slots <= ((1ull << 62) - 1) / ((uint64_t)c->planes * c->heads * row_bytes(c));
 }
 
-uint32_t row_bytes(const lc_cache* c) { return (c->dim + 7) / 8 * c->bits; }
 uint32_t row_groups(const lc_cache* c) { return (c->dim + c->group - 1) / c->group; }
 
 CacheArgs cache_args(const lc_cache* c, uint64_t rows) {

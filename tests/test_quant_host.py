@@ -128,3 +128,17 @@ def test_the_cache_refuses():
 
 def test_the_words_for_a_bad_index():
     assert binding.lib().lc_strerror(binding.ERR_INDEX) == b"a slot or page that the cache does not have"
+
+
+def test_sizes_of_a_cache_do_not_wrap():
+    """A cache whose codes would take 2^62 bytes or more has no size and no call takes it: no small number left over from 2^64."""
+    L = binding.lib()
+    rows = (binding.LCRows * 2)((0x30000, 1 << 32, 1 << 16), (0x40000, 1 << 32, 1 << 16))
+    for planes, heads, dim, bits, group in ((2, 65536, 32767, 8, 128), (2, 65536, 32767, 4, 32), (1, 1, 65536, 8, 32), (2, 65536, 1, 4, 128), (2, 32768, 65535, 8, 64)):
+        for slots in (1 << 20, 1 << 30, 1 << 31, 1 << 32, 1 << 33, 1 << 36, (1 << 40) - 1):
+            c = binding.LCCache(0x10000, 0x20000, slots, planes, heads, dim, bits, group)
+            size = planes * slots * heads * (-(-dim // 8) * bits)
+            fits = size < 1 << 62
+            assert L.lc_cache_code_bytes(C.byref(c)) == (size if fits else 0), (slots, heads, dim)
+            assert L.lc_cache_scale_bytes(C.byref(c)) == (planes * slots * heads * -(-dim // group) * 2 if fits else 0), (slots, heads, dim)
+            assert L.lc_cache_write(C.byref(c), rows, 1, 0, 0x70000, None, None) == (binding.OK if fits else binding.ERR_ARG)
