@@ -74,7 +74,8 @@ __global__ void __launch_bounds__(kThreads) q4_quantize_kernel(const T* __restri
 }
 
 // The other way round: rows r and r + 8 of a block of 64 columns, in both halves of it 16 bytes of the output a lane, so that the lanes of
-// a row write whole runs: 4 lanes for a 16-bit output, 8 for fp32 (half the words each).
+// a row write whole runs: 4 lanes for a 16-bit output, 8 for fp32 (half the words each). Bound by memory: 4096 x 25088 to fp32 75 us, the
+// bytes take 71; 8192 x 8192 to fp16 29 us and 26.
 template <class T>
 __global__ void __launch_bounds__(kThreads) q4_read_kernel(const uint8_t* __restrict__ q4, Q4Layout L, T* __restrict__ out, uint64_t row_stride,
                                                            FastDiv by_blocks) {

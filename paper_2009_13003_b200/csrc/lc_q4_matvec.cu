@@ -15,6 +15,10 @@
 // multiplied by 2^80 when it is staged, so that sums keep all bits of an x down to 2^-72 and are exact to 2^-96 below. Where a sum comes
 // out as Inf or NaN (x holds one, or values of 2^48 and more, or a scale is beyond 2^74), the warp takes that tile again by plain
 // multiplications (slow_sums).
+//
+// Measured, the kernel alone over weights that the L2 does not hold: 28672 x 8192 (121 MB) with one bf16 vector 29 us, 4.2 TB/s; with 16
+// 51 us, with 32 100 us; 50257 x 2048 with 16 22 us; 4096 x 25088 with 4 fp32 vectors 28 us; 2048 x 2048 with one 3.8 us. The issue slots
+// of the first are 56 % busy: with the products left out and the loads kept it took 26 us, without the main loop 7.
 #include <type_traits>
 
 #include "lc_q4.cuh"
@@ -607,10 +611,10 @@ uint64_t plan_cycles(const Plan& p, uint32_t nt_log, uint32_t tiles, uint32_t pe
   return staged + (p.split > 1 ? 950 : 0) + blocks / slots * round(slots) + (blocks % slots ? round(blocks % slots) : 0);
 }
 
-Plan make_plan(uint32_t nt_log, const Q4Layout& L, uint32_t per_pass, uint32_t parts, uint32_t sms) {
+Plan plan_pass(uint32_t nt_log, const Q4Layout& L, uint32_t per_pass, uint32_t parts, uint32_t sms, uint64_t& least) {
   const uint32_t nt = 1u << nt_log;
   Plan best = {};
-  uint64_t least = ~0ull;
+  least = ~0ull;
   for (uint32_t mt = nt_log == 2 ? 2 : 1; mt <= 2; ++mt) {
     const uint32_t blocks = (L.tiles + mt - 1) / mt;
     if (mt == 2 && L.tiles <= sms && best.smem) break;  // too few tiles to put two together
@@ -642,6 +646,34 @@ Plan make_plan(uint32_t nt_log, const Q4Layout& L, uint32_t per_pass, uint32_t p
   return best;
 }
 
+// Of a product's vectors: how many go in a pass, and the logarithm of the eights of columns that it then has. A pass of 32 columns reads the
+// weights half as often, but has x and sums for fewer warps: 50257 x 2048 with 32 vectors 69 us, in passes of 16 42; 500 x 9000 with 64 18 and
+// 32 us. So make_plan takes the width whose passes take fewer cycles: over 39 shapes that the rule was not made on 3 % off the faster of the two
+// (35 % at most), where 32 columns always are 13 % off and 16 are 7 %.
+uint32_t tokens_per_pass(uint32_t tokens, uint32_t parts, uint32_t columns) {
+  const uint32_t most = columns / parts, passes = (tokens + most - 1) / most;
+  return (tokens + passes - 1) / passes;
+}
+uint32_t eights_log(uint32_t columns) { return columns <= 8 ? 0 : columns <= 16 ? 1 : 2; }
+constexpr uint32_t kMostTokens = 1u << 18;  // of a launch: 52429 passes of 5 fp32 vectors, where a grid has 65535 rows
+
+Plan make_plan(const Q4Layout& L, uint32_t tokens, uint32_t parts, uint32_t sms, uint32_t& per_pass, uint32_t& nt_log) {
+  Plan best = {};
+  uint64_t least = ~0ull;
+  for (uint32_t columns = tokens * parts <= 16 ? 16 : 32; columns >= 16; columns /= 2) {
+    const uint32_t per = tokens_per_pass(tokens, parts, columns), log = eights_log(per * parts);
+    uint64_t cycles;
+    const Plan p = plan_pass(log, L, per, parts, sms, cycles);
+    if (p.smem == 0) continue;
+    // passes that do not fill the device run side by side
+    const uint64_t slots = p.warps / p.ways, blocks = (L.tiles + p.mt - 1) / p.mt, room = (uint64_t)sms * ctas_per_sm(p.warps, p.smem);
+    const uint64_t wanted = (blocks + slots - 1) / slots * p.split, used = wanted < room ? wanted : room, passes = (tokens + per - 1) / per;
+    const uint64_t all = cycles * ((passes * used + room - 1) / room);
+    if (all < least) least = all, best = p, per_pass = per, nt_log = log;
+  }
+  return best;
+}
+
 template <class X, class M, int NT, int MT, int G>
 cudaError_t launch(const MatvecArgs& A, const Plan& p, uint32_t passes, uint32_t sms, cudaStream_t cs) {
   const uint32_t blocks = (A.L.tiles + MT - 1) / MT;
@@ -656,23 +688,9 @@ cudaError_t launch_group(const MatvecArgs& A, const Plan& p, uint32_t passes, ui
   return launch<X, M, NT, MT, 128>(A, p, passes, sms, cs);
 }
 
-// The tokens of a pass, and the logarithm of the eights of columns that the product then has. 64 columns in one pass hold twice the sums in
-// registers and x in shared memory, for fewer warps: 28672 x 8192, 64 vectors 321 us, in two passes 210.
-constexpr uint32_t kMostColumns = 32;
-uint32_t tokens_per_pass(uint32_t tokens, uint32_t parts) {
-  const uint32_t most = kMostColumns / parts, passes = (tokens + most - 1) / most;
-  return (tokens + passes - 1) / passes;
-}
-constexpr uint32_t kMostTokens = 1u << 19;  // of a launch: 52429 passes of 10 fp32 vectors, where a grid has 65535 rows
-uint32_t eights_log(uint32_t columns) { return columns <= 8 ? 0 : columns <= 16 ? 1 : 2; }
-
 template <class X, class M>
 cudaError_t launch_columns(MatvecArgs A, cudaStream_t cs) {
   constexpr uint32_t kParts = sizeof(X) == 4 ? 3 : 1;
-  A.per_pass = tokens_per_pass(A.tokens, kParts);
-  const uint32_t passes = (A.tokens + A.per_pass - 1) / A.per_pass;
-  A.by_count = FastDiv(A.per_pass);
-  const uint32_t columns = A.per_pass * kParts;
   A.aligned = (reinterpret_cast<uintptr_t>(A.x) & 15) == 0 && (A.tokens == 1 || A.x_stride % (16 / sizeof(X)) == 0);
   static int count[kMaxDevices];  // SMs
   const int dev = current_device_index();
@@ -684,9 +702,11 @@ cudaError_t launch_columns(MatvecArgs A, cudaStream_t cs) {
     count[dev] = n;
   }
   const uint32_t sms = (uint32_t)count[dev];
-  const uint32_t nt_log = eights_log(columns);
-  Plan p = make_plan(nt_log, A.L, A.per_pass, kParts, sms);
+  uint32_t nt_log = 0;
+  const Plan p = make_plan(A.L, A.tokens, kParts, sms, A.per_pass, nt_log);
   if (p.smem == 0) return cudaErrorInvalidConfiguration;
+  const uint32_t passes = (A.tokens + A.per_pass - 1) / A.per_pass;
+  A.by_count = FastDiv(A.per_pass);
   A.ways = p.ways;
   A.direct = p.direct;
   A.stages = p.stages;
@@ -726,8 +746,8 @@ extern "C" int lc_debug_q4_plan(uint64_t rows, uint64_t cols, int group, int typ
   using namespace lc;
   if (!plan || !group_ok(group) || !type_ok(type) || tokens == 0 || sms == 0 || rows == 0 || rows >= (1ull << 31) || cols >= (1ull << 31) - kQ4StepCols)
     return LC_ERR_ARG;
-  const uint32_t parts = type == LC_TYPE_F32 ? 3 : 1, per_pass = tokens_per_pass(tokens, parts), nt_log = eights_log(per_pass * parts);
-  const Plan p = make_plan(nt_log, q4_layout(rows, cols, group), per_pass, parts, sms);
+  uint32_t per_pass = 0, nt_log = 0;
+  const Plan p = make_plan(q4_layout(rows, cols, group), tokens < kMostTokens ? tokens : kMostTokens, type == LC_TYPE_F32 ? 3 : 1, sms, per_pass, nt_log);
   const uint32_t values[LC_Q4_PLAN_WORDS] = {per_pass, 1u << nt_log, p.mt, p.ways, p.split, p.warps, p.stages, p.slice, p.chunk, p.direct, p.smem};
   for (int i = 0; i < LC_Q4_PLAN_WORDS; ++i) plan[i] = values[i];
   return LC_OK;

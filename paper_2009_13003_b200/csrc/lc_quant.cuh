@@ -91,7 +91,7 @@ __device__ __forceinline__ void load8(const T* p, int valid, float* v) {
 
 // `n` neighbouring values the other way, 16 bytes of them where all are there. The lanes of a warp hold neighbouring runs, so that a store
 // of theirs is one run of bytes: with 32 bytes a lane and two stores of every other 16, memory pays for both halves of each 32 (0.4 GB of
-// fp32 from 4 bits: 98 us; so 72).
+// fp32 from 4 bits: 99 us; so 75).
 template <class T>
 constexpr int kRun = 16 / sizeof(T);
 template <bool kWhole = false, class T>
