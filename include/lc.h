@@ -388,9 +388,10 @@ int lc_q4_read(const void* q4, uint64_t q4_bytes, uint64_t rows, uint64_t cols, 
  * twice as many where that is expected to be faster; more are taken in several parts. For many tokens lc_q4_read and a matrix product
  * are the better way: measured on bf16, from between 16 and 32 tokens on for 4096 x 4096, between 32 and 48 for 28672 x 8192.
  * x          DEVICE, `type` LC_TYPE_*, vector t at x + t * x_stride values, x_stride >= cols or 0 (one vector for all); aligned like
- *            its type. All of its bits count, also in fp32 (of a group's sum, what lies below 2^-96 may be lost). A group's sum is formed
- *            before its scale is applied: it has to stay in fp32's range (|x| below 2^117 is always enough). Vectors with values of
- *            2^48 and more, Inf and NaN among them, take many times as long.
+ *            its type. All of its bits count, also in fp32: a term is rounded by its own size, |scale * code * x|, whatever else the vector
+ *            holds (a code of 0 takes nothing from the others); only what lies below 2^-140 may be lost. A group's sum
+ *            is formed before its scale is applied: it has to stay in fp32's range (|x| below 2^117 is always enough). Vectors with values
+ *            of 2^96 and more, Inf and NaN among them, and results of that size take many times as long.
  * out        DEVICE, `out_type` = type or LC_TYPE_F32, row t at out + t * out_stride, out_stride >= rows; aligned like its type.
  * tokens     0 ... LC_Q4_MAX_TOKENS. With cols = 0 the products are 0.
  * The same inputs give the same bits.

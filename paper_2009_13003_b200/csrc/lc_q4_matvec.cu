@@ -6,19 +6,19 @@
 // bits, more than bf16 has. An fp32 vector takes three columns of the product: its values cut into three bf16 numbers, 8 bits
 // each, whose sum they are, so that nothing of them is lost.
 //
-// What bounds it, once enough is in flight, is the work of making 16-bit operands of 4-bit codes, so that is as little as can be:
-// the codes are used as the low bits of a 16-bit float. In a float's lowest 8 (bf16) or 11 (fp16) bits a whole number N stands for
-// N * 2^-133 or N * 2^-24 (subnormal numbers, and the first binade above them, which goes on in the same steps): with n = code + 8,
-// a mask takes two n's out of a word for a row r, and the same mask four bits up two 16 n's for row r + 8. One shift and four masks
-// for eight codes. What is too much by it, 8 times the group's sum of x, is taken off the group's sum in fp32; it comes from products
-// with a constant, once a CTA. To keep the products with bf16 vectors (and parts of fp32 ones) in fp32's normal range, x is
-// multiplied by 2^80 when it is staged, so that sums keep all bits of an x down to 2^-72 and are exact to 2^-96 below. Where a sum comes
-// out as Inf or NaN (x holds one, or values of 2^48 and more, or a scale is beyond 2^74), the warp takes that tile again by plain
-// multiplications (slow_sums).
+// The operands are the codes themselves, signed: a large x under a code of 0 then adds nothing and costs the rest of its group no bits. (With
+// code + 8 as operands, which saves an instruction a pair, and 8 times the group's sum of x taken off afterwards, a weight of 7 beside 2^30
+// on a zero came out as 0.) They are made of 4-bit codes in as few instructions as can be. In a float's lowest 8 (bf16) or 11 (fp16) bits
+// a whole number N stands for N * 2^-133 or N * 2^-24 (subnormal numbers, and the first binade above them, which goes on in the same
+// steps): with n = code + 8, a mask takes two n's out of a word for a row r, and the same mask four bits up two 16 n's for row r + 8.
+// One fused multiplication then brings a pair into the normal range and takes off 8. One shift, four masks and four multiplications for
+// eight codes, exact; a row's sums are in units of kUnit until they are done. A 16-bit x enters as it is; an fp32 one is multiplied by 2^24
+// when it is staged, so that its smallest part is a normal bf16 number. Where a sum comes out as Inf or NaN (x holds one, or values of 2^96
+// and more, or a result is that large), the warp takes that tile again by plain multiplications (slow_sums).
 //
-// Measured, the kernel alone over weights that the L2 does not hold: 28672 x 8192 (121 MB) with one bf16 vector 29 us, 4.2 TB/s; with 16
-// 51 us, with 32 100 us; 50257 x 2048 with 16 22 us; 4096 x 25088 with 4 fp32 vectors 28 us; 2048 x 2048 with one 3.8 us. The issue slots
-// of the first are 56 % busy: with the products left out and the loads kept it took 26 us, without the main loop 7.
+// Measured, the kernel alone over weights that the L2 does not hold: 28672 x 8192 (121 MB) with one bf16 vector 31 us, 3.9 TB/s (with
+// code + 8 29 us); with 16 52 us, with 32 92 us; 50257 x 2048 with 16 22 us; 4096 x 25088 with 4 fp32 vectors 28 us; 2048 x 2048 with one
+// 3.3 us.
 #include <type_traits>
 
 #include "lc_q4.cuh"
@@ -79,28 +79,36 @@ __device__ __forceinline__ void mma_first<__half>(float (&d)[4], const uint32_t 
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
 }
 
-// The eight codes of a word, plus 8, as four pairs of tiny numbers: of row r, of row r + 8 (times 16), and so for two more columns.
-__device__ __forceinline__ void operands(uint32_t w, uint32_t (&a)[4]) {
-  a[0] = w & 0x000F000Fu;
-  a[1] = w & 0x00F000F0u;
-  w >>= 8;
-  a[2] = w & 0x000F000Fu;
-  a[3] = w & 0x00F000F0u;
-}
-// -8 as such a number, in both halves.
-constexpr uint32_t kMinus8 = 0x80088008u;
-
-// kUp: what x is multiplied by; kUnit: what the scale of row r is then to be multiplied by (row r + 8: a sixteenth of it).
+// Codes as numbers of type M, in units of 1 / kUnit (row r) and 16 / kUnit (row r + 8): kTimes takes a pair of subnormal numbers there, kMinus
+// (a row each) then takes off 8 units. kUp: what an fp32 vector is multiplied by.
 template <class M>
 struct Unit;
 template <>
 struct Unit<__nv_bfloat16> {
-  static constexpr float kUp = 0x1p80f, kUnit = 0x1p53f;
+  static constexpr uint32_t kTimes = 0x7F007F00u, kMinus[2] = {0xBE00BE00u, 0xC000C000u};  // 2^127, -2^-3, -2
+  static constexpr float kUnit = 0x1p6f, kUp = 0x1p24f;
 };
 template <>
 struct Unit<__half> {
-  static constexpr float kUnit = 0x1p24f;
+  static constexpr uint32_t kTimes = 0x78007800u, kMinus[2] = {0xA400A400u, 0xB400B400u};  // 2^15, -2^-6, -2^-2
+  static constexpr float kUnit = 0x1p9f;
 };
+template <class M>
+__device__ __forceinline__ uint32_t code_pair(uint32_t tiny, uint32_t minus) {
+  uint32_t d;
+  if constexpr (std::is_same<M, __half>::value) asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(tiny), "r"(Unit<M>::kTimes), "r"(minus));
+  else asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(tiny), "r"(Unit<M>::kTimes), "r"(minus));
+  return d;
+}
+// The eight codes of a word as four pairs: of row r, of row r + 8, and so for two more columns.
+template <class M>
+__device__ __forceinline__ void operands(uint32_t w, uint32_t (&a)[4]) {
+  a[0] = code_pair<M>(w & 0x000F000Fu, Unit<M>::kMinus[0]);
+  a[1] = code_pair<M>(w & 0x00F000F0u, Unit<M>::kMinus[1]);
+  w >>= 8;
+  a[2] = code_pair<M>(w & 0x000F000Fu, Unit<M>::kMinus[0]);
+  a[3] = code_pair<M>(w & 0x00F000F0u, Unit<M>::kMinus[1]);
+}
 
 // Eight values of a vector from column `col` on, as they are in memory; zeros behind the last column.
 template <class X>
@@ -145,17 +153,8 @@ __device__ __forceinline__ void store_piece(const uint32_t (&raw)[2 * sizeof(X)]
       for (int e = 0; e < 4; ++e) w[e] = __byte_perm(part[k][2 * e], part[k][2 * e + 1], 0x7632);
       to[k * stride] = make_uint4(w[0], w[1], w[2], w[3]);
     }
-  } else if constexpr (std::is_same<X, __half>::value) {
-    to[0] = make_uint4(raw[0], raw[1], raw[2], raw[3]);
   } else {
-    uint32_t w[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const __nv_bfloat162 up(__ushort_as_bfloat16(0x6780), __ushort_as_bfloat16(0x6780));  // 2^80
-      const __nv_bfloat162 v = __hmul2(reinterpret_cast<const __nv_bfloat162&>(raw[e]), up);
-      w[e] = reinterpret_cast<const uint32_t&>(v);
-    }
-    to[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    to[0] = make_uint4(raw[0], raw[1], raw[2], raw[3]);
   }
 }
 
@@ -181,7 +180,7 @@ __device__ __forceinline__ void copies_wait(uint32_t left) {
 // number of units (32 columns of the matrix, four pieces) of which lanes 4 r + t multiply piece t, so that eight columns lie in
 // eight different parts of the banks. Zeros behind the matrix's last column. Where the vectors are aligned, a thread first copies its
 // pieces as they are (an fp32 piece to where its first two parts will be), all of them on their way at once, and then changes
-// them in place; fp16 has nothing to change. (The code is short rather than unrolled: in a small product it runs once, and reading it
+// them in place; those of 16 bits stay as they are. (The code is short rather than unrolled: in a small product it runs once, and reading it
 // from memory takes as long as the loads; with four pieces a turn 2048 x 2048 took 4.9 us, with one 4.1.)
 template <class X>
 __device__ __forceinline__ void stage_x(const MatvecArgs& A, uint32_t first, uint32_t count, uint32_t begin, uint32_t end, uint32_t stride, uint4* xs, bool copy) {
@@ -199,7 +198,7 @@ __device__ __forceinline__ void stage_x(const MatvecArgs& A, uint32_t first, uin
       for (int k = 0; k < (int)sizeof(X) / 2; ++k) copy16(shared_address(to + k * stride), reinterpret_cast<const uint4*>(from) + k);
       continue;
     }
-    if (whole && std::is_same<X, __half>::value) continue;
+    if (whole && sizeof(X) == 2) continue;
     uint32_t raw[2 * sizeof(X)];
     if (whole) {
 #pragma unroll
@@ -211,28 +210,6 @@ __device__ __forceinline__ void stage_x(const MatvecArgs& A, uint32_t first, uin
       load_piece<X>(A, first + token, col, true, raw);
     }
     store_piece<X>(raw, to, stride);
-  }
-}
-
-// What is to be added to the sums of row r (16 times it to those of row r + 8), per group of the staged steps and column of the product.
-template <class M, int NT, int G>
-__device__ __forceinline__ void sum_groups(const uint4* const (&column)[NT], uint32_t steps, float* starts) {
-  const uint32_t lane = threadIdx.x & 31;
-  constexpr uint32_t kUnits = G / 32;
-  const uint32_t minus[4] = {kMinus8, kMinus8, kMinus8, kMinus8};
-#pragma unroll 1
-  for (uint32_t g = threadIdx.x >> 5; g < steps * 4 / kUnits; g += blockDim.x >> 5) {
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (uint32_t u = 0; u < kUnits; ++u) {
-        const uint4 b = column[n][(g * kUnits + u) * 4];
-        mma<M>(acc, minus, b.x, b.y);
-        mma<M>(acc, minus, b.z, b.w);
-      }
-      if (lane < 4) *reinterpret_cast<float2*>(starts + g * 8 * NT + 8 * n + 2 * lane) = make_float2(acc[0], acc[1]);
-    }
   }
 }
 
@@ -275,7 +252,7 @@ __device__ __forceinline__ void store_in_cluster(float* mine, uint32_t rank, flo
   asm volatile("{ .reg .u32 a; mapa.shared::cluster.u32 a, %0, %1; st.shared::cluster.f32 [a], %2; }" ::"r"(shared_address(mine)), "r"(rank), "f"(v) : "memory");
 }
 
-// Shared memory: the warps' rings, their sums, what the cluster's CTAs send each other, what is added to the sums of groups, x.
+// Shared memory: the warps' rings, their sums, what the cluster's CTAs send each other, x.
 template <int NT, int MT, int G>
 struct Shared {
   static constexpr uint32_t kGroups = kQ4StepCols / G, kSlot = kQ4StepBytes + kGroups * 32, kStage = MT * kSlot;  // codes and scales of a step
@@ -285,7 +262,6 @@ struct Shared {
   static __host__ __device__ __forceinline__ uint32_t part(uint32_t groups, uint32_t split, uint32_t per_pass) {  // [2][groups][split][part_tokens][kRows] floats
     return 2 * groups * split * part_tokens(per_pass, split) * kRows * 4;
   }
-  static __host__ __device__ __forceinline__ uint32_t starts(uint32_t steps) { return steps * kGroups * 8 * NT * 4; }
   static __host__ __device__ __forceinline__ uint64_t x(uint32_t columns, uint32_t steps) { return (uint64_t)columns * (steps * 256 + 64); }
 };
 constexpr uint32_t kMostWarps = 16;  // on an SM, by their registers
@@ -318,8 +294,7 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid
   float* red = reinterpret_cast<float*>(base + warps * ring_bytes);
   const uint32_t part_tokens = S::part_tokens(A.per_pass, split), red_columns = A.per_pass * kParts;
   float* part = red + S::red(A.direct, warps, red_columns) / 4;
-  float* starts = part + S::part(groups, split, A.per_pass) / 4;
-  uint4* xs = reinterpret_cast<uint4*>(starts + S::starts(A.chunk) / 4);
+  uint4* xs = reinterpret_cast<uint4*>(part + S::part(groups, split, A.per_pass) / 4);
   const uint32_t x_stride = A.chunk * 16 + 4;
   const bool resident = A.chunk >= A.slice;
   if (resident && A.aligned) stage_x<X>(A, first, count, slice, slice_end, x_stride, xs, true);
@@ -391,9 +366,7 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid
         } else {
           copies_wait(A.stages - 1);
         }
-        if (!std::is_same<X, __half>::value || !A.aligned || A.L.cols % kQ4StepCols != 0) stage_x<X>(A, first, count, begin, end, x_stride, xs, false);
-        __syncthreads();
-        sum_groups<M, NT, G>(column, end - begin, starts);
+        if (kParts > 1 || !A.aligned || A.L.cols % kQ4StepCols != 0) stage_x<X>(A, first, count, begin, end, x_stride, xs, false);
         __syncthreads();
       }
       if (!there) continue;
@@ -406,7 +379,6 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid
         slot = slot + kStage == ring_bytes ? 0 : slot + kStage;
         float acc[MT][NT][4];
         const uint32_t at = (step - begin) * 16;
-        const Two* start = reinterpret_cast<const Two*>(starts + (step - begin) * kGroups * 8 * NT) + t;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           uint4 v[MT];
@@ -418,8 +390,8 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid
             uint32_t a[MT][2][4];
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-              operands(u & 1 ? v[m].z : v[m].x, a[m][0]);
-              operands(u & 1 ? v[m].w : v[m].y, a[m][1]);
+              operands<M>(u & 1 ? v[m].z : v[m].x, a[m][0]);
+              operands<M>(u & 1 ? v[m].w : v[m].y, a[m][1]);
             }
             constexpr int kSide = NT < 2 ? 1 : 2;  // eights of columns at a time: products that do not wait for each other
 #pragma unroll
@@ -445,12 +417,11 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid
 #pragma unroll
               for (int m = 0; m < MT; ++m) {
                 const uint32_t s = *reinterpret_cast<const uint32_t*>(w + m * kSlot + kQ4StepBytes + (u * 32 / G * 8 + r) * 4);
-                const float s_lo = __uint_as_float(s << 16) * Unit<M>::kUnit, s_hi = __uint_as_float(s & 0xFFFF0000u) * (Unit<M>::kUnit / 16);
+                const float s_lo = __uint_as_float(s << 16), s_hi = __uint_as_float(s & 0xFFFF0000u);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                  const Two f = start[(u * 32 / G * NT + n) * 4];
-                  sum[m][n][0] = fma_two(two(s_lo, s_lo), add_two(two(acc[m][n][0], acc[m][n][1]), f), sum[m][n][0]);
-                  sum[m][n][1] = fma_two(two(s_hi, s_hi), fma_two(two(16.0f, 16.0f), f, two(acc[m][n][2], acc[m][n][3])), sum[m][n][1]);
+                  sum[m][n][0] = fma_two(two(s_lo, s_lo), two(acc[m][n][0], acc[m][n][1]), sum[m][n][0]);
+                  sum[m][n][1] = fma_two(two(s_hi, s_hi), two(acc[m][n][2], acc[m][n][3]), sum[m][n][1]);
                 }
               }
             }
@@ -462,13 +433,14 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         if (m > 0 && block * MT + m >= A.L.tiles) break;
+        constexpr float kLow = kParts == 1 ? Unit<M>::kUnit : Unit<M>::kUnit / Unit<__nv_bfloat16>::kUp;  // row r + 8: a sixteenth
         float y[NT][4];
         bool fine = true;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
           for (int i = 0; i < 4; i += 2) {
-            split_two(sum[m][n][i / 2], y[n][i], y[n][i + 1]);
+            split_two(mul_two(sum[m][n][i / 2], i == 0 ? two(kLow, kLow) : two(kLow / 16, kLow / 16)), y[n][i], y[n][i + 1]);
             fine &= fabsf(y[n][i]) < __uint_as_float(0x7F800000u) && fabsf(y[n][i + 1]) < __uint_as_float(0x7F800000u);
           }
         }
@@ -582,6 +554,7 @@ struct Plan {
   uint32_t mt, ways, split, warps, stages, slice, chunk, direct, smem;
 };
 
+// The areas of Shared, and 4 bytes for each group and column of the product that stay free behind them.
 uint64_t plan_bytes(const Plan& p, uint32_t nt, uint32_t group, uint32_t per_pass, uint32_t parts, uint32_t steps) {
   const uint32_t columns = per_pass * parts, rows = p.mt * kQ4TileRows, groups = kQ4StepCols / group;
   const uint32_t stage = p.mt * (kQ4StepBytes + groups * 32), part_tokens = p.split > 1 ? (per_pass + p.split - 1) / p.split : 0;
