@@ -391,7 +391,8 @@ int lc_q4_read(const void* q4, uint64_t q4_bytes, uint64_t rows, uint64_t cols, 
  *            its type. All of its bits count, also in fp32: a term is rounded by its own size, |scale * code * x|, whatever else the vector
  *            holds (a code of 0 takes nothing from the others); only what lies below 2^-140 may be lost. A group's sum
  *            is formed before its scale is applied: it has to stay in fp32's range (|x| below 2^117 is always enough). Vectors with values
- *            of 2^96 and more, Inf and NaN among them, and results of that size take many times as long.
+ *            of 2^96 and more, Inf and NaN among them, and results of that size take many times as long (measured, 28672 x 8192, bf16:
+ *            183 us for one, 31 without; 16 of them 2.5 ms); what the other vectors of the call give stays the same to the bit.
  * out        DEVICE, `out_type` = type or LC_TYPE_F32, row t at out + t * out_stride, out_stride >= rows; aligned like its type.
  * tokens     0 ... LC_Q4_MAX_TOKENS. With cols = 0 the products are 0.
  * The same inputs give the same bits.

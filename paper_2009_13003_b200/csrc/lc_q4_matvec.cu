@@ -14,7 +14,7 @@
 // One fused multiplication then brings a pair into the normal range and takes off 8. One shift, four masks and four multiplications for
 // eight codes, exact; a row's sums are in units of kUnit until they are done. A 16-bit x enters as it is; an fp32 one is multiplied by 2^24
 // when it is staged, so that its smallest part is a normal bf16 number. Where a sum comes out as Inf or NaN (x holds one, or values of 2^96
-// and more, or a result is that large), the warp takes that tile again by plain multiplications (slow_sums).
+// and more, or a result is that large), the warp takes that vector's 16 sums again by plain multiplications (slow_sums).
 //
 // Measured, the kernel alone over weights that the L2 does not hold: 28672 x 8192 (121 MB) with one bf16 vector 31 us, 3.9 TB/s (with
 // code + 8 29 us); with 16 52 us, with 32 92 us; 50257 x 2048 with 16 22 us; 4096 x 25088 with 4 fp32 vectors 28 us; 2048 x 2048 with one
@@ -435,36 +435,39 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid
         if (m > 0 && block * MT + m >= A.L.tiles) break;
         constexpr float kLow = kParts == 1 ? Unit<M>::kUnit : Unit<M>::kUnit / Unit<__nv_bfloat16>::kUp;  // row r + 8: a sixteenth
         float y[NT][4];
-        bool fine = true;
+        uint32_t bad = 0;  // bit 2 n + i: a sum of column 8 n + 2 t + i is Inf or NaN
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
           for (int i = 0; i < 4; i += 2) {
             split_two(mul_two(sum[m][n][i / 2], i == 0 ? two(kLow, kLow) : two(kLow / 16, kLow / 16)), y[n][i], y[n][i + 1]);
-            fine &= fabsf(y[n][i]) < __uint_as_float(0x7F800000u) && fabsf(y[n][i + 1]) < __uint_as_float(0x7F800000u);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) bad |= fabsf(y[n][i + k]) < __uint_as_float(0x7F800000u) ? 0u : 1u << (2 * n + k);
           }
         }
-        if (__all_sync(0xFFFFFFFFu, fine)) {
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
+        for (int n = 0; n < NT; ++n) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t col = 8 * n + 2 * t + (i & 1), row = m * 16 + r + 8 * (i >> 1);
-              if (col >= columns) continue;
-              if (kParts == 1 && A.direct) put(col, row, y[n][i]);
-              else mine[col * kRedStride + row] = y[n][i];
-            }
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t col = 8 * n + 2 * t + (i & 1), row = m * 16 + r + 8 * (i >> 1);
+            if (col >= columns) continue;
+            if (kParts == 1 && A.direct) put(col, row, y[n][i]);
+            else mine[col * kRedStride + row] = y[n][i];
           }
-        } else {
-          for (uint32_t token = 0; token < count; ++token) {
-            const float2 y = slow_sums<X>(A, block * MT + m, first + token, slice + way, slice_end);
-            const uint32_t row = m * 16 + r;
-            if (kParts == 1 && A.direct) {
-              if (t == 0) put(token, row, y.x), put(token, row + 8, y.y);
-            } else if (t < kParts) {
-              mine[(token * kParts + t) * kRedStride + row] = t == 0 ? y.x : 0.0f;
-              mine[(token * kParts + t) * kRedStride + row + 8] = t == 0 ? y.y : 0.0f;
-            }
+        }
+        if (!__any_sync(0xFFFFFFFFu, bad != 0)) continue;
+        for (int d = 4; d < 32; d *= 2) bad |= __shfl_xor_sync(0xFFFFFFFFu, bad, d);
+        for (uint32_t token = 0; token < count; ++token) {  // those vectors alone: the others keep their sums
+          uint32_t again = 0;
+          for (uint32_t col = token * kParts; col < (token + 1) * kParts; ++col) again |= __shfl_sync(0xFFFFFFFFu, bad, (col & 7) / 2) >> (2 * (col / 8) + (col & 1)) & 1u;
+          if (!again) continue;
+          const float2 z = slow_sums<X>(A, block * MT + m, first + token, slice + way, slice_end);  // behind a __syncwarp: after the stores above
+          const uint32_t row = m * 16 + r;
+          if (kParts == 1 && A.direct) {
+            if (t == 0) put(token, row, z.x), put(token, row + 8, z.y);
+          } else if (t < kParts) {
+            mine[(token * kParts + t) * kRedStride + row] = t == 0 ? z.x : 0.0f;
+            mine[(token * kParts + t) * kRedStride + row + 8] = t == 0 ? z.y : 0.0f;
           }
         }
       }
