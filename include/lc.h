@@ -354,7 +354,7 @@ int lc_compress_noalloc(const float* base, const float* cur, uint64_t n, int nbi
  *   scale = bf16(max |w| / Q), Q = 7 (4 bits) or 127 (8 bits), rounded once to nearest even; 0 if below 2^-126
  *   code  = the whole number nearest to w / scale, ties to even; 0 if the scale is 0
  * and a code stands for code * scale, which fp32 holds exactly. The last group of a row may be shorter. A group with an Inf or
- * a NaN has a scale of NaN: all of it reads as NaN.
+ * a NaN has a scale of NaN: all of it reads as NaN. A finite number of 16 bits reads as a finite number of its type (docs/QUANT.md, section 1).
  * The calls below return without waiting; their buffers must not overlap except where that is said.
  */
 #define LC_TYPE_F32 0

@@ -184,6 +184,7 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(CacheArgs C, Plane
       if (!whole && first >= C.dim) continue;
       float v[n];
       values_in_row<kBits, n>(w[k], scale, v);
+      keep_in_type<T, kBits>(scale, v);
       store_run<kWhole>(o + k * kLanes * n, (int)min(n, C.dim - first), v);
     }
   }

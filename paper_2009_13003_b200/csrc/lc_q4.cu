@@ -107,6 +107,7 @@ __global__ void __launch_bounds__(kThreads) q4_read_kernel(const uint8_t* __rest
       for (uint32_t e = 0; e < n; ++e) codes[e] = ((e < 4 ? w[u].x : w[u].y) >> (16 * (e & 1) + 4 * (h + 2 * ((e >> 1) & 1)))) & 15u;
       float v[n];
       values_of<4>(codes, scale, v);
+      keep_in_type<T, 4>(scale, v);
       if (row < L.rows && col < L.cols) store_run(out + row * row_stride + col, (int)min(n, L.cols - col), v);
     }
   }

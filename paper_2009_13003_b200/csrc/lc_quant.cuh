@@ -14,6 +14,8 @@
 #include <cuda_fp16.h>
 #include <string.h>
 
+#include <type_traits>
+
 #include "lc_common.cuh"
 
 namespace lc {
@@ -279,6 +281,27 @@ __device__ __forceinline__ void values_of(const uint32_t (&n)[count], float scal
   for (int e = 0; e < count; e += 2) {
     const Two x = two(__uint_as_float(n[e] | 0x4B000000u), __uint_as_float(n[e + 1] | 0x4B000000u));
     split_two(mul_two(add_two(x, two(kOffset, kOffset)), two(scale, scale)), v[e], v[e + 1]);
+  }
+}
+// Reading into the type T: the scale of a group whose largest magnitude is T's largest number, where that scale was rounded up so far that
+// its largest code stands for more than T holds, and that number. Such values read as the largest number, not as Inf: what was a number of
+// T when it was written stays one. (A larger scale comes from a value beyond T, and a smaller one stays within it.) 0: none. 127 * 516 =
+// 65532 rounds to Inf in fp16, 7 * 9344 does not; 127 * 1.0078125 * 2^121 and 7 * 1.140625 * 2^125 do in bf16.
+template <class T, int kBits>
+constexpr uint32_t kLastScale = 0;
+template <>
+constexpr uint32_t kLastScale<__half, 8> = 0x44010000u;
+template <>
+constexpr uint32_t kLastScale<__nv_bfloat16, 8> = 0x7C010000u;
+template <>
+constexpr uint32_t kLastScale<__nv_bfloat16, 4> = 0x7E120000u;
+template <class T, int kBits, int count>
+__device__ __forceinline__ void keep_in_type(float scale, float (&v)[count]) {
+  if constexpr (kLastScale<T, kBits> != 0) {
+    if (__float_as_uint(scale) != kLastScale<T, kBits>) return;
+    constexpr float kMost = std::is_same<T, __half>::value ? 65504.0f : 0x1.FEp127f;
+#pragma unroll
+    for (int e = 0; e < count; ++e) v[e] = fminf(fmaxf(v[e], -kMost), kMost);
   }
 }
 // The first `count` values of eight in a row of a cache.
