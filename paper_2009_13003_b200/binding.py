@@ -533,7 +533,8 @@ TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 Q4_MAX_TOKENS = 1048576
 
 
-_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+# absent where torch was built without CUDA, and no tensor gets as far as a call
+_raw_stream, _current_device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
 _functions = {}  # of the library, by name
 
 
