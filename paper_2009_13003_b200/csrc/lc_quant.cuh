@@ -91,6 +91,23 @@ __device__ __forceinline__ void load8(const T* p, int valid, float* v) {
   }
 }
 
+// A value read into the type T, rounded to nearest. bf16: numbers beyond the largest are the largest, not Inf; the scale of a group with
+// the largest may be rounded up past it (to 1.0078125 * 2^121 in 8 bits, 1.140625 * 2^125 in 4).
+__device__ __forceinline__ void read_as(float v, float& x) { x = v; }
+__device__ __forceinline__ void read_as(float v, __half& x) { x = __float2half_rn(v); }
+__device__ __forceinline__ void read_as(float v, __nv_bfloat16& x) {
+  unsigned short h;
+  asm("cvt.rn.satfinite.bf16.f32 %0, %1;" : "=h"(h) : "f"(v));
+  x = __ushort_as_bfloat16(h);
+}
+template <class T>
+__device__ __forceinline__ uint32_t read_two(float a, float b) {
+  uint32_t r;
+  if constexpr (std::is_same<T, __half>::value) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  else asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
+
 // `n` neighbouring values the other way, 16 bytes of them where all are there. The lanes of a warp hold neighbouring runs, so that a store
 // of theirs is one run of bytes: with 32 bytes a lane and two stores of every other 16, memory pays for both halves of each 32 (0.4 GB of
 // fp32 from 4 bits: 99 us; so 75).
@@ -101,11 +118,8 @@ __device__ __forceinline__ void store_run(T* p, int valid, const float* v) {
   constexpr int n = kRun<T>;
   const uintptr_t at = reinterpret_cast<uintptr_t>(p);
   if (kWhole || (valid >= n && (at & 15) == 0)) {
-    uint4 raw;
-    T* e = reinterpret_cast<T*>(&raw);
-#pragma unroll
-    for (int i = 0; i < n; ++i) from_float(v[i], e[i]);
-    *reinterpret_cast<uint4*>(p) = raw;
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint4*>(p) = make_uint4(read_two<T>(v[0], v[1]), read_two<T>(v[2], v[3]), read_two<T>(v[4], v[5]), read_two<T>(v[6], v[7]));
+    else *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
     return;
   }
   if constexpr (!kWhole) {
@@ -115,12 +129,12 @@ __device__ __forceinline__ void store_run(T* p, int valid, const float* v) {
         uint2 raw;
         T* e = reinterpret_cast<T*>(&raw);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) from_float(v[h + i], e[i]);
+        for (int i = 0; i < 4; ++i) read_as(v[h + i], e[i]);
         *reinterpret_cast<uint2*>(p + h) = raw;
       } else if (sizeof(T) == 2 && valid >= h + 4) {
         T e[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) from_float(v[h + i], e[i]);
+        for (int i = 0; i < 4; ++i) read_as(v[h + i], e[i]);
         uint32_t w[2];
         memcpy(w, e, sizeof w);
         if (at & 2) {
@@ -134,7 +148,7 @@ __device__ __forceinline__ void store_run(T* p, int valid, const float* v) {
       } else {
 #pragma unroll
         for (int i = h; i < h + 4; ++i)
-          if (i < valid) from_float(v[i], p[i]);
+          if (i < valid) read_as(v[i], p[i]);
       }
     }
   }
@@ -283,25 +297,15 @@ __device__ __forceinline__ void values_of(const uint32_t (&n)[count], float scal
     split_two(mul_two(add_two(x, two(kOffset, kOffset)), two(scale, scale)), v[e], v[e + 1]);
   }
 }
-// Reading into the type T: the scale of a group whose largest magnitude is T's largest number, where that scale was rounded up so far that
-// its largest code stands for more than T holds, and that number. Such values read as the largest number, not as Inf: what was a number of
-// T when it was written stays one. (A larger scale comes from a value beyond T, and a smaller one stays within it.) 0: none. 127 * 516 =
-// 65532 rounds to Inf in fp16, 7 * 9344 does not; 127 * 1.0078125 * 2^121 and 7 * 1.140625 * 2^125 do in bf16.
-template <class T, int kBits>
-constexpr uint32_t kLastScale = 0;
-template <>
-constexpr uint32_t kLastScale<__half, 8> = 0x44010000u;
-template <>
-constexpr uint32_t kLastScale<__nv_bfloat16, 8> = 0x7C010000u;
-template <>
-constexpr uint32_t kLastScale<__nv_bfloat16, 4> = 0x7E120000u;
+// Reading into fp16 from 8 bits: the scale of a group whose largest magnitude is 65504 or next to it was rounded up to 516, and 127 * 516 =
+// 65532 rounds to Inf. Such values read as 65504: what was a number of fp16 when it was written stays one. (A larger scale comes from
+// a value beyond fp16, a smaller one stays within it, and so does 7 * 9344, from 4 bits. For bf16 see read_as.)
 template <class T, int kBits, int count>
 __device__ __forceinline__ void keep_in_type(float scale, float (&v)[count]) {
-  if constexpr (kLastScale<T, kBits> != 0) {
-    if (__float_as_uint(scale) != kLastScale<T, kBits>) return;
-    constexpr float kMost = std::is_same<T, __half>::value ? 65504.0f : 0x1.FEp127f;
+  if constexpr (std::is_same<T, __half>::value && kBits == 8) {
+    if (scale != 516.0f) return;
 #pragma unroll
-    for (int e = 0; e < count; ++e) v[e] = fminf(fmaxf(v[e], -kMost), kMost);
+    for (int e = 0; e < count; ++e) v[e] = fminf(fmaxf(v[e], -65504.0f), 65504.0f);
   }
 }
 // The first `count` values of eight in a row of a cache.

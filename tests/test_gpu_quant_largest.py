@@ -74,3 +74,16 @@ def test_what_a_narrower_type_cannot_hold_is_still_inf(lc):
     got = lc.cache_read(cache, at, dtype=torch.float16)[0].cpu()
     assert bool((got[0] == float("inf")).all()) and bool((got[1] == -float("inf")).all())
     assert bool(got[2, 0, :32].isnan().all()) and bool((got[2, 0, 32:] == float("inf")).all())
+
+
+def test_beyond_the_largest_of_bf16(lc):
+    x = torch.full((2, 1, 64), torch.finfo(torch.float32).max, device=DEV)
+    x[1] = -x[1]
+    for bits in (4, 8):
+        cache = lc.alloc_cache(2, 1, 64, bits, 32, DEV, planes=1)
+        at = torch.arange(2, device=DEV)
+        lc.cache_write(cache, x, None, at)
+        got, top = lc.cache_read(cache, at, dtype=torch.bfloat16)[0], torch.finfo(torch.bfloat16).max
+        assert bool((got[0] == top).all()) and bool((got[1] == -top).all())
+    got = lc.q4_read(lc.q4_quantize(x.view(2, 64), 32), dtype=torch.bfloat16)
+    assert bool((got[0] == top).all()) and bool((got[1] == -top).all())
