@@ -386,7 +386,7 @@ int lc_q4_read(const void* q4, uint64_t q4_bytes, uint64_t rows, uint64_t cols, 
  *   out[t, r] = sum over the groups G of row r of scale[r, G] * (sum over c in G of code[r, c] * x[t, c]),
  * sums in fp32, one rounding to the output's type. The weights are read once for up to 16 tokens (5 if x is fp32), and once for up to
  * twice as many where that is expected to be faster; more are taken in several parts. For many tokens lc_q4_read and a matrix product
- * are the better way: measured on bf16, from between 16 and 32 tokens on for 4096 x 4096, between 32 and 48 for 28672 x 8192.
+ * are the better way: measured on bf16, from 32 tokens on for 4096 x 4096, from 64 for 28672 x 8192.
  * x          DEVICE, `type` LC_TYPE_*, vector t at x + t * x_stride values, x_stride >= cols or 0 (one vector for all); aligned like
  *            its type. All of its bits count, also in fp32: a term is rounded by its own size, |scale * code * x|, whatever else the vector
  *            holds (a code of 0 takes nothing from the others); only what lies below 2^-140 may be lost. A group's sum

@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) matvec_kernel(const __grid
     __syncwarp();
     cluster_wait();
   }
-  const uint4* column[NT];  // this lane's column of each eight; one of zeros for those that are not there
+  const uint4* column[NT];  // this lane's column of each eight; column 0 for those that are not there, whose sums nobody takes
 #pragma unroll
   for (int n = 0; n < NT; ++n) column[n] = xs + (8 * n + r < columns ? 8 * n + r : 0) * x_stride + t;
 
@@ -566,8 +566,10 @@ uint64_t plan_bytes(const Plan& p, uint32_t nt, uint32_t group, uint32_t per_pas
 }
 
 // About how many cycles a layout takes: a step takes a warp `alone` cycles and an SM with all its warps `busy`; every CTA stages x; the
-// sums of a round of blocks are added up behind it. The numbers are fitted to 37 shapes of 1 to 40 vectors in up to 64 layouts each;
-// what the rule then takes is 3 % slower than the fastest of them (geometric mean; 12 % at most but for x of over 16 vectors).
+// sums of a round of blocks are added up behind it. The numbers were fitted to 37 shapes of 1 to 40 vectors in up to 64 layouts each,
+// with a loop that made its operands in fewer instructions. What the rule takes is now 5.6 % slower than the fastest of them (geometric mean; 17 %
+// at most, but for x of over 16 vectors 33 %), and 6.4 % over 30 other shapes (19 % at most). Numbers fitted anew to both came to 5 to 6 %
+// over shapes that they had not seen.
 constexpr uint32_t kStepAlone[2][3] = {{825, 1130, 1750}, {1270, 1800, 3000}}, kStepBusy[2][3] = {{71, 110, 200}, {130, 190, 390}};
 uint64_t plan_cycles(const Plan& p, uint32_t nt_log, uint32_t tiles, uint32_t per_pass, uint32_t parts, uint32_t sms) {
   const uint32_t per_sm = ctas_per_sm(p.warps, p.smem);
@@ -623,9 +625,9 @@ Plan plan_pass(uint32_t nt_log, const Q4Layout& L, uint32_t per_pass, uint32_t p
 }
 
 // Of a product's vectors: how many go in a pass, and the logarithm of the eights of columns that it then has. A pass of 32 columns reads the
-// weights half as often, but has x and sums for fewer warps: 50257 x 2048 with 32 vectors 69 us, in passes of 16 42; 500 x 9000 with 64 18 and
-// 32 us. So make_plan takes the width whose passes take fewer cycles: over 39 shapes that the rule was not made on 3 % off the faster of the two
-// (35 % at most), where 32 columns always are 13 % off and 16 are 7 %.
+// weights half as often, but has x and sums for fewer warps: 50257 x 2048 with 32 vectors 66 us, in passes of 16 41; 500 x 9000 with 64 16 and
+// 29 us. So make_plan takes the width whose passes take fewer cycles: over 39 shapes that the rule was not made on 3 % off the faster of the two
+// (33 % at most), where 32 columns always are 13 % off and 16 are 8 %.
 uint32_t tokens_per_pass(uint32_t tokens, uint32_t parts, uint32_t columns) {
   const uint32_t most = columns / parts, passes = (tokens + most - 1) / most;
   return (tokens + passes - 1) / passes;

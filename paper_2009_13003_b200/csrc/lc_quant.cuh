@@ -191,7 +191,8 @@ __device__ __forceinline__ float load16(const T* p, float (&v)[16]) {
   }
 }
 
-// The largest magnitude over the `lanes` neighbouring lanes (a power of two, aligned) that hold a group. All 32 lanes take part.
+// The largest magnitude over the `lanes` neighbouring lanes (a power of two, aligned) that hold a group. All lanes of the warp
+// take part that have not left it: rows share a warp whole groups of lanes each, and the lanes of a row leave together.
 __device__ __forceinline__ float max_over_lanes(float m, int lanes) {
   for (int d = 1; d < lanes; d <<= 1) m = max_magnitude(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
   return m;
@@ -236,7 +237,8 @@ __device__ __forceinline__ Two mul_two(Two a, Two b) {
 
 // The codes of `n` values of type T, each plus 2^(bits - 1) in the low bits of a float's pattern (x + 1.5 * 2^23 rounds x to a whole number,
 // ties to even, and holds it there). With at most 11 bits in a value and 8 in the scale, a quotient is a tie or far from one, and one
-// step of refinement makes it the nearest fp32 number, which a tie is itself. An fp32 value can be anywhere: its code is a guess
+// step of refinement makes it the nearest fp32 number, which a tie is itself (also where the scale is next to 2^-126 and the remainder is rounded
+// to 2^-149: all numbers of both types at all scales of the lowest binades are tested). An fp32 value can be anywhere: its code is a guess
 // that the exact remainder confirms, or, hardly ever, moves by one.
 template <class T, int kBits, int n>
 __device__ __forceinline__ void codes(const float (&v)[n], uint32_t scale_bits, float (&t)[n]) {
