@@ -442,6 +442,75 @@ int lc_cache_read_pages(const lc_cache* cache, const lc_rows* out, int type, uin
                         uint64_t table_stride, uint32_t width, uint32_t page, const int32_t* begin, const int32_t* first,
                         uint32_t sequences, int32_t* status, lc_cuda_stream_t cs);
 
+/*
+ * The plan of a step. A cache's slots are dealt out in pages of `page` neighbouring ones. Who has which is kept on the DEVICE:
+ *   table    [sequences][table_stride] entries, `width` of them in use: the pages of each sequence, in the order of its positions
+ *   held     [sequences] positions that a sequence holds, 0 ... width * page and below 2^31
+ *   spare    [pages] numbers of the pages that no sequence has: the first *count
+ * lc_cache_plan, for `tokens` (DEVICE, one per sequence) new positions of each, or one below 0 for a sequence that ends:
+ *   - an ended sequence's ceil(held / page) pages go behind the spare ones, sequence by sequence; it holds 0 positions then
+ *   - then each sequence in turn takes the pages that it lacks for held + tokens positions from the end of the spare ones, the last first
+ *   - begin[s] (sequences + 1 entries): the first row of sequence s in a batch that has the new tokens one behind the other
+ *   - first[s]: the position of that row, which is what the sequence held (0 if it has ended)
+ *   - slots[r] (rows entries): the slot of row r, for lc_cache_write; -1 from row begin[sequences] on
+ *   - held_after, count_after: the books after the step. May be `held` and `count` themselves. If they are others, the same step
+ *     can be planned again: nothing that it read has changed then.
+ * begin and first are what lc_cache_attend and lc_cache_read_pages take.
+ * All or nothing: if a sequence would outgrow its row of the table, pages run out or the rows are more than `rows` (LC_ERR_CAPACITY), or the
+ * books contradict themselves (LC_ERR_INDEX), the status word receives that if it is 0, table and spare stay as they are, held_after and
+ * count_after say what held and count do, begin is all 0 and slots all -1. A page number of the table outside 0 ... pages - 1 sets LC_ERR_INDEX
+ * and its rows' slots to -1. Entries of `spare` from *count_after on mean nothing; those of an ended sequence in `table` stay.
+ * page, pages, rows, sequences below 2^31; table_stride >= width (if there are two sequences) and below 2^32. Only held / held_after and count / count_after may be the same memory.
+ */
+typedef struct lc_pages {
+  int32_t* table;
+  uint64_t table_stride;
+  const int32_t* held;
+  int32_t* spare;
+  const int32_t* count;
+  uint32_t width, page, pages;
+} lc_pages;
+int lc_cache_plan(const lc_pages* pages, const int32_t* tokens, uint32_t sequences, uint64_t rows, int32_t* begin, int32_t* first,
+                  int64_t* slots, int32_t* held_after, int32_t* count_after, int32_t* status, lc_cuda_stream_t cs);
+
+/*
+ * Attention of new tokens to a cache of keys and values (planes 2, dim at most 256), read where it lies. Row j of sequence s (its rows are
+ * begin[s] ... begin[s + 1] - 1 of q) is at position i = first[s] + j; the sequence has first[s] + its number of rows positions, whose keys and
+ * values are in the pages that the table names, the new ones' too (lc_cache_write comes first). For each of `heads` heads of q, head h of
+ * which reads head h / (heads / cache heads):
+ *   t(i, p) = scale * q_i . k_p;  cap > 0: cap * tanh(t / cap);  slopes: less slopes[h] * |i - p|
+ *   out_i = sum over the positions p that i sees of exp(t(i, p)) v_p / sum of exp(t(i, p))
+ * i sees p <= i (window > 0: the last `window` of those, i itself among them), and in any case p < prefix[s] (of the sequence's own positions).
+ * q, out     `rows` rows of `heads` heads of dim values of `type`, as for the cache's calls; rows of out must not share memory (LC_ERR_ARG), nor may
+ *            q and out. Rows ahead of begin[0] and from begin[sequences] on are left as they are.
+ * table, table_stride, width, page, begin, first, sequences   as for lc_cache_read_pages.
+ * longest    no sequence has more rows than that; 0: not known. A smaller bound may choose a faster kernel.
+ * slopes     DEVICE fp32, one per head of q, or NULL.     prefix   DEVICE, one per sequence, or NULL for 0.
+ * scale      finite; cap finite, 0 for none. window below 2^31, 0 for none. heads <= 65536, a multiple of the cache's; rows * heads < 2^30.
+ * status     as for lc_cache_read_pages: LC_ERR_INDEX if a sequence has rows or positions that are not there (begin outside of q, more rows than
+ *            `longest`, positions below 0 or beyond its row of the table: its rows are left as they are), or a page that the cache does not
+ *            have (its keys and values count as zeros).
+ * workspace  DEVICE, 256-byte aligned, lc_cache_attend_bytes (0 on bad arguments; the number of slots does not matter); two calls that overlap in time
+ *            need two. scales of the cache are on 4 bytes here.
+ * Scores, sums and what they are divided by are fp32. Rows of bf16 and of fp16 round probabilities to 8 and 11 bits or more, and may round keys and
+ * values to their type, as lc_cache_read does; fp32 rounds neither. An Inf or NaN that a row does not see changes no bit of it. The same inputs give
+ * the same bits.
+ */
+typedef struct lc_attend {
+  const int32_t* table;
+  uint64_t table_stride;
+  uint32_t width, page;
+  const int32_t* begin;
+  const int32_t* first;
+  uint32_t sequences, longest, heads, window;
+  float scale, cap;
+  const float* slopes;
+  const int32_t* prefix;
+} lc_attend;
+uint64_t lc_cache_attend_bytes(const lc_cache* cache, uint32_t sequences);
+int lc_cache_attend(const lc_cache* cache, const lc_rows* q, const lc_rows* out, int type, uint64_t rows, const lc_attend* how,
+                    void* workspace, uint64_t workspace_bytes, int32_t* status, lc_cuda_stream_t cs);
+
 #ifdef __cplusplus
 }
 #endif

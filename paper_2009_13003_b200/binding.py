@@ -29,6 +29,7 @@ SYMBOLS = (
     "lc_compress_noalloc",
     "lc_q4_bytes", "lc_q4_quantize", "lc_recover_q4", "lc_q4_read", "lc_q4_matvec", "lc_debug_q4_plan",
     "lc_cache_code_bytes", "lc_cache_scale_bytes", "lc_cache_write", "lc_cache_read", "lc_cache_read_pages",
+    "lc_cache_plan", "lc_cache_attend_bytes", "lc_cache_attend",
 )
 NOALLOC_MAX_N = 4194304
 
@@ -49,6 +50,17 @@ class LCCache(C.Structure):
 
 class LCRows(C.Structure):
     _fields_ = [("data", C.c_void_p), ("row_stride", C.c_uint64), ("head_stride", C.c_uint64)]
+
+
+class LCPages(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("table_stride", C.c_uint64), ("held", C.c_void_p), ("spare", C.c_void_p), ("count", C.c_void_p),
+                ("width", C.c_uint32), ("page", C.c_uint32), ("pages", C.c_uint32)]
+
+
+class LCAttend(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("table_stride", C.c_uint64), ("width", C.c_uint32), ("page", C.c_uint32), ("begin", C.c_void_p), ("first", C.c_void_p),
+                ("sequences", C.c_uint32), ("longest", C.c_uint32), ("heads", C.c_uint32), ("window", C.c_uint32), ("scale", C.c_float), ("cap", C.c_float),
+                ("slopes", C.c_void_p), ("prefix", C.c_void_p)]
 
 
 class LCError(RuntimeError):
@@ -122,6 +134,9 @@ def lib():
         f.argtypes, f.restype = [cache], u64
     L.lc_cache_write.argtypes = L.lc_cache_read.argtypes = [vp, vp, i32, u64, vp, vp, vp]
     L.lc_cache_read_pages.argtypes = [vp, vp, i32, u64, vp, u64, C.c_uint32, C.c_uint32, vp, vp, C.c_uint32, vp, vp]
+    L.lc_cache_plan.argtypes = [vp, vp, C.c_uint32, u64, vp, vp, vp, vp, vp, vp, vp]
+    L.lc_cache_attend_bytes.argtypes, L.lc_cache_attend_bytes.restype = [cache, C.c_uint32], u64
+    L.lc_cache_attend.argtypes = [vp, vp, vp, i32, u64, vp, vp, u64, vp, vp]
     _lib = L
     return L
 
@@ -779,3 +794,120 @@ def cache_read_pages(cache, table, page, begin, outs, first=None, status=None):
     _call("lc_cache_read_pages", index, cache._at, out, kind, rows, table.data_ptr(), table.stride(0), width, page, at,
           None if first is None else _whole(first, "first", torch.int32, index), sequences, _status(status, index))
     return outs
+
+
+# ---- pages of a cache, and attention to it ------------------------------------------------------------------------
+
+
+class Pages:
+    """Who has which pages of a cache (lc_pages): ``table`` [sequences, width], ``held`` [sequences], ``spare`` [pages] and ``count`` [1],
+    int32 tensors of one CUDA device; ``page`` slots a page."""
+
+    def __init__(self, table, held, spare, count, page):
+        index = table.get_device()
+        if table.dim() != 2 or table.dtype != torch.int32 or index < 0 or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError("table must be a [sequences, width] int32 CUDA tensor, contiguous along its last axis")
+        for t, name in ((held, "held"), (spare, "spare"), (count, "count")):
+            _whole(t, name, torch.int32, index)
+        if held.shape != table.shape[:1] or spare.dim() != 1 or count.numel() != 1:
+            raise ValueError("held has an entry per sequence, spare one per page, count one")
+        self.table, self.held, self.spare, self.count, self.page = table, held, spare, count, page
+        self.sequences, self.device, self._index = table.shape[0], table.device, index
+        self._c = LCPages(table.data_ptr(), table.stride(0), held.data_ptr(), spare.data_ptr(), count.data_ptr(), table.shape[1], page, spare.numel())
+        self._at = C.addressof(self._c)
+
+
+def alloc_pages(sequences, width, pages, page, device) -> Pages:
+    """Books of ``sequences`` sequences that hold nothing yet, of at most ``width`` pages each, and ``pages`` spare pages."""
+    whole = lambda *shape: torch.zeros(*shape, dtype=torch.int32, device=device)
+    return Pages(whole(sequences, width), whole(sequences), torch.arange(pages - 1, -1, -1, dtype=torch.int32, device=device),
+                 torch.full((1,), pages, dtype=torch.int32, device=device), page)
+
+
+class Plan(NamedTuple):
+    """A step of a batch (lc_cache_plan): ``begin`` [sequences + 1], ``first`` [sequences], ``slots`` [rows], and the books after it."""
+
+    begin: torch.Tensor
+    first: torch.Tensor
+    slots: torch.Tensor
+    held: torch.Tensor
+    count: torch.Tensor
+
+
+def alloc_plan(pages, rows, in_place=True) -> Plan:
+    """Room for a step of up to ``rows`` rows. in_place: the step advances ``pages``; else its books go to tensors of their own."""
+    whole = lambda n, dtype=torch.int32: torch.empty(n, dtype=dtype, device=pages.device)
+    held, count = (pages.held, pages.count) if in_place else (torch.empty_like(pages.held), torch.empty_like(pages.count))
+    return Plan(whole(pages.sequences + 1), whole(pages.sequences), whole(rows, torch.int64), held, count)
+
+
+def cache_plan(pages, tokens, rows=None, plan=None, status=None) -> Plan:
+    """lc_cache_plan on the current stream: pages and slots for ``tokens`` [sequences] int32 new positions of each sequence (below 0: it has
+    ended, its pages go back). ``plan``, or ``rows`` for a new one that advances ``pages``. A step that does not fit changes nothing
+    and shows in ``status``."""
+    if plan is None:
+        if rows is None:
+            raise ValueError("rows or a plan is needed")
+        plan = alloc_plan(pages, rows)
+    index, sequences = pages._index, pages.sequences
+    begin, first, slots, held, count = plan
+    if tokens.numel() != sequences or begin.numel() != sequences + 1 or first.numel() != sequences or held.numel() != sequences or count.numel() != 1:
+        raise ValueError("tokens, first and held have an entry per sequence, begin one more, count one")
+    i32 = torch.int32
+    _call("lc_cache_plan", index, pages._at, _whole(tokens, "tokens", i32, index), sequences, slots.numel(), _whole(begin, "begin", i32, index),
+          _whole(first, "first", i32, index), _whole(slots, "slots", torch.int64, index), _whole(held, "held", i32, index), _whole(count, "count", i32, index),
+          _status(status, index))
+    return plan
+
+
+def alloc_attend_workspace(cache, sequences) -> torch.Tensor:
+    """A workspace for cache_attend of up to ``sequences`` sequences."""
+    size = int(lib().lc_cache_attend_bytes(cache._c, sequences))
+    if size == 0:
+        raise LCError(ERR_ARG, "lc_cache_attend_bytes")
+    return torch.empty(size, dtype=torch.uint8, device=cache.device)
+
+
+_attend = struct.Struct("=QQIIQQIIIIffQQ").pack  # an lc_attend
+
+
+def cache_attend(cache, q, table, page, begin, out=None, first=None, scale=None, cap=0.0, slopes=None, window=0, prefix=None, longest=0, workspace=None,
+                 status=None):
+    """Attention of the rows of ``q`` [rows, heads, dim] to the cache, on the current stream: ``out`` (like q; rows of no sequence stay as they are,
+    in a new one they are 0). ``table`` [sequences, width] int32, ``page``, ``begin`` [sequences + 1] and ``first`` [sequences] (0 if None) as for
+    cache_read_pages, the new rows' keys and values being in the cache already. Scores: ``scale`` (None: 1 / sqrt(dim)) times the products,
+    capped by ``cap`` * tanh(score / cap) if that is not 0, less ``slopes`` [heads] float32 times the distance. A row sees the positions up to
+    its own, only the last ``window`` of them if that is not 0, and those ahead of ``prefix`` [sequences] int32. ``longest``: the most rows that a
+    sequence has (0: not known). ``workspace``: alloc_attend_workspace; calls that overlap in time need their own. No gradient is kept."""
+    index = cache._index
+    kind, shape, strides = _numbers(q, "q", 3, index)
+    rows, heads, dim = shape
+    if cache.planes != 2 or dim != cache.dim or heads % cache.heads:
+        raise ValueError("q must be [rows, heads, dim] with the cache's dim and a multiple of its heads, and the cache have keys and values")
+    if q.requires_grad and torch.is_grad_enabled():
+        raise ValueError("cache_attend has no gradient: detach q, or call it under torch.no_grad()")
+    if out is None:
+        out = torch.zeros(rows, heads, dim, dtype=q.dtype, device=q.device)
+    kind2, shape2, strides2 = _numbers(out, "out", 3, index)
+    if kind2 != kind or shape2 != shape:
+        raise ValueError("q and out differ in shape or type")
+    if table.dim() != 2 or table.dtype != torch.int32 or table.get_device() != index or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError("table must be [sequences, width] int32 on the cache's device, contiguous along its last axis")
+    sequences, width = table.shape
+    if begin.numel() != sequences + 1 or (first is not None and first.numel() != sequences) or (prefix is not None and prefix.numel() != sequences):
+        raise ValueError("begin has an entry per sequence and one more, first and prefix one per sequence")
+    if slopes is not None and slopes.numel() != heads:
+        raise ValueError("slopes has an entry per head of q")
+    if not (0 <= window < 1 << 31 and 0 <= longest < 1 << 32 and 0 <= page < 1 << 32):
+        raise LCError(ERR_ARG, "lc_cache_attend")
+    if workspace is None:
+        workspace = alloc_attend_workspace(cache, sequences)
+    elif workspace.get_device() != index:
+        raise ValueError("workspace is on another device")
+    i32 = torch.int32
+    how = _attend(table.data_ptr(), table.stride(0), width, page, _whole(begin, "begin", i32, index), 0 if first is None else _whole(first, "first", i32, index),
+                  sequences, longest, heads, window, dim ** -0.5 if scale is None else scale, cap,
+                  0 if slopes is None else _whole(slopes, "slopes", torch.float32, index), 0 if prefix is None else _whole(prefix, "prefix", i32, index))
+    _call("lc_cache_attend", index, cache._at, _one_plane(q.data_ptr(), strides[0], strides[1]), _one_plane(out.data_ptr(), strides2[0], strides2[1]), kind, rows,
+          how, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _status(status, index))
+    return out

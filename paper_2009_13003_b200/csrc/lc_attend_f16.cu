@@ -1,0 +1,8 @@
+// The kernels of lc_attend_rows.cuh for queries of fp16.
+#include "lc_attend_rows.cuh"
+
+namespace lc {
+
+cudaError_t launch_attend_f16(const AttendArgs& a, int bits, cudaStream_t cs) { return bits == 4 ? launch_dim<4, 2>(a, cs) : launch_dim<8, 2>(a, cs); }
+
+}  // namespace lc
