@@ -492,8 +492,9 @@ int lc_cache_plan(const lc_pages* pages, const int32_t* tokens, uint32_t sequenc
  *            have (its keys and values count as zeros).
  * workspace  DEVICE, 256-byte aligned, lc_cache_attend_bytes (0 on bad arguments; the number of slots does not matter); two calls that overlap in time
  *            need two. scales of the cache are on 4 bytes here.
- * Scores, sums and what they are divided by are fp32. Rows of bf16 and of fp16 round probabilities to 8 and 11 bits or more, and may round keys and
- * values to their type, as lc_cache_read does; fp32 rounds neither. An Inf or NaN that a row does not see changes no bit of it. The same inputs give
+ * Scores, sums and what they are divided by are fp32. Rows of bf16 and of fp16 round probabilities to 8 and 11 bits or more (fp16: those
+ * below 2^-21 of a row's largest to multiples of 2^-31 of it), and may round keys and values to their type, numbers beyond it to its largest; fp32 rounds
+ * neither. An Inf or NaN that a row does not see changes no bit of it. The same inputs give
  * the same bits.
  */
 typedef struct lc_attend {

@@ -6,6 +6,9 @@ namespace {
 
 uint64_t flat_bytes(uint64_t sequences) { return (8 * (sequences + 1) + 255) / 256 * 256; }
 
+// Queries of a sequence for one head of the cache up to which the kernel for few rows takes it.
+constexpr uint32_t kFewQueries = 64;
+
 // A cache that can be attended to, whatever the number of its slots.
 bool shape_ok(const lc_cache* cache) {
   if (!cache || cache->planes != 2 || cache->dim > kAttendDim) return false;
@@ -22,7 +25,7 @@ using namespace lc;
 extern "C" {
 
 uint64_t lc_cache_attend_bytes(const lc_cache* cache, uint32_t sequences) {
-  return shape_ok(cache) && sequences < (1u << 31) ? flat_bytes(sequences) + 2 * kMaxParts * kPartBytes : 0;
+  return shape_ok(cache) && sequences < (1u << 31) ? 2 * flat_bytes(sequences) + 2 * (kMaxParts * kPartBytes + kTileCtas * kTilePartBytes) : 0;
 }
 
 int lc_cache_attend(const lc_cache* cache, const lc_rows* q, const lc_rows* out, int type, uint64_t rows, const lc_attend* how, void* workspace,
@@ -84,13 +87,24 @@ int lc_cache_attend(const lc_cache* cache, const lc_rows* q, const lc_rows* out,
   a.cap = how->cap;
   a.status = status;
   a.flat = static_cast<unsigned long long*>(workspace);
-  a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + flat_bytes(how->sequences));
+  a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + 2 * flat_bytes(how->sequences));
   a.by_page = FastDiv(how->page);
   a.by_shared = FastDiv(a.shared);
   const uint32_t piece = a.row_bytes & (0u - a.row_bytes);
   a.by_pieces = FastDiv(a.row_bytes / (piece > 16 ? 16 : piece));
   const int bits = (int)cache->bits;
-  const cudaError_t e = type == LC_TYPE_BF16 ? launch_attend_bf16(a, bits, cs) : type == LC_TYPE_F16 ? launch_attend_f16(a, bits, cs) : launch_attend_f32(a, bits, cs);
+  cudaError_t e = cudaSuccess;
+  const bool tiles = type != LC_TYPE_F32 && a.dim <= kTileDim && (uint64_t)a.most * a.shared > kFewQueries;
+  if (tiles) a.longest = kFewQueries / a.shared;
+  if (a.longest > 0) e = type == LC_TYPE_BF16 ? launch_attend_bf16(a, bits, cs) : type == LC_TYPE_F16 ? launch_attend_f16(a, bits, cs) : launch_attend_f32(a, bits, cs);
+  if (tiles && e == cudaSuccess) {
+    AttendArgs b = a;
+    b.shortest = a.longest + 1;
+    b.longest = a.most;
+    b.flat = reinterpret_cast<unsigned long long*>(reinterpret_cast<uint8_t*>(a.flat) + flat_bytes(how->sequences));
+    b.parts = a.parts + 2 * kMaxParts * kPartBytes / 4;
+    e = launch_attend_tiles(b, bits, type, a.longest > 0, cs);
+  }
   return e == cudaSuccess ? LC_OK : LC_ERR_CUDA;
 }
 

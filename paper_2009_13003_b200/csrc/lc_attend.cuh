@@ -44,6 +44,7 @@ struct Sequence {
 __device__ __forceinline__ uint32_t first_seen(const AttendArgs& A, uint32_t position) {  // ignoring the prefix
   return A.window && position >= A.window ? position - A.window + 1 : 0;
 }
+template <uint32_t kTile = kKeyTile>
 __device__ __forceinline__ Sequence sequence_of(const AttendArgs& A, uint32_t s, bool report) {
   Sequence q = {};
   const int64_t begin = A.begin[s], n = (int64_t)A.begin[s + 1] - begin;
@@ -60,9 +61,9 @@ __device__ __forceinline__ Sequence sequence_of(const AttendArgs& A, uint32_t s,
   q.length = (uint32_t)(first + n);
   const int32_t prefix = A.prefix ? A.prefix[s] : 0;
   q.prefix = prefix <= 0 ? 0 : min((uint32_t)prefix, q.length);
-  q.ahead = (q.prefix + kKeyTile - 1) / kKeyTile;
-  q.from = max(q.ahead, first_seen(A, q.first) / kKeyTile);
-  q.tiles = q.ahead + max((q.length + kKeyTile - 1) / kKeyTile, q.from) - q.from;
+  q.ahead = (q.prefix + kTile - 1) / kTile;
+  q.from = max(q.ahead, first_seen(A, q.first) / kTile);
+  q.tiles = q.ahead + max((q.length + kTile - 1) / kTile, q.from) - q.from;
   return q;
 }
 __device__ __forceinline__ uint32_t blocks_of(const AttendArgs& A, const Sequence& q, uint32_t columns) {
@@ -84,6 +85,13 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 constexpr uint64_t kPartBytes = 4ull * (kMaxColumns * 128 + 2 * kMaxColumns);  // of a partial result: 32 queries of 128 values, or 16 of 256
 
+constexpr uint32_t kTileCtas = 160;     // CTAs of the kernel for many rows, at most: one on each SM
+constexpr uint32_t kTileRows = 256;     // queries of its blocks
+constexpr uint32_t kTileDim = 128;      // longest rows that it takes
+constexpr uint64_t kTilePartBytes = 4ull * kTileRows * (kTileDim + 2);
+
+// The kernel for sequences of many rows (lc_attend_tiles.cu): queries of bf16 or fp16. overlap: behind a launch of the same call.
+cudaError_t launch_attend_tiles(const AttendArgs& a, int bits, int type, bool overlap, cudaStream_t cs);
 cudaError_t launch_attend_bf16(const AttendArgs& a, int bits, cudaStream_t cs);
 cudaError_t launch_attend_f16(const AttendArgs& a, int bits, cudaStream_t cs);
 cudaError_t launch_attend_f32(const AttendArgs& a, int bits, cudaStream_t cs);

@@ -664,7 +664,7 @@ cudaError_t launch(const AttendArgs& a, cudaStream_t cs) {
 
 template <int kBits, int NB, int kParts>
 cudaError_t launch_columns(const AttendArgs& a, cudaStream_t cs) {
-  const uint64_t columns = (uint64_t)a.most * a.shared;
+  const uint64_t columns = (uint64_t)a.longest * a.shared;
   if (columns <= 8) return launch<kBits, NB, 1, kParts>(a, cs);
   if constexpr (NB == 8) return launch<kBits, NB, 2, kParts>(a, cs);
   else {

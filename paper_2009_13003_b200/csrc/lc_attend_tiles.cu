@@ -1,0 +1,790 @@
+// Attention to a quantised cache for sequences of many new rows: the products on the tensor cores' own memory (tcgen05).
+//
+// A CTA takes blocks of 256 queries of one head of the cache (its tokens, times the heads that share it) as two tiles of 128, and goes through the keys
+// 128 at a time with a running maximum and sum of each query. Its warps have one task each: four read codes, turn them into numbers of the queries' type
+// and store them as operands (keys and values in one layout, rows of 64 values with the 128-byte swizzle: keys are read along a row, values across);
+// one thread issues the products; a warpgroup for each tile takes the scores out of tensor memory, a query a thread, and puts the probabilities back
+// there, over the scores, as the first operand of the product with the values. While one tile's scores are in the warps the products of the other run.
+// The sums of the values stay in tensor memory; they are scaled down only where a maximum rises by more than a factor of 2^kSlack.
+//
+// What a code stands for is rounded to the type once. bf16: code / 64 is exact (see lc_attend_rows.cuh) and times the scale rounded; the 64 comes in
+// with the scores' factor, so that nothing overflows. fp16: keys in units of a power of two of their tile, so that no magnitude of them is out of the
+// type; values as lc_cache_read gives them, but numbers beyond the type as its largest. A value of NaN enters as 0, or rows that do not see it would
+// get 0 * NaN; rows that do get their NaN at the end.
+//
+// Blocks differ in how many keys they see. Each weighs about as many as it does and a block's own cost; a CTA gets an equal share of the weight, and
+// of a block that it shares with its neighbours the tiles in proportion. Those parts are joined by a second launch, in a fixed order.
+#include "lc_attend.cuh"
+
+namespace lc {
+namespace {
+
+constexpr uint32_t kRows = 128, kKeys = 128;            // of a tile of queries, of keys
+constexpr uint32_t kSoftmaxWarps = 8, kReadWarps = 4;   // then the warp that issues
+constexpr uint32_t kThreads = 32 * (kSoftmaxWarps + kReadWarps + 1), kReaders = 32 * kReadWarps;
+constexpr uint32_t kStages = 2;
+constexpr uint32_t kMemo = 4;                           // tiles whose exponents and flags are kept: the scores of a tile are done before the third behind it is read
+constexpr float kSlack = 8.0f;
+constexpr long long kWaitCycles = 4ll << 30;            // how long a barrier is waited for before the kernel gives up: some two seconds
+constexpr uint32_t kBlockCost = 192;                    // what a block costs beyond its keys, in keys
+
+// ---- barriers and tensor memory -----------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+__device__ __forceinline__ void barrier_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// Waits for the end of the barrier's phase of that parity. False, and `dead` set for all, if it does not come within some seconds.
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, volatile uint32_t* dead) {
+  long long since = 0;
+  for (;;) {
+    uint32_t done;
+    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    if (done) return true;
+    const long long now = clock64();
+    if (since == 0) since = now;
+    if (now - since > kWaitCycles) *dead = 1;
+    if (*dead) return false;
+  }
+}
+// The same for a warp as a whole: its threads go on together or not at all.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* dead) { return __all_sync(0xFFFFFFFFu, barrier_wait(bar, parity, dead)); }
+__device__ __forceinline__ void order_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void order_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void commit_to(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// d (tensor memory) = or += a * b; a in shared or tensor memory.
+__device__ __forceinline__ void product(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
+  asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void product_of_tensor(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add) {
+  asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d), "r"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
+}
+// An operand in rows of 128 bytes, swizzled, in groups of eight rows: `lead` bytes from one run of 64 values to the next where it is read across the rows.
+__device__ __forceinline__ uint64_t operand_at(uint32_t address, uint32_t lead) {
+  return (uint64_t)(address >> 4 & 0x3FFF) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// The product's shape and types: fp32 sums, m = 128.
+__device__ __forceinline__ uint32_t product_kind(bool bf16, uint32_t n, bool across) {
+  return 1u << 4 | (uint32_t)bf16 << 7 | (uint32_t)bf16 << 10 | (uint32_t)across << 16 | (n >> 3) << 17 | (kRows >> 4) << 24;
+}
+
+// 32 columns of the 32 lanes of a warp, a lane a thread.
+__device__ __forceinline__ void tensor_load(uint32_t at, float (&x)[32]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+               : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]), "=f"(x[8]), "=f"(x[9]), "=f"(x[10]), "=f"(x[11]), "=f"(x[12]),
+                 "=f"(x[13]), "=f"(x[14]), "=f"(x[15]), "=f"(x[16]), "=f"(x[17]), "=f"(x[18]), "=f"(x[19]), "=f"(x[20]), "=f"(x[21]), "=f"(x[22]), "=f"(x[23]), "=f"(x[24]),
+                 "=f"(x[25]), "=f"(x[26]), "=f"(x[27]), "=f"(x[28]), "=f"(x[29]), "=f"(x[30]), "=f"(x[31])
+               : "r"(at));
+}
+__device__ __forceinline__ void tensor_store(uint32_t at, const float (&x)[32]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"f"(x[0]),
+               "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]), "f"(x[8]), "f"(x[9]), "f"(x[10]), "f"(x[11]), "f"(x[12]), "f"(x[13]), "f"(x[14]), "f"(x[15]),
+               "f"(x[16]), "f"(x[17]), "f"(x[18]), "f"(x[19]), "f"(x[20]), "f"(x[21]), "f"(x[22]), "f"(x[23]), "f"(x[24]), "f"(x[25]), "f"(x[26]), "f"(x[27]), "f"(x[28]), "f"(x[29]),
+               "f"(x[30]), "f"(x[31]), "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t (&x)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]),
+               "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]), "r"(x[9]), "r"(x[10]), "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15]), "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ void tensor_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tensor_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// What generic stores have put into shared memory is there for the products that follow.
+__device__ __forceinline__ void order_for_products() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+template <bool kBf16>
+__device__ __forceinline__ uint32_t rounded(float low, float high) {
+  uint32_t r;
+  if constexpr (kBf16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(high), "f"(low));
+  else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(high), "f"(low));
+  return r;
+}
+
+// ---- what weighs how much -----------------------------------------------------------------------------------------
+// The blocks of a sequence weigh prefix + min(base + step * b, most), each once for every head of the cache; see above.
+struct Weights {
+  uint64_t base, most;
+  uint32_t step, prefix, blocks, crossing;  // crossing: blocks ahead of it weigh less than `most`
+};
+__device__ __forceinline__ Weights weights_of(const AttendArgs& A, const Sequence& q) {
+  Weights w;
+  w.blocks = blocks_of(A, q, kTileRows);
+  w.step = A.shared < kTileRows ? kTileRows / A.shared : 1;
+  w.base = (uint64_t)q.first + w.step + kKeys / 2 + kBlockCost;
+  w.prefix = A.window ? q.prefix : 0;
+  w.most = A.window ? (uint64_t)A.window + w.step + kKeys + kBlockCost : 1ull << 62;
+  w.crossing = w.most <= w.base ? 0 : (uint32_t)min((uint64_t)w.blocks, (w.most - w.base + w.step - 1) / w.step);
+  return w;
+}
+__device__ __forceinline__ uint64_t weight_of(const Weights& w, uint32_t b) { return w.prefix + (b < w.crossing ? w.base + (uint64_t)w.step * b : w.most); }
+__device__ __forceinline__ uint64_t weight_ahead(const Weights& w, uint32_t b) {  // of the blocks ahead of b
+  const uint64_t n = min(b, w.crossing);
+  return (uint64_t)w.prefix * b + n * w.base + w.step * (n * (n - 1) / 2) + (b > w.crossing ? (b - w.crossing) * w.most : 0);
+}
+// A block that some weight falls into.
+struct Place {
+  uint32_t block, head;
+  uint64_t offset, weight;  // within the block; the block's
+};
+__device__ __forceinline__ Place place_of(const AttendArgs& A, const Weights& w, uint64_t rest) {
+  uint32_t lo = 0, hi = w.blocks;  // the last block at or ahead of it
+  while (hi - lo > 1) {
+    const uint32_t mid = (lo + hi) / 2;
+    if (weight_ahead(w, mid) * A.heads <= rest) lo = mid;
+    else hi = mid;
+  }
+  Place p;
+  p.block = lo;
+  p.weight = weight_of(w, lo);
+  rest -= weight_ahead(w, lo) * A.heads;
+  p.head = (uint32_t)(rest / p.weight);
+  p.offset = rest - p.head * p.weight;
+  return p;
+}
+// The tiles of keys that a block sees, numbered from 0: those of the prefix, then the others.
+struct Tiles {
+  uint32_t low, high;    // positions of its first and last query
+  uint32_t ahead, from, count;
+  __device__ __forceinline__ uint32_t key(uint32_t j) const { return (j < ahead ? j : from + j - ahead) * kKeys; }
+};
+__device__ __forceinline__ Tiles tiles_of(const AttendArgs& A, const Sequence& q, uint32_t block) {
+  Tiles t;
+  t.low = q.first + A.by_shared.div(block * kTileRows);
+  t.high = q.first + min(A.by_shared.div(block * kTileRows + kTileRows - 1), q.rows - 1);
+  t.ahead = q.ahead;
+  t.from = max(q.ahead, first_seen(A, t.low) / kKeys);
+  t.count = q.ahead + max(t.high / kKeys + 1, t.from) - t.from;
+  return t;
+}
+__device__ __forceinline__ uint32_t tile_at(uint64_t offset, uint32_t tiles, uint64_t weight) { return offset >= weight ? tiles : (uint32_t)(offset * tiles / weight); }
+__device__ __forceinline__ uint64_t share_of(uint64_t all, uint32_t ctas) { return max((all + ctas - 1) / ctas, (uint64_t)(2 * kKeys)); }
+
+// ---- the kernel ---------------------------------------------------------------------------------------------------
+template <uint32_t DP>
+struct Layout {
+  static constexpr uint32_t kRuns = DP / 64;                         // of 64 values
+  static constexpr uint32_t kQueries = kRuns * kRows * 128;          // bytes of a tile of queries
+  static constexpr uint32_t kOperand = kRuns * kKeys * 128;          // of a tile of keys or values
+  static constexpr uint32_t kWhole = 2 * kQueries + 2 * kStages * kOperand + 1024;
+  static constexpr uint32_t kScoresAt = 0, kSumsAt = 2 * kKeys;      // columns of tensor memory; the second tile's kKeys and DP columns behind
+};
+
+struct Shared {
+  unsigned long long full_k[kStages], empty_k[kStages], full_v[kStages], empty_v[kStages], scores[2], weights[2], sums[2];  // barriers
+  unsigned long long scan[kThreads / 32], found_base;
+  unsigned long long places[2][kKeys];  // slot * heads + head of a tile's keys; ~0: none
+  uint32_t found, tensor, dead;
+  uint32_t most_scale[kMemo][kReadWarps];
+  uint32_t flags[kMemo][kReadWarps];  // whether a scale of the tile's values is no number
+};
+
+template <int kBits, uint32_t DP, bool kBf16>
+struct Kernel {
+  using L = Layout<DP>;
+  using T = typename TypeOf<kBf16 ? LC_TYPE_BF16 : LC_TYPE_F16>::T;
+  // fp16 weights are held 2^7 times as large, up to 2^(7 + kSlack): next to its smallest numbers the type has few bits
+  static constexpr float kLift = kBf16 ? 0.0f : 7.0f;
+  static constexpr uint32_t kUnits = DP * kBits / 8 / 16;  // of 16 bytes of a row's codes, at most
+
+  // A block's queries as operands. A negative scale goes to their signs.
+  static __device__ __forceinline__ void load_queries(const AttendArgs& A, const Sequence& q, uint32_t block, uint32_t head, uint8_t* queries) {
+    const uint32_t flip = A.scale < 0.0f ? 0x80008000u : 0u;
+    const bool whole = A.dim % 8 == 0 && ((reinterpret_cast<uintptr_t>(A.q) / 2 | A.q_row | A.q_head) & 7) == 0;
+    for (uint32_t i = threadIdx.x; i < kTileRows * (DP / 8); i += kThreads) {
+      const uint32_t row = i / (DP / 8), c = i % (DP / 8), r = block * kTileRows + row, token = A.by_shared.div(r);
+      uint32_t w[4] = {0, 0, 0, 0};
+      if (token < q.rows && c * 8 < A.dim) {
+        const unsigned short* p = static_cast<const unsigned short*>(A.q) + (uint64_t)(q.row + token) * A.q_row + (uint64_t)(head * A.shared + (r - token * A.shared)) * A.q_head + c * 8;
+        if (whole) {
+          const uint4 x = *reinterpret_cast<const uint4*>(p);
+          w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+        } else {
+          for (uint32_t e = 0; e < 8; ++e)
+            if (c * 8 + e < A.dim) w[e / 2] |= (uint32_t)p[e] << (16 * (e & 1));
+        }
+      }
+      const uint32_t tile = row / kRows, at = row % kRows;
+      *reinterpret_cast<uint4*>(queries + tile * L::kQueries + (c / 8) * (kRows * 128) + at * 128 + (((c & 7) ^ (at & 7)) << 4)) =
+          make_uint4(w[0] ^ flip, w[1] ^ flip, w[2] ^ flip, w[3] ^ flip);
+    }
+  }
+
+  // The codes and scales of a thread's units of a tile: unit u of the tile is 16 bytes (or what is left of the row) of key u / units.
+  struct Codes {
+    uint4 w[kUnits];
+    unsigned short scale[kUnits];
+  };
+  static __device__ __forceinline__ void read_codes(const AttendArgs& A, const unsigned long long* places, bool values, uint32_t reader, Codes& c) {
+    const uint32_t units = A.by_pieces.d;
+    const uint8_t* codes = A.codes + (values ? A.plane_codes : 0);
+    const unsigned short* scales = A.scales + (values ? A.plane_scales : 0);
+    const uint32_t group = A.per_group * (kBits == 8 ? 2 : 1);  // units of a group
+#pragma unroll
+    for (uint32_t i = 0; i < kUnits; ++i) {
+      c.w[i] = make_uint4(0, 0, 0, 0);
+      c.scale[i] = 0;
+      if (i >= units) continue;
+      const uint32_t u = reader + i * kReaders, row = A.by_pieces.div(u), part = u - row * units;
+      const unsigned long long place = places[row];
+      if (place == ~0ull) continue;
+      const uint8_t* p = codes + place * A.row_bytes + part * 16;
+      if ((A.row_bytes & 15) == 0) {
+        c.w[i] = __ldg(reinterpret_cast<const uint4*>(p));
+      } else {
+        const uint32_t* x = reinterpret_cast<const uint32_t*>(p);
+        const uint32_t left = (A.row_bytes - part * 16) / 4;
+        c.w[i].x = __ldg(x);
+        if (left > 1) c.w[i].y = __ldg(x + 1);
+        if (left > 2) c.w[i].z = __ldg(x + 2);
+        if (left > 3) c.w[i].w = __ldg(x + 3);
+      }
+      c.scale[i] = __ldg(scales + place * A.groups + part / group);
+    }
+  }
+  // Four pairs of numbers from eight codes. scale: of bf16 two of it, of fp16 a float's bits.
+  static __device__ __forceinline__ uint4 numbers(uint32_t a, uint32_t b, uint32_t scale) {
+    uint32_t r[4];
+    if constexpr (kBf16) {
+      constexpr uint32_t kLow = 0x7F007F00u, kHigh = 0x7D007D00u, minus = kBits == 4 ? 0xBE00BE00u : 0xC000C000u;  // 2^127, 2^123; -2^-3, -2
+      uint32_t x[4], times[4] = {kLow, kLow, kLow, kLow};
+      if constexpr (kBits == 4) {
+        x[0] = a & 0x000F000Fu, x[1] = a & 0x00F000F0u, x[2] = a >> 8 & 0x000F000Fu, x[3] = a >> 8 & 0x00F000F0u;
+        times[1] = times[3] = kHigh;
+      } else {
+        x[0] = __byte_perm(a, 0, 0x4140), x[1] = __byte_perm(a, 0, 0x4342), x[2] = __byte_perm(b, 0, 0x4140), x[3] = __byte_perm(b, 0, 0x4342);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r[e]) : "r"(x[e]), "r"(times[e]), "r"(minus));
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r[e]) : "r"(r[e]), "r"(scale));
+      }
+    } else {
+      float v[8];
+      values_in_row<kBits, 8>(make_uint2(a, b), __uint_as_float(scale), v);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r[e]) : "f"(v[2 * e + 1]), "f"(v[2 * e]));
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+  }
+  // exponent: what the scales are multiplied by (fp16). values: scales that are no numbers count as 0.
+  static __device__ __forceinline__ void store_numbers(const AttendArgs& A, const Codes& c, bool values, float exponent, uint32_t reader, uint8_t* operand) {
+    const uint32_t units = A.by_pieces.d;
+#pragma unroll
+    for (uint32_t i = 0; i < kUnits; ++i) {
+      if (i >= units) continue;
+      const uint32_t u = reader + i * kReaders, row = A.by_pieces.div(u), part = u - row * units;
+      uint32_t s = c.scale[i];
+      if (values && (s & 0x7F80u) == 0x7F80u) s = 0;
+      s = kBf16 ? s | s << 16 : __float_as_uint(__uint_as_float(s << 16) * exponent);
+      const uint32_t w[4] = {c.w[i].x, c.w[i].y, c.w[i].z, c.w[i].w};
+      uint8_t* to = operand + row * 128;
+#pragma unroll
+      for (uint32_t k = 0; k < 16 / kBits; ++k) {  // 8 bits: two runs of eight values, 4 bits: four
+        const uint32_t n = part * (16 / kBits) + k;
+        *reinterpret_cast<uint4*>(to + (n / 8) * (kKeys * 128) + (((n & 7) ^ (row & 7)) << 4)) = kBits == 8 ? numbers(w[2 * k], w[2 * k + 1], s) : numbers(w[k], 0, s);
+      }
+    }
+  }
+  static __device__ __forceinline__ unsigned long long look_up(const AttendArgs& A, const Sequence& q, uint32_t s, uint32_t head, uint32_t key) {
+    if (key >= q.length) return ~0ull;
+    const uint32_t page = A.by_page.div(key);
+    const int32_t number = __ldg(A.table + s * A.table_stride + page);
+    const int64_t slot = (int64_t)number * A.by_page.d + (key - page * A.by_page.d);
+    if (number < 0 || slot >= (int64_t)A.slots) {
+      if (A.status) set_status(A.status, LC_ERR_INDEX);
+      return ~0ull;
+    }
+    return (unsigned long long)slot * A.heads + head;
+  }
+
+  static __device__ __forceinline__ void run(const AttendArgs& A) {
+    extern __shared__ uint8_t raw[];
+    __shared__ Shared S;
+    uint8_t* const smem = raw + (1024 - (shared_address(raw) & 1023)) % 1024;
+    uint8_t* const queries = smem;
+    uint8_t* const keys = smem + 2 * L::kQueries;
+    uint8_t* const values = keys + kStages * L::kOperand;
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    begin_next();
+
+    if (threadIdx.x == 0) {
+      S.dead = 0;
+      for (uint32_t i = 0; i < kStages; ++i) {
+        barrier_init(shared_address(&S.full_k[i]), kReaders);
+        barrier_init(shared_address(&S.empty_k[i]), 1);
+        barrier_init(shared_address(&S.full_v[i]), kReaders);
+        barrier_init(shared_address(&S.empty_v[i]), 1);
+      }
+      for (uint32_t t = 0; t < 2; ++t) {
+        barrier_init(shared_address(&S.scores[t]), 1);
+        barrier_init(shared_address(&S.weights[t]), kRows);
+        barrier_init(shared_address(&S.sums[t]), 1);
+      }
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+
+    // this CTA's share of the weight
+    unsigned long long all = 0;
+    for (uint32_t s = threadIdx.x; s < A.sequences; s += kThreads) {
+      const Sequence q = sequence_of<kKeys>(A, s, blockIdx.x == 0);
+      if (q.rows) {
+        const Weights w = weights_of(A, q);
+        all += weight_ahead(w, w.blocks) * A.heads;
+      }
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, d);
+    if (lane == 0) S.scan[warp] = all;
+    __syncthreads();
+    all = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < kThreads / 32; ++w) all += S.scan[w];
+    const unsigned long long share = share_of(all, gridDim.x), from = blockIdx.x * share, to = min(from + share, all);
+    if (blockIdx.x == 0 || from < all) {
+      unsigned long long base = 0;
+      for (uint32_t s0 = 0; s0 < A.sequences; s0 += kThreads) {
+        const uint32_t s = s0 + threadIdx.x;
+        unsigned long long mine = 0;
+        if (s < A.sequences) {
+          const Sequence q = sequence_of<kKeys>(A, s, false);
+          if (q.rows) {
+            const Weights w = weights_of(A, q);
+            mine = weight_ahead(w, w.blocks) * A.heads;
+          }
+        }
+        unsigned long long upto = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const unsigned long long x = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+          if (lane >= (uint32_t)d) upto += x;
+        }
+        __syncthreads();
+        if (lane == 31) S.scan[warp] = upto;
+        __syncthreads();
+        unsigned long long ahead = base + upto - mine;
+#pragma unroll
+        for (uint32_t w = 0; w < kThreads / 32; ++w) {
+          if (w < warp) ahead += S.scan[w];
+          base += S.scan[w];
+        }
+        if (blockIdx.x == 0 && s < A.sequences) A.flat[s] = ahead;  // for the launch that joins
+        if (from >= ahead && from < ahead + mine) {
+          S.found = s;
+          S.found_base = ahead;
+        }
+        if (blockIdx.x != 0 && base > from) break;
+      }
+      if (blockIdx.x == 0 && threadIdx.x == 0) A.flat[A.sequences] = all;
+    }
+    __syncthreads();
+    if (from >= to) {
+      wait_previous();
+      return;
+    }
+    if (warp == kSoftmaxWarps + kReadWarps) {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_address(&S.tensor)), "n"(512) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+      order_before();
+    }
+
+    uint32_t s = S.found;
+    Sequence q = sequence_of<kKeys>(A, s, false);
+    Weights W = weights_of(A, q);
+    Place P = place_of(A, W, from - S.found_base);
+    const float scale = fabsf(A.scale) * (kBf16 ? 64.0f : 1.0f);
+    uint32_t done = 0;  // tiles of keys so far: what the barriers' phases go by
+    volatile uint32_t* dead = &S.dead;
+
+    for (unsigned long long at = from; at < to;) {
+      const uint64_t upto = min((uint64_t)(to - at) + P.offset, P.weight);
+      const Tiles tiles = tiles_of(A, q, P.block);
+      const uint32_t j0 = tile_at(P.offset, tiles.count, P.weight), j1 = tile_at(upto, tiles.count, P.weight), n = j1 - j0;
+      const uint32_t block = P.block, head = P.head;
+      if (n > 0) {
+        load_queries(A, q, block, head, queries);
+        order_for_products();
+        __syncthreads();
+        order_after();
+        const uint32_t tensor = S.tensor;
+
+        if (warp < kSoftmaxWarps) {
+          // ---- scores to probabilities: a query a thread
+          const uint32_t t = warp / 4, row = threadIdx.x % kRows, r = block * kTileRows + t * kRows + row, token = A.by_shared.div(r), in_group = r - token * A.shared;
+          const uint32_t lanes = tensor + ((warp & 3) * 32 << 16), scores = lanes + L::kScoresAt + t * kKeys, sums = lanes + L::kSumsAt + t * DP;
+          const uint32_t position = q.first + min(token, q.rows - 1);
+          const float slope = A.slopes ? A.slopes[head * A.shared + in_group] * kLog2e : 0.0f;
+          const float cap_out = A.cap * kLog2e;
+          // positions of this warp's first and last query
+          const uint32_t low = __shfl_sync(0xFFFFFFFFu, position, 0), high = __shfl_sync(0xFFFFFFFFu, position, 31);
+          float m = -INFINITY, l = 0.0f;
+          uint32_t broken = 0;  // groups whose value is no number for this query
+          bool good = false;  // all tiles are through
+          for (uint32_t i = 0; i < n; ++i) {
+            const uint32_t number = done + i, memo = number % kMemo, key = tiles.key(j0 + i);
+            if (!warp_wait(shared_address(&S.full_v[number % kStages]), number / kStages & 1, dead)) break;
+            if (!warp_wait(shared_address(&S.scores[t]), number & 1, dead)) break;
+            order_after();
+            float unit = 1.0f;  // of the tile's keys
+            if constexpr (!kBf16) unit = unit_of(S, memo);
+            const float factor = scale * unit * kLog2e, cap_in = A.cap > 0.0f ? 2.0f * factor / A.cap : 0.0f;
+            const bool full = key + kKeys - 1 <= low && (A.window == 0 || high - key < A.window);
+            auto visible = [&](uint32_t at_key) { return (at_key <= position && (A.window == 0 || position - at_key < A.window)) || at_key < q.prefix; };
+            auto capped = [&](float x) { return A.cap > 0.0f ? fmaf(-2.0f * cap_out, reciprocal(1.0f + exp2_fast(x * cap_in)), cap_out) : x * factor; };
+            auto biased = [&](float y, uint32_t at_key) { return fmaf(-slope, fabsf((float)(int32_t)(position - at_key)), y); };
+            float top = -INFINITY;
+#pragma unroll 1
+            for (uint32_t c = 0; c < kKeys; c += 32) {
+              float x[32];
+              tensor_load(scores + c, x);
+              tensor_loaded();
+              if (A.slopes) {
+#pragma unroll
+                for (uint32_t e = 0; e < 32; ++e) x[e] = biased(capped(x[e]), key + c + e);
+              }
+              if (!full) {
+#pragma unroll
+                for (uint32_t e = 0; e < 32; ++e)
+                  if (!visible(key + c + e)) x[e] = -INFINITY;
+              }
+#pragma unroll
+              for (uint32_t e = 0; e < 32; ++e) top = fmaxf(top, x[e]);
+            }
+            if (!A.slopes && top != -INFINITY) top = capped(top);  // both grow with the product
+            const bool rises = top > m + kSlack;
+            if (__any_sync(0xFFFFFFFFu, rises)) {
+              const float now = rises ? top : m, down = rises ? exp2_fast(m - now) : 1.0f;
+              if (i > 0) {
+                if (!warp_wait(shared_address(&S.sums[t]), (number - 1) & 1, dead)) break;
+                order_after();
+#pragma unroll 1
+                for (uint32_t c = 0; c < DP; c += 32) {
+                  float x[32];
+                  tensor_load(sums + c, x);
+                  tensor_loaded();
+#pragma unroll
+                  for (uint32_t e = 0; e < 32; ++e) x[e] *= down;
+                  tensor_store(sums + c, x);
+                }
+              }
+              m = now;
+              l *= down;
+            }
+            const float base = (m == -INFINITY ? 0.0f : m) - kLift;
+#pragma unroll 1
+            for (uint32_t c = 0; c < kKeys; c += 32) {
+              float x[32];
+              tensor_load(scores + c, x);
+              tensor_loaded();
+              if (A.cap > 0.0f || A.slopes) {
+#pragma unroll
+                for (uint32_t e = 0; e < 32; ++e) x[e] = biased(capped(x[e]), key + c + e) - base;
+              } else {
+#pragma unroll
+                for (uint32_t e = 0; e < 32; ++e) x[e] = fmaf(x[e], factor, -base);
+              }
+              if (!full) {
+#pragma unroll
+                for (uint32_t e = 0; e < 32; ++e)
+                  if (!visible(key + c + e)) x[e] = -INFINITY;
+              }
+              uint32_t p[16];
+#pragma unroll
+              for (uint32_t e = 0; e < 32; e += 2) {
+                x[e] = exp2_fast(x[e]), x[e + 1] = exp2_fast(x[e + 1]);
+                l += x[e] + x[e + 1];
+                p[e / 2] = rounded<kBf16>(x[e], x[e + 1]);
+              }
+              tensor_store(scores + c / 2, p);
+            }
+            tensor_stored();
+            order_before();
+            barrier_arrive(shared_address(&S.weights[t]));
+            good = i + 1 == n;
+            uint32_t flags = 0;
+#pragma unroll
+            for (uint32_t w = 0; w < kReadWarps; ++w) flags |= S.flags[memo][w];
+            if (flags) {  // some value of the tile is no number: which of them this query sees
+              for (uint32_t k = 0; k < kKeys && key + k < q.length; ++k) {
+                const unsigned long long place = look_up(A, q, s, head, key + k);
+                if (place == ~0ull || !visible(key + k)) continue;
+                for (uint32_t g = 0; g < A.groups; ++g)
+                  if ((A.scales[A.plane_scales + place * A.groups + g] & 0x7F80u) == 0x7F80u) broken |= 1u << g;
+              }
+            }
+          }
+          if (good && warp_wait(shared_address(&S.sums[t]), (done + n - 1) & 1, dead)) {
+            order_after();
+            const bool whole = j0 == 0 && j1 == tiles.count, there = token < q.rows;
+            float* part = A.parts + (2ull * blockIdx.x + (at == from ? 0 : 1)) * (kTilePartBytes / 4);
+            T* out = static_cast<T*>(A.out) + (uint64_t)(q.row + min(token, q.rows - 1)) * A.out_row + (uint64_t)(head * A.shared + in_group) * A.out_head;
+            const bool aligned = ((reinterpret_cast<uintptr_t>(A.out) / 2 | A.out_row | A.out_head) & 7) == 0;
+            const float over = whole ? (kBf16 ? 64.0f : 1.0f) / l : 1.0f;
+            const uint32_t shift = 5 + (A.per_group > 1) + (A.per_group > 2);  // values of a group
+#pragma unroll 1
+            for (uint32_t c = 0; c < A.dim; c += 32) {
+              float x[32];
+              tensor_load(sums + c, x);
+              tensor_loaded();
+#pragma unroll
+              for (uint32_t e = 0; e < 32; ++e) x[e] *= over;
+              if (broken >> (c >> shift) & 1) {
+#pragma unroll
+                for (uint32_t e = 0; e < 32; ++e) x[e] = __uint_as_float(0x7FFFFFFFu);
+              }
+              if (!there) continue;
+              if (whole) {
+#pragma unroll
+                for (uint32_t e = 0; e < 32; e += 8) {
+                  const uint32_t w[4] = {rounded<kBf16>(x[e], x[e + 1]), rounded<kBf16>(x[e + 2], x[e + 3]), rounded<kBf16>(x[e + 4], x[e + 5]), rounded<kBf16>(x[e + 6], x[e + 7])};
+                  if (aligned && c + e + 8 <= A.dim) {
+                    *reinterpret_cast<uint4*>(out + c + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                  } else {
+#pragma unroll
+                    for (uint32_t k = 0; k < 8; ++k)
+                      if (c + e + k < A.dim) reinterpret_cast<unsigned short*>(out)[c + e + k] = (unsigned short)(w[k / 2] >> (16 * (k & 1)));
+                  }
+                }
+              } else {
+#pragma unroll
+                for (uint32_t e = 0; e < 32; e += 4)
+                  *reinterpret_cast<float4*>(part + ((c + e) / 4 * kTileRows + t * kRows + row) * 4) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+              }
+            }
+            if (!whole) {
+              part[kTileRows * kTileDim + t * kRows + row] = m;
+              part[kTileRows * (kTileDim + 1) + t * kRows + row] = l;
+            }
+          }
+        } else if (warp < kSoftmaxWarps + kReadWarps) {
+          // ---- codes to operands
+          const uint32_t reader = threadIdx.x - 32 * kSoftmaxWarps, mine = warp - kSoftmaxWarps;
+          auto meet = [&] { asm volatile("bar.sync 1, %0;" ::"n"(kReaders) : "memory"); };
+          auto look = [&](uint32_t i) { return i < n ? look_up(A, q, s, head, tiles.key(j0 + i) + reader) : ~0ull; };
+          Codes k, v;
+          meet();  // the places of the block before are read
+          S.places[0][reader] = look(0);
+          unsigned long long next = look(1);
+          meet();
+          read_codes(A, S.places[0], false, reader, k);
+          read_codes(A, S.places[0], true, reader, v);
+          bool good = true;
+          for (uint32_t i = 0; i < n; ++i) {
+            const uint32_t number = done + i, stage = number % kStages, turn = number / kStages, memo = number % kMemo;
+            S.places[(i + 1) & 1][reader] = next;
+            uint32_t most = 0, flag = 0;
+#pragma unroll
+            for (uint32_t x = 0; x < kUnits; ++x) {
+              if (!kBf16 && (k.scale[x] & 0x7F80u) != 0x7F80u) most = max(most, (uint32_t)k.scale[x]);
+              flag |= (v.scale[x] & 0x7F80u) == 0x7F80u;
+            }
+            if constexpr (!kBf16) {
+              most = __reduce_max_sync(0xFFFFFFFFu, most);
+              if (lane == 0) S.most_scale[memo][mine] = most;
+            }
+            flag = __any_sync(0xFFFFFFFFu, flag);
+            if (lane == 0) S.flags[memo][mine] = flag;
+            meet();
+            next = look(i + 2);
+            float down = 1.0f;
+            if constexpr (!kBf16) down = 1.0f / unit_of(S, memo);
+            if (good && turn > 0) good = barrier_wait(shared_address(&S.empty_k[stage]), (turn - 1) & 1, dead);
+            if (good) {
+              store_numbers(A, k, false, down, reader, keys + stage * L::kOperand);
+              order_for_products();
+              barrier_arrive(shared_address(&S.full_k[stage]));
+            }
+            if (i + 1 < n) read_codes(A, S.places[(i + 1) & 1], false, reader, k);
+            if (good && turn > 0) good = barrier_wait(shared_address(&S.empty_v[stage]), (turn - 1) & 1, dead);
+            if (good) {
+              store_numbers(A, v, true, 1.0f, reader, values + stage * L::kOperand);
+              order_for_products();
+              barrier_arrive(shared_address(&S.full_v[stage]));
+            }
+            if (i + 1 < n) read_codes(A, S.places[(i + 1) & 1], true, reader, v);
+          }
+        } else if (lane == 0) {
+          // ---- the products
+          const uint32_t steps = (A.dim + 15) / 16, scores_kind = product_kind(kBf16, kKeys, false), sums_kind = product_kind(kBf16, steps * 16, true);
+          auto multiply_keys = [&](uint32_t t, uint32_t stage) {
+            const uint32_t a = shared_address(queries + t * L::kQueries), b = shared_address(keys + stage * L::kOperand);
+            for (uint32_t x = 0; x < steps; ++x)
+              product(tensor + L::kScoresAt + t * kKeys, operand_at(a + (x / 4) * (kRows * 128) + (x % 4) * 32, 16), operand_at(b + (x / 4) * (kKeys * 128) + (x % 4) * 32, 16), scores_kind, x > 0);
+            commit_to(shared_address(&S.scores[t]));
+          };
+          auto multiply_values = [&](uint32_t t, uint32_t stage, bool add) {
+            const uint32_t b = shared_address(values + stage * L::kOperand);
+#pragma unroll
+            for (uint32_t x = 0; x < kKeys / 16; ++x)
+              product_of_tensor(tensor + L::kSumsAt + t * DP, tensor + L::kScoresAt + t * kKeys + x * 8, operand_at(b + x * 2048, kKeys * 128), sums_kind, add || x > 0);
+            commit_to(shared_address(&S.sums[t]));
+          };
+          bool good = barrier_wait(shared_address(&S.full_k[done % kStages]), done / kStages & 1, dead);
+          if (good) {
+            order_after();
+            multiply_keys(0, done % kStages);
+            multiply_keys(1, done % kStages);
+            commit_to(shared_address(&S.empty_k[done % kStages]));
+          }
+          for (uint32_t i = 0; i < n && good; ++i) {
+            const uint32_t number = done + i, stage = number % kStages, behind = (number + 1) % kStages;
+            good = barrier_wait(shared_address(&S.full_v[stage]), number / kStages & 1, dead);
+            for (uint32_t t = 0; t < 2 && good; ++t) {
+              good = barrier_wait(shared_address(&S.weights[t]), number & 1, dead);
+              if (!good) break;
+              order_after();
+              multiply_values(t, stage, i > 0);
+              if (t == 1) commit_to(shared_address(&S.empty_v[stage]));
+              if (i + 1 < n) {
+                if (t == 0) good = barrier_wait(shared_address(&S.full_k[behind]), (number + 1) / kStages & 1, dead);
+                if (!good) break;
+                order_after();
+                multiply_keys(t, behind);
+                if (t == 1) commit_to(shared_address(&S.empty_k[behind]));
+              }
+            }
+          }
+        }
+        __syncwarp();
+        order_before();
+        __syncthreads();  // the block is done: queries, places and tensor memory are free
+        order_after();
+        done += n;
+        if (*dead) break;  // the same for all threads: none sets it before the next block's queries are there
+      }
+      at += upto - P.offset;
+      if (at < to) {
+        P.offset = 0;
+        if (++P.head == A.heads) {
+          P.head = 0;
+          if (++P.block == W.blocks) {
+            do {
+              q = sequence_of<kKeys>(A, ++s, false);
+            } while (q.rows == 0);
+            W = weights_of(A, q);
+            P.block = 0;
+          }
+          P.weight = weight_of(W, P.block);
+        }
+      }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0 && S.dead && A.status) set_status(A.status, LC_ERR_TIMEOUT);
+    if (warp == kSoftmaxWarps + kReadWarps) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(S.tensor), "n"(512) : "memory");
+    wait_previous();
+  }
+
+  // fp16: the power of two that a tile's keys are in units of, from the largest of their scales.
+  static __device__ __forceinline__ float unit_of(const Shared& S, uint32_t memo) {
+    uint32_t most = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < kReadWarps; ++w) most = max(most, S.most_scale[memo][w]);
+    return most ? __uint_as_float(min(max(most << 16 & 0x7F800000u, 0x01000000u), 0x7E000000u)) : 1.0f;
+  }
+};
+
+template <int kBits, uint32_t DP, bool kBf16>
+__global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs A) {
+  Kernel<kBits, DP, kBf16>::run(A);
+}
+
+// Joins the parts of the blocks that CTAs share (see join_kernel of lc_attend_rows.cuh): a query a thread, blockIdx.y a run of 16 values.
+template <bool kBf16>
+__global__ void __launch_bounds__(kTileRows) join_tiles_kernel(AttendArgs A, uint32_t ctas) {
+  using T = typename TypeOf<kBf16 ? LC_TYPE_BF16 : LC_TYPE_F16>::T;
+  __shared__ uint32_t found;
+  wait_previous();
+  const unsigned long long all = A.flat[A.sequences], share = share_of(all, ctas), border = (blockIdx.x + 1) * share;
+  if (border >= all) return;
+  if (threadIdx.x < 32) {
+    uint32_t lo = 0, count = A.sequences;
+    while (count > 1) {
+      const uint32_t step = (count + 31) / 32, at = threadIdx.x * step;
+      const uint32_t n = __popc(__ballot_sync(0xFFFFFFFFu, at < count && A.flat[lo + at] <= border)) - 1;
+      lo += n * step;
+      count = min(step, count - n * step);
+    }
+    if (threadIdx.x == 0) found = lo;
+  }
+  __syncthreads();
+  const uint32_t s = found;
+  const Sequence q = sequence_of<kKeys>(A, s, false);
+  const Weights W = weights_of(A, q);
+  const Place P = place_of(A, W, border - A.flat[s]);
+  const unsigned long long begin = border - P.offset, end = begin + P.weight;
+  if (P.offset == 0 || begin + share < border) return;
+  const uint32_t first = blockIdx.x, last = (uint32_t)((end - 1) / share), r = P.block * kTileRows + threadIdx.x, token = A.by_shared.div(r);
+  if (token >= q.rows) return;
+  const Tiles tiles = tiles_of(A, q, P.block);
+  auto part_of = [&](uint32_t cta) -> const float* {  // null: no tile of the block is that CTA's
+    const unsigned long long from = cta * share, to = from + share;
+    const uint32_t j0 = tile_at(from > begin ? from - begin : 0, tiles.count, P.weight), j1 = tile_at(to - begin, tiles.count, P.weight);
+    return j0 == j1 || (j0 == 0 && j1 == tiles.count) ? nullptr : A.parts + (2ull * cta + (begin <= from ? 0 : 1)) * (kTilePartBytes / 4);
+  };
+  float most = -INFINITY, sum = 0.0f, v[16] = {};
+  uint32_t parts = 0;
+  for (uint32_t c = first; c <= last; ++c)
+    if (const float* p = part_of(c)) most = fmaxf(most, p[kTileRows * kTileDim + threadIdx.x]), ++parts;
+  if (parts == 0) return;  // one CTA has had them all
+  const uint32_t d0 = blockIdx.y * 16;
+  for (uint32_t c = first; c <= last; ++c) {
+    const float* p = part_of(c);
+    if (!p) continue;
+    const float m = p[kTileRows * kTileDim + threadIdx.x], down = m == most ? 1.0f : exp2_fast(m - most);
+    sum += p[kTileRows * (kTileDim + 1) + threadIdx.x] * down;
+#pragma unroll
+    for (uint32_t e = 0; e < 16; e += 4) {
+      if (d0 + e >= A.dim) break;
+      const float4 x = *reinterpret_cast<const float4*>(p + ((d0 + e) / 4 * kTileRows + threadIdx.x) * 4);
+      v[e] = fmaf(x.x, down, v[e]), v[e + 1] = fmaf(x.y, down, v[e + 1]), v[e + 2] = fmaf(x.z, down, v[e + 2]), v[e + 3] = fmaf(x.w, down, v[e + 3]);
+    }
+  }
+  T* out = static_cast<T*>(A.out) + (uint64_t)(q.row + token) * A.out_row + (uint64_t)(P.head * A.shared + (r - token * A.shared)) * A.out_head + d0;
+  const float over = (kBf16 ? 64.0f : 1.0f) / sum;
+#pragma unroll
+  for (uint32_t e = 0; e < 16; ++e)
+    if (d0 + e < A.dim) from_float(v[e] * over, out[e]);
+}
+
+template <int kBits, uint32_t DP, bool kBf16>
+cudaError_t launch(const AttendArgs& a, bool overlap, cudaStream_t cs) {
+  static int sms[kMaxDevices] = {};  // by device ordinal: 0 not looked at yet
+  const int dev = current_device_index();
+  if (dev < 0) return cudaErrorInvalidDevice;
+  auto kernel = attend_tiles_kernel<kBits, DP, kBf16>;
+  if (!sms[dev]) {
+    int n = 0;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Layout<DP>::kWhole);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return e;
+    sms[dev] = n;
+  }
+  const uint32_t ctas = (uint32_t)sms[dev] < kTileCtas ? (uint32_t)sms[dev] : kTileCtas;
+  cudaError_t e = launch_kernel(overlap, kernel, ctas, kThreads, Layout<DP>::kWhole, cs, a);
+  if (e != cudaSuccess || ctas < 2) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ctas - 1, (a.dim + 15) / 16);
+  cfg.blockDim = dim3(kTileRows);
+  cfg.stream = cs;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, join_tiles_kernel<kBf16>, a, ctas);
+}
+template <int kBits, bool kBf16>
+cudaError_t launch_dim(const AttendArgs& a, bool overlap, cudaStream_t cs) {
+  return a.dim <= 64 ? launch<kBits, 64, kBf16>(a, overlap, cs) : launch<kBits, 128, kBf16>(a, overlap, cs);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_tiles(const AttendArgs& args, int bits, int type, bool overlap, cudaStream_t cs) {
+  AttendArgs a = args;
+  a.by_pieces = FastDiv((a.row_bytes + 15) / 16);
+  if (type == LC_TYPE_BF16) return bits == 4 ? launch_dim<4, true>(a, overlap, cs) : launch_dim<8, true>(a, overlap, cs);
+  return bits == 4 ? launch_dim<4, false>(a, overlap, cs) : launch_dim<8, false>(a, overlap, cs);
+}
+
+}  // namespace lc

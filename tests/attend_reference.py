@@ -14,7 +14,7 @@ def attend(q, k, v, positions, scale, cap=0.0, slopes=None, window=0, prefix=0):
     at = torch.arange(length, device=q.device)
     away = positions[:, None] - at[None, :]
     seen = (away >= 0) & ((away < window) if window else True) | (at[None, :] < prefix)
-    out, size = torch.zeros_like(q), torch.zeros_like(q)
+    out, size, plain = torch.zeros_like(q), torch.zeros_like(q), torch.zeros_like(q)
     products, bias = torch.zeros(n, heads, dtype=torch.float64, device=q.device), torch.zeros(n, heads, dtype=torch.float64, device=q.device)
     for h in range(heads):
         kk, vv = k[:, h // shared], v[:, h // shared]
@@ -33,20 +33,22 @@ def attend(q, k, v, positions, scale, cap=0.0, slopes=None, window=0, prefix=0):
         hidden = lambda x: torch.where(seen.any(0)[:, None], x, 0.0)
         out[:, h] = (p @ hidden(vv)) / total
         size[:, h] = (p @ hidden(vv.abs())) / total
-    return out, size, products, bias
+        plain[:, h] = seen.double() @ hidden(vv.abs())
+    return out, size, products, bias, plain
 
 
-def bound(kind, out, size, products, bias, dim, cap=0.0):
+def bound(kind, out, size, products, bias, plain, dim, cap=0.0):
     """How far an output may be off, for a type whose products are rounded as lc.h says. With u half a step of the type (2^-8 for bf16): keys
     rounded to the type move a score by u * sum |q k|, sums in fp32 by (dim + 32) 2^-24 of that, a bias by 2^-22 of its size (keys that it lowers
     by 20 or more do not count: they weigh e^-20 together with their error); the cap halves none of this and its own function is good to cap * 2^-20; exp
     is good to 2^-20. A score that is off by d moves its weight by d of itself, and so does the sum that divides: 2 d. Probabilities and values
-    rounded to the type: 2 u of the mean of |v|; the result's own rounding: u of itself."""
+    rounded to the type: 2 u of the mean of |v|; the result's own rounding: u of itself. A probability of fp16 that is small has fewer bits: held 2^7 times as large beside a largest one of 1 or more, it is
+    on a grid of 2^-24 at worst, so off by 2^-25 / 2^7 of the largest, and so of their sum: 2^-32 for every |v| that is seen."""
     u = HALF_STEP[kind]
     given = 0.0 if kind == torch.float32 else u
     d = (given + (dim + 32) * 2.0 ** -24) * products + 2.0 ** -22 * bias + cap * 2.0 ** -20 + 2.0 ** -20
     d = torch.expm1(d)[..., None]  # for scores that are off by much
-    return (2 * max(given, 2.0 ** -22) + 2 * d) * size * 1.01 + u * out.abs() * 1.01 + 2.0 ** -24 * (kind == torch.float16) + 1e-30
+    return (2 * max(given, 2.0 ** -22) + 2 * d) * size * 1.01 + u * out.abs() * 1.01 + (2.0 ** -24 + 2.0 ** -32 * plain) * (kind == torch.float16) + 1e-30
 
 
 def plan(table, held, spare, count, tokens, page, rows):
