@@ -103,6 +103,7 @@ int lc_cache_attend(const lc_cache* cache, const lc_rows* q, const lc_rows* out,
     b.longest = a.most;
     b.flat = reinterpret_cast<unsigned long long*>(reinterpret_cast<uint8_t*>(a.flat) + flat_bytes(how->sequences));
     b.parts = a.parts + 2 * kMaxParts * kPartBytes / 4;
+    if (cache->slots == 0) b.codes = static_cast<const uint8_t*>(workspace);  // keys without a place are read from the first one, and count as zeros
     e = launch_attend_tiles(b, bits, type, a.longest > 0, cs);
   }
   return e == cudaSuccess ? LC_OK : LC_ERR_CUDA;

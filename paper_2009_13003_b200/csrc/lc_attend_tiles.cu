@@ -1,8 +1,8 @@
 // Attention to a quantised cache for sequences of many new rows: the products on the tensor cores' own memory (tcgen05).
 //
 // A CTA takes blocks of 256 queries of one head of the cache (its tokens, times the heads that share it) as two tiles of 128, and goes through the keys
-// 128 at a time with a running maximum and sum of each query. Its warps have one task each: four read codes, turn them into numbers of the queries' type
-// and store them as operands (keys and values in one layout, rows of 64 values with the 128-byte swizzle: keys are read along a row, values across);
+// 128 at a time with a running maximum and sum of each query. Its warps have one task each: four read the keys' codes and four the values', turn them into
+// numbers of the queries' type and store them as operands (both in one layout, rows of 64 values with the 128-byte swizzle: keys are read along a row, values across);
 // one thread issues the products; a warpgroup for each tile takes the scores out of tensor memory, a query a thread, and puts the probabilities back
 // there, over the scores, as the first operand of the product with the values. While one tile's scores are in the warps the products of the other run.
 // The sums of the values stay in tensor memory; they are scaled down only where a maximum rises by more than a factor of 2^kSlack.
@@ -20,8 +20,12 @@ namespace lc {
 namespace {
 
 constexpr uint32_t kRows = 128, kKeys = 128;            // of a tile of queries, of keys
-constexpr uint32_t kSoftmaxWarps = 8, kReadWarps = 4;   // then the warp that issues
-constexpr uint32_t kThreads = 32 * (kSoftmaxWarps + kReadWarps + 1), kReaders = 32 * kReadWarps;
+constexpr uint32_t kSoftmaxWarps = 8, kReadWarps = 4;   // kReadWarps each for keys and for values, then the warp that issues
+constexpr uint32_t kThreads = 32 * (kSoftmaxWarps + 2 * kReadWarps + 4), kReaders = 32 * kReadWarps;
+// Registers of a thread: as launched, and what each warpgroup then has (together no more than before).
+constexpr uint32_t kRegsAtLaunch = 96, kRegsSoftmax = 136, kRegsReader = 80, kRegsIssue = 48;
+static_assert(2 * kRegsSoftmax + 2 * kRegsReader + kRegsIssue <= 5 * kRegsAtLaunch && kThreads == 5 * 128, "registers of five warpgroups");
+static_assert(kReaders == kKeys, "a reader looks up a key");
 constexpr uint32_t kStages = 2;
 constexpr uint32_t kMemo = 4;                           // tiles whose exponents and flags are kept: the scores of a tile are done before the third behind it is read
 constexpr float kSlack = 8.0f;
@@ -52,16 +56,25 @@ __device__ __forceinline__ void order_after() { asm volatile("tcgen05.fence::aft
 __device__ __forceinline__ void commit_to(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-// d (tensor memory) = or += a * b; a in shared or tensor memory.
-__device__ __forceinline__ void product(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
-  asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
+// An operand in rows of 128 bytes, swizzled, in groups of eight rows, 1024 bytes apart: the lower half of its descriptor, with `lead` bytes from one run of
+// 64 values to the next where it is read across the rows (an address further on is a larger number), and the upper half.
+__device__ __forceinline__ uint32_t operand_at(uint32_t address, uint32_t lead) { return (address >> 4 & 0x3FFF) | lead >> 4 << 16; }
+constexpr uint32_t kOperandKind = 1024 >> 4 | 1u << 14 | 2u << 29;
+// d (tensor memory) = or += a * b; a in shared or tensor memory. One thread issues all of a CTA's products, beside busy warps: few instructions each.
+__device__ __forceinline__ void product(uint32_t d, uint32_t a, uint32_t b, uint32_t what, bool add) {
+  asm volatile("{ .reg .pred p; .reg .b64 a, b; mov.b64 a, {%1, %5}; mov.b64 b, {%2, %5}; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p; }" ::"r"(d), "r"(a),
+               "r"(b), "r"(what), "r"((uint32_t)add), "r"(kOperandKind)
+               : "memory");
 }
-__device__ __forceinline__ void product_of_tensor(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add) {
-  asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d), "r"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
+__device__ __forceinline__ void product_of_tensor(uint32_t d, uint32_t a, uint32_t b, uint32_t what, bool add) {
+  asm volatile("{ .reg .pred p; .reg .b64 b; mov.b64 b, {%2, %5}; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p; }" ::"r"(d), "r"(a), "r"(b), "r"(what),
+               "r"((uint32_t)add), "r"(kOperandKind)
+               : "memory");
 }
-// An operand in rows of 128 bytes, swizzled, in groups of eight rows: `lead` bytes from one run of 64 values to the next where it is read across the rows.
-__device__ __forceinline__ uint64_t operand_at(uint32_t address, uint32_t lead) {
-  return (uint64_t)(address >> 4 & 0x3FFF) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+__device__ __forceinline__ bool one_lane() {
+  uint32_t yes;
+  asm volatile("{ .reg .pred p; elect.sync _|p, 0xFFFFFFFF; selp.u32 %0, 1, 0, p; }" : "=r"(yes));
+  return yes;
 }
 // The product's shape and types: fp32 sums, m = 128.
 __device__ __forceinline__ uint32_t product_kind(bool bf16, uint32_t n, bool across) {
@@ -88,7 +101,13 @@ __device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t (&x)[16
                "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]), "r"(x[9]), "r"(x[10]), "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15]), "r"(at)
                : "memory");
 }
-__device__ __forceinline__ void tensor_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// The numbers are there. They go through it, so that nothing that uses them is moved ahead of it.
+__device__ __forceinline__ void tensor_loaded(float (&x)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]), "+f"(x[8]), "+f"(x[9]), "+f"(x[10]), "+f"(x[11]), "+f"(x[12]), "+f"(x[13]), "+f"(x[14]), "+f"(x[15]), "+f"(x[16]), "+f"(x[17]), "+f"(x[18]), "+f"(x[19]), "+f"(x[20]), "+f"(x[21]), "+f"(x[22]), "+f"(x[23]), "+f"(x[24]), "+f"(x[25]), "+f"(x[26]), "+f"(x[27]), "+f"(x[28]), "+f"(x[29]), "+f"(x[30]), "+f"(x[31])
+               :
+               : "memory");
+}
 __device__ __forceinline__ void tensor_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // What generic stores have put into shared memory is there for the products that follow.
 __device__ __forceinline__ void order_for_products() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -99,6 +118,14 @@ __device__ __forceinline__ uint32_t rounded(float low, float high) {
   if constexpr (kBf16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(high), "f"(low));
   else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(high), "f"(low));
   return r;
+}
+
+// The bits of the first n of 32.
+__device__ __forceinline__ uint32_t bits_below(int32_t n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1u; }
+__device__ __forceinline__ float max_of(float a, float b, float c) {
+  float m;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+  return m;
 }
 
 // ---- what weighs how much -----------------------------------------------------------------------------------------
@@ -160,6 +187,51 @@ __device__ __forceinline__ Tiles tiles_of(const AttendArgs& A, const Sequence& q
 __device__ __forceinline__ uint32_t tile_at(uint64_t offset, uint32_t tiles, uint64_t weight) { return offset >= weight ? tiles : (uint32_t)(offset * tiles / weight); }
 __device__ __forceinline__ uint64_t share_of(uint64_t all, uint32_t ctas) { return max((all + ctas - 1) / ctas, (uint64_t)(2 * kKeys)); }
 
+// A CTA's way through its share: the blocks of which it has tiles, and which tiles.
+struct Walk {
+  Sequence q;
+  Weights w;
+  Place place;
+  Tiles tiles;
+  uint32_t s, block, head, j0, n;
+  bool first;  // the block lies at the share's beginning, perhaps the CTA ahead has a part of it
+  uint64_t at, from, to;
+  __device__ __forceinline__ Walk(const AttendArgs& A, uint32_t sequence, uint64_t rest, uint64_t from_, uint64_t to_) : s(sequence), at(from_), from(from_), to(to_) {
+    q = sequence_of<kKeys>(A, s, false);
+    w = weights_of(A, q);
+    place = place_of(A, w, rest);
+  }
+  __device__ __forceinline__ bool next(const AttendArgs& A) {
+    while (at < to) {
+      if (place.offset == place.weight) step(A);
+      const uint64_t upto = min(to - at + place.offset, place.weight);
+      block = place.block, head = place.head;
+      tiles = tiles_of(A, q, block);
+      j0 = tile_at(place.offset, tiles.count, place.weight);
+      n = tile_at(upto, tiles.count, place.weight) - j0;
+      first = at == from;
+      at += upto - place.offset;
+      place.offset = upto;
+      if (n > 0) return true;
+    }
+    return false;
+  }
+  __device__ __forceinline__ void step(const AttendArgs& A) {
+    place.offset = 0;
+    if (++place.head == A.heads) {
+      place.head = 0;
+      if (++place.block == w.blocks) {
+        do {
+          q = sequence_of<kKeys>(A, ++s, false);
+        } while (q.rows == 0);
+        w = weights_of(A, q);
+        place.block = 0;
+      }
+      place.weight = weight_of(w, place.block);
+    }
+  }
+};
+
 // ---- the kernel ---------------------------------------------------------------------------------------------------
 template <uint32_t DP>
 struct Layout {
@@ -170,16 +242,18 @@ struct Layout {
   static constexpr uint32_t kScoresAt = 0, kSumsAt = 2 * kKeys;      // columns of tensor memory; the second tile's kKeys and DP columns behind
 };
 
+constexpr unsigned long long kNone = ~0ull;
 struct Shared {
-  unsigned long long full_k[kStages], empty_k[kStages], full_v[kStages], empty_v[kStages], scores[2], weights[2], sums[2];  // barriers
+  unsigned long long full_k[kStages], empty_k[kStages], full_v[kStages], empty_v[kStages], queries[2], scores[2], weights[2], sums[2];  // barriers
   unsigned long long scan[kThreads / 32], found_base;
-  unsigned long long places[2][kKeys];  // slot * heads + head of a tile's keys; ~0: none
+  ulonglong2 places[2][2][kKeys];  // of a tile's keys, for the readers of keys and of values: where codes and scales begin; kNone: zeros
   uint32_t found, tensor, dead;
   uint32_t most_scale[kMemo][kReadWarps];
   uint32_t flags[kMemo][kReadWarps];  // whether a scale of the tile's values is no number
 };
 
-template <int kBits, uint32_t DP, bool kBf16>
+// kCap, kBias: scores are capped, lowered by distance.
+template <int kBits, uint32_t DP, bool kBf16, bool kCap, bool kBias>
 struct Kernel {
   using L = Layout<DP>;
   using T = typename TypeOf<kBf16 ? LC_TYPE_BF16 : LC_TYPE_F16>::T;
@@ -187,59 +261,72 @@ struct Kernel {
   static constexpr float kLift = kBf16 ? 0.0f : 7.0f;
   static constexpr uint32_t kUnits = DP * kBits / 8 / 16;  // of 16 bytes of a row's codes, at most
 
-  // A block's queries as operands. A negative scale goes to their signs.
-  static __device__ __forceinline__ void load_queries(const AttendArgs& A, const Sequence& q, uint32_t block, uint32_t head, uint8_t* queries) {
+  // A tile of a block's queries as an operand, by the warpgroup that takes its scores. A negative scale goes to their signs.
+  static __device__ __forceinline__ void load_queries(const AttendArgs& A, const Sequence& q, uint32_t first, uint32_t head, uint32_t thread, uint8_t* to) {
     const uint32_t flip = A.scale < 0.0f ? 0x80008000u : 0u;
     const bool whole = A.dim % 8 == 0 && ((reinterpret_cast<uintptr_t>(A.q) / 2 | A.q_row | A.q_head) & 7) == 0;
-    for (uint32_t i = threadIdx.x; i < kTileRows * (DP / 8); i += kThreads) {
-      const uint32_t row = i / (DP / 8), c = i % (DP / 8), r = block * kTileRows + row, token = A.by_shared.div(r);
+#pragma unroll
+    for (uint32_t i = thread; i < kRows * (DP / 8); i += kRows) {
+      const uint32_t row = i / (DP / 8), c = i % (DP / 8), r = first + row, token = A.by_shared.div(r);
       uint32_t w[4] = {0, 0, 0, 0};
       if (token < q.rows && c * 8 < A.dim) {
         const unsigned short* p = static_cast<const unsigned short*>(A.q) + (uint64_t)(q.row + token) * A.q_row + (uint64_t)(head * A.shared + (r - token * A.shared)) * A.q_head + c * 8;
         if (whole) {
-          const uint4 x = *reinterpret_cast<const uint4*>(p);
+          const uint4 x = __ldg(reinterpret_cast<const uint4*>(p));
           w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
         } else {
+#pragma unroll
           for (uint32_t e = 0; e < 8; ++e)
-            if (c * 8 + e < A.dim) w[e / 2] |= (uint32_t)p[e] << (16 * (e & 1));
+            if (c * 8 + e < A.dim) w[e / 2] |= (uint32_t)__ldg(p + e) << (16 * (e & 1));
         }
       }
-      const uint32_t tile = row / kRows, at = row % kRows;
-      *reinterpret_cast<uint4*>(queries + tile * L::kQueries + (c / 8) * (kRows * 128) + at * 128 + (((c & 7) ^ (at & 7)) << 4)) =
-          make_uint4(w[0] ^ flip, w[1] ^ flip, w[2] ^ flip, w[3] ^ flip);
+      *reinterpret_cast<uint4*>(to + (c / 8) * (kRows * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = make_uint4(w[0] ^ flip, w[1] ^ flip, w[2] ^ flip, w[3] ^ flip);
     }
   }
 
-  // The codes and scales of a thread's units of a tile: unit u of the tile is 16 bytes (or what is left of the row) of key u / units.
+  // A reader takes one piece of 16 bytes of several keys' codes: of keys first + i * kStep. Lanes are dealt to pieces and keys so that eight lanes in a
+  // row store to different banks: 8 bits, four pieces of two neighbouring keys (their runs of eight values are every other one, which the
+  // swizzle puts into the even and the odd places), 4 bits, two pieces of four.
+  static constexpr uint32_t kStep = 32 / kUnits * kReadWarps;
+  struct Reader {
+    uint32_t first, part, group;
+    bool there;
+  };
+  static __device__ __forceinline__ Reader reader_of(const AttendArgs& A, uint32_t warp, uint32_t lane) {
+    Reader r;
+    uint32_t row;
+    if (kBits == 8) r.part = kUnits == 8 ? (lane & 3) | (lane >> 1 & 4) : lane & 3, row = kUnits == 8 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
+    else r.part = kUnits == 4 ? (lane & 1) | (lane >> 2 & 2) : lane & 1, row = kUnits == 4 ? (lane >> 1 & 3) | (lane >> 2 & 4) : lane >> 1;
+    r.first = warp * (32 / kUnits) + row;
+    r.there = r.part * 16 < A.row_bytes;
+    r.group = r.part / (A.per_group * (kBits == 8 ? 2 : 1));
+    return r;
+  }
   struct Codes {
     uint4 w[kUnits];
     unsigned short scale[kUnits];
   };
-  static __device__ __forceinline__ void read_codes(const AttendArgs& A, const unsigned long long* places, bool values, uint32_t reader, Codes& c) {
-    const uint32_t units = A.by_pieces.d;
-    const uint8_t* codes = A.codes + (values ? A.plane_codes : 0);
-    const unsigned short* scales = A.scales + (values ? A.plane_scales : 0);
-    const uint32_t group = A.per_group * (kBits == 8 ? 2 : 1);  // units of a group
+  static __device__ __forceinline__ void read_codes(const AttendArgs& A, const ulonglong2* places, const uint8_t* codes, const unsigned short* scales, const Reader& r, Codes& c) {
+    if (!r.there) return;
+    codes += r.part * 16;
+    scales += r.group;
+    const bool whole = (A.row_bytes & 15) == 0;
+    const uint32_t left = (A.row_bytes - r.part * 16) / 4;
 #pragma unroll
     for (uint32_t i = 0; i < kUnits; ++i) {
-      c.w[i] = make_uint4(0, 0, 0, 0);
+      const ulonglong2 place = places[r.first + i * kStep];
+      const uint8_t* p = codes + place.x;
       c.scale[i] = 0;
-      if (i >= units) continue;
-      const uint32_t u = reader + i * kReaders, row = A.by_pieces.div(u), part = u - row * units;
-      const unsigned long long place = places[row];
-      if (place == ~0ull) continue;
-      const uint8_t* p = codes + place * A.row_bytes + part * 16;
-      if ((A.row_bytes & 15) == 0) {
+      if (place.y != kNone) c.scale[i] = __ldg(scales + place.y);
+      if (whole) {
         c.w[i] = __ldg(reinterpret_cast<const uint4*>(p));
       } else {
         const uint32_t* x = reinterpret_cast<const uint32_t*>(p);
-        const uint32_t left = (A.row_bytes - part * 16) / 4;
         c.w[i].x = __ldg(x);
-        if (left > 1) c.w[i].y = __ldg(x + 1);
-        if (left > 2) c.w[i].z = __ldg(x + 2);
-        if (left > 3) c.w[i].w = __ldg(x + 3);
+        c.w[i].y = left > 1 ? __ldg(x + 1) : 0u;
+        c.w[i].z = left > 2 ? __ldg(x + 2) : 0u;
+        c.w[i].w = left > 3 ? __ldg(x + 3) : 0u;
       }
-      c.scale[i] = __ldg(scales + place * A.groups + part / group);
     }
   }
   // Four pairs of numbers from eight codes. scale: of bf16 two of it, of fp16 a float's bits.
@@ -267,33 +354,32 @@ struct Kernel {
     }
     return make_uint4(r[0], r[1], r[2], r[3]);
   }
-  // exponent: what the scales are multiplied by (fp16). values: scales that are no numbers count as 0.
-  static __device__ __forceinline__ void store_numbers(const AttendArgs& A, const Codes& c, bool values, float exponent, uint32_t reader, uint8_t* operand) {
-    const uint32_t units = A.by_pieces.d;
+  // down: what the scales are multiplied by (fp16). values: scales that are no numbers count as 0.
+  static __device__ __forceinline__ void store_numbers(const Codes& c, bool values, float down, const Reader& r, uint8_t* operand) {
+    if (!r.there) return;
 #pragma unroll
     for (uint32_t i = 0; i < kUnits; ++i) {
-      if (i >= units) continue;
-      const uint32_t u = reader + i * kReaders, row = A.by_pieces.div(u), part = u - row * units;
+      const uint32_t row = r.first + i * kStep;
       uint32_t s = c.scale[i];
       if (values && (s & 0x7F80u) == 0x7F80u) s = 0;
-      s = kBf16 ? s | s << 16 : __float_as_uint(__uint_as_float(s << 16) * exponent);
+      s = kBf16 ? s | s << 16 : __float_as_uint(__uint_as_float(s << 16) * down);
       const uint32_t w[4] = {c.w[i].x, c.w[i].y, c.w[i].z, c.w[i].w};
       uint8_t* to = operand + row * 128;
 #pragma unroll
       for (uint32_t k = 0; k < 16 / kBits; ++k) {  // 8 bits: two runs of eight values, 4 bits: four
-        const uint32_t n = part * (16 / kBits) + k;
+        const uint32_t n = r.part * (16 / kBits) + k;
         *reinterpret_cast<uint4*>(to + (n / 8) * (kKeys * 128) + (((n & 7) ^ (row & 7)) << 4)) = kBits == 8 ? numbers(w[2 * k], w[2 * k + 1], s) : numbers(w[k], 0, s);
       }
     }
   }
   static __device__ __forceinline__ unsigned long long look_up(const AttendArgs& A, const Sequence& q, uint32_t s, uint32_t head, uint32_t key) {
-    if (key >= q.length) return ~0ull;
+    if (key >= q.length) return kNone;
     const uint32_t page = A.by_page.div(key);
     const int32_t number = __ldg(A.table + s * A.table_stride + page);
     const int64_t slot = (int64_t)number * A.by_page.d + (key - page * A.by_page.d);
     if (number < 0 || slot >= (int64_t)A.slots) {
       if (A.status) set_status(A.status, LC_ERR_INDEX);
-      return ~0ull;
+      return kNone;
     }
     return (unsigned long long)slot * A.heads + head;
   }
@@ -317,6 +403,7 @@ struct Kernel {
         barrier_init(shared_address(&S.empty_v[i]), 1);
       }
       for (uint32_t t = 0; t < 2; ++t) {
+        barrier_init(shared_address(&S.queries[t]), kRows);
         barrier_init(shared_address(&S.scores[t]), 1);
         barrier_init(shared_address(&S.weights[t]), kRows);
         barrier_init(shared_address(&S.sums[t]), 1);
@@ -382,75 +469,81 @@ struct Kernel {
       wait_previous();
       return;
     }
-    if (warp == kSoftmaxWarps + kReadWarps) {
+    if (warp == kSoftmaxWarps + 2 * kReadWarps) {
       asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_address(&S.tensor)), "n"(512) : "memory");
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
       order_before();
     }
 
-    uint32_t s = S.found;
-    Sequence q = sequence_of<kKeys>(A, s, false);
-    Weights W = weights_of(A, q);
-    Place P = place_of(A, W, from - S.found_base);
+    __syncthreads();
+    order_after();
+    const uint32_t tensor = S.tensor;
     const float scale = fabsf(A.scale) * (kBf16 ? 64.0f : 1.0f);
-    uint32_t done = 0;  // tiles of keys so far: what the barriers' phases go by
     volatile uint32_t* dead = &S.dead;
+    Walk walk(A, S.found, from - S.found_base, from, to);
+    uint32_t done = 0;  // tiles of keys so far: what the barriers' phases go by
 
-    for (unsigned long long at = from; at < to;) {
-      const uint64_t upto = min((uint64_t)(to - at) + P.offset, P.weight);
-      const Tiles tiles = tiles_of(A, q, P.block);
-      const uint32_t j0 = tile_at(P.offset, tiles.count, P.weight), j1 = tile_at(upto, tiles.count, P.weight), n = j1 - j0;
-      const uint32_t block = P.block, head = P.head;
-      if (n > 0) {
-        load_queries(A, q, block, head, queries);
-        order_for_products();
-        __syncthreads();
-        order_after();
-        const uint32_t tensor = S.tensor;
-
-        if (warp < kSoftmaxWarps) {
+    if (warp < kSoftmaxWarps) {
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+      bool good = true;
+      while (good && walk.next(A)) {
+        const Sequence& q = walk.q;
+        const Tiles& tiles = walk.tiles;
+        const uint32_t block = walk.block, head = walk.head, j0 = walk.j0, n = walk.n, s = walk.s;
+        {
           // ---- scores to probabilities: a query a thread
           const uint32_t t = warp / 4, row = threadIdx.x % kRows, r = block * kTileRows + t * kRows + row, token = A.by_shared.div(r), in_group = r - token * A.shared;
           const uint32_t lanes = tensor + ((warp & 3) * 32 << 16), scores = lanes + L::kScoresAt + t * kKeys, sums = lanes + L::kSumsAt + t * DP;
           const uint32_t position = q.first + min(token, q.rows - 1);
-          const float slope = A.slopes ? A.slopes[head * A.shared + in_group] * kLog2e : 0.0f;
+          const float slope = kBias ? A.slopes[head * A.shared + in_group] * kLog2e : 0.0f;
           const float cap_out = A.cap * kLog2e;
           // positions of this warp's first and last query
           const uint32_t low = __shfl_sync(0xFFFFFFFFu, position, 0), high = __shfl_sync(0xFFFFFFFFu, position, 31);
-          float m = -INFINITY, l = 0.0f;
+          float m = -INFINITY;
+          Two l = two(0.0f, 0.0f);
           uint32_t broken = 0;  // groups whose value is no number for this query
-          bool good = false;  // all tiles are through
+          load_queries(A, q, block * kTileRows + t * kRows, head, row, queries + t * L::kQueries);
+          order_for_products();
+          order_before();  // the sums of the block before are read
+          barrier_arrive(shared_address(&S.queries[t]));
+          good = false;  // all tiles are through
           for (uint32_t i = 0; i < n; ++i) {
             const uint32_t number = done + i, memo = number % kMemo, key = tiles.key(j0 + i);
-            if (!warp_wait(shared_address(&S.full_v[number % kStages]), number / kStages & 1, dead)) break;
             if (!warp_wait(shared_address(&S.scores[t]), number & 1, dead)) break;
             order_after();
+            float x[2][32];
+            tensor_load(scores, x[0]);
             float unit = 1.0f;  // of the tile's keys
             if constexpr (!kBf16) unit = unit_of(S, memo);
-            const float factor = scale * unit * kLog2e, cap_in = A.cap > 0.0f ? 2.0f * factor / A.cap : 0.0f;
+            const float factor = scale * unit * kLog2e, cap_in = kCap ? 2.0f * factor / A.cap : 0.0f, away = (float)(int32_t)(position - key);
+            // of the tile's keys a query sees those from `begin` on and ahead of `end`, and those ahead of `prefix`
             const bool full = key + kKeys - 1 <= low && (A.window == 0 || high - key < A.window);
-            auto visible = [&](uint32_t at_key) { return (at_key <= position && (A.window == 0 || position - at_key < A.window)) || at_key < q.prefix; };
-            auto capped = [&](float x) { return A.cap > 0.0f ? fmaf(-2.0f * cap_out, reciprocal(1.0f + exp2_fast(x * cap_in)), cap_out) : x * factor; };
-            auto biased = [&](float y, uint32_t at_key) { return fmaf(-slope, fabsf((float)(int32_t)(position - at_key)), y); };
+            const int32_t end = (int32_t)(position - key) + 1, begin = A.window ? end - (int32_t)A.window : 0, prefix = (int32_t)(q.prefix - key);
+            auto seen = [&](uint32_t c) { return (bits_below(end - (int32_t)c) & ~bits_below(begin - (int32_t)c)) | bits_below(prefix - (int32_t)c); };
+            auto hide = [&](float (&y)[32], uint32_t c) {
+              const uint32_t bits = seen(c);
+#pragma unroll
+              for (uint32_t e = 0; e < 32; ++e) y[e] = bits >> e & 1 ? y[e] : -INFINITY;
+            };
+            auto capped = [&](float y) {
+              return kCap ? fmaf(-2.0f * cap_out, reciprocal(1.0f + exp2_fast(y * cap_in)), cap_out) : y * factor;
+            };
+            auto score = [&](float y, uint32_t c) { return kBias ? fmaf(-slope, fabsf(away - (float)c), capped(y)) : capped(y); };
             float top = -INFINITY;
-#pragma unroll 1
-            for (uint32_t c = 0; c < kKeys; c += 32) {
-              float x[32];
-              tensor_load(scores + c, x);
-              tensor_loaded();
-              if (A.slopes) {
 #pragma unroll
-                for (uint32_t e = 0; e < 32; ++e) x[e] = biased(capped(x[e]), key + c + e);
+            for (uint32_t c = 0; c < kKeys / 32; ++c) {
+              float (&y)[32] = x[c & 1];
+              tensor_loaded(y);
+              tensor_load(scores + (c + 1) % (kKeys / 32) * 32, x[(c + 1) & 1]);  // behind the last ones the first again
+              if constexpr (kBias) {
+#pragma unroll
+                for (uint32_t e = 0; e < 32; ++e) y[e] = score(y[e], c * 32 + e);
               }
-              if (!full) {
+              if (!full) hide(y, c * 32);
 #pragma unroll
-                for (uint32_t e = 0; e < 32; ++e)
-                  if (!visible(key + c + e)) x[e] = -INFINITY;
-              }
-#pragma unroll
-              for (uint32_t e = 0; e < 32; ++e) top = fmaxf(top, x[e]);
+              for (uint32_t e = 0; e < 32; e += 2) top = max_of(top, y[e], y[e + 1]);
             }
-            if (!A.slopes && top != -INFINITY) top = capped(top);  // both grow with the product
+            if (!kBias && top != -INFINITY) top = capped(top);  // both grow with the product
             const bool rises = top > m + kSlack;
             if (__any_sync(0xFFFFFFFFu, rises)) {
               const float now = rises ? top : m, down = rises ? exp2_fast(m - now) : 1.0f;
@@ -459,47 +552,44 @@ struct Kernel {
                 order_after();
 #pragma unroll 1
                 for (uint32_t c = 0; c < DP; c += 32) {
-                  float x[32];
-                  tensor_load(sums + c, x);
-                  tensor_loaded();
+                  float y[32];
+                  tensor_load(sums + c, y);
+                  tensor_loaded(y);
 #pragma unroll
-                  for (uint32_t e = 0; e < 32; ++e) x[e] *= down;
-                  tensor_store(sums + c, x);
+                  for (uint32_t e = 0; e < 32; ++e) y[e] *= down;
+                  tensor_store(sums + c, y);
                 }
               }
               m = now;
-              l *= down;
+              l = mul_two(l, two(down, down));
             }
             const float base = (m == -INFINITY ? 0.0f : m) - kLift;
-#pragma unroll 1
-            for (uint32_t c = 0; c < kKeys; c += 32) {
-              float x[32];
-              tensor_load(scores + c, x);
-              tensor_loaded();
-              if (A.cap > 0.0f || A.slopes) {
 #pragma unroll
-                for (uint32_t e = 0; e < 32; ++e) x[e] = biased(capped(x[e]), key + c + e) - base;
+            for (uint32_t c = 0; c < kKeys / 32; ++c) {
+              float (&y)[32] = x[c & 1];
+              tensor_loaded(y);
+              if (c + 1 < kKeys / 32) tensor_load(scores + (c + 1) * 32, x[(c + 1) & 1]);
+              if constexpr (!kCap && !kBias) {
+#pragma unroll
+                for (uint32_t e = 0; e < 32; e += 2) split_two(fma_two(two(y[e], y[e + 1]), two(factor, factor), two(-base, -base)), y[e], y[e + 1]);
               } else {
 #pragma unroll
-                for (uint32_t e = 0; e < 32; ++e) x[e] = fmaf(x[e], factor, -base);
+                for (uint32_t e = 0; e < 32; ++e) y[e] = score(y[e], c * 32 + e) - base;
               }
-              if (!full) {
-#pragma unroll
-                for (uint32_t e = 0; e < 32; ++e)
-                  if (!visible(key + c + e)) x[e] = -INFINITY;
-              }
+              if (!full) hide(y, c * 32);
               uint32_t p[16];
 #pragma unroll
               for (uint32_t e = 0; e < 32; e += 2) {
-                x[e] = exp2_fast(x[e]), x[e + 1] = exp2_fast(x[e + 1]);
-                l += x[e] + x[e + 1];
-                p[e / 2] = rounded<kBf16>(x[e], x[e + 1]);
+                y[e] = exp2_fast(y[e]), y[e + 1] = exp2_fast(y[e + 1]);
+                l = add_two(l, two(y[e], y[e + 1]));
+                p[e / 2] = rounded<kBf16>(y[e], y[e + 1]);
               }
-              tensor_store(scores + c / 2, p);
+              tensor_store(scores + c * 16, p);
             }
             tensor_stored();
             order_before();
             barrier_arrive(shared_address(&S.weights[t]));
+            if (!warp_wait(shared_address(&S.full_v[number % kStages]), number / kStages & 1, dead)) break;
             good = i + 1 == n;
             uint32_t flags = 0;
 #pragma unroll
@@ -507,25 +597,29 @@ struct Kernel {
             if (flags) {  // some value of the tile is no number: which of them this query sees
               for (uint32_t k = 0; k < kKeys && key + k < q.length; ++k) {
                 const unsigned long long place = look_up(A, q, s, head, key + k);
-                if (place == ~0ull || !visible(key + k)) continue;
+                if (place == kNone || !(seen(k) & 1)) continue;
                 for (uint32_t g = 0; g < A.groups; ++g)
                   if ((A.scales[A.plane_scales + place * A.groups + g] & 0x7F80u) == 0x7F80u) broken |= 1u << g;
               }
             }
           }
-          if (good && warp_wait(shared_address(&S.sums[t]), (done + n - 1) & 1, dead)) {
+          good = good && warp_wait(shared_address(&S.sums[t]), (done + n - 1) & 1, dead);
+          if (good) {
             order_after();
-            const bool whole = j0 == 0 && j1 == tiles.count, there = token < q.rows;
-            float* part = A.parts + (2ull * blockIdx.x + (at == from ? 0 : 1)) * (kTilePartBytes / 4);
+            const bool whole = j0 == 0 && n == tiles.count, there = token < q.rows;
+            float* part = A.parts + (2ull * blockIdx.x + (walk.first ? 0 : 1)) * (kTilePartBytes / 4);
             T* out = static_cast<T*>(A.out) + (uint64_t)(q.row + min(token, q.rows - 1)) * A.out_row + (uint64_t)(head * A.shared + in_group) * A.out_head;
             const bool aligned = ((reinterpret_cast<uintptr_t>(A.out) / 2 | A.out_row | A.out_head) & 7) == 0;
-            const float over = whole ? (kBf16 ? 64.0f : 1.0f) / l : 1.0f;
+            float sum, other;
+            split_two(l, sum, other);
+            sum += other;
+            const float over = whole ? (kBf16 ? 64.0f : 1.0f) / sum : 1.0f;
             const uint32_t shift = 5 + (A.per_group > 1) + (A.per_group > 2);  // values of a group
 #pragma unroll 1
             for (uint32_t c = 0; c < A.dim; c += 32) {
               float x[32];
               tensor_load(sums + c, x);
-              tensor_loaded();
+              tensor_loaded(x);
 #pragma unroll
               for (uint32_t e = 0; e < 32; ++e) x[e] *= over;
               if (broken >> (c >> shift) & 1) {
@@ -553,124 +647,139 @@ struct Kernel {
             }
             if (!whole) {
               part[kTileRows * kTileDim + t * kRows + row] = m;
-              part[kTileRows * (kTileDim + 1) + t * kRows + row] = l;
+              part[kTileRows * (kTileDim + 1) + t * kRows + row] = sum;
             }
           }
-        } else if (warp < kSoftmaxWarps + kReadWarps) {
+        }
+        done += n;
+      }
+    } else if (warp < kSoftmaxWarps + 2 * kReadWarps) {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsReader));
+      bool good = true;
+      while (good && walk.next(A)) {
+        const Sequence& q = walk.q;
+        const Tiles& tiles = walk.tiles;
+        const uint32_t head = walk.head, j0 = walk.j0, n = walk.n, s = walk.s;
+        {
           // ---- codes to operands
-          const uint32_t reader = threadIdx.x - 32 * kSoftmaxWarps, mine = warp - kSoftmaxWarps;
-          auto meet = [&] { asm volatile("bar.sync 1, %0;" ::"n"(kReaders) : "memory"); };
-          auto look = [&](uint32_t i) { return i < n ? look_up(A, q, s, head, tiles.key(j0 + i) + reader) : ~0ull; };
-          Codes k, v;
-          meet();  // the places of the block before are read
-          S.places[0][reader] = look(0);
-          unsigned long long next = look(1);
+          const uint32_t set = (warp - kSoftmaxWarps) / kReadWarps, mine = (warp - kSoftmaxWarps) % kReadWarps, reader = mine * 32 + lane;  // set: 0 keys, 1 values
+          const uint8_t* codes = A.codes + (set ? A.plane_codes : 0);
+          const unsigned short* scales = A.scales + (set ? A.plane_scales : 0);
+          uint8_t* operands = set ? values : keys;
+          unsigned long long* const full = set ? S.full_v : S.full_k;
+          unsigned long long* const empty = set ? S.empty_v : S.empty_k;
+          const Reader R = reader_of(A, mine, lane);
+          auto meet = [&] { asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + set), "n"(kReaders) : "memory"); };
+          auto look = [&](uint32_t i) {
+            const unsigned long long place = i < n ? look_up(A, q, s, head, tiles.key(j0 + i) + reader) : kNone;
+            return place == kNone ? make_ulonglong2(0, kNone) : make_ulonglong2(place * A.row_bytes, place * A.groups);
+          };
+          Codes c = {};
+          S.places[set][0][reader] = look(0);
+          ulonglong2 next = look(1);
           meet();
-          read_codes(A, S.places[0], false, reader, k);
-          read_codes(A, S.places[0], true, reader, v);
-          bool good = true;
+          read_codes(A, S.places[set][0], codes, scales, R, c);
           for (uint32_t i = 0; i < n; ++i) {
             const uint32_t number = done + i, stage = number % kStages, turn = number / kStages, memo = number % kMemo;
-            S.places[(i + 1) & 1][reader] = next;
-            uint32_t most = 0, flag = 0;
+            S.places[set][(i + 1) & 1][reader] = next;
+            float down = 1.0f;
+            if (set) {
+              bool flag = false;
 #pragma unroll
-            for (uint32_t x = 0; x < kUnits; ++x) {
-              if (!kBf16 && (k.scale[x] & 0x7F80u) != 0x7F80u) most = max(most, (uint32_t)k.scale[x]);
-              flag |= (v.scale[x] & 0x7F80u) == 0x7F80u;
-            }
-            if constexpr (!kBf16) {
+              for (uint32_t x = 0; x < kUnits; ++x) flag |= (c.scale[x] & 0x7F80u) == 0x7F80u;
+              flag = __any_sync(0xFFFFFFFFu, flag);
+              if (lane == 0) S.flags[memo][mine] = flag;
+            } else if constexpr (!kBf16) {
+              uint32_t most = 0;
+#pragma unroll
+              for (uint32_t x = 0; x < kUnits; ++x)
+                if ((c.scale[x] & 0x7F80u) != 0x7F80u) most = max(most, (uint32_t)c.scale[x]);
               most = __reduce_max_sync(0xFFFFFFFFu, most);
               if (lane == 0) S.most_scale[memo][mine] = most;
             }
-            flag = __any_sync(0xFFFFFFFFu, flag);
-            if (lane == 0) S.flags[memo][mine] = flag;
             meet();
             next = look(i + 2);
-            float down = 1.0f;
-            if constexpr (!kBf16) down = 1.0f / unit_of(S, memo);
-            if (good && turn > 0) good = barrier_wait(shared_address(&S.empty_k[stage]), (turn - 1) & 1, dead);
+            if (!kBf16 && !set) down = 1.0f / unit_of(S, memo);
+            if (good && turn > 0) good = barrier_wait(shared_address(&empty[stage]), (turn - 1) & 1, dead);
             if (good) {
-              store_numbers(A, k, false, down, reader, keys + stage * L::kOperand);
+              store_numbers(c, set, down, R, operands + stage * L::kOperand);
               order_for_products();
-              barrier_arrive(shared_address(&S.full_k[stage]));
+              barrier_arrive(shared_address(&full[stage]));
             }
-            if (i + 1 < n) read_codes(A, S.places[(i + 1) & 1], false, reader, k);
-            if (good && turn > 0) good = barrier_wait(shared_address(&S.empty_v[stage]), (turn - 1) & 1, dead);
-            if (good) {
-              store_numbers(A, v, true, 1.0f, reader, values + stage * L::kOperand);
-              order_for_products();
-              barrier_arrive(shared_address(&S.full_v[stage]));
-            }
-            if (i + 1 < n) read_codes(A, S.places[(i + 1) & 1], true, reader, v);
+            if (i + 1 < n) read_codes(A, S.places[set][(i + 1) & 1], codes, scales, R, c);
           }
-        } else if (lane == 0) {
-          // ---- the products
-          const uint32_t steps = (A.dim + 15) / 16, scores_kind = product_kind(kBf16, kKeys, false), sums_kind = product_kind(kBf16, steps * 16, true);
-          auto multiply_keys = [&](uint32_t t, uint32_t stage) {
-            const uint32_t a = shared_address(queries + t * L::kQueries), b = shared_address(keys + stage * L::kOperand);
-            for (uint32_t x = 0; x < steps; ++x)
-              product(tensor + L::kScoresAt + t * kKeys, operand_at(a + (x / 4) * (kRows * 128) + (x % 4) * 32, 16), operand_at(b + (x / 4) * (kKeys * 128) + (x % 4) * 32, 16), scores_kind, x > 0);
-            commit_to(shared_address(&S.scores[t]));
-          };
-          auto multiply_values = [&](uint32_t t, uint32_t stage, bool add) {
-            const uint32_t b = shared_address(values + stage * L::kOperand);
+        }
+        done += n;
+        // the places are read; the readers go on together or not at all
+        uint32_t together;
+        asm volatile("{ .reg .pred p, r; setp.ne.b32 p, %3, 0; barrier.cta.red.and.pred r, %1, %2, p; selp.u32 %0, 1, 0, r; }"
+                     : "=r"(together)
+                     : "r"(1 + (warp - kSoftmaxWarps) / kReadWarps), "n"(kReaders), "r"((uint32_t)good)
+                     : "memory");
+        good = together;
+      }
+    } else {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
+      if (warp == kSoftmaxWarps + 2 * kReadWarps) {
+        // ---- the products: the warp as a whole goes through the tiles, with numbers that the compiler knows to be the same for all lanes; one lane issues
+        const uint32_t all_lanes = 0xFFFFFFFFu, at_tensor = __shfl_sync(all_lanes, tensor, 0);
+        const uint32_t steps = (A.dim + 15) / 16, scores_kind = product_kind(kBf16, kKeys, false), sums_kind = product_kind(kBf16, steps * 16, true);
+        const uint32_t query_at = operand_at(shared_address(queries), 16), key_at = operand_at(shared_address(keys), 16), value_at = operand_at(shared_address(values), kKeys * 128);
+        auto multiply_keys = [&](uint32_t t, uint32_t stage, bool last) {
+          const uint32_t a = query_at + t * (L::kQueries >> 4), b = key_at + stage * (L::kOperand >> 4), d = at_tensor + L::kScoresAt + t * kKeys;
+          if (one_lane()) {
 #pragma unroll
-            for (uint32_t x = 0; x < kKeys / 16; ++x)
-              product_of_tensor(tensor + L::kSumsAt + t * DP, tensor + L::kScoresAt + t * kKeys + x * 8, operand_at(b + x * 2048, kKeys * 128), sums_kind, add || x > 0);
+            for (uint32_t x = 0; x < DP / 16; ++x)
+              if (x < steps) product(d, a + ((x / 4) * (kRows * 128) + (x % 4) * 32 >> 4), b + ((x / 4) * (kKeys * 128) + (x % 4) * 32 >> 4), scores_kind, x > 0);
+            commit_to(shared_address(&S.scores[t]));
+            if (last) commit_to(shared_address(&S.empty_k[stage]));
+          }
+          __syncwarp();
+        };
+        auto multiply_values = [&](uint32_t t, uint32_t stage, bool add, bool last) {
+          const uint32_t a = at_tensor + L::kScoresAt + t * kKeys, b = value_at + stage * (L::kOperand >> 4), d = at_tensor + L::kSumsAt + t * DP;
+          if (one_lane()) {
+#pragma unroll
+            for (uint32_t x = 0; x < kKeys / 16; ++x) product_of_tensor(d, a + x * 8, b + (x * 2048 >> 4), sums_kind, add || x > 0);
             commit_to(shared_address(&S.sums[t]));
-          };
-          bool good = barrier_wait(shared_address(&S.full_k[done % kStages]), done / kStages & 1, dead);
-          if (good) {
+            if (last) commit_to(shared_address(&S.empty_v[stage]));
+          }
+          __syncwarp();
+        };
+        bool good = true;
+        for (uint32_t count = 0; good && walk.next(A); ++count) {
+          const uint32_t n = __shfl_sync(all_lanes, walk.n, 0);
+          good = warp_wait(shared_address(&S.full_k[done % kStages]), done / kStages & 1, dead);
+          for (uint32_t t = 0; t < 2 && good; ++t) {
+            good = warp_wait(shared_address(&S.queries[t]), count & 1, dead);
+            if (!good) break;
             order_after();
-            multiply_keys(0, done % kStages);
-            multiply_keys(1, done % kStages);
-            commit_to(shared_address(&S.empty_k[done % kStages]));
+            multiply_keys(t, done % kStages, t == 1);
           }
           for (uint32_t i = 0; i < n && good; ++i) {
             const uint32_t number = done + i, stage = number % kStages, behind = (number + 1) % kStages;
-            good = barrier_wait(shared_address(&S.full_v[stage]), number / kStages & 1, dead);
+            good = warp_wait(shared_address(&S.full_v[stage]), number / kStages & 1, dead);
             for (uint32_t t = 0; t < 2 && good; ++t) {
-              good = barrier_wait(shared_address(&S.weights[t]), number & 1, dead);
+              good = warp_wait(shared_address(&S.weights[t]), number & 1, dead);
               if (!good) break;
               order_after();
-              multiply_values(t, stage, i > 0);
-              if (t == 1) commit_to(shared_address(&S.empty_v[stage]));
+              multiply_values(t, stage, i > 0, t == 1);
               if (i + 1 < n) {
-                if (t == 0) good = barrier_wait(shared_address(&S.full_k[behind]), (number + 1) / kStages & 1, dead);
+                if (t == 0) good = warp_wait(shared_address(&S.full_k[behind]), (number + 1) / kStages & 1, dead);
                 if (!good) break;
                 order_after();
-                multiply_keys(t, behind);
-                if (t == 1) commit_to(shared_address(&S.empty_k[behind]));
+                multiply_keys(t, behind, t == 1);
               }
             }
           }
-        }
-        __syncwarp();
-        order_before();
-        __syncthreads();  // the block is done: queries, places and tensor memory are free
-        order_after();
-        done += n;
-        if (*dead) break;  // the same for all threads: none sets it before the next block's queries are there
-      }
-      at += upto - P.offset;
-      if (at < to) {
-        P.offset = 0;
-        if (++P.head == A.heads) {
-          P.head = 0;
-          if (++P.block == W.blocks) {
-            do {
-              q = sequence_of<kKeys>(A, ++s, false);
-            } while (q.rows == 0);
-            W = weights_of(A, q);
-            P.block = 0;
-          }
-          P.weight = weight_of(W, P.block);
+          done += n;
         }
       }
     }
+    order_before();
     __syncthreads();
     if (threadIdx.x == 0 && S.dead && A.status) set_status(A.status, LC_ERR_TIMEOUT);
-    if (warp == kSoftmaxWarps + kReadWarps) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(S.tensor), "n"(512) : "memory");
+    if (warp == kSoftmaxWarps + 2 * kReadWarps) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(S.tensor), "n"(512) : "memory");
     wait_previous();
   }
 
@@ -683,9 +792,9 @@ struct Kernel {
   }
 };
 
-template <int kBits, uint32_t DP, bool kBf16>
+template <int kBits, uint32_t DP, bool kBf16, bool kCap, bool kBias>
 __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(AttendArgs A) {
-  Kernel<kBits, DP, kBf16>::run(A);
+  Kernel<kBits, DP, kBf16, kCap, kBias>::run(A);
 }
 
 // Joins the parts of the blocks that CTAs share (see join_kernel of lc_attend_rows.cuh): a query a thread, blockIdx.y a run of 16 values.
@@ -746,12 +855,12 @@ __global__ void __launch_bounds__(kTileRows) join_tiles_kernel(AttendArgs A, uin
     if (d0 + e < A.dim) from_float(v[e] * over, out[e]);
 }
 
-template <int kBits, uint32_t DP, bool kBf16>
+template <int kBits, uint32_t DP, bool kBf16, bool kCap, bool kBias>
 cudaError_t launch(const AttendArgs& a, bool overlap, cudaStream_t cs) {
   static int sms[kMaxDevices] = {};  // by device ordinal: 0 not looked at yet
   const int dev = current_device_index();
   if (dev < 0) return cudaErrorInvalidDevice;
-  auto kernel = attend_tiles_kernel<kBits, DP, kBf16>;
+  auto kernel = attend_tiles_kernel<kBits, DP, kBf16, kCap, kBias>;
   if (!sms[dev]) {
     int n = 0;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Layout<DP>::kWhole);
@@ -773,18 +882,21 @@ cudaError_t launch(const AttendArgs& a, bool overlap, cudaStream_t cs) {
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, join_tiles_kernel<kBf16>, a, ctas);
 }
-template <int kBits, bool kBf16>
+template <int kBits, bool kBf16, bool kCap, bool kBias>
 cudaError_t launch_dim(const AttendArgs& a, bool overlap, cudaStream_t cs) {
-  return a.dim <= 64 ? launch<kBits, 64, kBf16>(a, overlap, cs) : launch<kBits, 128, kBf16>(a, overlap, cs);
+  return a.dim <= 64 ? launch<kBits, 64, kBf16, kCap, kBias>(a, overlap, cs) : launch<kBits, 128, kBf16, kCap, kBias>(a, overlap, cs);
+}
+template <int kBits, bool kBf16>
+cudaError_t launch_scores(const AttendArgs& a, bool overlap, cudaStream_t cs) {
+  if (a.cap > 0.0f) return a.slopes ? launch_dim<kBits, kBf16, true, true>(a, overlap, cs) : launch_dim<kBits, kBf16, true, false>(a, overlap, cs);
+  return a.slopes ? launch_dim<kBits, kBf16, false, true>(a, overlap, cs) : launch_dim<kBits, kBf16, false, false>(a, overlap, cs);
 }
 
 }  // namespace
 
-cudaError_t launch_attend_tiles(const AttendArgs& args, int bits, int type, bool overlap, cudaStream_t cs) {
-  AttendArgs a = args;
-  a.by_pieces = FastDiv((a.row_bytes + 15) / 16);
-  if (type == LC_TYPE_BF16) return bits == 4 ? launch_dim<4, true>(a, overlap, cs) : launch_dim<8, true>(a, overlap, cs);
-  return bits == 4 ? launch_dim<4, false>(a, overlap, cs) : launch_dim<8, false>(a, overlap, cs);
+cudaError_t launch_attend_tiles(const AttendArgs& a, int bits, int type, bool overlap, cudaStream_t cs) {
+  if (type == LC_TYPE_BF16) return bits == 4 ? launch_scores<4, true>(a, overlap, cs) : launch_scores<8, true>(a, overlap, cs);
+  return bits == 4 ? launch_scores<4, false>(a, overlap, cs) : launch_scores<8, false>(a, overlap, cs);
 }
 
 }  // namespace lc
