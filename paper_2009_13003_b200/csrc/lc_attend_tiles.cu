@@ -4,8 +4,9 @@
 // 128 at a time with a running maximum and sum of each query. Its warps have one task each: four read the keys' codes and four the values', turn them into
 // numbers of the queries' type and store them as operands (both in one layout, rows of 64 values with the 128-byte swizzle: keys are read along a row, values across);
 // one thread issues the products; a warpgroup for each tile takes the scores out of tensor memory, a query a thread, and puts the probabilities back
-// there, over the scores, as the first operand of the product with the values. While one tile's scores are in the warps the products of the other run.
-// The sums of the values stay in tensor memory; they are scaled down only where a maximum rises by more than a factor of 2^kSlack.
+// there, over the scores, as the first operand of the product with the values. Scores go to the warps 64 keys at a time: while one half of a tile is with
+// them, the products of the other half, and of the other tile, run.
+// The sums of the values stay in tensor memory; they are scaled down only where a score exceeds the maximum so far by more than a factor of 2^kSlack.
 //
 // What a code stands for is rounded to the type once. bf16: code / 64 is exact (see lc_attend_rows.cuh) and times the scale rounded; the 64 comes in
 // with the scores' factor, so that nothing overflows. fp16: keys in units of a power of two of their tile, so that no magnitude of them is out of the
@@ -19,7 +20,7 @@
 namespace lc {
 namespace {
 
-constexpr uint32_t kRows = 128, kKeys = 128;            // of a tile of queries, of keys
+constexpr uint32_t kRows = 128, kKeys = 128, kHalf = 64;  // of a tile of queries, of keys, of the keys that are between products and warps at a time
 constexpr uint32_t kSoftmaxWarps = 8, kReadWarps = 4;   // kReadWarps each for keys and for values, then the warp that issues
 constexpr uint32_t kThreads = 32 * (kSoftmaxWarps + 2 * kReadWarps + 4), kReaders = 32 * kReadWarps;
 // Registers of a thread: as launched, and what each warpgroup then has (together no more than before).
@@ -81,31 +82,36 @@ __device__ __forceinline__ uint32_t product_kind(bool bf16, uint32_t n, bool acr
   return 1u << 4 | (uint32_t)bf16 << 7 | (uint32_t)bf16 << 10 | (uint32_t)across << 16 | (n >> 3) << 17 | (kRows >> 4) << 24;
 }
 
-// 32 columns of the 32 lanes of a warp, a lane a thread.
+// 16, 32 or 64 columns of the 32 lanes of a warp, a lane a thread. tensor_loaded: the numbers are there; they go through it, so that nothing that uses them
+// is moved ahead of it. The load of 16 waits itself.
+__device__ __forceinline__ void tensor_load(uint32_t at, uint32_t (&x)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\ttcgen05.wait::ld.sync.aligned;"
+               : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]), "=r"(x[8]), "=r"(x[9]), "=r"(x[10]), "=r"(x[11]), "=r"(x[12]), "=r"(x[13]), "=r"(x[14]), "=r"(x[15])
+               : "r"(at)
+               : "memory");
+}
 __device__ __forceinline__ void tensor_load(uint32_t at, float (&x)[32]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-               : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]), "=f"(x[8]), "=f"(x[9]), "=f"(x[10]), "=f"(x[11]), "=f"(x[12]),
-                 "=f"(x[13]), "=f"(x[14]), "=f"(x[15]), "=f"(x[16]), "=f"(x[17]), "=f"(x[18]), "=f"(x[19]), "=f"(x[20]), "=f"(x[21]), "=f"(x[22]), "=f"(x[23]), "=f"(x[24]),
-                 "=f"(x[25]), "=f"(x[26]), "=f"(x[27]), "=f"(x[28]), "=f"(x[29]), "=f"(x[30]), "=f"(x[31])
+               : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]), "=f"(x[8]), "=f"(x[9]), "=f"(x[10]), "=f"(x[11]), "=f"(x[12]), "=f"(x[13]), "=f"(x[14]), "=f"(x[15]), "=f"(x[16]), "=f"(x[17]), "=f"(x[18]), "=f"(x[19]), "=f"(x[20]), "=f"(x[21]), "=f"(x[22]), "=f"(x[23]), "=f"(x[24]), "=f"(x[25]), "=f"(x[26]), "=f"(x[27]), "=f"(x[28]), "=f"(x[29]), "=f"(x[30]), "=f"(x[31])
                : "r"(at));
 }
-__device__ __forceinline__ void tensor_store(uint32_t at, const float (&x)[32]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"f"(x[0]),
-               "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]), "f"(x[8]), "f"(x[9]), "f"(x[10]), "f"(x[11]), "f"(x[12]), "f"(x[13]), "f"(x[14]), "f"(x[15]),
-               "f"(x[16]), "f"(x[17]), "f"(x[18]), "f"(x[19]), "f"(x[20]), "f"(x[21]), "f"(x[22]), "f"(x[23]), "f"(x[24]), "f"(x[25]), "f"(x[26]), "f"(x[27]), "f"(x[28]), "f"(x[29]),
-               "f"(x[30]), "f"(x[31]), "r"(at)
-               : "memory");
+__device__ __forceinline__ void tensor_load(uint32_t at, float (&x)[64]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];"
+               : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]), "=f"(x[8]), "=f"(x[9]), "=f"(x[10]), "=f"(x[11]), "=f"(x[12]), "=f"(x[13]), "=f"(x[14]), "=f"(x[15]), "=f"(x[16]), "=f"(x[17]), "=f"(x[18]), "=f"(x[19]), "=f"(x[20]), "=f"(x[21]), "=f"(x[22]), "=f"(x[23]), "=f"(x[24]), "=f"(x[25]), "=f"(x[26]), "=f"(x[27]), "=f"(x[28]), "=f"(x[29]), "=f"(x[30]), "=f"(x[31]), "=f"(x[32]), "=f"(x[33]), "=f"(x[34]), "=f"(x[35]), "=f"(x[36]), "=f"(x[37]), "=f"(x[38]), "=f"(x[39]), "=f"(x[40]), "=f"(x[41]), "=f"(x[42]), "=f"(x[43]), "=f"(x[44]), "=f"(x[45]), "=f"(x[46]), "=f"(x[47]), "=f"(x[48]), "=f"(x[49]), "=f"(x[50]), "=f"(x[51]), "=f"(x[52]), "=f"(x[53]), "=f"(x[54]), "=f"(x[55]), "=f"(x[56]), "=f"(x[57]), "=f"(x[58]), "=f"(x[59]), "=f"(x[60]), "=f"(x[61]), "=f"(x[62]), "=f"(x[63])
+               : "r"(at));
+}
+template <int n>
+__device__ __forceinline__ void tensor_loaded(float (&x)[n]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < n; ++i) asm volatile("" : "+f"(x[i]));
 }
 __device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t (&x)[16]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]),
-               "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]), "r"(x[9]), "r"(x[10]), "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15]), "r"(at)
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]), "r"(x[9]), "r"(x[10]), "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15]), "r"(at)
                : "memory");
 }
-// The numbers are there. They go through it, so that nothing that uses them is moved ahead of it.
-__device__ __forceinline__ void tensor_loaded(float (&x)[32]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]), "+f"(x[8]), "+f"(x[9]), "+f"(x[10]), "+f"(x[11]), "+f"(x[12]), "+f"(x[13]), "+f"(x[14]), "+f"(x[15]), "+f"(x[16]), "+f"(x[17]), "+f"(x[18]), "+f"(x[19]), "+f"(x[20]), "+f"(x[21]), "+f"(x[22]), "+f"(x[23]), "+f"(x[24]), "+f"(x[25]), "+f"(x[26]), "+f"(x[27]), "+f"(x[28]), "+f"(x[29]), "+f"(x[30]), "+f"(x[31])
-               :
+__device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t (&x)[32]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]), "r"(x[9]), "r"(x[10]), "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15]), "r"(x[16]), "r"(x[17]), "r"(x[18]), "r"(x[19]), "r"(x[20]), "r"(x[21]), "r"(x[22]), "r"(x[23]), "r"(x[24]), "r"(x[25]), "r"(x[26]), "r"(x[27]), "r"(x[28]), "r"(x[29]), "r"(x[30]), "r"(x[31]), "r"(at)
                : "memory");
 }
 __device__ __forceinline__ void tensor_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -120,6 +126,14 @@ __device__ __forceinline__ uint32_t rounded(float low, float high) {
   return r;
 }
 
+// 16 columns of sums times a number.
+__device__ __forceinline__ void scale_sums(uint32_t at, float down) {
+  uint32_t x[16];
+  tensor_load(at, x);
+#pragma unroll
+  for (uint32_t e = 0; e < 16; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * down);
+  tensor_store(at, x);
+}
 // The bits of the first n of 32.
 __device__ __forceinline__ uint32_t bits_below(int32_t n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1u; }
 __device__ __forceinline__ float max_of(float a, float b, float c) {
@@ -184,7 +198,9 @@ __device__ __forceinline__ Tiles tiles_of(const AttendArgs& A, const Sequence& q
   t.count = q.ahead + max(t.high / kKeys + 1, t.from) - t.from;
   return t;
 }
-__device__ __forceinline__ uint32_t tile_at(uint64_t offset, uint32_t tiles, uint64_t weight) { return offset >= weight ? tiles : (uint32_t)(offset * tiles / weight); }
+__device__ __forceinline__ uint32_t tile_at(uint64_t offset, uint32_t tiles, uint64_t weight) {
+  return offset == 0 ? 0 : offset >= weight ? tiles : (uint32_t)(offset * tiles / weight);
+}
 __device__ __forceinline__ uint64_t share_of(uint64_t all, uint32_t ctas) { return max((all + ctas - 1) / ctas, (uint64_t)(2 * kKeys)); }
 
 // A CTA's way through its share: the blocks of which it has tiles, and which tiles.
@@ -244,12 +260,11 @@ struct Layout {
 
 constexpr unsigned long long kNone = ~0ull;
 struct Shared {
-  unsigned long long full_k[kStages], empty_k[kStages], full_v[kStages], empty_v[kStages], queries[2], scores[2], weights[2], sums[2];  // barriers
+  unsigned long long full_k[kStages], empty_k[kStages], full_v[kStages], empty_v[kStages], queries[2], scores[2][2], weights[2][2], sums[2][2];  // barriers
   unsigned long long scan[kThreads / 32], found_base;
   ulonglong2 places[2][2][kKeys];  // of a tile's keys, for the readers of keys and of values: where codes and scales begin; kNone: zeros
-  uint32_t found, tensor, dead;
+  uint32_t found, tensor, dead, broken;  // broken: a scale of the values so far was no number
   uint32_t most_scale[kMemo][kReadWarps];
-  uint32_t flags[kMemo][kReadWarps];  // whether a scale of the tile's values is no number
 };
 
 // kCap, kBias: scores are capped, lowered by distance.
@@ -395,7 +410,7 @@ struct Kernel {
     begin_next();
 
     if (threadIdx.x == 0) {
-      S.dead = 0;
+      S.dead = S.broken = 0;
       for (uint32_t i = 0; i < kStages; ++i) {
         barrier_init(shared_address(&S.full_k[i]), kReaders);
         barrier_init(shared_address(&S.empty_k[i]), 1);
@@ -404,9 +419,11 @@ struct Kernel {
       }
       for (uint32_t t = 0; t < 2; ++t) {
         barrier_init(shared_address(&S.queries[t]), kRows);
-        barrier_init(shared_address(&S.scores[t]), 1);
-        barrier_init(shared_address(&S.weights[t]), kRows);
-        barrier_init(shared_address(&S.sums[t]), 1);
+        for (uint32_t h = 0; h < 2; ++h) {
+          barrier_init(shared_address(&S.scores[t][h]), 1);
+          barrier_init(shared_address(&S.weights[t][h]), kRows);
+          barrier_init(shared_address(&S.sums[t][h]), 1);
+        }
       }
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -478,7 +495,7 @@ struct Kernel {
     __syncthreads();
     order_after();
     const uint32_t tensor = S.tensor;
-    const float scale = fabsf(A.scale) * (kBf16 ? 64.0f : 1.0f);
+    const float scale = fmaxf(fabsf(A.scale), 1e-30f) * (kBf16 ? 64.0f : 1.0f);  // 0: times -Inf, a key that is not seen, would be no number
     volatile uint32_t* dead = &S.dead;
     Walk walk(A, S.found, from - S.found_base, from, to);
     uint32_t done = 0;  // tiles of keys so far: what the barriers' phases go by
@@ -507,105 +524,82 @@ struct Kernel {
           order_before();  // the sums of the block before are read
           barrier_arrive(shared_address(&S.queries[t]));
           good = false;  // all tiles are through
-          for (uint32_t i = 0; i < n; ++i) {
-            const uint32_t number = done + i, memo = number % kMemo, key = tiles.key(j0 + i);
-            if (!warp_wait(shared_address(&S.scores[t]), number & 1, dead)) break;
+          for (uint32_t i = 0; i < 2 * n; ++i) {
+            const uint32_t number = done + i / 2, half = i & 1, key = tiles.key(j0 + i / 2) + half * kHalf, at = scores + half * kHalf;
+            if (!warp_wait(shared_address(&S.scores[t][half]), number & 1, dead)) break;
             order_after();
-            float x[2][32];
-            tensor_load(scores, x[0]);
+            float y[kHalf];
+            tensor_load(at, y);
             float unit = 1.0f;  // of the tile's keys
-            if constexpr (!kBf16) unit = unit_of(S, memo);
-            const float factor = scale * unit * kLog2e, cap_in = kCap ? 2.0f * factor / A.cap : 0.0f, away = (float)(int32_t)(position - key);
-            // of the tile's keys a query sees those from `begin` on and ahead of `end`, and those ahead of `prefix`
-            const bool full = key + kKeys - 1 <= low && (A.window == 0 || high - key < A.window);
-            const int32_t end = (int32_t)(position - key) + 1, begin = A.window ? end - (int32_t)A.window : 0, prefix = (int32_t)(q.prefix - key);
-            auto seen = [&](uint32_t c) { return (bits_below(end - (int32_t)c) & ~bits_below(begin - (int32_t)c)) | bits_below(prefix - (int32_t)c); };
-            auto hide = [&](float (&y)[32], uint32_t c) {
-              const uint32_t bits = seen(c);
+            if constexpr (!kBf16) unit = unit_of(S, number % kMemo);
+            const float factor = scale * unit * kLog2e;
+            const bool full = key + kHalf - 1 <= low && (A.window == 0 || high - key < A.window);
+            tensor_loaded(y);
+            if constexpr (kCap || kBias) {
+              const float cap_in = kCap ? 2.0f * factor / A.cap : 0.0f, away = (float)(int32_t)(position - key);
 #pragma unroll
-              for (uint32_t e = 0; e < 32; ++e) y[e] = bits >> e & 1 ? y[e] : -INFINITY;
-            };
-            auto capped = [&](float y) {
-              return kCap ? fmaf(-2.0f * cap_out, reciprocal(1.0f + exp2_fast(y * cap_in)), cap_out) : y * factor;
-            };
-            auto score = [&](float y, uint32_t c) { return kBias ? fmaf(-slope, fabsf(away - (float)c), capped(y)) : capped(y); };
-            float top = -INFINITY;
-#pragma unroll
-            for (uint32_t c = 0; c < kKeys / 32; ++c) {
-              float (&y)[32] = x[c & 1];
-              tensor_loaded(y);
-              tensor_load(scores + (c + 1) % (kKeys / 32) * 32, x[(c + 1) & 1]);  // behind the last ones the first again
-              if constexpr (kBias) {
-#pragma unroll
-                for (uint32_t e = 0; e < 32; ++e) y[e] = score(y[e], c * 32 + e);
+              for (uint32_t e = 0; e < kHalf; ++e) {
+                y[e] = kCap ? fmaf(-2.0f * cap_out, reciprocal(1.0f + exp2_fast(y[e] * cap_in)), cap_out) : y[e] * factor;
+                if constexpr (kBias) y[e] = fmaf(-slope, fabsf(away - (float)e), y[e]);
               }
-              if (!full) hide(y, c * 32);
-#pragma unroll
-              for (uint32_t e = 0; e < 32; e += 2) top = max_of(top, y[e], y[e + 1]);
             }
-            if (!kBias && top != -INFINITY) top = capped(top);  // both grow with the product
+            if (!full) {
+              // of these keys a query sees those from `begin` on and ahead of `end`, and those ahead of `prefix`
+              const int32_t end = (int32_t)(position - key) + 1, begin = A.window ? end - (int32_t)A.window : 0, prefix = (int32_t)(q.prefix - key);
+#pragma unroll
+              for (uint32_t c = 0; c < kHalf; c += 32) {
+                const uint32_t seen = (bits_below(end - (int32_t)c) & ~bits_below(begin - (int32_t)c)) | bits_below(prefix - (int32_t)c);
+#pragma unroll
+                for (uint32_t e = 0; e < 32; ++e) y[c + e] = seen >> e & 1 ? y[c + e] : -INFINITY;
+              }
+            }
+            float top = y[0], top2 = y[kHalf / 2];
+#pragma unroll
+            for (uint32_t e = 1; e < kHalf / 2 - 1; e += 2) top = max_of(top, y[e], y[e + 1]), top2 = max_of(top2, y[kHalf / 2 + e], y[kHalf / 2 + e + 1]);
+            top = fmaxf(max_of(top, top2, y[kHalf / 2 - 1]), y[kHalf - 1]);
+            if (!kCap && !kBias) top *= factor;  // grows with the product
             const bool rises = top > m + kSlack;
             if (__any_sync(0xFFFFFFFFu, rises)) {
               const float now = rises ? top : m, down = rises ? exp2_fast(m - now) : 1.0f;
               if (i > 0) {
-                if (!warp_wait(shared_address(&S.sums[t]), (number - 1) & 1, dead)) break;
+                // the product before (the one before that has ended, or these scores would not be there)
+                if (!warp_wait(shared_address(&S.sums[t][1 - half]), (done + (i - 1) / 2) & 1, dead)) break;
                 order_after();
 #pragma unroll 1
-                for (uint32_t c = 0; c < DP; c += 32) {
-                  float y[32];
-                  tensor_load(sums + c, y);
-                  tensor_loaded(y);
-#pragma unroll
-                  for (uint32_t e = 0; e < 32; ++e) y[e] *= down;
-                  tensor_store(sums + c, y);
-                }
+                for (uint32_t d = 0; d < DP; d += 16) scale_sums(sums + d, down);
               }
               m = now;
               l = mul_two(l, two(down, down));
             }
             const float base = (m == -INFINITY ? 0.0f : m) - kLift;
+            uint32_t p[kHalf / 2];
 #pragma unroll
-            for (uint32_t c = 0; c < kKeys / 32; ++c) {
-              float (&y)[32] = x[c & 1];
-              tensor_loaded(y);
-              if (c + 1 < kKeys / 32) tensor_load(scores + (c + 1) * 32, x[(c + 1) & 1]);
-              if constexpr (!kCap && !kBias) {
-#pragma unroll
-                for (uint32_t e = 0; e < 32; e += 2) split_two(fma_two(two(y[e], y[e + 1]), two(factor, factor), two(-base, -base)), y[e], y[e + 1]);
-              } else {
-#pragma unroll
-                for (uint32_t e = 0; e < 32; ++e) y[e] = score(y[e], c * 32 + e) - base;
-              }
-              if (!full) hide(y, c * 32);
-              uint32_t p[16];
-#pragma unroll
-              for (uint32_t e = 0; e < 32; e += 2) {
-                y[e] = exp2_fast(y[e]), y[e + 1] = exp2_fast(y[e + 1]);
-                l = add_two(l, two(y[e], y[e + 1]));
-                p[e / 2] = rounded<kBf16>(y[e], y[e + 1]);
-              }
-              tensor_store(scores + c * 16, p);
+            for (uint32_t e = 0; e < kHalf; e += 2) {
+              if constexpr (!kCap && !kBias) split_two(fma_two(two(y[e], y[e + 1]), two(factor, factor), two(-base, -base)), y[e], y[e + 1]);
+              else split_two(add_two(two(y[e], y[e + 1]), two(-base, -base)), y[e], y[e + 1]);
+              y[e] = exp2_fast(y[e]), y[e + 1] = exp2_fast(y[e + 1]);
+              l = add_two(l, two(y[e], y[e + 1]));
+              p[e / 2] = rounded<kBf16>(y[e], y[e + 1]);
             }
+            tensor_store(at, p);
             tensor_stored();
             order_before();
-            barrier_arrive(shared_address(&S.weights[t]));
-            if (!warp_wait(shared_address(&S.full_v[number % kStages]), number / kStages & 1, dead)) break;
-            good = i + 1 == n;
-            uint32_t flags = 0;
-#pragma unroll
-            for (uint32_t w = 0; w < kReadWarps; ++w) flags |= S.flags[memo][w];
-            if (flags) {  // some value of the tile is no number: which of them this query sees
-              for (uint32_t k = 0; k < kKeys && key + k < q.length; ++k) {
-                const unsigned long long place = look_up(A, q, s, head, key + k);
-                if (place == kNone || !(seen(k) & 1)) continue;
+            barrier_arrive(shared_address(&S.weights[t][half]));
+            good = i + 1 == 2 * n;
+          }
+          for (uint32_t h = 0; h < 2; ++h) good = good && warp_wait(shared_address(&S.sums[t][h]), (done + n - 1) & 1, dead);
+          if (good) {
+            order_after();
+            if (S.broken) {  // some value was no number: which of this block's are, and this query sees
+              for (uint32_t k = 0; k < n * kKeys; ++k) {
+                const uint32_t at_key = tiles.key(j0 + k / kKeys) + k % kKeys;
+                const bool visible = (at_key <= position && (A.window == 0 || position - at_key < A.window)) || at_key < q.prefix;
+                const unsigned long long place = look_up(A, q, s, head, at_key);
+                if (place == kNone || !visible) continue;
                 for (uint32_t g = 0; g < A.groups; ++g)
                   if ((A.scales[A.plane_scales + place * A.groups + g] & 0x7F80u) == 0x7F80u) broken |= 1u << g;
               }
             }
-          }
-          good = good && warp_wait(shared_address(&S.sums[t]), (done + n - 1) & 1, dead);
-          if (good) {
-            order_after();
             const bool whole = j0 == 0 && n == tiles.count, there = token < q.rows;
             float* part = A.parts + (2ull * blockIdx.x + (walk.first ? 0 : 1)) * (kTilePartBytes / 4);
             T* out = static_cast<T*>(A.out) + (uint64_t)(q.row + min(token, q.rows - 1)) * A.out_row + (uint64_t)(head * A.shared + in_group) * A.out_head;
@@ -687,8 +681,7 @@ struct Kernel {
               bool flag = false;
 #pragma unroll
               for (uint32_t x = 0; x < kUnits; ++x) flag |= (c.scale[x] & 0x7F80u) == 0x7F80u;
-              flag = __any_sync(0xFFFFFFFFu, flag);
-              if (lane == 0) S.flags[memo][mine] = flag;
+              if (flag) S.broken = 1;
             } else if constexpr (!kBf16) {
               uint32_t most = 0;
 #pragma unroll
@@ -723,26 +716,26 @@ struct Kernel {
       if (warp == kSoftmaxWarps + 2 * kReadWarps) {
         // ---- the products: the warp as a whole goes through the tiles, with numbers that the compiler knows to be the same for all lanes; one lane issues
         const uint32_t all_lanes = 0xFFFFFFFFu, at_tensor = __shfl_sync(all_lanes, tensor, 0);
-        const uint32_t steps = (A.dim + 15) / 16, scores_kind = product_kind(kBf16, kKeys, false), sums_kind = product_kind(kBf16, steps * 16, true);
+        const uint32_t steps = (A.dim + 15) / 16, scores_kind = product_kind(kBf16, kHalf, false), sums_kind = product_kind(kBf16, steps * 16, true);
         const uint32_t query_at = operand_at(shared_address(queries), 16), key_at = operand_at(shared_address(keys), 16), value_at = operand_at(shared_address(values), kKeys * 128);
-        auto multiply_keys = [&](uint32_t t, uint32_t stage, bool last) {
-          const uint32_t a = query_at + t * (L::kQueries >> 4), b = key_at + stage * (L::kOperand >> 4), d = at_tensor + L::kScoresAt + t * kKeys;
+        auto multiply_keys = [&](uint32_t t, uint32_t half, uint32_t stage) {
+          const uint32_t a = query_at + t * (L::kQueries >> 4), b = key_at + stage * (L::kOperand >> 4) + half * (kHalf * 128 >> 4), d = at_tensor + L::kScoresAt + t * kKeys + half * kHalf;
           if (one_lane()) {
 #pragma unroll
             for (uint32_t x = 0; x < DP / 16; ++x)
               if (x < steps) product(d, a + ((x / 4) * (kRows * 128) + (x % 4) * 32 >> 4), b + ((x / 4) * (kKeys * 128) + (x % 4) * 32 >> 4), scores_kind, x > 0);
-            commit_to(shared_address(&S.scores[t]));
-            if (last) commit_to(shared_address(&S.empty_k[stage]));
+            commit_to(shared_address(&S.scores[t][half]));
+            if (t & half) commit_to(shared_address(&S.empty_k[stage]));
           }
           __syncwarp();
         };
-        auto multiply_values = [&](uint32_t t, uint32_t stage, bool add, bool last) {
-          const uint32_t a = at_tensor + L::kScoresAt + t * kKeys, b = value_at + stage * (L::kOperand >> 4), d = at_tensor + L::kSumsAt + t * DP;
+        auto multiply_values = [&](uint32_t t, uint32_t half, uint32_t stage, bool add) {
+          const uint32_t a = at_tensor + L::kScoresAt + t * kKeys + half * kHalf, b = value_at + stage * (L::kOperand >> 4) + half * (kHalf * 128 >> 4), d = at_tensor + L::kSumsAt + t * DP;
           if (one_lane()) {
 #pragma unroll
-            for (uint32_t x = 0; x < kKeys / 16; ++x) product_of_tensor(d, a + x * 8, b + (x * 2048 >> 4), sums_kind, add || x > 0);
-            commit_to(shared_address(&S.sums[t]));
-            if (last) commit_to(shared_address(&S.empty_v[stage]));
+            for (uint32_t x = 0; x < kHalf / 16; ++x) product_of_tensor(d, a + x * 8, b + (x * 2048 >> 4), sums_kind, add || x > 0);
+            commit_to(shared_address(&S.sums[t][half]));
+            if (t & half) commit_to(shared_address(&S.empty_v[stage]));
           }
           __syncwarp();
         };
@@ -750,25 +743,26 @@ struct Kernel {
         for (uint32_t count = 0; good && walk.next(A); ++count) {
           const uint32_t n = __shfl_sync(all_lanes, walk.n, 0);
           good = warp_wait(shared_address(&S.full_k[done % kStages]), done / kStages & 1, dead);
-          for (uint32_t t = 0; t < 2 && good; ++t) {
-            good = warp_wait(shared_address(&S.queries[t]), count & 1, dead);
+          for (uint32_t x = 0; x < 4 && good; ++x) {
+            if (x < 2) good = warp_wait(shared_address(&S.queries[x]), count & 1, dead);
             if (!good) break;
             order_after();
-            multiply_keys(t, done % kStages, t == 1);
+            multiply_keys(x & 1, x >> 1, done % kStages);
           }
           for (uint32_t i = 0; i < n && good; ++i) {
             const uint32_t number = done + i, stage = number % kStages, behind = (number + 1) % kStages;
             good = warp_wait(shared_address(&S.full_v[stage]), number / kStages & 1, dead);
-            for (uint32_t t = 0; t < 2 && good; ++t) {
-              good = warp_wait(shared_address(&S.weights[t]), number & 1, dead);
+            for (uint32_t x = 0; x < 4 && good; ++x) {
+              const uint32_t t = x & 1, half = x >> 1;
+              good = warp_wait(shared_address(&S.weights[t][half]), number & 1, dead);
               if (!good) break;
               order_after();
-              multiply_values(t, stage, i > 0, t == 1);
+              multiply_values(t, half, stage, i > 0 || half > 0);
               if (i + 1 < n) {
-                if (t == 0) good = warp_wait(shared_address(&S.full_k[behind]), (number + 1) / kStages & 1, dead);
+                if (x == 0) good = warp_wait(shared_address(&S.full_k[behind]), (number + 1) / kStages & 1, dead);
                 if (!good) break;
                 order_after();
-                multiply_keys(t, behind, t == 1);
+                multiply_keys(t, half, behind);
               }
             }
           }
