@@ -94,7 +94,7 @@ int lc_cache_attend(const lc_cache* cache, const lc_rows* q, const lc_rows* out,
   a.by_pieces = FastDiv(a.row_bytes / (piece > 16 ? 16 : piece));
   const int bits = (int)cache->bits;
   cudaError_t e = cudaSuccess;
-  const bool tiles = type != LC_TYPE_F32 && a.dim <= kTileDim && (uint64_t)a.most * a.shared > kFewQueries;
+  const bool tiles = type != LC_TYPE_F32 && a.dim <= kTileDim && cache->slots < 0xFFFFFFFFull / cache->heads && (uint64_t)a.most * a.shared > kFewQueries;
   if (tiles) a.longest = kFewQueries / a.shared;
   if (a.longest > 0) e = type == LC_TYPE_BF16 ? launch_attend_bf16(a, bits, cs) : type == LC_TYPE_F16 ? launch_attend_f16(a, bits, cs) : launch_attend_f32(a, bits, cs);
   if (tiles && e == cudaSuccess) {

@@ -26,7 +26,7 @@ constexpr uint32_t kThreads = 32 * (kSoftmaxWarps + 2 * kReadWarps + 4), kReader
 // Registers of a thread: as launched, and what each warpgroup then has (together no more than before).
 constexpr uint32_t kRegsAtLaunch = 96, kRegsSoftmax = 136, kRegsReader = 80, kRegsIssue = 48;
 static_assert(2 * kRegsSoftmax + 2 * kRegsReader + kRegsIssue <= 5 * kRegsAtLaunch && kThreads == 5 * 128, "registers of five warpgroups");
-static_assert(kReaders == kKeys, "a reader looks up a key");
+static_assert(kReaders == kKeys && kHalf == 64, "a reader looks up a key; a half of a tile is that of two warps");
 constexpr uint32_t kStages = 2;
 constexpr uint32_t kMemo = 4;                           // tiles whose exponents and flags are kept: the scores of a tile are done before the third behind it is read
 constexpr float kSlack = 8.0f;
@@ -258,13 +258,12 @@ struct Layout {
   static constexpr uint32_t kScoresAt = 0, kSumsAt = 2 * kKeys;      // columns of tensor memory; the second tile's kKeys and DP columns behind
 };
 
-constexpr unsigned long long kNone = ~0ull;
+constexpr uint32_t kNone = ~0u;  // a key without a place
 struct Shared {
   unsigned long long full_k[kStages], empty_k[kStages], full_v[kStages], empty_v[kStages], queries[2], scores[2][2], weights[2][2], sums[2][2];  // barriers
   unsigned long long scan[kThreads / 32], found_base;
-  ulonglong2 places[2][2][kKeys];  // of a tile's keys, for the readers of keys and of values: where codes and scales begin; kNone: zeros
   uint32_t found, tensor, dead, broken;  // broken: a scale of the values so far was no number
-  uint32_t most_scale[kMemo][kReadWarps];
+  float units[kMemo][kReadWarps];  // fp16: the power of two that 32 keys of a tile are in units of, from the largest of their scales
 };
 
 // kCap, kBias: scores are capped, lowered by distance.
@@ -299,48 +298,57 @@ struct Kernel {
     }
   }
 
-  // A reader takes one piece of 16 bytes of several keys' codes: of keys first + i * kStep. Lanes are dealt to pieces and keys so that eight lanes in a
-  // row store to different banks: 8 bits, four pieces of two neighbouring keys (their runs of eight values are every other one, which the
-  // swizzle puts into the even and the odd places), 4 bits, two pieces of four.
-  static constexpr uint32_t kStep = 32 / kUnits * kReadWarps;
+  // A warp of readers takes 32 keys of a tile: its lanes look up a key each, and a lane takes one piece of 16 bytes of kUnits keys, kStep apart. Lanes are
+  // dealt to pieces and keys so that eight lanes in a row store to different banks: 8 bits, four pieces of two neighbouring keys (their runs of eight
+  // values are every other one, which the swizzle puts into the even and the odd places), 4 bits, two pieces of four.
+  static constexpr uint32_t kStep = 32 / kUnits, kRuns = 16 / kBits;  // kRuns: of eight values in a piece
   struct Reader {
-    uint32_t first, part, group;
-    bool there;
+    uint32_t row, left;            // first key; words of the row from the piece on
+    uint32_t at[kRuns];            // where its runs go for the first key
+    const uint8_t* codes;
+    const unsigned short* scales;
   };
-  static __device__ __forceinline__ Reader reader_of(const AttendArgs& A, uint32_t warp, uint32_t lane) {
+  static __device__ __forceinline__ Reader reader_of(const AttendArgs& A, uint32_t set, uint32_t warp, uint32_t lane) {
     Reader r;
-    uint32_t row;
-    if (kBits == 8) r.part = kUnits == 8 ? (lane & 3) | (lane >> 1 & 4) : lane & 3, row = kUnits == 8 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
-    else r.part = kUnits == 4 ? (lane & 1) | (lane >> 2 & 2) : lane & 1, row = kUnits == 4 ? (lane >> 1 & 3) | (lane >> 2 & 4) : lane >> 1;
-    r.first = warp * (32 / kUnits) + row;
-    r.there = r.part * 16 < A.row_bytes;
-    r.group = r.part / (A.per_group * (kBits == 8 ? 2 : 1));
+    uint32_t part;
+    if (kBits == 8) part = kUnits == 8 ? (lane & 3) | (lane >> 1 & 4) : lane & 3, r.row = kUnits == 8 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
+    else part = kUnits == 4 ? (lane & 1) | (lane >> 2 & 2) : lane & 1, r.row = kUnits == 4 ? (lane >> 1 & 3) | (lane >> 2 & 4) : lane >> 1;
+    r.left = part * 16 < A.row_bytes ? (A.row_bytes - part * 16) / 4 : 0;
+    r.codes = A.codes + (set ? A.plane_codes : 0) + (r.left ? part * 16 : 0);  // behind the row's end: read, not used
+    r.scales = A.scales + (set ? A.plane_scales : 0) + (r.left ? part / (A.per_group * (kBits == 8 ? 2 : 1)) : 0);
+#pragma unroll
+    for (uint32_t k = 0; k < kRuns; ++k) {
+      const uint32_t n = part * kRuns + k;
+      r.at[k] = (n / 8) * (kKeys * 128) + (warp * 32 + r.row) * 128 + (((n & 7) ^ (r.row & 7)) << 4);
+    }
     return r;
   }
   struct Codes {
     uint4 w[kUnits];
-    unsigned short scale[kUnits];
+    uint32_t scale[kUnits];
   };
-  static __device__ __forceinline__ void read_codes(const AttendArgs& A, const ulonglong2* places, const uint8_t* codes, const unsigned short* scales, const Reader& r, Codes& c) {
-    if (!r.there) return;
-    codes += r.part * 16;
-    scales += r.group;
-    const bool whole = (A.row_bytes & 15) == 0;
-    const uint32_t left = (A.row_bytes - r.part * 16) / 4;
+  // The pieces of a tile's keys and their scales on their way; place: of the lane's key.
+  template <uint32_t kFrom, uint32_t kTo>
+  static __device__ __forceinline__ void read_codes(const AttendArgs& A, uint32_t place, const Reader& r, Codes& c) {
+    uint32_t at[kTo - kFrom];
 #pragma unroll
-    for (uint32_t i = 0; i < kUnits; ++i) {
-      const ulonglong2 place = places[r.first + i * kStep];
-      const uint8_t* p = codes + place.x;
-      c.scale[i] = 0;
-      if (place.y != kNone) c.scale[i] = __ldg(scales + place.y);
-      if (whole) {
-        c.w[i] = __ldg(reinterpret_cast<const uint4*>(p));
-      } else {
-        const uint32_t* x = reinterpret_cast<const uint32_t*>(p);
+    for (uint32_t i = kFrom; i < kTo; ++i) {
+      at[i - kFrom] = __shfl_sync(0xFFFFFFFFu, place, r.row + i * kStep);
+      c.scale[i] = 0;  // keys without a place are read from the first one, and count as zeros
+      if (at[i - kFrom] != kNone) c.scale[i] = __ldg(r.scales + (uint64_t)at[i - kFrom] * A.groups);
+      else at[i - kFrom] = 0;
+    }
+    if ((A.row_bytes & 15) == 0) {
+#pragma unroll
+      for (uint32_t i = kFrom; i < kTo; ++i) c.w[i] = __ldg(reinterpret_cast<const uint4*>(r.codes + (uint64_t)at[i - kFrom] * A.row_bytes));
+    } else {
+#pragma unroll
+      for (uint32_t i = kFrom; i < kTo; ++i) {
+        const uint32_t* x = reinterpret_cast<const uint32_t*>(r.codes + (uint64_t)at[i - kFrom] * A.row_bytes);
         c.w[i].x = __ldg(x);
-        c.w[i].y = left > 1 ? __ldg(x + 1) : 0u;
-        c.w[i].z = left > 2 ? __ldg(x + 2) : 0u;
-        c.w[i].w = left > 3 ? __ldg(x + 3) : 0u;
+        c.w[i].y = r.left > 1 ? __ldg(x + 1) : 0u;
+        c.w[i].z = r.left > 2 ? __ldg(x + 2) : 0u;
+        c.w[i].w = r.left > 3 ? __ldg(x + 3) : 0u;
       }
     }
   }
@@ -369,25 +377,25 @@ struct Kernel {
     }
     return make_uint4(r[0], r[1], r[2], r[3]);
   }
-  // down: what the scales are multiplied by (fp16). values: scales that are no numbers count as 0.
-  static __device__ __forceinline__ void store_numbers(const Codes& c, bool values, float down, const Reader& r, uint8_t* operand) {
-    if (!r.there) return;
+  // down: what the scales are multiplied by (fp16).
+  template <uint32_t kFrom, uint32_t kTo>
+  static __device__ __forceinline__ void store_numbers(const Codes& c, float down, const Reader& r, uint32_t operand) {
+    if (r.left == 0) return;
 #pragma unroll
-    for (uint32_t i = 0; i < kUnits; ++i) {
-      const uint32_t row = r.first + i * kStep;
-      uint32_t s = c.scale[i];
-      if (values && (s & 0x7F80u) == 0x7F80u) s = 0;
-      s = kBf16 ? s | s << 16 : __float_as_uint(__uint_as_float(s << 16) * down);
+    for (uint32_t i = kFrom; i < kTo; ++i) {
+      const uint32_t s = kBf16 ? c.scale[i] | c.scale[i] << 16 : __float_as_uint(__uint_as_float(c.scale[i] << 16) * down);
       const uint32_t w[4] = {c.w[i].x, c.w[i].y, c.w[i].z, c.w[i].w};
-      uint8_t* to = operand + row * 128;
 #pragma unroll
-      for (uint32_t k = 0; k < 16 / kBits; ++k) {  // 8 bits: two runs of eight values, 4 bits: four
-        const uint32_t n = r.part * (16 / kBits) + k;
-        *reinterpret_cast<uint4*>(to + (n / 8) * (kKeys * 128) + (((n & 7) ^ (row & 7)) << 4)) = kBits == 8 ? numbers(w[2 * k], w[2 * k + 1], s) : numbers(w[k], 0, s);
+      for (uint32_t k = 0; k < kRuns; ++k) {
+        const uint4 x = kBits == 8 ? numbers(w[2 * k], w[2 * k + 1], s) : numbers(w[k], 0, s);
+        // kStep 4: every second key's places are the others of the swizzle's upper bit (its row's number differs by 4)
+        const uint32_t at = operand + (kStep == 4 && (i & 1) ? r.at[k] ^ 64u : r.at[k]) + i * (kStep * 128);
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
       }
     }
   }
-  static __device__ __forceinline__ unsigned long long look_up(const AttendArgs& A, const Sequence& q, uint32_t s, uint32_t head, uint32_t key) {
+  // Where a key lies: slot * heads + head, which is below 2^32 in this kernel.
+  static __device__ __forceinline__ uint32_t look_up(const AttendArgs& A, const Sequence& q, uint32_t s, uint32_t head, uint32_t key) {
     if (key >= q.length) return kNone;
     const uint32_t page = A.by_page.div(key);
     const int32_t number = __ldg(A.table + s * A.table_stride + page);
@@ -396,7 +404,7 @@ struct Kernel {
       if (A.status) set_status(A.status, LC_ERR_INDEX);
       return kNone;
     }
-    return (unsigned long long)slot * A.heads + head;
+    return (uint32_t)slot * A.heads + head;
   }
 
   static __device__ __forceinline__ void run(const AttendArgs& A) {
@@ -530,16 +538,15 @@ struct Kernel {
             order_after();
             float y[kHalf];
             tensor_load(at, y);
-            float unit = 1.0f;  // of the tile's keys
-            if constexpr (!kBf16) unit = unit_of(S, number % kMemo);
-            const float factor = scale * unit * kLog2e;
+            // of the first and of the last 32 keys
+            const float factor[2] = {scale * kLog2e * (kBf16 ? 1.0f : S.units[number % kMemo][2 * half]), scale * kLog2e * (kBf16 ? 1.0f : S.units[number % kMemo][2 * half + 1])};
             const bool full = key + kHalf - 1 <= low && (A.window == 0 || high - key < A.window);
             tensor_loaded(y);
             if constexpr (kCap || kBias) {
-              const float cap_in = kCap ? 2.0f * factor / A.cap : 0.0f, away = (float)(int32_t)(position - key);
+              const float cap_in[2] = {kCap ? 2.0f * factor[0] / A.cap : 0.0f, kCap ? 2.0f * factor[1] / A.cap : 0.0f}, away = (float)(int32_t)(position - key);
 #pragma unroll
               for (uint32_t e = 0; e < kHalf; ++e) {
-                y[e] = kCap ? fmaf(-2.0f * cap_out, reciprocal(1.0f + exp2_fast(y[e] * cap_in)), cap_out) : y[e] * factor;
+                y[e] = kCap ? fmaf(-2.0f * cap_out, reciprocal(1.0f + exp2_fast(y[e] * cap_in[e / 32])), cap_out) : y[e] * factor[e / 32];
                 if constexpr (kBias) y[e] = fmaf(-slope, fabsf(away - (float)e), y[e]);
               }
             }
@@ -556,8 +563,9 @@ struct Kernel {
             float top = y[0], top2 = y[kHalf / 2];
 #pragma unroll
             for (uint32_t e = 1; e < kHalf / 2 - 1; e += 2) top = max_of(top, y[e], y[e + 1]), top2 = max_of(top2, y[kHalf / 2 + e], y[kHalf / 2 + e + 1]);
-            top = fmaxf(max_of(top, top2, y[kHalf / 2 - 1]), y[kHalf - 1]);
-            if (!kCap && !kBias) top *= factor;  // grows with the product
+            top = fmaxf(top, y[kHalf / 2 - 1]), top2 = fmaxf(top2, y[kHalf - 1]);
+            if (kCap || kBias) top = fmaxf(top, top2);
+            else top = fmaxf(top * factor[0], top2 * factor[1]);  // grows with the product
             const bool rises = top > m + kSlack;
             if (__any_sync(0xFFFFFFFFu, rises)) {
               const float now = rises ? top : m, down = rises ? exp2_fast(m - now) : 1.0f;
@@ -575,7 +583,7 @@ struct Kernel {
             uint32_t p[kHalf / 2];
 #pragma unroll
             for (uint32_t e = 0; e < kHalf; e += 2) {
-              if constexpr (!kCap && !kBias) split_two(fma_two(two(y[e], y[e + 1]), two(factor, factor), two(-base, -base)), y[e], y[e + 1]);
+              if constexpr (!kCap && !kBias) split_two(fma_two(two(y[e], y[e + 1]), two(factor[e / 32], factor[e / 32]), two(-base, -base)), y[e], y[e + 1]);
               else split_two(add_two(two(y[e], y[e + 1]), two(-base, -base)), y[e], y[e + 1]);
               y[e] = exp2_fast(y[e]), y[e + 1] = exp2_fast(y[e + 1]);
               l = add_two(l, two(y[e], y[e + 1]));
@@ -594,10 +602,10 @@ struct Kernel {
               for (uint32_t k = 0; k < n * kKeys; ++k) {
                 const uint32_t at_key = tiles.key(j0 + k / kKeys) + k % kKeys;
                 const bool visible = (at_key <= position && (A.window == 0 || position - at_key < A.window)) || at_key < q.prefix;
-                const unsigned long long place = look_up(A, q, s, head, at_key);
+                const uint32_t place = look_up(A, q, s, head, at_key);
                 if (place == kNone || !visible) continue;
                 for (uint32_t g = 0; g < A.groups; ++g)
-                  if ((A.scales[A.plane_scales + place * A.groups + g] & 0x7F80u) == 0x7F80u) broken |= 1u << g;
+                  if ((A.scales[A.plane_scales + (uint64_t)place * A.groups + g] & 0x7F80u) == 0x7F80u) broken |= 1u << g;
               }
             }
             const bool whole = j0 == 0 && n == tiles.count, there = token < q.rows;
@@ -648,68 +656,59 @@ struct Kernel {
         done += n;
       }
     } else if (warp < kSoftmaxWarps + 2 * kReadWarps) {
+      // ---- codes to operands
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsReader));
+      const uint32_t set = (warp - kSoftmaxWarps) / kReadWarps, mine = (warp - kSoftmaxWarps) % kReadWarps;  // set: 0 keys, 1 values
+      const uint32_t operands = shared_address(set ? values : keys);
+      unsigned long long* const full = set ? S.full_v : S.full_k;
+      unsigned long long* const empty = set ? S.empty_v : S.empty_k;
+      const Reader R = reader_of(A, set, mine, lane);
       bool good = true;
       while (good && walk.next(A)) {
-        const Sequence& q = walk.q;
-        const Tiles& tiles = walk.tiles;
-        const uint32_t head = walk.head, j0 = walk.j0, n = walk.n, s = walk.s;
-        {
-          // ---- codes to operands
-          const uint32_t set = (warp - kSoftmaxWarps) / kReadWarps, mine = (warp - kSoftmaxWarps) % kReadWarps, reader = mine * 32 + lane;  // set: 0 keys, 1 values
-          const uint8_t* codes = A.codes + (set ? A.plane_codes : 0);
-          const unsigned short* scales = A.scales + (set ? A.plane_scales : 0);
-          uint8_t* operands = set ? values : keys;
-          unsigned long long* const full = set ? S.full_v : S.full_k;
-          unsigned long long* const empty = set ? S.empty_v : S.empty_k;
-          const Reader R = reader_of(A, mine, lane);
-          auto meet = [&] { asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + set), "n"(kReaders) : "memory"); };
-          auto look = [&](uint32_t i) {
-            const unsigned long long place = i < n ? look_up(A, q, s, head, tiles.key(j0 + i) + reader) : kNone;
-            return place == kNone ? make_ulonglong2(0, kNone) : make_ulonglong2(place * A.row_bytes, place * A.groups);
-          };
-          Codes c = {};
-          S.places[set][0][reader] = look(0);
-          ulonglong2 next = look(1);
-          meet();
-          read_codes(A, S.places[set][0], codes, scales, R, c);
-          for (uint32_t i = 0; i < n; ++i) {
-            const uint32_t number = done + i, stage = number % kStages, turn = number / kStages, memo = number % kMemo;
-            S.places[set][(i + 1) & 1][reader] = next;
-            float down = 1.0f;
-            if (set) {
-              bool flag = false;
+        const uint32_t n = walk.n;
+        auto look = [&](uint32_t i) { return i < n ? look_up(A, walk.q, walk.s, walk.head, walk.tiles.key(walk.j0 + i) + mine * 32 + lane) : kNone; };
+        Codes c;
+        uint32_t next = look(0);
+        read_codes<0, kUnits>(A, next, R, c);
+        next = look(1);
+        for (uint32_t i = 0; i < n; ++i) {
+          const uint32_t number = done + i, stage = number % kStages, turn = number / kStages;
+          if (turn > 0) good = warp_wait(shared_address(&empty[stage]), (turn - 1) & 1, dead);
+          if (!good) break;
+          // scales that are no numbers: hardly ever
+          uint32_t most = 0;
 #pragma unroll
-              for (uint32_t x = 0; x < kUnits; ++x) flag |= (c.scale[x] & 0x7F80u) == 0x7F80u;
-              if (flag) S.broken = 1;
-            } else if constexpr (!kBf16) {
-              uint32_t most = 0;
+          for (uint32_t x = 0; x < kUnits; ++x) most = max(most, c.scale[x] & 0x7FFFu);
+          if (set) {
+            if (most >= 0x7F80u) {
+              S.broken = 1;
 #pragma unroll
-              for (uint32_t x = 0; x < kUnits; ++x)
-                if ((c.scale[x] & 0x7F80u) != 0x7F80u) most = max(most, (uint32_t)c.scale[x]);
-              most = __reduce_max_sync(0xFFFFFFFFu, most);
-              if (lane == 0) S.most_scale[memo][mine] = most;
+              for (uint32_t x = 0; x < kUnits; ++x) c.scale[x] = (c.scale[x] & 0x7FFFu) >= 0x7F80u ? 0 : c.scale[x];
             }
-            meet();
-            next = look(i + 2);
-            if (!kBf16 && !set) down = 1.0f / unit_of(S, memo);
-            if (good && turn > 0) good = barrier_wait(shared_address(&empty[stage]), (turn - 1) & 1, dead);
-            if (good) {
-              store_numbers(c, set, down, R, operands + stage * L::kOperand);
-              order_for_products();
-              barrier_arrive(shared_address(&full[stage]));
-            }
-            if (i + 1 < n) read_codes(A, S.places[set][(i + 1) & 1], codes, scales, R, c);
+            __syncwarp();
           }
+          float down = 1.0f;
+          if (!kBf16 && !set) {  // the unit of these 32 keys
+            if (most >= 0x7F80u) {
+              most = 0;
+#pragma unroll
+              for (uint32_t x = 0; x < kUnits; ++x) most = max(most, (c.scale[x] & 0x7FFFu) >= 0x7F80u ? 0 : c.scale[x] & 0x7FFFu);
+            }
+            most = __reduce_max_sync(0xFFFFFFFFu, most);
+            const float unit = most ? __uint_as_float(min(max(most << 16 & 0x7F800000u, 0x01000000u), 0x7E000000u)) : 1.0f;
+            if (lane == 0) S.units[number % kMemo][mine] = unit;
+            down = 1.0f / unit;
+          }
+          const uint32_t operand = operands + stage * L::kOperand;
+          store_numbers<0, kUnits / 2>(c, down, R, operand);
+          if (i + 1 < n) read_codes<0, kUnits / 2>(A, next, R, c);
+          store_numbers<kUnits / 2, kUnits>(c, down, R, operand);
+          order_for_products();
+          barrier_arrive(shared_address(&full[stage]));
+          if (i + 1 < n) read_codes<kUnits / 2, kUnits>(A, next, R, c);
+          next = look(i + 2);
         }
         done += n;
-        // the places are read; the readers go on together or not at all
-        uint32_t together;
-        asm volatile("{ .reg .pred p, r; setp.ne.b32 p, %3, 0; barrier.cta.red.and.pred r, %1, %2, p; selp.u32 %0, 1, 0, r; }"
-                     : "=r"(together)
-                     : "r"(1 + (warp - kSoftmaxWarps) / kReadWarps), "n"(kReaders), "r"((uint32_t)good)
-                     : "memory");
-        good = together;
       }
     } else {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
@@ -775,14 +774,6 @@ struct Kernel {
     if (threadIdx.x == 0 && S.dead && A.status) set_status(A.status, LC_ERR_TIMEOUT);
     if (warp == kSoftmaxWarps + 2 * kReadWarps) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(S.tensor), "n"(512) : "memory");
     wait_previous();
-  }
-
-  // fp16: the power of two that a tile's keys are in units of, from the largest of their scales.
-  static __device__ __forceinline__ float unit_of(const Shared& S, uint32_t memo) {
-    uint32_t most = 0;
-#pragma unroll
-    for (uint32_t w = 0; w < kReadWarps; ++w) most = max(most, S.most_scale[memo][w]);
-    return most ? __uint_as_float(min(max(most << 16 & 0x7F800000u, 0x01000000u), 0x7E000000u)) : 1.0f;
   }
 };
 
