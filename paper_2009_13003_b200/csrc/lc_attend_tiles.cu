@@ -3,7 +3,7 @@
 // A CTA takes blocks of 256 queries of one head of the cache (its tokens, times the heads that share it) as two tiles of 128, and goes through the keys
 // 128 at a time with a running maximum and sum of each query. Its warps have one task each: four read the keys' codes and four the values', turn them into
 // numbers of the queries' type and store them as operands (both in one layout, rows of 64 values with the 128-byte swizzle: keys are read along a row, values across);
-// one thread issues the products; a warpgroup for each tile takes the scores out of tensor memory, a query a thread, and puts the probabilities back
+// a thread for each tile issues its products; a warpgroup for each tile takes the scores out of tensor memory, a query a thread, and puts the probabilities back
 // there, over the scores, as the first operand of the product with the values. Scores go to the warps 64 keys at a time: while one half of a tile is with
 // them, the products of the other half, and of the other tile, run.
 // The sums of the values stay in tensor memory; they are scaled down only where a score exceeds the maximum so far by more than a factor of 2^kSlack.
@@ -24,11 +24,13 @@ constexpr uint32_t kRows = 128, kKeys = 128, kHalf = 64;  // of a tile of querie
 constexpr uint32_t kSoftmaxWarps = 8, kReadWarps = 4;   // kReadWarps each for keys and for values, then the warp that issues
 constexpr uint32_t kThreads = 32 * (kSoftmaxWarps + 2 * kReadWarps + 4), kReaders = 32 * kReadWarps;
 // Registers of a thread: as launched, and what each warpgroup then has (together no more than before).
-constexpr uint32_t kRegsAtLaunch = 96, kRegsSoftmax = 136, kRegsReader = 80, kRegsIssue = 48;
+constexpr uint32_t kRegsAtLaunch = 96, kRegsSoftmax = 152, kRegsReader = 64, kRegsIssue = 48;
 static_assert(2 * kRegsSoftmax + 2 * kRegsReader + kRegsIssue <= 5 * kRegsAtLaunch && kThreads == 5 * 128, "registers of five warpgroups");
 static_assert(kReaders == kKeys && kHalf == 64, "a reader looks up a key; a half of a tile is that of two warps");
-constexpr uint32_t kStages = 2;
-constexpr uint32_t kMemo = 4;                           // tiles whose exponents and flags are kept: the scores of a tile are done before the third behind it is read
+constexpr uint32_t kStages = 3;                         // halves of a tile of keys, and of values, as operands
+constexpr uint32_t kAhead = 3;                          // halves whose codes are on their way
+constexpr uint32_t kFound = 4;                          // tiles whose keys have been looked up
+constexpr uint32_t kMemo = 8;                           // tiles whose units are kept: scores of a tile are done before the keys of the seventh behind it are looked up
 constexpr float kSlack = 8.0f;
 constexpr long long kWaitCycles = 4ll << 30;            // how long a barrier is waited for before the kernel gives up: some two seconds
 constexpr uint32_t kBlockCost = 192;                    // what a block costs beyond its keys, in keys
@@ -249,31 +251,35 @@ struct Walk {
 };
 
 // ---- the kernel ---------------------------------------------------------------------------------------------------
-template <uint32_t DP>
+template <int kBits, uint32_t DP>
 struct Layout {
   static constexpr uint32_t kRuns = DP / 64;                         // of 64 values
   static constexpr uint32_t kQueries = kRuns * kRows * 128;          // bytes of a tile of queries
-  static constexpr uint32_t kOperand = kRuns * kKeys * 128;          // of a tile of keys or values
-  static constexpr uint32_t kWhole = 2 * kQueries + 2 * kStages * kOperand + 1024;
+  static constexpr uint32_t kOperand = kRuns * kHalf * 128;          // of half a tile of keys or values
+  static constexpr uint32_t kRow = DP * kBits / 8, kCodes = kHalf * kRow;  // of a key's codes, of half a tile's, on their way
+  static constexpr uint32_t kOperandsAt = 2 * kQueries, kCodesAt = kOperandsAt + 2 * kStages * kOperand;
+  static constexpr uint32_t kWhole = kCodesAt + 2 * kAhead * kCodes + 1024;
   static constexpr uint32_t kScoresAt = 0, kSumsAt = 2 * kKeys;      // columns of tensor memory; the second tile's kKeys and DP columns behind
 };
 
 constexpr uint32_t kNone = ~0u;  // a key without a place
 struct Shared {
-  unsigned long long full_k[kStages], empty_k[kStages], full_v[kStages], empty_v[kStages], queries[2], scores[2][2], weights[2][2], sums[2][2];  // barriers
+  unsigned long long full_k[kStages], empty_k[kStages], full_v[kStages], empty_v[kStages], found_full[2][kFound], found_empty[2][kFound], queries[2], scores[2][2], weights[2][2], sums[2][2];  // barriers
   unsigned long long scan[kThreads / 32], found_base;
   uint32_t found, tensor, dead, broken;  // broken: a scale of the values so far was no number
-  float units[kMemo][kReadWarps];  // fp16: the power of two that 32 keys of a tile are in units of, from the largest of their scales
+  uint2 scales[2][kFound][kKeys];          // for the readers of keys and of values: a key's scales, two in a word
+  uint32_t places[2][kFound][kKeys];       // slot * heads + head, which is below 2^32 in this kernel; kNone
+  float units[kMemo][kKeys / 16];          // fp16: the power of two that 16 keys are in units of, from the largest of their scales
 };
 
 // kCap, kBias: scores are capped, lowered by distance.
 template <int kBits, uint32_t DP, bool kBf16, bool kCap, bool kBias>
 struct Kernel {
-  using L = Layout<DP>;
+  using L = Layout<kBits, DP>;
   using T = typename TypeOf<kBf16 ? LC_TYPE_BF16 : LC_TYPE_F16>::T;
   // fp16 weights are held 2^7 times as large, up to 2^(7 + kSlack): next to its smallest numbers the type has few bits
   static constexpr float kLift = kBf16 ? 0.0f : 7.0f;
-  static constexpr uint32_t kUnits = DP * kBits / 8 / 16;  // of 16 bytes of a row's codes, at most
+  static constexpr uint32_t kParts = L::kRow / 16, kUnits = kParts / 2;  // pieces of 16 bytes of a row's codes, at most; of half a tile that a reader takes
 
   // A tile of a block's queries as an operand, by the warpgroup that takes its scores. A negative scale goes to their signs.
   static __device__ __forceinline__ void load_queries(const AttendArgs& A, const Sequence& q, uint32_t first, uint32_t head, uint32_t thread, uint8_t* to) {
@@ -298,60 +304,52 @@ struct Kernel {
     }
   }
 
-  // A warp of readers takes 32 keys of a tile: its lanes look up a key each, and a lane takes one piece of 16 bytes of kUnits keys, kStep apart. Lanes are
-  // dealt to pieces and keys so that eight lanes in a row store to different banks: 8 bits, four pieces of two neighbouring keys (their runs of eight
-  // values are every other one, which the swizzle puts into the even and the odd places), 4 bits, two pieces of four.
-  static constexpr uint32_t kStep = 32 / kUnits, kRuns = 16 / kBits;  // kRuns: of eight values in a piece
+  // A reader takes one piece of 16 bytes of kUnits keys' codes of half a tile, kStep apart, which come by asynchronous copies, kAhead halves ahead, to places of
+  // its own. Lanes are dealt to pieces and keys so that eight lanes in a row store to different banks: 8 bits, four pieces of two neighbouring keys
+  // (their runs of eight values are every other one, which the swizzle puts into the even and the odd places), 4 bits, two pieces of four.
+  static constexpr uint32_t kStep = 32 / kParts, kRuns = 16 / kBits;  // kRuns: of eight values in a piece
+  static_assert(kStep * kUnits == 16, "a warp's keys of a half");
   struct Reader {
-    uint32_t row, left;            // first key; words of the row from the piece on
-    uint32_t at[kRuns];            // where its runs go for the first key
+    uint32_t key, group;     // first key of a half; group of the piece
+    uint32_t left;           // words of the row from the piece on
+    uint32_t at[kRuns];      // where its runs go for the first key
+    uint32_t copies;         // where its copies go
     const uint8_t* codes;
-    const unsigned short* scales;
   };
-  static __device__ __forceinline__ Reader reader_of(const AttendArgs& A, uint32_t set, uint32_t warp, uint32_t lane) {
+  static __device__ __forceinline__ Reader reader_of(const AttendArgs& A, uint32_t set, uint32_t warp, uint32_t lane, uint32_t copies) {
     Reader r;
-    uint32_t part;
-    if (kBits == 8) part = kUnits == 8 ? (lane & 3) | (lane >> 1 & 4) : lane & 3, r.row = kUnits == 8 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
-    else part = kUnits == 4 ? (lane & 1) | (lane >> 2 & 2) : lane & 1, r.row = kUnits == 4 ? (lane >> 1 & 3) | (lane >> 2 & 4) : lane >> 1;
+    uint32_t part, row;
+    if (kBits == 8) part = kParts == 8 ? (lane & 3) | (lane >> 1 & 4) : lane & 3, row = kParts == 8 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
+    else part = kParts == 4 ? (lane & 1) | (lane >> 2 & 2) : lane & 1, row = kParts == 4 ? (lane >> 1 & 3) | (lane >> 2 & 4) : lane >> 1;
+    r.key = warp * 16 + row;
     r.left = part * 16 < A.row_bytes ? (A.row_bytes - part * 16) / 4 : 0;
-    r.codes = A.codes + (set ? A.plane_codes : 0) + (r.left ? part * 16 : 0);  // behind the row's end: read, not used
-    r.scales = A.scales + (set ? A.plane_scales : 0) + (r.left ? part / (A.per_group * (kBits == 8 ? 2 : 1)) : 0);
+    r.group = r.left ? part / (A.per_group * (kBits == 8 ? 2 : 1)) : 0;
+    r.copies = copies + (warp * 32 + lane) * 16;
+    r.codes = A.codes + (set ? A.plane_codes : 0) + (r.left ? part * 16 : 0);
 #pragma unroll
     for (uint32_t k = 0; k < kRuns; ++k) {
       const uint32_t n = part * kRuns + k;
-      r.at[k] = (n / 8) * (kKeys * 128) + (warp * 32 + r.row) * 128 + (((n & 7) ^ (r.row & 7)) << 4);
+      r.at[k] = (n / 8) * (kHalf * 128) + r.key * 128 + (((n & 7) ^ (r.key & 7)) << 4);
     }
     return r;
   }
-  struct Codes {
-    uint4 w[kUnits];
-    uint32_t scale[kUnits];
-  };
-  // The pieces of a tile's keys and their scales on their way; place: of the lane's key.
-  template <uint32_t kFrom, uint32_t kTo>
-  static __device__ __forceinline__ void read_codes(const AttendArgs& A, uint32_t place, const Reader& r, Codes& c) {
-    uint32_t at[kTo - kFrom];
+  // Starts the copies of a half into slot `slot`; places: of its keys. Nothing is read for keys without a place.
+  static __device__ __forceinline__ void copy_half(const AttendArgs& A, const uint32_t* places, uint32_t slot, const Reader& r) {
 #pragma unroll
-    for (uint32_t i = kFrom; i < kTo; ++i) {
-      at[i - kFrom] = __shfl_sync(0xFFFFFFFFu, place, r.row + i * kStep);
-      c.scale[i] = 0;  // keys without a place are read from the first one, and count as zeros
-      if (at[i - kFrom] != kNone) c.scale[i] = __ldg(r.scales + (uint64_t)at[i - kFrom] * A.groups);
-      else at[i - kFrom] = 0;
-    }
-    if ((A.row_bytes & 15) == 0) {
+    for (uint32_t i = 0; i < kUnits; ++i) {
+      const uint32_t place = places[r.key + i * kStep], to = r.copies + slot * L::kCodes + i * (kReaders * 16);
+      const bool there = place != kNone && r.left > 0;
+      const uint8_t* p = r.codes + (uint64_t)(there ? place : 0) * A.row_bytes;
+      if ((A.row_bytes & 15) == 0) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(p), "r"(there ? 16 : 0) : "memory");
+      } else {
 #pragma unroll
-      for (uint32_t i = kFrom; i < kTo; ++i) c.w[i] = __ldg(reinterpret_cast<const uint4*>(r.codes + (uint64_t)at[i - kFrom] * A.row_bytes));
-    } else {
-#pragma unroll
-      for (uint32_t i = kFrom; i < kTo; ++i) {
-        const uint32_t* x = reinterpret_cast<const uint32_t*>(r.codes + (uint64_t)at[i - kFrom] * A.row_bytes);
-        c.w[i].x = __ldg(x);
-        c.w[i].y = r.left > 1 ? __ldg(x + 1) : 0u;
-        c.w[i].z = r.left > 2 ? __ldg(x + 2) : 0u;
-        c.w[i].w = r.left > 3 ? __ldg(x + 3) : 0u;
+        for (uint32_t w = 0; w < 4; ++w)
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + 4 * w), "l"(p + (w < r.left ? 4 * w : 0)), "r"(there && w < r.left ? 4 : 0) : "memory");
       }
     }
   }
+  static __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
   // Four pairs of numbers from eight codes. scale: of bf16 two of it, of fp16 a float's bits.
   static __device__ __forceinline__ uint4 numbers(uint32_t a, uint32_t b, uint32_t scale) {
     uint32_t r[4];
@@ -377,29 +375,31 @@ struct Kernel {
     }
     return make_uint4(r[0], r[1], r[2], r[3]);
   }
-  // down: what the scales are multiplied by (fp16).
-  template <uint32_t kFrom, uint32_t kTo>
-  static __device__ __forceinline__ void store_numbers(const Codes& c, float down, const Reader& r, uint32_t operand) {
+  // A half's pieces as operands. scales: of its keys, down: what they are multiplied by (fp16).
+  static __device__ __forceinline__ void store_numbers(const AttendArgs& A, const uint2* scales, float down, uint32_t slot, const Reader& r, uint32_t operand) {
     if (r.left == 0) return;
+    const uint32_t* pairs = reinterpret_cast<const uint32_t*>(scales + r.key) + r.group / 2;
 #pragma unroll
-    for (uint32_t i = kFrom; i < kTo; ++i) {
-      const uint32_t s = kBf16 ? c.scale[i] | c.scale[i] << 16 : __float_as_uint(__uint_as_float(c.scale[i] << 16) * down);
-      const uint32_t w[4] = {c.w[i].x, c.w[i].y, c.w[i].z, c.w[i].w};
+    for (uint32_t i = 0; i < kUnits; ++i) {
+      const uint32_t x = pairs[i * kStep * 2], scale = kBf16 ? __byte_perm(x, 0, r.group & 1 ? 0x3232 : 0x1010) : __float_as_uint(__uint_as_float(r.group & 1 ? x & 0xFFFF0000u : x << 16) * down);
+      uint32_t w[4];
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(r.copies + slot * L::kCodes + i * (kReaders * 16)) : "memory");
 #pragma unroll
       for (uint32_t k = 0; k < kRuns; ++k) {
-        const uint4 x = kBits == 8 ? numbers(w[2 * k], w[2 * k + 1], s) : numbers(w[k], 0, s);
+        const uint4 y = kBits == 8 ? numbers(w[2 * k], w[2 * k + 1], scale) : numbers(w[k], 0, scale);
         // kStep 4: every second key's places are the others of the swizzle's upper bit (its row's number differs by 4)
         const uint32_t at = operand + (kStep == 4 && (i & 1) ? r.at[k] ^ 64u : r.at[k]) + i * (kStep * 128);
-        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(y.x), "r"(y.y), "r"(y.z), "r"(y.w) : "memory");
       }
     }
   }
-  // Where a key lies: slot * heads + head, which is below 2^32 in this kernel.
-  static __device__ __forceinline__ uint32_t look_up(const AttendArgs& A, const Sequence& q, uint32_t s, uint32_t head, uint32_t key) {
+  // Where a key lies, in two steps: the page's number as the table has it, and what follows from it.
+  static __device__ __forceinline__ int32_t page_of(const AttendArgs& A, const Sequence& q, uint32_t s, uint32_t key) {
+    return key < q.length ? __ldg(A.table + s * A.table_stride + A.by_page.div(key)) : 0;
+  }
+  static __device__ __forceinline__ uint32_t place_of_key(const AttendArgs& A, const Sequence& q, uint32_t head, uint32_t key, int32_t number) {
     if (key >= q.length) return kNone;
-    const uint32_t page = A.by_page.div(key);
-    const int32_t number = __ldg(A.table + s * A.table_stride + page);
-    const int64_t slot = (int64_t)number * A.by_page.d + (key - page * A.by_page.d);
+    const int64_t slot = (int64_t)number * A.by_page.d + (key - A.by_page.div(key) * A.by_page.d);
     if (number < 0 || slot >= (int64_t)A.slots) {
       if (A.status) set_status(A.status, LC_ERR_INDEX);
       return kNone;
@@ -412,7 +412,7 @@ struct Kernel {
     __shared__ Shared S;
     uint8_t* const smem = raw + (1024 - (shared_address(raw) & 1023)) % 1024;
     uint8_t* const queries = smem;
-    uint8_t* const keys = smem + 2 * L::kQueries;
+    uint8_t* const keys = smem + L::kOperandsAt;
     uint8_t* const values = keys + kStages * L::kOperand;
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     begin_next();
@@ -421,9 +421,13 @@ struct Kernel {
       S.dead = S.broken = 0;
       for (uint32_t i = 0; i < kStages; ++i) {
         barrier_init(shared_address(&S.full_k[i]), kReaders);
-        barrier_init(shared_address(&S.empty_k[i]), 1);
+        barrier_init(shared_address(&S.empty_k[i]), 2);
         barrier_init(shared_address(&S.full_v[i]), kReaders);
-        barrier_init(shared_address(&S.empty_v[i]), 1);
+        barrier_init(shared_address(&S.empty_v[i]), 2);
+      }
+      for (uint32_t i = 0; i < 2 * kFound; ++i) {
+        barrier_init(shared_address(&S.found_full[i / kFound][i % kFound]), 1);
+        barrier_init(shared_address(&S.found_empty[i / kFound][i % kFound]), kReadWarps);
       }
       for (uint32_t t = 0; t < 2; ++t) {
         barrier_init(shared_address(&S.queries[t]), kRows);
@@ -538,15 +542,16 @@ struct Kernel {
             order_after();
             float y[kHalf];
             tensor_load(at, y);
-            // of the first and of the last 32 keys
-            const float factor[2] = {scale * kLog2e * (kBf16 ? 1.0f : S.units[number % kMemo][2 * half]), scale * kLog2e * (kBf16 ? 1.0f : S.units[number % kMemo][2 * half + 1])};
+            float factor[kHalf / 16];  // of 16 keys each
+#pragma unroll
+            for (uint32_t c = 0; c < kHalf / 16; ++c) factor[c] = scale * kLog2e * (kBf16 ? 1.0f : S.units[number % kMemo][half * 4 + c]);
             const bool full = key + kHalf - 1 <= low && (A.window == 0 || high - key < A.window);
             tensor_loaded(y);
             if constexpr (kCap || kBias) {
-              const float cap_in[2] = {kCap ? 2.0f * factor[0] / A.cap : 0.0f, kCap ? 2.0f * factor[1] / A.cap : 0.0f}, away = (float)(int32_t)(position - key);
+              const float cap_in = kCap ? 2.0f / A.cap : 0.0f, away = (float)(int32_t)(position - key);
 #pragma unroll
               for (uint32_t e = 0; e < kHalf; ++e) {
-                y[e] = kCap ? fmaf(-2.0f * cap_out, reciprocal(1.0f + exp2_fast(y[e] * cap_in[e / 32])), cap_out) : y[e] * factor[e / 32];
+                y[e] = kCap ? fmaf(-2.0f * cap_out, reciprocal(1.0f + exp2_fast(y[e] * factor[e / 16] * cap_in)), cap_out) : y[e] * factor[e / 16];
                 if constexpr (kBias) y[e] = fmaf(-slope, fabsf(away - (float)e), y[e]);
               }
             }
@@ -560,12 +565,14 @@ struct Kernel {
                 for (uint32_t e = 0; e < 32; ++e) y[c + e] = seen >> e & 1 ? y[c + e] : -INFINITY;
               }
             }
-            float top = y[0], top2 = y[kHalf / 2];
+            float top = -INFINITY;
 #pragma unroll
-            for (uint32_t e = 1; e < kHalf / 2 - 1; e += 2) top = max_of(top, y[e], y[e + 1]), top2 = max_of(top2, y[kHalf / 2 + e], y[kHalf / 2 + e + 1]);
-            top = fmaxf(top, y[kHalf / 2 - 1]), top2 = fmaxf(top2, y[kHalf - 1]);
-            if (kCap || kBias) top = fmaxf(top, top2);
-            else top = fmaxf(top * factor[0], top2 * factor[1]);  // grows with the product
+            for (uint32_t c = 0; c < kHalf; c += 16) {
+              float x = fmaxf(y[c], y[c + 1]);
+#pragma unroll
+              for (uint32_t e = 2; e < 16; e += 2) x = max_of(x, y[c + e], y[c + e + 1]);
+              top = fmaxf(top, kCap || kBias ? x : x * factor[c / 16]);  // grows with the product
+            }
             const bool rises = top > m + kSlack;
             if (__any_sync(0xFFFFFFFFu, rises)) {
               const float now = rises ? top : m, down = rises ? exp2_fast(m - now) : 1.0f;
@@ -583,7 +590,7 @@ struct Kernel {
             uint32_t p[kHalf / 2];
 #pragma unroll
             for (uint32_t e = 0; e < kHalf; e += 2) {
-              if constexpr (!kCap && !kBias) split_two(fma_two(two(y[e], y[e + 1]), two(factor[e / 32], factor[e / 32]), two(-base, -base)), y[e], y[e + 1]);
+              if constexpr (!kCap && !kBias) split_two(fma_two(two(y[e], y[e + 1]), two(factor[e / 16], factor[e / 16]), two(-base, -base)), y[e], y[e + 1]);
               else split_two(add_two(two(y[e], y[e + 1]), two(-base, -base)), y[e], y[e + 1]);
               y[e] = exp2_fast(y[e]), y[e + 1] = exp2_fast(y[e + 1]);
               l = add_two(l, two(y[e], y[e + 1]));
@@ -602,7 +609,7 @@ struct Kernel {
               for (uint32_t k = 0; k < n * kKeys; ++k) {
                 const uint32_t at_key = tiles.key(j0 + k / kKeys) + k % kKeys;
                 const bool visible = (at_key <= position && (A.window == 0 || position - at_key < A.window)) || at_key < q.prefix;
-                const uint32_t place = look_up(A, q, s, head, at_key);
+                const uint32_t place = place_of_key(A, q, head, at_key, page_of(A, q, s, at_key));
                 if (place == kNone || !visible) continue;
                 for (uint32_t g = 0; g < A.groups; ++g)
                   if ((A.scales[A.plane_scales + (uint64_t)place * A.groups + g] & 0x7F80u) == 0x7F80u) broken |= 1u << g;
@@ -662,116 +669,159 @@ struct Kernel {
       const uint32_t operands = shared_address(set ? values : keys);
       unsigned long long* const full = set ? S.full_v : S.full_k;
       unsigned long long* const empty = set ? S.empty_v : S.empty_k;
-      const Reader R = reader_of(A, set, mine, lane);
+      const Reader R = reader_of(A, set, mine, lane, shared_address(smem) + L::kCodesAt + set * kAhead * L::kCodes);
+      uint32_t stage = 0, turn = 0;  // of the operands
       bool good = true;
       while (good && walk.next(A)) {
         const uint32_t n = walk.n;
-        auto look = [&](uint32_t i) { return i < n ? look_up(A, walk.q, walk.s, walk.head, walk.tiles.key(walk.j0 + i) + mine * 32 + lane) : kNone; };
-        Codes c;
-        uint32_t next = look(0);
-        read_codes<0, kUnits>(A, next, R, c);
-        next = look(1);
-        for (uint32_t i = 0; i < n; ++i) {
-          const uint32_t number = done + i, stage = number % kStages, turn = number / kStages;
+        auto found = [&](uint32_t tile) {  // of the block: waits until its keys have been looked up
+          const uint32_t x = done + tile;
+          return warp_wait(shared_address(&S.found_full[set][x % kFound]), x / kFound & 1, dead);
+        };
+        auto places = [&](uint32_t half) { return S.places[set][(done + half / 2) % kFound] + (half & 1) * kHalf; };
+        uint32_t slot = 0;
+        good = found(0);
+        if (!good) break;
+        copy_half(A, places(0), 0, R);
+        copies_end();
+        copy_half(A, places(1), 1, R);
+        copies_end();
+        if (n > 1) {
+          good = found(1);
+          if (!good) break;
+          copy_half(A, places(2), 2, R);
+        }
+        copies_end();
+        for (uint32_t i = 0; i < 2 * n; ++i) {
           if (turn > 0) good = warp_wait(shared_address(&empty[stage]), (turn - 1) & 1, dead);
           if (!good) break;
-          // scales that are no numbers: hardly ever
-          uint32_t most = 0;
-#pragma unroll
-          for (uint32_t x = 0; x < kUnits; ++x) most = max(most, c.scale[x] & 0x7FFFu);
-          if (set) {
-            if (most >= 0x7F80u) {
-              S.broken = 1;
-#pragma unroll
-              for (uint32_t x = 0; x < kUnits; ++x) c.scale[x] = (c.scale[x] & 0x7FFFu) >= 0x7F80u ? 0 : c.scale[x];
-            }
-            __syncwarp();
-          }
+          asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
           float down = 1.0f;
-          if (!kBf16 && !set) {  // the unit of these 32 keys
-            if (most >= 0x7F80u) {
-              most = 0;
-#pragma unroll
-              for (uint32_t x = 0; x < kUnits; ++x) most = max(most, (c.scale[x] & 0x7FFFu) >= 0x7F80u ? 0 : c.scale[x] & 0x7FFFu);
-            }
-            most = __reduce_max_sync(0xFFFFFFFFu, most);
-            const float unit = most ? __uint_as_float(min(max(most << 16 & 0x7F800000u, 0x01000000u), 0x7E000000u)) : 1.0f;
-            if (lane == 0) S.units[number % kMemo][mine] = unit;
-            down = 1.0f / unit;
-          }
-          const uint32_t operand = operands + stage * L::kOperand;
-          store_numbers<0, kUnits / 2>(c, down, R, operand);
-          if (i + 1 < n) read_codes<0, kUnits / 2>(A, next, R, c);
-          store_numbers<kUnits / 2, kUnits>(c, down, R, operand);
+          if (!kBf16 && !set) down = 1.0f / S.units[(done + i / 2) % kMemo][(i & 1) * 4 + mine];
+          store_numbers(A, S.scales[set][(done + i / 2) % kFound] + (i & 1) * kHalf, down, slot, R, operands + stage * L::kOperand);
           order_for_products();
           barrier_arrive(shared_address(&full[stage]));
-          if (i + 1 < n) read_codes<kUnits / 2, kUnits>(A, next, R, c);
-          next = look(i + 2);
+          if (i + kAhead < 2 * n) {
+            if (i & 1) good = found((i + kAhead) / 2);
+            if (!good) break;
+            copy_half(A, places(i + kAhead), slot, R);
+          }
+          copies_end();
+          if (i & 1) {
+            __syncwarp();
+            if (lane == 0) barrier_arrive(shared_address(&S.found_empty[set][(done + i / 2) % kFound]));
+          }
+          slot = slot + 1 == kAhead ? 0 : slot + 1;
+          if (++stage == kStages) stage = 0, ++turn;
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");
         done += n;
       }
     } else {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
-      if (warp == kSoftmaxWarps + 2 * kReadWarps) {
-        // ---- the products: the warp as a whole goes through the tiles, with numbers that the compiler knows to be the same for all lanes; one lane issues
-        const uint32_t all_lanes = 0xFFFFFFFFu, at_tensor = __shfl_sync(all_lanes, tensor, 0);
+      if (warp < kSoftmaxWarps + 2 * kReadWarps + 2) {
+        // ---- the products, a warp for each tile of queries: the warp as a whole goes through the keys, with numbers that the compiler knows to be the same for all
+        // lanes; one lane issues
+        const uint32_t all_lanes = 0xFFFFFFFFu, at_tensor = __shfl_sync(all_lanes, tensor, 0), t = __shfl_sync(all_lanes, warp, 0) - (kSoftmaxWarps + 2 * kReadWarps);
         const uint32_t steps = (A.dim + 15) / 16, scores_kind = product_kind(kBf16, kHalf, false), sums_kind = product_kind(kBf16, steps * 16, true);
-        const uint32_t query_at = operand_at(shared_address(queries), 16), key_at = operand_at(shared_address(keys), 16), value_at = operand_at(shared_address(values), kKeys * 128);
-        auto multiply_keys = [&](uint32_t t, uint32_t half, uint32_t stage) {
-          const uint32_t a = query_at + t * (L::kQueries >> 4), b = key_at + stage * (L::kOperand >> 4) + half * (kHalf * 128 >> 4), d = at_tensor + L::kScoresAt + t * kKeys + half * kHalf;
-          if (one_lane()) {
+        const uint32_t query_at = operand_at(shared_address(queries) + t * L::kQueries, 16), key_at = operand_at(shared_address(keys), 16), value_at = operand_at(shared_address(values), kHalf * 128);
+        const uint32_t scores_at = at_tensor + L::kScoresAt + t * kKeys, sums_at = at_tensor + L::kSumsAt + t * DP;
+        auto multiply_keys = [&](uint32_t half, uint32_t stage) {
+          const uint32_t b = key_at + stage * (L::kOperand >> 4), d = scores_at + half * kHalf;
 #pragma unroll
-            for (uint32_t x = 0; x < DP / 16; ++x)
-              if (x < steps) product(d, a + ((x / 4) * (kRows * 128) + (x % 4) * 32 >> 4), b + ((x / 4) * (kKeys * 128) + (x % 4) * 32 >> 4), scores_kind, x > 0);
-            commit_to(shared_address(&S.scores[t][half]));
-            if (t & half) commit_to(shared_address(&S.empty_k[stage]));
-          }
-          __syncwarp();
-        };
-        auto multiply_values = [&](uint32_t t, uint32_t half, uint32_t stage, bool add) {
-          const uint32_t a = at_tensor + L::kScoresAt + t * kKeys + half * kHalf, b = value_at + stage * (L::kOperand >> 4) + half * (kHalf * 128 >> 4), d = at_tensor + L::kSumsAt + t * DP;
-          if (one_lane()) {
-#pragma unroll
-            for (uint32_t x = 0; x < kHalf / 16; ++x) product_of_tensor(d, a + x * 8, b + (x * 2048 >> 4), sums_kind, add || x > 0);
-            commit_to(shared_address(&S.sums[t][half]));
-            if (t & half) commit_to(shared_address(&S.empty_v[stage]));
-          }
-          __syncwarp();
+          for (uint32_t x = 0; x < DP / 16; ++x)
+            if (x < steps) product(d, query_at + ((x / 4) * (kRows * 128) + (x % 4) * 32 >> 4), b + ((x / 4) * (kHalf * 128) + (x % 4) * 32 >> 4), scores_kind, x > 0);
+          commit_to(shared_address(&S.scores[t][half]));
+          commit_to(shared_address(&S.empty_k[stage]));
         };
         bool good = true;
+        uint32_t k_stage = 0, k_turn = 0, v_stage = 0, v_turn = 0;
+        auto wait_keys = [&] { return warp_wait(shared_address(&S.full_k[k_stage]), k_turn & 1, dead); };
+        auto next_keys = [&] { if (++k_stage == kStages) k_stage = 0, ++k_turn; };
         for (uint32_t count = 0; good && walk.next(A); ++count) {
           const uint32_t n = __shfl_sync(all_lanes, walk.n, 0);
-          good = warp_wait(shared_address(&S.full_k[done % kStages]), done / kStages & 1, dead);
-          for (uint32_t x = 0; x < 4 && good; ++x) {
-            if (x < 2) good = warp_wait(shared_address(&S.queries[x]), count & 1, dead);
+          good = warp_wait(shared_address(&S.queries[t]), count & 1, dead);
+          for (uint32_t half = 0; half < 2 && good; ++half) {
+            good = wait_keys();
             if (!good) break;
             order_after();
-            multiply_keys(x & 1, x >> 1, done % kStages);
+            if (one_lane()) multiply_keys(half, k_stage);
+            __syncwarp();
+            next_keys();
           }
-          for (uint32_t i = 0; i < n && good; ++i) {
-            const uint32_t number = done + i, stage = number % kStages, behind = (number + 1) % kStages;
-            good = warp_wait(shared_address(&S.full_v[stage]), number / kStages & 1, dead);
-            for (uint32_t x = 0; x < 4 && good; ++x) {
-              const uint32_t t = x & 1, half = x >> 1;
-              good = warp_wait(shared_address(&S.weights[t][half]), number & 1, dead);
-              if (!good) break;
-              order_after();
-              multiply_values(t, half, stage, i > 0 || half > 0);
-              if (i + 1 < n) {
-                if (x == 0) good = warp_wait(shared_address(&S.full_k[behind]), (number + 1) / kStages & 1, dead);
-                if (!good) break;
-                order_after();
-                multiply_keys(t, half, behind);
-              }
+          for (uint32_t i = 0; i < 2 * n && good; ++i) {
+            const uint32_t half = i & 1;
+            const bool more = i + 2 < 2 * n;
+            good = (!more || wait_keys()) && warp_wait(shared_address(&S.full_v[v_stage]), v_turn & 1, dead) && warp_wait(shared_address(&S.weights[t][half]), (done + i / 2) & 1, dead);
+            if (!good) break;
+            order_after();
+            if (one_lane()) {
+              const uint32_t a = scores_at + half * kHalf, b = value_at + v_stage * (L::kOperand >> 4);
+#pragma unroll
+              for (uint32_t x = 0; x < kHalf / 16; ++x) product_of_tensor(sums_at, a + x * 8, b + (x * 2048 >> 4), sums_kind, i > 0 || x > 0);
+              commit_to(shared_address(&S.sums[t][half]));
+              commit_to(shared_address(&S.empty_v[v_stage]));
+              if (more) multiply_keys(half, k_stage);
             }
+            __syncwarp();
+            if (more) next_keys();
+            if (++v_stage == kStages) v_stage = 0, ++v_turn;
           }
           done += n;
+        }
+      } else {
+        // ---- where keys lie, and their scales: a warp for the readers of keys, one for those of values
+        const uint32_t set = warp - (kSoftmaxWarps + 2 * kReadWarps + 2);
+        const unsigned short* const scales = A.scales + (set ? A.plane_scales : 0);
+        bool good = true;
+        while (good && walk.next(A)) {
+          for (uint32_t i = 0; i < walk.n; ++i) {
+            const uint32_t x = done + i, slot = x % kFound;
+            if (x >= kFound) good = warp_wait(shared_address(&S.found_empty[set][slot]), (x / kFound - 1) & 1, dead);
+            if (!good) break;
+            const uint32_t key = walk.tiles.key(walk.j0 + i) + lane;
+            int32_t page[kKeys / 32];
+            uint32_t place[kKeys / 32], all_scales[kKeys / 32][4] = {};  // a key without a place counts as zeros
+#pragma unroll
+            for (uint32_t k = 0; k < kKeys / 32; ++k) page[k] = page_of(A, walk.q, walk.s, key + 32 * k);
+#pragma unroll
+            for (uint32_t k = 0; k < kKeys / 32; ++k) place[k] = place_of_key(A, walk.q, walk.head, key + 32 * k, page[k]);
+#pragma unroll
+            for (uint32_t k = 0; k < kKeys / 32; ++k)
+#pragma unroll
+              for (uint32_t g = 0; g < 4; ++g)
+                if (place[k] != kNone && g < A.groups) all_scales[k][g] = __ldg(scales + (uint64_t)place[k] * A.groups + g);
+#pragma unroll
+            for (uint32_t k = 0; k < kKeys / 32; ++k) {
+              uint32_t (&y)[4] = all_scales[k];
+              if (set) {  // scales that are no numbers
+#pragma unroll
+                for (uint32_t g = 0; g < 4; ++g)
+                  if ((y[g] & 0x7F80u) == 0x7F80u) y[g] = 0, S.broken = 1;
+              } else if constexpr (!kBf16) {
+                uint32_t most = 0;
+#pragma unroll
+                for (uint32_t g = 0; g < 4; ++g) most = max(most, (y[g] & 0x7F80u) == 0x7F80u ? 0u : y[g] & 0x7F80u);
+#pragma unroll
+                for (int d = 8; d; d >>= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
+                if (lane % 16 == 0) S.units[x % kMemo][2 * k + lane / 16] = most ? __uint_as_float(min(max(most << 16, 0x01000000u), 0x7E000000u)) : 1.0f;
+              }
+              S.scales[set][slot][lane + 32 * k] = make_uint2(y[0] | y[1] << 16, y[2] | y[3] << 16);
+              S.places[set][slot][lane + 32 * k] = place[k];
+            }
+            __syncwarp();
+            if (lane == 0) barrier_arrive(shared_address(&S.found_full[set][slot]));
+          }
+          done += walk.n;
         }
       }
     }
     order_before();
     __syncthreads();
-    if (threadIdx.x == 0 && S.dead && A.status) set_status(A.status, LC_ERR_TIMEOUT);
+    if (S.dead) {  // copies and products on their way have ended long before this
+      if (threadIdx.x == 0 && A.status) set_status(A.status, LC_ERR_TIMEOUT);
+      for (const long long since = clock64(); clock64() - since < (1 << 22);) {}
+    }
     if (warp == kSoftmaxWarps + 2 * kReadWarps) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(S.tensor), "n"(512) : "memory");
     wait_previous();
   }
@@ -848,13 +898,13 @@ cudaError_t launch(const AttendArgs& a, bool overlap, cudaStream_t cs) {
   auto kernel = attend_tiles_kernel<kBits, DP, kBf16, kCap, kBias>;
   if (!sms[dev]) {
     int n = 0;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Layout<DP>::kWhole);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Layout<kBits, DP>::kWhole);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return e;
     sms[dev] = n;
   }
   const uint32_t ctas = (uint32_t)sms[dev] < kTileCtas ? (uint32_t)sms[dev] : kTileCtas;
-  cudaError_t e = launch_kernel(overlap, kernel, ctas, kThreads, Layout<DP>::kWhole, cs, a);
+  cudaError_t e = launch_kernel(overlap, kernel, ctas, kThreads, Layout<kBits, DP>::kWhole, cs, a);
   if (e != cudaSuccess || ctas < 2) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ctas - 1, (a.dim + 15) / 16);
