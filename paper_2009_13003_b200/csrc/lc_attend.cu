@@ -7,7 +7,7 @@ namespace {
 uint64_t flat_bytes(uint64_t sequences) { return (8 * (sequences + 1) + 255) / 256 * 256; }
 
 // Queries of a sequence for one head of the cache up to which the kernel for few rows takes it.
-constexpr uint32_t kFewQueries = 64;
+constexpr uint32_t kFewQueries = 16;
 
 // A cache that can be attended to, whatever the number of its slots.
 bool shape_ok(const lc_cache* cache) {
@@ -95,17 +95,19 @@ int lc_cache_attend(const lc_cache* cache, const lc_rows* q, const lc_rows* out,
   const int bits = (int)cache->bits;
   cudaError_t e = cudaSuccess;
   const bool tiles = type != LC_TYPE_F32 && a.dim <= kTileDim && cache->slots < 0xFFFFFFFFull / cache->heads && (uint64_t)a.most * a.shared > kFewQueries;
-  if (tiles) a.longest = kFewQueries / a.shared;
-  if (a.longest > 0) e = type == LC_TYPE_BF16 ? launch_attend_bf16(a, bits, cs) : type == LC_TYPE_F16 ? launch_attend_f16(a, bits, cs) : launch_attend_f32(a, bits, cs);
-  if (tiles && e == cudaSuccess) {
-    AttendArgs b = a;
+  // The long sequences first: the short ones then fill the SMs as those end.
+  AttendArgs b = a;
+  if (tiles) {
+    a.longest = kFewQueries / a.shared;
     b.shortest = a.longest + 1;
-    b.longest = a.most;
     b.flat = reinterpret_cast<unsigned long long*>(reinterpret_cast<uint8_t*>(a.flat) + flat_bytes(how->sequences));
     b.parts = a.parts + 2 * kMaxParts * kPartBytes / 4;
-    if (cache->slots == 0) b.codes = static_cast<const uint8_t*>(workspace);  // keys without a place are read from the first one, and count as zeros
-    e = launch_attend_tiles(b, bits, type, a.longest > 0, cs);
+    if (cache->slots == 0) b.codes = static_cast<const uint8_t*>(workspace);  // nothing is read there, but the address is formed
+    e = launch_attend_tiles(b, bits, type, cs);
   }
+  if (e == cudaSuccess && a.longest > 0)
+    e = type == LC_TYPE_BF16 ? launch_attend_bf16(a, bits, tiles, cs) : type == LC_TYPE_F16 ? launch_attend_f16(a, bits, tiles, cs) : launch_attend_f32(a, bits, tiles, cs);
+  if (tiles && e == cudaSuccess) e = launch_join_tiles(b, type, cs);
   return e == cudaSuccess ? LC_OK : LC_ERR_CUDA;
 }
 

@@ -90,10 +90,12 @@ constexpr uint32_t kTileRows = 256;     // queries of its blocks
 constexpr uint32_t kTileDim = 128;      // longest rows that it takes
 constexpr uint64_t kTilePartBytes = 4ull * kTileRows * (kTileDim + 2);
 
-// The kernel for sequences of many rows (lc_attend_tiles.cu): queries of bf16 or fp16. overlap: behind a launch of the same call.
-cudaError_t launch_attend_tiles(const AttendArgs& a, int bits, int type, bool overlap, cudaStream_t cs);
-cudaError_t launch_attend_bf16(const AttendArgs& a, int bits, cudaStream_t cs);
-cudaError_t launch_attend_f16(const AttendArgs& a, int bits, cudaStream_t cs);
-cudaError_t launch_attend_f32(const AttendArgs& a, int bits, cudaStream_t cs);
+// The kernel for sequences of many rows (lc_attend_tiles.cu), for queries of bf16 or fp16, and what joins its parts, behind it and other launches of the call.
+cudaError_t launch_attend_tiles(const AttendArgs& a, int bits, int type, cudaStream_t cs);
+cudaError_t launch_join_tiles(const AttendArgs& a, int type, cudaStream_t cs);
+// The kernel for few rows (lc_attend_rows.cuh) and what joins its parts. overlap: behind a launch of the same call.
+cudaError_t launch_attend_bf16(const AttendArgs& a, int bits, bool overlap, cudaStream_t cs);
+cudaError_t launch_attend_f16(const AttendArgs& a, int bits, bool overlap, cudaStream_t cs);
+cudaError_t launch_attend_f32(const AttendArgs& a, int bits, bool overlap, cudaStream_t cs);
 
 }  // namespace lc

@@ -3,6 +3,6 @@
 
 namespace lc {
 
-cudaError_t launch_attend_bf16(const AttendArgs& a, int bits, cudaStream_t cs) { return bits == 4 ? launch_dim<4, 1>(a, cs) : launch_dim<8, 1>(a, cs); }
+cudaError_t launch_attend_bf16(const AttendArgs& a, int bits, bool overlap, cudaStream_t cs) { return bits == 4 ? launch_dim<4, 1>(a, overlap, cs) : launch_dim<8, 1>(a, overlap, cs); }
 
 }  // namespace lc

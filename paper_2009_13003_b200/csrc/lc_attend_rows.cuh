@@ -564,6 +564,7 @@ constexpr int kPerSm = NB * NT <= 4 ? 4 : NB * NT <= 8 ? 3 : 2;
 template <int kBits, int NB, int NT, int kParts>
 __global__ void __launch_bounds__(kThreads, (kPerSm<kBits, NB, NT, kParts>)) attend_rows_kernel(AttendArgs A) {
   Kernel<kBits, NB, NT, kParts>::run(A);
+  wait_previous();  // so that what joins both kernels' parts waits for both
 }
 
 // Joins the parts of the blocks that CTAs share. CTA c looks at the border between the shares of CTAs c and c + 1: if that is the first one that
@@ -633,7 +634,7 @@ __global__ void __launch_bounds__(256 * NT) join_kernel(AttendArgs A, uint32_t c
 }
 
 template <int kBits, int NB, int NT, int kParts>
-cudaError_t launch(const AttendArgs& a, cudaStream_t cs) {
+cudaError_t launch(const AttendArgs& a, bool overlap, cudaStream_t cs) {
   using S = Shape<kBits, NB, NT, kParts>;
   constexpr int per_sm = kPerSm<kBits, NB, NT, kParts>;
   static int sms[kMaxDevices] = {};  // by device ordinal: 0 not looked at yet
@@ -657,24 +658,24 @@ cudaError_t launch(const AttendArgs& a, cudaStream_t cs) {
   uint64_t ctas = (uint64_t)sms[dev] * fit[dev];
   if (ctas > kMaxParts) ctas = kMaxParts;
   if (ctas > (tiles + 1) / 2) ctas = (tiles + 1) / 2;
-  cudaError_t e = launch_kernel(false, kernel, (unsigned)ctas, kThreads, S::kWhole, cs, a);
+  cudaError_t e = launch_kernel(overlap, kernel, (unsigned)ctas, kThreads, S::kWhole, cs, a);
   if (e == cudaSuccess && ctas > 1) e = launch_kernel(true, join_kernel<NB, NT, typename Query<kParts>::T>, (unsigned)ctas - 1, 256 * NT, 0, cs, a, (uint32_t)ctas);
   return e;
 }
 
 template <int kBits, int NB, int kParts>
-cudaError_t launch_columns(const AttendArgs& a, cudaStream_t cs) {
+cudaError_t launch_columns(const AttendArgs& a, bool overlap, cudaStream_t cs) {
   const uint64_t columns = (uint64_t)a.longest * a.shared;
-  if (columns <= 8) return launch<kBits, NB, 1, kParts>(a, cs);
-  if constexpr (NB == 8) return launch<kBits, NB, 2, kParts>(a, cs);
+  if (columns <= 8) return launch<kBits, NB, 1, kParts>(a, overlap, cs);
+  if constexpr (NB == 8) return launch<kBits, NB, 2, kParts>(a, overlap, cs);
   else {
-    if (columns <= 16) return launch<kBits, NB, 2, kParts>(a, cs);
-    return launch<kBits, NB, 4, kParts>(a, cs);
+    if (columns <= 16) return launch<kBits, NB, 2, kParts>(a, overlap, cs);
+    return launch<kBits, NB, 4, kParts>(a, overlap, cs);
   }
 }
 template <int kBits, int kParts>
-cudaError_t launch_dim(const AttendArgs& a, cudaStream_t cs) {
-  return a.dim <= 64 ? launch_columns<kBits, 2, kParts>(a, cs) : a.dim <= 128 ? launch_columns<kBits, 4, kParts>(a, cs) : launch_columns<kBits, 8, kParts>(a, cs);
+cudaError_t launch_dim(const AttendArgs& a, bool overlap, cudaStream_t cs) {
+  return a.dim <= 64 ? launch_columns<kBits, 2, kParts>(a, overlap, cs) : a.dim <= 128 ? launch_columns<kBits, 4, kParts>(a, overlap, cs) : launch_columns<kBits, 8, kParts>(a, overlap, cs);
 }
 constexpr uint64_t kLargestPart = 4ull * (Shape<8, 8, 2, 1>::kPart > Shape<8, 4, 4, 1>::kPart ? Shape<8, 8, 2, 1>::kPart : Shape<8, 4, 4, 1>::kPart);
 static_assert(kLargestPart <= kPartBytes, "room for a part in the workspace");

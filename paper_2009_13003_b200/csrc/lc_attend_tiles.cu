@@ -33,7 +33,7 @@ constexpr uint32_t kFound = 4;                          // tiles whose keys have
 constexpr uint32_t kMemo = 8;                           // tiles whose units are kept: scores of a tile are done before the keys of the seventh behind it are looked up
 constexpr float kSlack = 8.0f;
 constexpr long long kWaitCycles = 4ll << 30;            // how long a barrier is waited for before the kernel gives up: some two seconds
-constexpr uint32_t kBlockCost = 192;                    // what a block costs beyond its keys, in keys
+constexpr uint32_t kBlockCost = 320;                    // what a block costs beyond its keys, in keys
 
 // ---- barriers and tensor memory -----------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -281,26 +281,39 @@ struct Kernel {
   static constexpr float kLift = kBf16 ? 0.0f : 7.0f;
   static constexpr uint32_t kParts = L::kRow / 16, kUnits = kParts / 2;  // pieces of 16 bytes of a row's codes, at most; of half a tile that a reader takes
 
-  // A tile of a block's queries as an operand, by the warpgroup that takes its scores. A negative scale goes to their signs.
+  // A tile of a block's queries as an operand, by the warpgroup that takes its scores. A negative scale goes to their signs. All of a thread's loads are on their
+  // way at once.
   static __device__ __forceinline__ void load_queries(const AttendArgs& A, const Sequence& q, uint32_t first, uint32_t head, uint32_t thread, uint8_t* to) {
-    const uint32_t flip = A.scale < 0.0f ? 0x80008000u : 0u;
-    const bool whole = A.dim % 8 == 0 && ((reinterpret_cast<uintptr_t>(A.q) / 2 | A.q_row | A.q_head) & 7) == 0;
+    const uint32_t flip = A.scale < 0.0f ? 0x80008000u : 0u, c = thread % (DP / 8);
+    constexpr uint32_t kRowsAtOnce = kRows / (DP / 8);  // rows that the threads take together
+    const unsigned short* const from = static_cast<const unsigned short*>(A.q) + (uint64_t)(head * A.shared) * A.q_head + c * 8;
+    auto row_at = [&](uint32_t i) { return i * kRowsAtOnce + thread / (DP / 8); };
+    auto put = [&](uint32_t row, uint4 x) {
+      *reinterpret_cast<uint4*>(to + (c / 8) * (kRows * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = make_uint4(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
+    };
+    if (A.dim % 8 == 0 && ((reinterpret_cast<uintptr_t>(A.q) / 2 | A.q_row | A.q_head) & 7) == 0) {
+      uint4 x[DP / 8];
 #pragma unroll
-    for (uint32_t i = thread; i < kRows * (DP / 8); i += kRows) {
-      const uint32_t row = i / (DP / 8), c = i % (DP / 8), r = first + row, token = A.by_shared.div(r);
-      uint32_t w[4] = {0, 0, 0, 0};
-      if (token < q.rows && c * 8 < A.dim) {
-        const unsigned short* p = static_cast<const unsigned short*>(A.q) + (uint64_t)(q.row + token) * A.q_row + (uint64_t)(head * A.shared + (r - token * A.shared)) * A.q_head + c * 8;
-        if (whole) {
-          const uint4 x = __ldg(reinterpret_cast<const uint4*>(p));
-          w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
-        } else {
-#pragma unroll
-          for (uint32_t e = 0; e < 8; ++e)
-            if (c * 8 + e < A.dim) w[e / 2] |= (uint32_t)__ldg(p + e) << (16 * (e & 1));
-        }
+      for (uint32_t i = 0; i < DP / 8; ++i) {
+        const uint32_t r = first + row_at(i), token = A.by_shared.div(r);
+        x[i] = make_uint4(0, 0, 0, 0);
+        if (token < q.rows && c * 8 < A.dim) x[i] = __ldg(reinterpret_cast<const uint4*>(from + (uint64_t)(q.row + token) * A.q_row + (uint64_t)(r - token * A.shared) * A.q_head));
       }
-      *reinterpret_cast<uint4*>(to + (c / 8) * (kRows * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = make_uint4(w[0] ^ flip, w[1] ^ flip, w[2] ^ flip, w[3] ^ flip);
+#pragma unroll
+      for (uint32_t i = 0; i < DP / 8; ++i) put(row_at(i), x[i]);
+    } else {
+#pragma unroll 1
+      for (uint32_t i = 0; i < DP / 8; ++i) {
+        const uint32_t r = first + row_at(i), token = A.by_shared.div(r);
+        const unsigned short* p = from + (uint64_t)(q.row + token) * A.q_row + (uint64_t)(r - token * A.shared) * A.q_head;
+        unsigned short x[8];
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e) {
+          x[e] = 0;
+          if (token < q.rows && c * 8 + e < A.dim) x[e] = __ldg(p + e);
+        }
+        put(row_at(i), make_uint4(x[0] | (uint32_t)x[1] << 16, x[2] | (uint32_t)x[3] << 16, x[4] | (uint32_t)x[5] << 16, x[6] | (uint32_t)x[7] << 16));
+      }
     }
   }
 
@@ -494,10 +507,7 @@ struct Kernel {
       if (blockIdx.x == 0 && threadIdx.x == 0) A.flat[A.sequences] = all;
     }
     __syncthreads();
-    if (from >= to) {
-      wait_previous();
-      return;
-    }
+    if (from >= to) return;
     if (warp == kSoftmaxWarps + 2 * kReadWarps) {
       asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_address(&S.tensor)), "n"(512) : "memory");
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -823,7 +833,6 @@ struct Kernel {
       for (const long long since = clock64(); clock64() - since < (1 << 22);) {}
     }
     if (warp == kSoftmaxWarps + 2 * kReadWarps) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(S.tensor), "n"(512) : "memory");
-    wait_previous();
   }
 };
 
@@ -890,21 +899,56 @@ __global__ void __launch_bounds__(kTileRows) join_tiles_kernel(AttendArgs A, uin
     if (d0 + e < A.dim) from_float(v[e] * over, out[e]);
 }
 
-template <int kBits, uint32_t DP, bool kBf16, bool kCap, bool kBias>
-cudaError_t launch(const AttendArgs& a, bool overlap, cudaStream_t cs) {
+// CTAs of the kernel: one on each SM.
+cudaError_t tile_ctas(uint32_t& ctas) {
   static int sms[kMaxDevices] = {};  // by device ordinal: 0 not looked at yet
   const int dev = current_device_index();
   if (dev < 0) return cudaErrorInvalidDevice;
-  auto kernel = attend_tiles_kernel<kBits, DP, kBf16, kCap, kBias>;
   if (!sms[dev]) {
     int n = 0;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Layout<kBits, DP>::kWhole);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+    const cudaError_t e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return e;
     sms[dev] = n;
   }
-  const uint32_t ctas = (uint32_t)sms[dev] < kTileCtas ? (uint32_t)sms[dev] : kTileCtas;
-  cudaError_t e = launch_kernel(overlap, kernel, ctas, kThreads, Layout<kBits, DP>::kWhole, cs, a);
+  ctas = (uint32_t)sms[dev] < kTileCtas ? (uint32_t)sms[dev] : kTileCtas;
+  return cudaSuccess;
+}
+
+template <int kBits, uint32_t DP, bool kBf16, bool kCap, bool kBias>
+cudaError_t launch(const AttendArgs& a, cudaStream_t cs) {
+  static bool ready[kMaxDevices] = {};  // by device ordinal: the kernel may have its shared memory
+  const int dev = current_device_index();
+  if (dev < 0) return cudaErrorInvalidDevice;
+  auto kernel = attend_tiles_kernel<kBits, DP, kBf16, kCap, kBias>;
+  if (!ready[dev]) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Layout<kBits, DP>::kWhole);
+    if (e != cudaSuccess) return e;
+    ready[dev] = true;
+  }
+  uint32_t ctas = 0;
+  const cudaError_t e = tile_ctas(ctas);
+  return e != cudaSuccess ? e : launch_kernel(false, kernel, ctas, kThreads, Layout<kBits, DP>::kWhole, cs, a);
+}
+template <int kBits, bool kBf16, bool kCap, bool kBias>
+cudaError_t launch_dim(const AttendArgs& a, cudaStream_t cs) {
+  return a.dim <= 64 ? launch<kBits, 64, kBf16, kCap, kBias>(a, cs) : launch<kBits, 128, kBf16, kCap, kBias>(a, cs);
+}
+template <int kBits, bool kBf16>
+cudaError_t launch_scores(const AttendArgs& a, cudaStream_t cs) {
+  if (a.cap > 0.0f) return a.slopes ? launch_dim<kBits, kBf16, true, true>(a, cs) : launch_dim<kBits, kBf16, true, false>(a, cs);
+  return a.slopes ? launch_dim<kBits, kBf16, false, true>(a, cs) : launch_dim<kBits, kBf16, false, false>(a, cs);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_tiles(const AttendArgs& a, int bits, int type, cudaStream_t cs) {
+  if (type == LC_TYPE_BF16) return bits == 4 ? launch_scores<4, true>(a, cs) : launch_scores<8, true>(a, cs);
+  return bits == 4 ? launch_scores<4, false>(a, cs) : launch_scores<8, false>(a, cs);
+}
+
+cudaError_t launch_join_tiles(const AttendArgs& a, int type, cudaStream_t cs) {
+  uint32_t ctas = 0;
+  const cudaError_t e = tile_ctas(ctas);
   if (e != cudaSuccess || ctas < 2) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ctas - 1, (a.dim + 15) / 16);
@@ -915,23 +959,7 @@ cudaError_t launch(const AttendArgs& a, bool overlap, cudaStream_t cs) {
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, join_tiles_kernel<kBf16>, a, ctas);
-}
-template <int kBits, bool kBf16, bool kCap, bool kBias>
-cudaError_t launch_dim(const AttendArgs& a, bool overlap, cudaStream_t cs) {
-  return a.dim <= 64 ? launch<kBits, 64, kBf16, kCap, kBias>(a, overlap, cs) : launch<kBits, 128, kBf16, kCap, kBias>(a, overlap, cs);
-}
-template <int kBits, bool kBf16>
-cudaError_t launch_scores(const AttendArgs& a, bool overlap, cudaStream_t cs) {
-  if (a.cap > 0.0f) return a.slopes ? launch_dim<kBits, kBf16, true, true>(a, overlap, cs) : launch_dim<kBits, kBf16, true, false>(a, overlap, cs);
-  return a.slopes ? launch_dim<kBits, kBf16, false, true>(a, overlap, cs) : launch_dim<kBits, kBf16, false, false>(a, overlap, cs);
-}
-
-}  // namespace
-
-cudaError_t launch_attend_tiles(const AttendArgs& a, int bits, int type, bool overlap, cudaStream_t cs) {
-  if (type == LC_TYPE_BF16) return bits == 4 ? launch_scores<4, true>(a, overlap, cs) : launch_scores<8, true>(a, overlap, cs);
-  return bits == 4 ? launch_scores<4, false>(a, overlap, cs) : launch_scores<8, false>(a, overlap, cs);
+  return type == LC_TYPE_BF16 ? cudaLaunchKernelEx(&cfg, join_tiles_kernel<true>, a, ctas) : cudaLaunchKernelEx(&cfg, join_tiles_kernel<false>, a, ctas);
 }
 
 }  // namespace lc
