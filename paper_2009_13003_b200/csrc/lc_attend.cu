@@ -83,6 +83,7 @@ int lc_cache_attend(const lc_cache* cache, const lc_rows* q, const lc_rows* out,
   a.longest = a.most;
   a.shared = how->heads / cache->heads;
   a.window = how->window;
+  a.near = cache->slots < 0xFFFFFFFFull / cache->heads;
   a.scale = how->scale;
   a.cap = how->cap;
   a.status = status;
@@ -94,7 +95,7 @@ int lc_cache_attend(const lc_cache* cache, const lc_rows* q, const lc_rows* out,
   a.by_pieces = FastDiv(a.row_bytes / (piece > 16 ? 16 : piece));
   const int bits = (int)cache->bits;
   cudaError_t e = cudaSuccess;
-  const bool tiles = type != LC_TYPE_F32 && a.dim <= kTileDim && cache->slots < 0xFFFFFFFFull / cache->heads && (uint64_t)a.most * a.shared > kFewQueries;
+  const bool tiles = type != LC_TYPE_F32 && a.dim <= kTileDim && a.near && (uint64_t)a.most * a.shared > kFewQueries;
   // The long sequences first: the short ones then fill the SMs as those end.
   AttendArgs b = a;
   if (tiles) {

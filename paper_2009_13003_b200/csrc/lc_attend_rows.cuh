@@ -106,7 +106,8 @@ __device__ __forceinline__ uint64_t share_of(uint64_t tiles, uint32_t ctas) {
   return share < 2 ? 2 : share;
 }
 
-template <int kBits, int NB, int NT, int kParts>
+// kWide: 4 bits, groups of 64 values or more: a word of eight values may be dealt to products of 64 rows.
+template <int kBits, int NB, int NT, int kParts, bool kWide>
 struct Kernel {
   using S = Shape<kBits, NB, NT, kParts>;
   using T = typename Query<kParts>::T;
@@ -133,37 +134,64 @@ struct Kernel {
     }
   }
 
-  // The keys and values of one key a lane (lane & 15; values from lane 16 on) on their way into a stage.
-  template <int kPiece>
-  static __device__ __forceinline__ void copy_rows(const AttendArgs& A, uint64_t place, uint32_t there, uint8_t* stage) {
+  // The keys and values of a tile's keys on their way into a stage: lane 16 * plane + key holds where that key's row is (`place`, slot * heads + head) and
+  // whether it is there. Lanes share rows, `pieces` lanes a row.
+  template <int kPiece, class P>
+  static __device__ __forceinline__ void copy_rows(const AttendArgs& A, P place, uint32_t there, uint8_t* stage) {
     const uint32_t lane = threadIdx.x & 31, pieces = A.by_pieces.d;
-    for (uint32_t i = lane; i < 32 * pieces; i += 32) {
-      const uint32_t row = A.by_pieces.div(i), piece = i - row * pieces;
-      const uint64_t at = __shfl_sync(0xFFFFFFFFu, place, row & 15);
-      if (there >> (row & 15) & 1)
-        copy_async<kPiece>(shared_address(stage + row * S::kPitch + piece * kPiece), A.codes + (row >> 4) * A.plane_codes + at * A.row_bytes + piece * kPiece);
+    if ((pieces & (pieces - 1)) == 0 && pieces <= 16) {  // a power of two: the piece is the same in all turns, and planes have turns of their own
+      const uint32_t log = __ffs(pieces) - 1, piece = lane & (pieces - 1), step = 32 >> log, half = pieces / 2;
+      uint32_t row = lane >> log, to = shared_address(stage) + row * S::kPitch + piece * kPiece;
+      const uint8_t* codes = A.codes + piece * kPiece;
+      if (pieces == 1) codes += (row >> 4) * A.plane_codes;
+#pragma unroll 4
+      for (uint32_t i = 0; i < pieces; ++i, row += step, to += step * S::kPitch) {
+        if (i == half && i > 0) codes += A.plane_codes;
+        const P at = __shfl_sync(0xFFFFFFFFu, place, row & 15);
+        if (there >> (row & 15) & 1) copy_async<kPiece>(to, codes + (uint64_t)at * A.row_bytes);
+      }
+    } else {
+      for (uint32_t i = lane; i < 32 * pieces; i += 32) {
+        const uint32_t row = A.by_pieces.div(i), piece = i - row * pieces;
+        const P at = __shfl_sync(0xFFFFFFFFu, place, row & 15);
+        if (there >> (row & 15) & 1)
+          copy_async<kPiece>(shared_address(stage + row * S::kPitch + piece * kPiece), A.codes + (row >> 4) * A.plane_codes + (uint64_t)at * A.row_bytes + piece * kPiece);
+      }
     }
   }
-  static __device__ __forceinline__ void issue(const AttendArgs& A, int64_t slot, uint32_t head, uint8_t* stage) {
+  template <class P>
+  static __device__ __forceinline__ void issue_rows(const AttendArgs& A, P place, int64_t slot, uint8_t* stage) {
     const uint32_t lane = threadIdx.x & 31;
-    const uint64_t place = (uint64_t)slot * A.heads + head;
     const uint32_t there = __ballot_sync(0xFFFFFFFFu, slot >= 0) & 0xFFFFu;
     const uint32_t piece = A.row_bytes & (0u - A.row_bytes);  // the largest power of two that divides the rows
     if (piece >= 16) copy_rows<16>(A, place, there, stage);
     else if (piece == 8) copy_rows<8>(A, place, there, stage);
     else copy_rows<4>(A, place, there, stage);
-    // scales: the words that a row's numbers lie in
-    uint32_t* to = reinterpret_cast<uint32_t*>(stage + S::kScales) + lane * S::kScaleWords;
-    const uint64_t at = (lane >> 4) * A.plane_scales + place * A.groups, word = at / 2;
+    // scales: the words that a row's numbers lie in, which begin in the middle of one where groups are odd in number
+    const uint32_t to = shared_address(stage + S::kScales) + lane * 4 * S::kScaleWords;
+    const uint64_t at = (lane >> 4) * A.plane_scales + (uint64_t)place * A.groups, word = at / 2;
+    const uint32_t* from = reinterpret_cast<const uint32_t*>(A.scales) + word;
     if (slot >= 0) {
-      const uint32_t words = ((uint32_t)(at & 1) + A.groups + 1) / 2;
-      for (uint32_t w = 0; w < words; ++w)
-        copy_scales(shared_address(to + w), reinterpret_cast<const uint32_t*>(A.scales) + word + w, (word + w) * 2 + 1 < A.scale_count ? 4 : 2);
+      if (A.groups & 1) {
+#pragma unroll
+        for (uint32_t w = 0; w < S::kScaleWords; ++w)
+          if (w * 2 < ((uint32_t)at & 1) + A.groups) copy_scales(to + 4 * w, from + w, (word + w) * 2 + 1 < A.scale_count ? 4 : 2);
+      } else {
+#pragma unroll
+        for (uint32_t w = 0; w < S::kScaleWords - 1; ++w)
+          if (w * 2 < A.groups) copy_async<4>(to + 4 * w, from + w);
+      }
     } else if (slot == -2) {  // a page that does not exist: its keys count as zeros
-      for (uint32_t w = 0; w < S::kScaleWords; ++w) to[w] = 0;
+      for (uint32_t w = 0; w < S::kScaleWords; ++w) asm volatile("st.shared.u32 [%0], %1;" ::"r"(to + 4 * w), "r"(0) : "memory");
     }
-    const uint32_t odd = __ballot_sync(0xFFFFFFFFu, at & 1);
-    if (lane == 0) *reinterpret_cast<uint32_t*>(stage + S::kParity) = odd;
+    if (A.groups & 1) {
+      const uint32_t odd = __ballot_sync(0xFFFFFFFFu, at & 1);
+      if (lane == 0) *reinterpret_cast<uint32_t*>(stage + S::kParity) = odd;
+    }
+  }
+  static __device__ __forceinline__ void issue(const AttendArgs& A, int64_t slot, uint32_t head, uint8_t* stage) {
+    if (A.near) issue_rows<uint32_t>(A, (uint32_t)slot * A.heads + head, slot, stage);
+    else issue_rows<unsigned long long>(A, (unsigned long long)slot * A.heads + head, slot, stage);
   }
   // The slot of a key; -1 behind the sequence's end, -2 if its page does not exist.
   static __device__ __forceinline__ int64_t slot_of(const AttendArgs& A, const Sequence& q, uint32_t s, uint32_t key) {
@@ -181,8 +209,7 @@ struct Kernel {
     __shared__ float maxima[kWarps][S::kColumns], sums[kWarps][S::kColumns];
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const uint32_t words = (A.dim + 31) / 32;  // blocks of 32 values that are there
-    const bool wide = kBits == 8 || A.per_group > 1;  // 4 bits: whether a word of eight values may be dealt to products of 64 rows
-    const uint32_t value_blocks = kBits == 4 && wide ? (words + 1) & ~1u : words;
+    const uint32_t value_blocks = kWide ? (words + 1) & ~1u : words;
     const float factor = kUnit * A.scale * kLog2e, cap_in = 2.0f * factor / A.cap, cap_out = A.cap * kLog2e;
     begin_next();
 
@@ -316,9 +343,11 @@ struct Kernel {
         for (int c = 0; c < NT; ++c)
 #pragma unroll
           for (int e = 0; e < 4; ++e) score[c][e] = 0.0f;
-        const uint32_t row_a = key_of<kBits>(g), row_b = row_a + 8, odd = *reinterpret_cast<const uint32_t*>(stage + S::kParity);
-        const unsigned short* scales = reinterpret_cast<const unsigned short*>(stage + S::kScales);
-        auto scale_at = [&](uint32_t row, uint32_t group) { return bf16_float(scales[row * (2 * S::kScaleWords) + (odd >> row & 1) + group]); };
+        const uint32_t row_a = key_of<kBits>(g), row_b = row_a + 8, odd = A.groups & 1 ? *reinterpret_cast<const uint32_t*>(stage + S::kParity) : 0u;
+        // where the scales of this lane's two keys begin, and of their values
+        const unsigned short* const scales = reinterpret_cast<const unsigned short*>(stage + S::kScales);
+        auto scales_of = [&](uint32_t row) { return scales + row * (2 * S::kScaleWords) + (odd >> row & 1); };
+        const unsigned short *key_scale_a = scales_of(row_a), *key_scale_b = scales_of(row_b), *value_scale_a = scales_of(16 + row_a), *value_scale_b = scales_of(16 + row_b);
         float part[NT][4];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
@@ -349,8 +378,7 @@ struct Kernel {
             }
           }
           if (ends) {
-            const uint32_t group = b / A.per_group;
-            const float sa = scale_at(row_a, group), sb = scale_at(row_b, group);
+            const float sa = bf16_float(*key_scale_a++), sb = bf16_float(*key_scale_b++);
 #pragma unroll
             for (int c = 0; c < NT; ++c) {
               score[c][0] = fmaf(part[c][0], sa, score[c][0]);
@@ -431,8 +459,7 @@ struct Kernel {
         for (int b = 0; b < NB; ++b) {
           if ((uint32_t)b >= value_blocks) break;
           if ((b & (A.per_group - 1)) == 0) {
-            const uint32_t group = b / A.per_group;
-            const float sa = scale_at(16 + row_a, group), sb = scale_at(16 + row_b, group);
+            const float sa = bf16_float(*value_scale_a++), sb = bf16_float(*value_scale_b++);
 #pragma unroll
             for (int c = 0; c < NT; ++c) {
               float p[4];
@@ -452,7 +479,7 @@ struct Kernel {
           const uint8_t* value = stage + kKeys * S::kPitch;
           const uint32_t r0 = key_of<kBits>(2 * t), r1 = key_of<kBits>(2 * t + 1);
           if constexpr (kBits == 4) {
-            const uint32_t word = wide ? (b >> 1) * 8 + g : b * 4 + (g >> 1), shift = wide ? 8 * (b & 1) : 8 * (g & 1);
+            const uint32_t word = kWide ? (b >> 1) * 8 + g : b * 4 + (g >> 1), shift = kWide ? 8 * (b & 1) : 8 * (g & 1);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {  // keys 2 t, 2 t + 1, and 8 behind
               const uint32_t x = *reinterpret_cast<const uint32_t*>(value + (r0 + 8 * h) * S::kPitch + word * 4), y = *reinterpret_cast<const uint32_t*>(value + (r1 + 8 * h) * S::kPitch + word * 4);
@@ -510,7 +537,7 @@ struct Kernel {
               for (int e = 0; e < 2; ++e) {
                 uint32_t d;
                 if (kBits == 8) d = b * 32 + g * 4 + 2 * x + e;
-                else if (wide) d = (b >> 1) * 64 + g * 8 + 4 * (b & 1) + 2 * x + e;
+                else if (kWide) d = (b >> 1) * 64 + g * 8 + 4 * (b & 1) + 2 * x + e;
                 else d = b * 32 + g * 4 + 2 * x + e;
                 to_sum[d] = o[b][x][c][h + 2 * e] * down;
               }
@@ -561,9 +588,9 @@ struct Kernel {
 template <int kBits, int NB, int NT, int kParts>
 constexpr int kPerSm = NB * NT <= 4 ? 4 : NB * NT <= 8 ? 3 : 2;
 
-template <int kBits, int NB, int NT, int kParts>
+template <int kBits, int NB, int NT, int kParts, bool kWide>
 __global__ void __launch_bounds__(kThreads, (kPerSm<kBits, NB, NT, kParts>)) attend_rows_kernel(AttendArgs A) {
-  Kernel<kBits, NB, NT, kParts>::run(A);
+  Kernel<kBits, NB, NT, kParts, kWide>::run(A);
   wait_previous();  // so that what joins both kernels' parts waits for both
 }
 
@@ -633,7 +660,7 @@ __global__ void __launch_bounds__(256 * NT) join_kernel(AttendArgs A, uint32_t c
   }
 }
 
-template <int kBits, int NB, int NT, int kParts>
+template <int kBits, int NB, int NT, int kParts, bool kWide>
 cudaError_t launch(const AttendArgs& a, bool overlap, cudaStream_t cs) {
   using S = Shape<kBits, NB, NT, kParts>;
   constexpr int per_sm = kPerSm<kBits, NB, NT, kParts>;
@@ -641,7 +668,7 @@ cudaError_t launch(const AttendArgs& a, bool overlap, cudaStream_t cs) {
   static int fit[kMaxDevices] = {};  // CTAs on an SM
   const int dev = current_device_index();
   if (dev < 0) return cudaErrorInvalidDevice;
-  auto kernel = attend_rows_kernel<kBits, NB, NT, kParts>;
+  auto kernel = attend_rows_kernel<kBits, NB, NT, kParts, kWide>;
   if (!sms[dev]) {
     int n = 0, k = 0;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kWhole);
@@ -663,19 +690,25 @@ cudaError_t launch(const AttendArgs& a, bool overlap, cudaStream_t cs) {
   return e;
 }
 
-template <int kBits, int NB, int kParts>
+template <int kBits, int NB, int kParts, bool kWide>
 cudaError_t launch_columns(const AttendArgs& a, bool overlap, cudaStream_t cs) {
   const uint64_t columns = (uint64_t)a.longest * a.shared;
-  if (columns <= 8) return launch<kBits, NB, 1, kParts>(a, overlap, cs);
-  if constexpr (NB == 8) return launch<kBits, NB, 2, kParts>(a, overlap, cs);
+  if (columns <= 8) return launch<kBits, NB, 1, kParts, kWide>(a, overlap, cs);
+  if constexpr (NB == 8) return launch<kBits, NB, 2, kParts, kWide>(a, overlap, cs);
   else {
-    if (columns <= 16) return launch<kBits, NB, 2, kParts>(a, overlap, cs);
-    return launch<kBits, NB, 4, kParts>(a, overlap, cs);
+    if (columns <= 16) return launch<kBits, NB, 2, kParts, kWide>(a, overlap, cs);
+    return launch<kBits, NB, 4, kParts, kWide>(a, overlap, cs);
   }
+}
+template <int kBits, int NB, int kParts>
+cudaError_t launch_wide(const AttendArgs& a, bool overlap, cudaStream_t cs) {
+  if constexpr (kBits == 4)
+    if (a.per_group > 1) return launch_columns<kBits, NB, kParts, true>(a, overlap, cs);
+  return launch_columns<kBits, NB, kParts, false>(a, overlap, cs);
 }
 template <int kBits, int kParts>
 cudaError_t launch_dim(const AttendArgs& a, bool overlap, cudaStream_t cs) {
-  return a.dim <= 64 ? launch_columns<kBits, 2, kParts>(a, overlap, cs) : a.dim <= 128 ? launch_columns<kBits, 4, kParts>(a, overlap, cs) : launch_columns<kBits, 8, kParts>(a, overlap, cs);
+  return a.dim <= 64 ? launch_wide<kBits, 2, kParts>(a, overlap, cs) : a.dim <= 128 ? launch_wide<kBits, 4, kParts>(a, overlap, cs) : launch_wide<kBits, 8, kParts>(a, overlap, cs);
 }
 constexpr uint64_t kLargestPart = 4ull * (Shape<8, 8, 2, 1>::kPart > Shape<8, 4, 4, 1>::kPart ? Shape<8, 8, 2, 1>::kPart : Shape<8, 4, 4, 1>::kPart);
 static_assert(kLargestPart <= kPartBytes, "room for a part in the workspace");

@@ -871,32 +871,42 @@ __global__ void __launch_bounds__(kTileRows) join_tiles_kernel(AttendArgs A, uin
   const Tiles tiles = tiles_of(A, q, P.block);
   auto part_of = [&](uint32_t cta) -> const float* {  // null: no tile of the block is that CTA's
     const unsigned long long from = cta * share, to = from + share;
-    const uint32_t j0 = tile_at(from > begin ? from - begin : 0, tiles.count, P.weight), j1 = tile_at(to - begin, tiles.count, P.weight);
+    const uint32_t j0 = from > begin ? tile_at(from - begin, tiles.count, P.weight) : 0, j1 = to < end ? tile_at(to - begin, tiles.count, P.weight) : tiles.count;
     return j0 == j1 || (j0 == 0 && j1 == tiles.count) ? nullptr : A.parts + (2ull * cta + (begin <= from ? 0 : 1)) * (kTilePartBytes / 4);
   };
   float most = -INFINITY, sum = 0.0f, v[16] = {};
   uint32_t parts = 0;
-  for (uint32_t c = first; c <= last; ++c)
-    if (const float* p = part_of(c)) most = fmaxf(most, p[kTileRows * kTileDim + threadIdx.x]), ++parts;
-  if (parts == 0) return;  // one CTA has had them all
   const uint32_t d0 = blockIdx.y * 16;
   for (uint32_t c = first; c <= last; ++c) {
     const float* p = part_of(c);
     if (!p) continue;
-    const float m = p[kTileRows * kTileDim + threadIdx.x], down = m == most ? 1.0f : exp2_fast(m - most);
-    sum += p[kTileRows * (kTileDim + 1) + threadIdx.x] * down;
+    const float m = p[kTileRows * kTileDim + threadIdx.x], l = p[kTileRows * (kTileDim + 1) + threadIdx.x], now = fmaxf(most, m);
+    float4 x[4];
 #pragma unroll
-    for (uint32_t e = 0; e < 16; e += 4) {
-      if (d0 + e >= A.dim) break;
-      const float4 x = *reinterpret_cast<const float4*>(p + ((d0 + e) / 4 * kTileRows + threadIdx.x) * 4);
-      v[e] = fmaf(x.x, down, v[e]), v[e + 1] = fmaf(x.y, down, v[e + 1]), v[e + 2] = fmaf(x.z, down, v[e + 2]), v[e + 3] = fmaf(x.w, down, v[e + 3]);
+    for (uint32_t e = 0; e < 4; ++e) x[e] = d0 + 4 * e < A.dim ? *reinterpret_cast<const float4*>(p + ((d0 / 4 + e) * kTileRows + threadIdx.x) * 4) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const float old = most == now ? 1.0f : exp2_fast(most - now), here = m == now ? 1.0f : exp2_fast(m - now);
+    sum = sum * old + l * here;
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) {
+      v[4 * e] = v[4 * e] * old + x[e].x * here, v[4 * e + 1] = v[4 * e + 1] * old + x[e].y * here;
+      v[4 * e + 2] = v[4 * e + 2] * old + x[e].z * here, v[4 * e + 3] = v[4 * e + 3] * old + x[e].w * here;
     }
+    most = now;
+    ++parts;
   }
+  if (parts == 0) return;  // one CTA has had them all
   T* out = static_cast<T*>(A.out) + (uint64_t)(q.row + token) * A.out_row + (uint64_t)(P.head * A.shared + (r - token * A.shared)) * A.out_head + d0;
   const float over = (kBf16 ? 64.0f : 1.0f) / sum;
+  if (d0 + 16 <= A.dim && (reinterpret_cast<uintptr_t>(out) & 15) == 0) {
 #pragma unroll
-  for (uint32_t e = 0; e < 16; ++e)
-    if (d0 + e < A.dim) from_float(v[e] * over, out[e]);
+    for (uint32_t e = 0; e < 16; e += 8)
+      *reinterpret_cast<uint4*>(out + e) = make_uint4(rounded<kBf16>(v[e] * over, v[e + 1] * over), rounded<kBf16>(v[e + 2] * over, v[e + 3] * over),
+                                                      rounded<kBf16>(v[e + 4] * over, v[e + 5] * over), rounded<kBf16>(v[e + 6] * over, v[e + 7] * over));
+  } else {
+#pragma unroll
+    for (uint32_t e = 0; e < 16; ++e)
+      if (d0 + e < A.dim) from_float(v[e] * over, out[e]);
+  }
 }
 
 // CTAs of the kernel: one on each SM.
