@@ -6,7 +6,6 @@
 namespace lc {
 
 constexpr uint32_t kAttendDim = 256;   // longest rows
-constexpr uint32_t kKeyTile = 64;      // keys of a tile, the unit in which a sequence's keys are dealt out
 constexpr uint32_t kMaxParts = 592;    // CTAs that share a call's tiles, at most: four on each of 148 SMs
 constexpr uint32_t kMaxColumns = 32;   // queries of a block
 
@@ -45,7 +44,8 @@ struct Sequence {
 __device__ __forceinline__ uint32_t first_seen(const AttendArgs& A, uint32_t position) {  // ignoring the prefix
   return A.window && position >= A.window ? position - A.window + 1 : 0;
 }
-template <uint32_t kTile = kKeyTile>
+// kTile: keys of a tile.
+template <uint32_t kTile>
 __device__ __forceinline__ Sequence sequence_of(const AttendArgs& A, uint32_t s, bool report) {
   Sequence q = {};
   const int64_t begin = A.begin[s], n = (int64_t)A.begin[s + 1] - begin;

@@ -23,8 +23,12 @@ namespace lc {
 namespace {
 
 constexpr uint32_t kWarps = 4, kThreads = 32 * kWarps;
-constexpr uint32_t kKeys = kKeyTile / kWarps;  // of a warp
-static_assert(kKeys == 16, "the rows of a product");
+// Products of 16 keys that a warp has at a time: two, where registers and shared memory allow it, since what a step costs beyond its products is then paid half as
+// often (a maximum over eight lanes for each query, the places of its keys, waits).
+template <int NB, int NT>
+constexpr int kProducts = NB <= 4 && NT <= 2 ? 2 : 1;
+template <int NB, int NT>
+constexpr uint32_t kTileKeys = 16 * kProducts<NB, NT> * kWarps;  // of a CTA's step: the unit in which keys are dealt out
 constexpr float kUnit = 64.0f;  // operands are codes / kUnit
 constexpr float kSlack = 8.0f;  // a maximum is raised once the scores exceed it by a factor of 2^kSlack: sums are fp32 and have room for that
 
@@ -83,14 +87,16 @@ __device__ __forceinline__ uint32_t key_of(uint32_t row) { return kBits == 8 ? r
 // Shared memory of a CTA, in bytes. The rings of the warps and, once a block is done, the sums that the warps add up share their place.
 template <int kBits, int NB, int NT, int kParts>
 struct Shape {
+  static constexpr int M = kProducts<NB, NT>;
+  static constexpr uint32_t kKeys = 16 * M, kTile = kTileKeys<NB, NT>;  // of a warp's step, of the CTA's
   static constexpr uint32_t kBlockBytes = 32 * kBits / 8;  // of 32 codes
   // 16 (4 bits) or 32 (8 bits) times an odd number: see key_of
   static constexpr uint32_t kPitch = kBits == 4 ? (NB * kBlockBytes / 16 | 1) * 16 : (NB * kBlockBytes / 32 | 1) * 32;
   static constexpr uint32_t kScaleWords = NB / 2 + 1;  // of a key's row of scales, which may begin in the middle of a word
   static constexpr uint32_t kScales = 2 * kKeys * kPitch;        // where a stage's scales begin: a row's words, the keys' then the values'
-  static constexpr uint32_t kParity = kScales + 2 * kKeys * 4 * kScaleWords;  // which of them begin in the middle of a word
+  static constexpr uint32_t kParity = kScales + 2 * kKeys * 4 * kScaleWords;  // which of them begin in the middle of a word: a bit for each key, and each value
   static constexpr uint32_t kStage = kParity + 16;
-  static constexpr uint32_t kStages = kStage > 6 * 1024 ? 3 : 4;
+  static constexpr uint32_t kStages = kStage > 8 * 1024 ? 2 : 3;
   static constexpr uint32_t kColumns = 8 * NT;
   static constexpr uint32_t kQueryPitch = (NB * 64 / 64 | 1) * 64;  // an odd number of times 64 bytes: four lanes' 16 bytes of two neighbouring columns fill all banks
   static constexpr uint32_t kQueries = kParts * kColumns * kQueryPitch;
@@ -111,6 +117,8 @@ template <int kBits, int NB, int NT, int kParts, bool kWide>
 struct Kernel {
   using S = Shape<kBits, NB, NT, kParts>;
   using T = typename Query<kParts>::T;
+  static constexpr int M = S::M;
+  static constexpr uint32_t kKeys = S::kKeys, kTile = S::kTile;
 
   // The block's queries as bf16 parts, row by row; zeros behind the last value and the last query.
   static __device__ __forceinline__ void load_queries(const AttendArgs& A, const Sequence& q, uint32_t head, uint32_t block, uint8_t* smem) {
@@ -134,59 +142,63 @@ struct Kernel {
     }
   }
 
-  // The keys and values of a tile's keys on their way into a stage: lane 16 * plane + key holds where that key's row is (`place`, slot * heads + head) and
-  // whether it is there. Lanes share rows, `pieces` lanes a row.
+  // The keys and values of a step's keys on their way into a stage: lane `key` (of 16 keys, also lane 16 + key) holds where that key's row is (`place`, slot *
+  // heads + head) and whether it is there. Lanes share rows, `pieces` lanes a row.
   template <int kPiece, class P>
   static __device__ __forceinline__ void copy_rows(const AttendArgs& A, P place, uint32_t there, uint8_t* stage) {
     const uint32_t lane = threadIdx.x & 31, pieces = A.by_pieces.d;
-    if ((pieces & (pieces - 1)) == 0 && pieces <= 16) {  // a power of two: the piece is the same in all turns, and planes have turns of their own
-      const uint32_t log = __ffs(pieces) - 1, piece = lane & (pieces - 1), step = 32 >> log, half = pieces / 2;
+    if ((pieces & (pieces - 1)) == 0 && pieces * M >= 2 && pieces <= 16) {  // a power of two: the piece is the same in all turns, and planes have turns of their own
+      const uint32_t log = __ffs(pieces) - 1, piece = lane & (pieces - 1), step = 32 >> log, half = pieces * M / 2;
       uint32_t row = lane >> log, to = shared_address(stage) + row * S::kPitch + piece * kPiece;
       const uint8_t* codes = A.codes + piece * kPiece;
-      if (pieces == 1) codes += (row >> 4) * A.plane_codes;
 #pragma unroll 4
-      for (uint32_t i = 0; i < pieces; ++i, row += step, to += step * S::kPitch) {
-        if (i == half && i > 0) codes += A.plane_codes;
-        const P at = __shfl_sync(0xFFFFFFFFu, place, row & 15);
-        if (there >> (row & 15) & 1) copy_async<kPiece>(to, codes + (uint64_t)at * A.row_bytes);
+      for (uint32_t i = 0; i < pieces * M; ++i, row += step, to += step * S::kPitch) {
+        if (i == half) codes += A.plane_codes;
+        const P at = __shfl_sync(0xFFFFFFFFu, place, row % kKeys);
+        if (there >> (row % kKeys) & 1) copy_async<kPiece>(to, codes + (uint64_t)at * A.row_bytes);
       }
     } else {
-      for (uint32_t i = lane; i < 32 * pieces; i += 32) {
+      for (uint32_t i = lane; i < 2 * kKeys * pieces; i += 32) {
         const uint32_t row = A.by_pieces.div(i), piece = i - row * pieces;
-        const P at = __shfl_sync(0xFFFFFFFFu, place, row & 15);
-        if (there >> (row & 15) & 1)
-          copy_async<kPiece>(shared_address(stage + row * S::kPitch + piece * kPiece), A.codes + (row >> 4) * A.plane_codes + (uint64_t)at * A.row_bytes + piece * kPiece);
+        const P at = __shfl_sync(0xFFFFFFFFu, place, row % kKeys);
+        if (there >> (row % kKeys) & 1)
+          copy_async<kPiece>(shared_address(stage + row * S::kPitch + piece * kPiece), A.codes + (row / kKeys) * A.plane_codes + (uint64_t)at * A.row_bytes + piece * kPiece);
       }
     }
   }
   template <class P>
   static __device__ __forceinline__ void issue_rows(const AttendArgs& A, P place, int64_t slot, uint8_t* stage) {
     const uint32_t lane = threadIdx.x & 31;
-    const uint32_t there = __ballot_sync(0xFFFFFFFFu, slot >= 0) & 0xFFFFu;
+    const uint32_t there = __ballot_sync(0xFFFFFFFFu, slot >= 0);
     const uint32_t piece = A.row_bytes & (0u - A.row_bytes);  // the largest power of two that divides the rows
     if (piece >= 16) copy_rows<16>(A, place, there, stage);
     else if (piece == 8) copy_rows<8>(A, place, there, stage);
     else copy_rows<4>(A, place, there, stage);
     // scales: the words that a row's numbers lie in, which begin in the middle of one where groups are odd in number
-    const uint32_t to = shared_address(stage + S::kScales) + lane * 4 * S::kScaleWords;
-    const uint64_t at = (lane >> 4) * A.plane_scales + (uint64_t)place * A.groups, word = at / 2;
-    const uint32_t* from = reinterpret_cast<const uint32_t*>(A.scales) + word;
-    if (slot >= 0) {
-      if (A.groups & 1) {
 #pragma unroll
-        for (uint32_t w = 0; w < S::kScaleWords; ++w)
-          if (w * 2 < ((uint32_t)at & 1) + A.groups) copy_scales(to + 4 * w, from + w, (word + w) * 2 + 1 < A.scale_count ? 4 : 2);
-      } else {
+    for (uint32_t x = 0; x < (uint32_t)M; ++x) {  // a lane's key and its value one after the other, or, of 16 keys, one of them
+      const uint32_t plane = M == 2 ? x : lane >> 4, to = shared_address(stage + S::kScales) + (plane * kKeys + lane % kKeys) * 4 * S::kScaleWords;
+      const uint64_t at = plane * A.plane_scales + (uint64_t)place * A.groups, word = at / 2;
+      const uint32_t* from = reinterpret_cast<const uint32_t*>(A.scales) + word;
+      if (slot >= 0) {
+        if (A.groups & 1) {
 #pragma unroll
-        for (uint32_t w = 0; w < S::kScaleWords - 1; ++w)
-          if (w * 2 < A.groups) copy_async<4>(to + 4 * w, from + w);
+          for (uint32_t w = 0; w < S::kScaleWords; ++w)
+            if (w * 2 < ((uint32_t)at & 1) + A.groups) copy_scales(to + 4 * w, from + w, (word + w) * 2 + 1 < A.scale_count ? 4 : 2);
+        } else {
+#pragma unroll
+          for (uint32_t w = 0; w < S::kScaleWords - 1; ++w)
+            if (w * 2 < A.groups) copy_async<4>(to + 4 * w, from + w);
+        }
+      } else if (slot == -2) {  // a page that does not exist: its keys count as zeros
+        for (uint32_t w = 0; w < S::kScaleWords; ++w) asm volatile("st.shared.u32 [%0], %1;" ::"r"(to + 4 * w), "r"(0) : "memory");
       }
-    } else if (slot == -2) {  // a page that does not exist: its keys count as zeros
-      for (uint32_t w = 0; w < S::kScaleWords; ++w) asm volatile("st.shared.u32 [%0], %1;" ::"r"(to + 4 * w), "r"(0) : "memory");
-    }
-    if (A.groups & 1) {
-      const uint32_t odd = __ballot_sync(0xFFFFFFFFu, at & 1);
-      if (lane == 0) *reinterpret_cast<uint32_t*>(stage + S::kParity) = odd;
+      if (A.groups & 1) {
+        const uint32_t odd = __ballot_sync(0xFFFFFFFFu, at & 1);
+        uint32_t* to_odd = reinterpret_cast<uint32_t*>(stage + S::kParity);
+        if (lane == 0 && M == 2) to_odd[x] = odd;
+        if (lane == 0 && M == 1) to_odd[0] = odd & 0xFFFFu, to_odd[1] = odd >> 16;
+      }
     }
   }
   static __device__ __forceinline__ void issue(const AttendArgs& A, int64_t slot, uint32_t head, uint8_t* stage) {
@@ -216,7 +228,7 @@ struct Kernel {
     // all tiles of the call, and where this CTA's begin
     unsigned long long all = 0;
     for (uint32_t s = threadIdx.x; s < A.sequences; s += kThreads) {
-      const Sequence q = sequence_of(A, s, blockIdx.x == 0);
+      const Sequence q = sequence_of<kTile>(A, s, blockIdx.x == 0);
       all += (unsigned long long)blocks_of(A, q, S::kColumns) * A.heads * q.tiles;
     }
 #pragma unroll
@@ -233,7 +245,7 @@ struct Kernel {
         const uint32_t s = s0 + threadIdx.x;
         unsigned long long mine = 0;
         if (s < A.sequences) {
-          const Sequence q = sequence_of(A, s, false);
+          const Sequence q = sequence_of<kTile>(A, s, false);
           mine = (unsigned long long)blocks_of(A, q, S::kColumns) * A.heads * q.tiles;
         }
         unsigned long long upto = mine;
@@ -264,7 +276,7 @@ struct Kernel {
     if (from >= to) return;
 
     uint32_t s = found;
-    Sequence q = sequence_of(A, s, false);
+    Sequence q = sequence_of<kTile>(A, s, false);
     uint64_t rest = from - found_base;
     uint32_t blocks = blocks_of(A, q, S::kColumns);
     uint32_t item = (uint32_t)(rest / q.tiles), j0 = (uint32_t)(rest - (uint64_t)item * q.tiles);  // item: block * heads + head
@@ -288,11 +300,11 @@ struct Kernel {
       const uint32_t high = q.first + min(A.by_shared.div(block * S::kColumns + S::kColumns - 1), q.rows - 1);
       // of the tiles j0 ... j1 - 1, those that some query of the block sees: some of the prefix's and some behind
       const uint32_t n0 = min(j1, q.ahead) - min(j0, q.ahead);
-      const uint32_t seen0 = max(first_seen(A, low) / kKeyTile, q.from) - q.from + q.ahead, seen1 = max(high / kKeyTile + 1, q.from) - q.from + q.ahead;
+      const uint32_t seen0 = max(first_seen(A, low) / kTile, q.from) - q.from + q.ahead, seen1 = max(high / kTile + 1, q.from) - q.from + q.ahead;
       const uint32_t b0 = max(j0, seen0), b1 = min(j1, seen1), n = n0 + (b1 > b0 ? b1 - b0 : 0);
       auto key0 = [&](uint32_t i) {  // first key of this warp in the i-th of those tiles
         const uint32_t j = i < n0 ? min(j0, q.ahead) + i : b0 + i - n0;
-        return (j < q.ahead ? j : q.from + j - q.ahead) * kKeyTile + warp * kKeys;
+        return (j < q.ahead ? j : q.from + j - q.ahead) * kTile + warp * kKeys;
       };
 
       float o[NB][2][NT][4];
@@ -309,14 +321,14 @@ struct Kernel {
       for (int c = 0; c < NT; ++c) m[c][0] = m[c][1] = -INFINITY, l[c][0] = l[c][1] = 0.0f;
 
       // the ring: the slots of the next tile's keys are looked up while this one's copies start
-      int64_t slot = n > 0 ? slot_of(A, q, s, key0(0) + (lane & 15)) : -1;
+      int64_t slot = n > 0 ? slot_of(A, q, s, key0(0) + lane % kKeys) : -1;
       __syncthreads();  // the queries are there, and the sums of the block before are read
 #pragma unroll
       for (uint32_t i = 0; i < S::kStages - 1; ++i) {
         if (i < n) {
           if (slot == -2 && A.status) set_status(A.status, LC_ERR_INDEX);
           issue(A, slot, head, ring + i * S::kStage);
-          slot = i + 1 < n ? slot_of(A, q, s, key0(i + 1) + (lane & 15)) : -1;
+          slot = i + 1 < n ? slot_of(A, q, s, key0(i + 1) + lane % kKeys) : -1;
         }
         copies_end();
       }
@@ -329,7 +341,7 @@ struct Kernel {
           if (next < n) {
             if (slot == -2 && A.status) set_status(A.status, LC_ERR_INDEX);
             issue(A, slot, head, ring + (stage_at == 0 ? S::kStages - 1 : stage_at - 1) * S::kStage);
-            slot = next + 1 < n ? slot_of(A, q, s, key0(next + 1) + (lane & 15)) : -1;
+            slot = next + 1 < n ? slot_of(A, q, s, key0(next + 1) + lane % kKeys) : -1;
           }
           copies_end();
         }
@@ -338,59 +350,77 @@ struct Kernel {
         const uint32_t key = key0(i);
 
         // ---- scores: codes times queries, a group at a time
-        float score[NT][4];
-#pragma unroll
-        for (int c = 0; c < NT; ++c)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) score[c][e] = 0.0f;
-        const uint32_t row_a = key_of<kBits>(g), row_b = row_a + 8, odd = A.groups & 1 ? *reinterpret_cast<const uint32_t*>(stage + S::kParity) : 0u;
-        // where the scales of this lane's two keys begin, and of their values
+        float score[M][NT][4] = {};
+        const uint32_t row = key_of<kBits>(g);  // of the first product; its other key is row + 8
+        const uint2 odd = A.groups & 1 ? *reinterpret_cast<const uint2*>(stage + S::kParity) : make_uint2(0, 0);
+        // where the scales of this lane's keys begin, and of their values
         const unsigned short* const scales = reinterpret_cast<const unsigned short*>(stage + S::kScales);
-        auto scales_of = [&](uint32_t row) { return scales + row * (2 * S::kScaleWords) + (odd >> row & 1); };
-        const unsigned short *key_scale_a = scales_of(row_a), *key_scale_b = scales_of(row_b), *value_scale_a = scales_of(16 + row_a), *value_scale_b = scales_of(16 + row_b);
-        float part[NT][4];
+        const unsigned short *key_scales[M][2], *value_scales[M][2];
+#pragma unroll
+        for (int x = 0; x < M; ++x)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t k = row + 16 * x + 8 * h;
+            key_scales[x][h] = scales + k * (2 * S::kScaleWords) + (odd.x >> k & 1);
+            value_scales[x][h] = scales + (kKeys + k) * (2 * S::kScaleWords) + (odd.y >> k & 1);
+          }
+        float part[M][NT][4];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
           if ((uint32_t)b >= words) break;
-          uint32_t a0[4], a1[4];
-          if constexpr (kBits == 4) {
-            const uint32_t x = *reinterpret_cast<const uint32_t*>(stage + row_a * S::kPitch + b * 16 + t * 4), y = *reinterpret_cast<const uint32_t*>(stage + row_b * S::kPitch + b * 16 + t * 4);
-            a0[0] = operand<4, false>(x & 0x000F000Fu), a0[1] = operand<4, false>(y & 0x000F000Fu);
-            a0[2] = operand<4, true>(x & 0x00F000F0u), a0[3] = operand<4, true>(y & 0x00F000F0u);
-            a1[0] = operand<4, false>(x >> 8 & 0x000F000Fu), a1[1] = operand<4, false>(y >> 8 & 0x000F000Fu);
-            a1[2] = operand<4, true>(x >> 8 & 0x00F000F0u), a1[3] = operand<4, true>(y >> 8 & 0x00F000F0u);
-          } else {
-            const uint2 x = *reinterpret_cast<const uint2*>(stage + row_a * S::kPitch + b * 32 + t * 8), y = *reinterpret_cast<const uint2*>(stage + row_b * S::kPitch + b * 32 + t * 8);
-            a0[0] = operand<8, false>(__byte_perm(x.x, 0, 0x4140)), a0[1] = operand<8, false>(__byte_perm(y.x, 0, 0x4140));
-            a0[2] = operand<8, false>(__byte_perm(x.x, 0, 0x4342)), a0[3] = operand<8, false>(__byte_perm(y.x, 0, 0x4342));
-            a1[0] = operand<8, false>(__byte_perm(x.y, 0, 0x4140)), a1[1] = operand<8, false>(__byte_perm(y.y, 0, 0x4140));
-            a1[2] = operand<8, false>(__byte_perm(x.y, 0, 0x4342)), a1[3] = operand<8, false>(__byte_perm(y.y, 0, 0x4342));
+          uint32_t a[M][2][4];
+#pragma unroll
+          for (int x = 0; x < M; ++x) {
+            const uint8_t *p = stage + (row + 16 * x) * S::kPitch, *r = p + 8 * S::kPitch;
+            uint32_t (&a0)[4] = a[x][0];
+            uint32_t (&a1)[4] = a[x][1];
+            if constexpr (kBits == 4) {
+              const uint32_t u = *reinterpret_cast<const uint32_t*>(p + b * 16 + t * 4), v = *reinterpret_cast<const uint32_t*>(r + b * 16 + t * 4);
+              a0[0] = operand<4, false>(u & 0x000F000Fu), a0[1] = operand<4, false>(v & 0x000F000Fu);
+              a0[2] = operand<4, true>(u & 0x00F000F0u), a0[3] = operand<4, true>(v & 0x00F000F0u);
+              a1[0] = operand<4, false>(u >> 8 & 0x000F000Fu), a1[1] = operand<4, false>(v >> 8 & 0x000F000Fu);
+              a1[2] = operand<4, true>(u >> 8 & 0x00F000F0u), a1[3] = operand<4, true>(v >> 8 & 0x00F000F0u);
+            } else {
+              const uint2 u = *reinterpret_cast<const uint2*>(p + b * 32 + t * 8), v = *reinterpret_cast<const uint2*>(r + b * 32 + t * 8);
+              a0[0] = operand<8, false>(__byte_perm(u.x, 0, 0x4140)), a0[1] = operand<8, false>(__byte_perm(v.x, 0, 0x4140));
+              a0[2] = operand<8, false>(__byte_perm(u.x, 0, 0x4342)), a0[3] = operand<8, false>(__byte_perm(v.x, 0, 0x4342));
+              a1[0] = operand<8, false>(__byte_perm(u.y, 0, 0x4140)), a1[1] = operand<8, false>(__byte_perm(v.y, 0, 0x4140));
+              a1[2] = operand<8, false>(__byte_perm(u.y, 0, 0x4342)), a1[3] = operand<8, false>(__byte_perm(v.y, 0, 0x4342));
+            }
           }
           const bool begins = (b & (A.per_group - 1)) == 0, ends = ((b + 1) & (A.per_group - 1)) == 0 || (uint32_t)b + 1 == words;
 #pragma unroll
           for (int c = 0; c < NT; ++c) {
-            if (begins) part[c][0] = part[c][1] = part[c][2] = part[c][3] = 0.0f;
+            if (begins) {
+#pragma unroll
+              for (int x = 0; x < M; ++x) part[x][c][0] = part[x][c][1] = part[x][c][2] = part[x][c][3] = 0.0f;
+            }
 #pragma unroll
             for (int k = 0; k < kParts; ++k) {
               const uint4 w = *reinterpret_cast<const uint4*>(smem + (k * S::kColumns + c * 8 + g) * S::kQueryPitch + b * 64 + t * 16);
-              mma_bf16(part[c], a0, w.x, w.y);
-              mma_bf16(part[c], a1, w.z, w.w);
+#pragma unroll
+              for (int x = 0; x < M; ++x) {
+                mma_bf16(part[x][c], a[x][0], w.x, w.y);
+                mma_bf16(part[x][c], a[x][1], w.z, w.w);
+              }
             }
           }
           if (ends) {
-            const float sa = bf16_float(*key_scale_a++), sb = bf16_float(*key_scale_b++);
 #pragma unroll
-            for (int c = 0; c < NT; ++c) {
-              score[c][0] = fmaf(part[c][0], sa, score[c][0]);
-              score[c][1] = fmaf(part[c][1], sa, score[c][1]);
-              score[c][2] = fmaf(part[c][2], sb, score[c][2]);
-              score[c][3] = fmaf(part[c][3], sb, score[c][3]);
+            for (int x = 0; x < M; ++x) {
+              const float sa = bf16_float(*key_scales[x][0]++), sb = bf16_float(*key_scales[x][1]++);
+#pragma unroll
+              for (int c = 0; c < NT; ++c) {
+                score[x][c][0] = fmaf(part[x][c][0], sa, score[x][c][0]);
+                score[x][c][1] = fmaf(part[x][c][1], sa, score[x][c][1]);
+                score[x][c][2] = fmaf(part[x][c][2], sb, score[x][c][2]);
+                score[x][c][3] = fmaf(part[x][c][3], sb, score[x][c][3]);
+              }
             }
           }
         }
 
         // ---- the running maximum and sum, base 2
-        const uint32_t key_a = key + row_a, key_b = key + row_b;
         const bool full = key + kKeys - 1 <= low && (A.window == 0 || high - key < A.window);
         uint32_t seen = 0xFFFFFFFFu;  // a bit for each score
         bool higher = false;
@@ -398,34 +428,37 @@ struct Kernel {
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t at_key = e < 2 ? key_a : key_b, p = position[2 * c + (e & 1)];
-            float y = score[c][e];
-            if (A.cap > 0.0f) {
-              // cap * tanh(x / cap), x = score * scale
-              const float u = exp2_fast(y * cap_in);
-              y = fmaf(-2.0f * cap_out, reciprocal(1.0f + u), cap_out);
-            } else {
-              y *= factor;
-            }
-            if (A.slopes) y = fmaf(-slope[2 * c + (e & 1)], fabsf((float)(int32_t)(p - at_key)), y);
-            if (!full) {
-              const bool visible = (at_key <= p && (A.window == 0 || p - at_key < A.window)) || at_key < q.prefix;
-              if (!visible) {
-                y = -INFINITY;
-                seen &= ~(1u << (4 * c + e));
+          for (int x = 0; x < M; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t at_key = key + row + 16 * x + 8 * (e / 2), p = position[2 * c + (e & 1)];
+              float y = score[x][c][e];
+              if (A.cap > 0.0f) {
+                // cap * tanh(z / cap), z = score * scale
+                const float u = exp2_fast(y * cap_in);
+                y = fmaf(-2.0f * cap_out, reciprocal(1.0f + u), cap_out);
+              } else {
+                y *= factor;
               }
+              if (A.slopes) y = fmaf(-slope[2 * c + (e & 1)], fabsf((float)(int32_t)(p - at_key)), y);
+              if (!full) {
+                const bool visible = (at_key <= p && (A.window == 0 || p - at_key < A.window)) || at_key < q.prefix;
+                if (!visible) {
+                  y = -INFINITY;
+                  seen &= ~(1u << (4 * (x * NT + c) + e));
+                }
+              }
+              score[x][c][e] = y;
             }
-            score[c][e] = y;
-          }
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            float x = fmaxf(score[c][h], score[c][h + 2]);
-            x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 4));
-            x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 8));
-            x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 16));
-            top[c][h] = x;
-            higher |= x > m[c][h] + kSlack;
+            float z = fmaxf(score[0][c][h], score[0][c][h + 2]);
+            if constexpr (M == 2) z = fmaxf(z, fmaxf(score[M - 1][c][h], score[M - 1][c][h + 2]));
+            z = fmaxf(z, __shfl_xor_sync(0xFFFFFFFFu, z, 4));
+            z = fmaxf(z, __shfl_xor_sync(0xFFFFFFFFu, z, 8));
+            z = fmaxf(z, __shfl_xor_sync(0xFFFFFFFFu, z, 16));
+            top[c][h] = z;
+            higher |= z > m[c][h] + kSlack;
           }
         }
         if (__any_sync(0xFFFFFFFFu, higher)) {
@@ -448,61 +481,72 @@ struct Kernel {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const float base = m[c][h] == -INFINITY ? 0.0f : m[c][h];
-            score[c][h] = exp2_fast(score[c][h] - base);
-            score[c][h + 2] = exp2_fast(score[c][h + 2] - base);
-            l[c][h] += score[c][h] + score[c][h + 2];
+#pragma unroll
+            for (int x = 0; x < M; ++x) {
+              score[x][c][h] = exp2_fast(score[x][c][h] - base);
+              score[x][c][h + 2] = exp2_fast(score[x][c][h + 2] - base);
+              l[c][h] += score[x][c][h] + score[x][c][h + 2];
+            }
           }
 
         // ---- probabilities, with the values' scales, times codes
-        uint32_t prob[NT][kParts][2];
+        uint32_t prob[M][NT][kParts][2];
+        const uint8_t* const value = stage + kKeys * S::kPitch;
+        const uint32_t r0 = key_of<kBits>(2 * t), r1 = key_of<kBits>(2 * t + 1);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
           if ((uint32_t)b >= value_blocks) break;
           if ((b & (A.per_group - 1)) == 0) {
-            const float sa = bf16_float(*value_scale_a++), sb = bf16_float(*value_scale_b++);
 #pragma unroll
-            for (int c = 0; c < NT; ++c) {
-              float p[4];
+            for (int x = 0; x < M; ++x) {
+              const float sa = bf16_float(*value_scales[x][0]++), sb = bf16_float(*value_scales[x][1]++);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) p[e] = seen >> (4 * c + e) & 1 ? score[c][e] * (e < 2 ? sa : sb) : 0.0f;
+              for (int c = 0; c < NT; ++c) {
+                float p[4];
 #pragma unroll
-              for (int k = 0; k < kParts; ++k) {
-                const uint32_t x = two_bf16(p[0], p[1]), y = two_bf16(p[2], p[3]);
-                prob[c][k][0] = transposed(x);
-                prob[c][k][1] = transposed(y);
-                p[0] -= __uint_as_float(x << 16), p[1] -= __uint_as_float(x & 0xFFFF0000u);
-                p[2] -= __uint_as_float(y << 16), p[3] -= __uint_as_float(y & 0xFFFF0000u);
+                for (int e = 0; e < 4; ++e) p[e] = score[x][c][e] * (e < 2 ? sa : sb);
+                if (!full) {  // what is not seen is 0, whatever its scale is
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) p[e] = seen >> (4 * (x * NT + c) + e) & 1 ? p[e] : 0.0f;
+                }
+#pragma unroll
+                for (int k = 0; k < kParts; ++k) {
+                  const uint32_t u = two_bf16(p[0], p[1]), v = two_bf16(p[2], p[3]);
+                  prob[x][c][k][0] = transposed(u);
+                  prob[x][c][k][1] = transposed(v);
+                  p[0] -= __uint_as_float(u << 16), p[1] -= __uint_as_float(u & 0xFFFF0000u);
+                  p[2] -= __uint_as_float(v << 16), p[3] -= __uint_as_float(v & 0xFFFF0000u);
+                }
               }
             }
           }
-          uint32_t a0[4], a1[4];
-          const uint8_t* value = stage + kKeys * S::kPitch;
-          const uint32_t r0 = key_of<kBits>(2 * t), r1 = key_of<kBits>(2 * t + 1);
-          if constexpr (kBits == 4) {
-            const uint32_t word = kWide ? (b >> 1) * 8 + g : b * 4 + (g >> 1), shift = kWide ? 8 * (b & 1) : 8 * (g & 1);
+#pragma unroll
+          for (int x = 0; x < M; ++x) {
+            uint32_t a0[4], a1[4];
+            const uint8_t *p = value + (16 * x + r0) * S::kPitch, *r = value + (16 * x + r1) * S::kPitch;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {  // keys 2 t, 2 t + 1, and 8 behind
-              const uint32_t x = *reinterpret_cast<const uint32_t*>(value + (r0 + 8 * h) * S::kPitch + word * 4), y = *reinterpret_cast<const uint32_t*>(value + (r1 + 8 * h) * S::kPitch + word * 4);
-              const uint32_t even = __byte_perm(x, y, 0x5410) >> shift, odds = __byte_perm(x, y, 0x7632) >> shift;
-              a0[2 * h] = operand<4, false>(even & 0x000F000Fu), a0[2 * h + 1] = operand<4, false>(odds & 0x000F000Fu);
-              a1[2 * h] = operand<4, true>(even & 0x00F000F0u), a1[2 * h + 1] = operand<4, true>(odds & 0x00F000F0u);
+              if constexpr (kBits == 4) {
+                const uint32_t word = kWide ? (b >> 1) * 8 + g : b * 4 + (g >> 1), shift = kWide ? 8 * (b & 1) : 8 * (g & 1);
+                const uint32_t u = *reinterpret_cast<const uint32_t*>(p + 8 * h * S::kPitch + word * 4), v = *reinterpret_cast<const uint32_t*>(r + 8 * h * S::kPitch + word * 4);
+                const uint32_t even = __byte_perm(u, v, 0x5410) >> shift, odds = __byte_perm(u, v, 0x7632) >> shift;
+                a0[2 * h] = operand<4, false>(even & 0x000F000Fu), a0[2 * h + 1] = operand<4, false>(odds & 0x000F000Fu);
+                a1[2 * h] = operand<4, true>(even & 0x00F000F0u), a1[2 * h + 1] = operand<4, true>(odds & 0x00F000F0u);
+              } else {
+                const uint32_t u = *reinterpret_cast<const uint32_t*>(p + 8 * h * S::kPitch + b * 32 + g * 4), v = *reinterpret_cast<const uint32_t*>(r + 8 * h * S::kPitch + b * 32 + g * 4);
+                const uint32_t even = __byte_perm(u, v, 0x6420), odds = __byte_perm(u, v, 0x7531);
+                a0[2 * h] = operand<8, false>(even & 0x00FF00FFu), a0[2 * h + 1] = operand<8, false>(odds & 0x00FF00FFu);
+                a1[2 * h] = operand<8, false>(__byte_perm(even, 0, 0x4341)), a1[2 * h + 1] = operand<8, false>(__byte_perm(odds, 0, 0x4341));
+              }
             }
-          } else {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const uint32_t x = *reinterpret_cast<const uint32_t*>(value + (r0 + 8 * h) * S::kPitch + b * 32 + g * 4), y = *reinterpret_cast<const uint32_t*>(value + (r1 + 8 * h) * S::kPitch + b * 32 + g * 4);
-              const uint32_t even = __byte_perm(x, y, 0x6420), odds = __byte_perm(x, y, 0x7531);
-              a0[2 * h] = operand<8, false>(even & 0x00FF00FFu), a0[2 * h + 1] = operand<8, false>(odds & 0x00FF00FFu);
-              a1[2 * h] = operand<8, false>(__byte_perm(even, 0, 0x4341)), a1[2 * h + 1] = operand<8, false>(__byte_perm(odds, 0, 0x4341));
-            }
+            for (int c = 0; c < NT; ++c)
+#pragma unroll
+              for (int k = 0; k < kParts; ++k) {
+                mma_bf16(o[b][0][c], a0, prob[x][c][k][0], prob[x][c][k][1]);
+                mma_bf16(o[b][1][c], a1, prob[x][c][k][0], prob[x][c][k][1]);
+              }
           }
-#pragma unroll
-          for (int c = 0; c < NT; ++c)
-#pragma unroll
-            for (int k = 0; k < kParts; ++k) {
-              mma_bf16(o[b][0][c], a0, prob[c][k][0], prob[c][k][1]);
-              mma_bf16(o[b][1][c], a1, prob[c][k][0], prob[c][k][1]);
-            }
         }
       }
 
@@ -575,7 +619,7 @@ struct Kernel {
       if (at < to && ++item == blocks * A.heads) {
         item = 0;
         do {
-          q = sequence_of(A, ++s, false);
+          q = sequence_of<kTile>(A, ++s, false);
         } while (q.rows == 0);
         blocks = blocks_of(A, q, S::kColumns);
       }
@@ -610,7 +654,7 @@ __global__ void __launch_bounds__(256 * NT) join_kernel(AttendArgs A, uint32_t c
     lo += found * step;
     count = min(step, count - found * step);
   }
-  const Sequence q = sequence_of(A, lo, false);
+  const Sequence q = sequence_of<kTileKeys<NB, NT>>(A, lo, false);
   const unsigned long long rest = border - A.flat[lo];
   const uint32_t item = (uint32_t)(rest / q.tiles), j = (uint32_t)(rest - (unsigned long long)item * q.tiles);
   const unsigned long long begin = border - j, end = begin + q.tiles;
@@ -681,7 +725,7 @@ cudaError_t launch(const AttendArgs& a, bool overlap, cudaStream_t cs) {
   }
   // no more CTAs than there can be work for
   const uint64_t blocks = (uint64_t)a.rows * a.shared / S::kColumns + (a.rows < a.sequences ? a.rows : a.sequences);
-  const uint64_t tiles = blocks * a.heads * ((a.room + kKeyTile - 1) / kKeyTile + 1);
+  const uint64_t tiles = blocks * a.heads * ((a.room + S::kTile - 1) / S::kTile + 1);
   uint64_t ctas = (uint64_t)sms[dev] * fit[dev];
   if (ctas > kMaxParts) ctas = kMaxParts;
   if (ctas > (tiles + 1) / 2) ctas = (tiles + 1) / 2;
