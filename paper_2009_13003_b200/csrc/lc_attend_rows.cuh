@@ -90,16 +90,18 @@ struct Shape {
   static constexpr int M = kProducts<NB, NT>;
   static constexpr uint32_t kKeys = 16 * M, kTile = kTileKeys<NB, NT>;  // of a warp's step, of the CTA's
   static constexpr uint32_t kBlockBytes = 32 * kBits / 8;  // of 32 codes
-  // 16 (4 bits) or 32 (8 bits) times an odd number: see key_of
-  static constexpr uint32_t kPitch = kBits == 4 ? (NB * kBlockBytes / 16 | 1) * 16 : (NB * kBlockBytes / 32 | 1) * 32;
+  // Rows of 128 bytes and more lie as they are, their 16 bytes swapped among each other by the key (place_in), shorter ones 16 (4 bits) or 32 (8 bits) times an
+  // odd number of bytes apart: see key_of.
+  static constexpr bool kSwapped = NB * kBlockBytes >= 128;
+  static constexpr uint32_t kPitch = kSwapped ? NB * kBlockBytes : kBits == 4 ? (NB * kBlockBytes / 16 | 1) * 16 : (NB * kBlockBytes / 32 | 1) * 32;
   static constexpr uint32_t kScaleWords = NB / 2 + 1;  // of a key's row of scales, which may begin in the middle of a word
   static constexpr uint32_t kScales = 2 * kKeys * kPitch;        // where a stage's scales begin: a row's words, the keys' then the values'
   static constexpr uint32_t kParity = kScales + 2 * kKeys * 4 * kScaleWords;  // which of them begin in the middle of a word: a bit for each key, and each value
-  static constexpr uint32_t kStage = kParity + 16;
-  static constexpr uint32_t kStages = kStage > 8 * 1024 ? 2 : 3;
+  static constexpr uint32_t kStage = (kParity + 16 + 255) / 256 * 256;
+  static constexpr uint32_t kStages = 2;  // CTAs on an SM bring more than stages: with three, a CTA less fits
   static constexpr uint32_t kColumns = 8 * NT;
   static constexpr uint32_t kQueryPitch = (NB * 64 / 64 | 1) * 64;  // an odd number of times 64 bytes: four lanes' 16 bytes of two neighbouring columns fill all banks
-  static constexpr uint32_t kQueries = kParts * kColumns * kQueryPitch;
+  static constexpr uint32_t kQueries = (kParts * kColumns * kQueryPitch + 255) / 256 * 256;
   static constexpr uint32_t kSumPitch = NB * 32 + 4;  // floats
   static constexpr uint32_t kRing = kWarps * kStages * kStage, kSums = kWarps * kColumns * kSumPitch * 4;
   static constexpr uint32_t kWhole = kQueries + (kRing > kSums ? kRing : kSums);
@@ -142,6 +144,22 @@ struct Kernel {
     }
   }
 
+  // Where a byte of a key's row is in a stage (of the keys, or of the values).
+  static __device__ __forceinline__ uint32_t place_in(uint32_t key, uint32_t byte) {
+    return key * S::kPitch + (S::kSwapped ? byte ^ ((key & 3) << 5 | (key & 4) << 2) : byte);
+  }
+  // The same a block of 32 values further on: rows begin on multiples of 256 bytes, or of 128 if they are no longer.
+  static __device__ __forceinline__ uint32_t block_on(uint32_t at, uint32_t block) { return S::kSwapped ? at ^ block * S::kBlockBytes : at + block * S::kBlockBytes; }
+  static __device__ __forceinline__ uint32_t word_at(uint32_t at) {
+    uint32_t x;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+    return x;
+  }
+  static __device__ __forceinline__ uint2 words_at(uint32_t at) {
+    uint2 x;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "r"(at) : "memory");
+    return x;
+  }
   // The keys and values of a step's keys on their way into a stage: lane `key` (of 16 keys, also lane 16 + key) holds where that key's row is (`place`, slot *
   // heads + head) and whether it is there. Lanes share rows, `pieces` lanes a row.
   template <int kPiece, class P>
@@ -149,20 +167,21 @@ struct Kernel {
     const uint32_t lane = threadIdx.x & 31, pieces = A.by_pieces.d;
     if ((pieces & (pieces - 1)) == 0 && pieces * M >= 2 && pieces <= 16) {  // a power of two: the piece is the same in all turns, and planes have turns of their own
       const uint32_t log = __ffs(pieces) - 1, piece = lane & (pieces - 1), step = 32 >> log, half = pieces * M / 2;
-      uint32_t row = lane >> log, to = shared_address(stage) + row * S::kPitch + piece * kPiece;
+      uint32_t row = lane >> log;
+      const uint32_t to = shared_address(stage);
       const uint8_t* codes = A.codes + piece * kPiece;
 #pragma unroll 4
-      for (uint32_t i = 0; i < pieces * M; ++i, row += step, to += step * S::kPitch) {
+      for (uint32_t i = 0; i < pieces * M; ++i, row += step) {
         if (i == half) codes += A.plane_codes;
         const P at = __shfl_sync(0xFFFFFFFFu, place, row % kKeys);
-        if (there >> (row % kKeys) & 1) copy_async<kPiece>(to, codes + (uint64_t)at * A.row_bytes);
+        if (there >> (row % kKeys) & 1) copy_async<kPiece>(to + place_in(row, piece * kPiece), codes + (uint64_t)at * A.row_bytes);
       }
     } else {
       for (uint32_t i = lane; i < 2 * kKeys * pieces; i += 32) {
         const uint32_t row = A.by_pieces.div(i), piece = i - row * pieces;
         const P at = __shfl_sync(0xFFFFFFFFu, place, row % kKeys);
         if (there >> (row % kKeys) & 1)
-          copy_async<kPiece>(shared_address(stage + row * S::kPitch + piece * kPiece), A.codes + (row / kKeys) * A.plane_codes + (uint64_t)at * A.row_bytes + piece * kPiece);
+          copy_async<kPiece>(shared_address(stage) + place_in(row, piece * kPiece), A.codes + (row / kKeys) * A.plane_codes + (uint64_t)at * A.row_bytes + piece * kPiece);
       }
     }
   }
@@ -215,7 +234,7 @@ struct Kernel {
   }
 
   static __device__ __forceinline__ void run(const AttendArgs& A) {
-    extern __shared__ __align__(16) uint8_t smem[];
+    extern __shared__ __align__(256) uint8_t smem[];
     __shared__ unsigned long long scan[kWarps], found_base;
     __shared__ uint32_t found;
     __shared__ float maxima[kWarps][S::kColumns], sums[kWarps][S::kColumns];
@@ -364,6 +383,7 @@ struct Kernel {
             key_scales[x][h] = scales + k * (2 * S::kScaleWords) + (odd.x >> k & 1);
             value_scales[x][h] = scales + (kKeys + k) * (2 * S::kScaleWords) + (odd.y >> k & 1);
           }
+        const uint32_t key_at = shared_address(stage) + place_in(row, t * kBits);  // of its first key: eight values a lane of four
         float part[M][NT][4];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
@@ -371,17 +391,17 @@ struct Kernel {
           uint32_t a[M][2][4];
 #pragma unroll
           for (int x = 0; x < M; ++x) {
-            const uint8_t *p = stage + (row + 16 * x) * S::kPitch, *r = p + 8 * S::kPitch;
+            const uint32_t p = block_on(key_at + 16 * x * S::kPitch, b), r = p + 8 * S::kPitch;
             uint32_t (&a0)[4] = a[x][0];
             uint32_t (&a1)[4] = a[x][1];
             if constexpr (kBits == 4) {
-              const uint32_t u = *reinterpret_cast<const uint32_t*>(p + b * 16 + t * 4), v = *reinterpret_cast<const uint32_t*>(r + b * 16 + t * 4);
+              const uint32_t u = word_at(p), v = word_at(r);
               a0[0] = operand<4, false>(u & 0x000F000Fu), a0[1] = operand<4, false>(v & 0x000F000Fu);
               a0[2] = operand<4, true>(u & 0x00F000F0u), a0[3] = operand<4, true>(v & 0x00F000F0u);
               a1[0] = operand<4, false>(u >> 8 & 0x000F000Fu), a1[1] = operand<4, false>(v >> 8 & 0x000F000Fu);
               a1[2] = operand<4, true>(u >> 8 & 0x00F000F0u), a1[3] = operand<4, true>(v >> 8 & 0x00F000F0u);
             } else {
-              const uint2 u = *reinterpret_cast<const uint2*>(p + b * 32 + t * 8), v = *reinterpret_cast<const uint2*>(r + b * 32 + t * 8);
+              const uint2 u = words_at(p), v = words_at(r);
               a0[0] = operand<8, false>(__byte_perm(u.x, 0, 0x4140)), a0[1] = operand<8, false>(__byte_perm(v.x, 0, 0x4140));
               a0[2] = operand<8, false>(__byte_perm(u.x, 0, 0x4342)), a0[3] = operand<8, false>(__byte_perm(v.x, 0, 0x4342));
               a1[0] = operand<8, false>(__byte_perm(u.y, 0, 0x4140)), a1[1] = operand<8, false>(__byte_perm(v.y, 0, 0x4140));
@@ -491,8 +511,9 @@ struct Kernel {
 
         // ---- probabilities, with the values' scales, times codes
         uint32_t prob[M][NT][kParts][2];
-        const uint8_t* const value = stage + kKeys * S::kPitch;
-        const uint32_t r0 = key_of<kBits>(2 * t), r1 = key_of<kBits>(2 * t + 1);
+        // where this lane's part of two neighbouring keys' values is; of 4 bits a word of eight values, dealt to products of 64 rows, or two lanes share one
+        const uint32_t part_of = kBits == 8 || kWide ? g * 4 : g / 2 * 4, values_at = shared_address(stage) + kKeys * S::kPitch;
+        const uint32_t value_a = values_at + place_in(key_of<kBits>(2 * t), part_of), value_b = values_at + place_in(key_of<kBits>(2 * t + 1), part_of);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
           if ((uint32_t)b >= value_blocks) break;
@@ -523,17 +544,16 @@ struct Kernel {
 #pragma unroll
           for (int x = 0; x < M; ++x) {
             uint32_t a0[4], a1[4];
-            const uint8_t *p = value + (16 * x + r0) * S::kPitch, *r = value + (16 * x + r1) * S::kPitch;
+            const uint32_t on = kWide ? b & ~1 : b, p = block_on(value_a + 16 * x * S::kPitch, on), r = block_on(value_b + 16 * x * S::kPitch, on);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {  // keys 2 t, 2 t + 1, and 8 behind
               if constexpr (kBits == 4) {
-                const uint32_t word = kWide ? (b >> 1) * 8 + g : b * 4 + (g >> 1), shift = kWide ? 8 * (b & 1) : 8 * (g & 1);
-                const uint32_t u = *reinterpret_cast<const uint32_t*>(p + 8 * h * S::kPitch + word * 4), v = *reinterpret_cast<const uint32_t*>(r + 8 * h * S::kPitch + word * 4);
+                const uint32_t shift = kWide ? 8 * (b & 1) : 8 * (g & 1), u = word_at(p + 8 * h * S::kPitch), v = word_at(r + 8 * h * S::kPitch);
                 const uint32_t even = __byte_perm(u, v, 0x5410) >> shift, odds = __byte_perm(u, v, 0x7632) >> shift;
                 a0[2 * h] = operand<4, false>(even & 0x000F000Fu), a0[2 * h + 1] = operand<4, false>(odds & 0x000F000Fu);
                 a1[2 * h] = operand<4, true>(even & 0x00F000F0u), a1[2 * h + 1] = operand<4, true>(odds & 0x00F000F0u);
               } else {
-                const uint32_t u = *reinterpret_cast<const uint32_t*>(p + 8 * h * S::kPitch + b * 32 + g * 4), v = *reinterpret_cast<const uint32_t*>(r + 8 * h * S::kPitch + b * 32 + g * 4);
+                const uint32_t u = word_at(p + 8 * h * S::kPitch), v = word_at(r + 8 * h * S::kPitch);
                 const uint32_t even = __byte_perm(u, v, 0x6420), odds = __byte_perm(u, v, 0x7531);
                 a0[2 * h] = operand<8, false>(even & 0x00FF00FFu), a0[2 * h + 1] = operand<8, false>(odds & 0x00FF00FFu);
                 a1[2 * h] = operand<8, false>(__byte_perm(even, 0, 0x4341)), a1[2 * h + 1] = operand<8, false>(__byte_perm(odds, 0, 0x4341));
