@@ -891,23 +891,31 @@ def cache_attend(cache, q, table, page, begin, out=None, first=None, scale=None,
     kind2, shape2, strides2 = _numbers(out, "out", 3, index)
     if kind2 != kind or shape2 != shape:
         raise ValueError("q and out differ in shape or type")
-    if table.dim() != 2 or table.dtype != torch.int32 or table.get_device() != index or (table.shape[1] > 1 and table.stride(1) != 1):
-        raise ValueError("table must be [sequences, width] int32 on the cache's device, contiguous along its last axis")
     sequences, width = table.shape
+    table_strides = table.stride()
+    if table.dtype != torch.int32 or table.get_device() != index or (width > 1 and table_strides[1] != 1):
+        raise ValueError("table must be [sequences, width] int32 on the cache's device, contiguous along its last axis")
+    i32 = torch.int32
+    at = _whole(begin, "begin", i32, index)
+    first_at = prefix_at = slopes_at = 0
+    if first is not None:
+        first_at = _whole(first, "first", i32, index)
+    if prefix is not None:
+        prefix_at = _whole(prefix, "prefix", i32, index)
     if begin.numel() != sequences + 1 or (first is not None and first.numel() != sequences) or (prefix is not None and prefix.numel() != sequences):
         raise ValueError("begin has an entry per sequence and one more, first and prefix one per sequence")
-    if slopes is not None and slopes.numel() != heads:
-        raise ValueError("slopes has an entry per head of q")
+    if slopes is not None:
+        slopes_at = _whole(slopes, "slopes", torch.float32, index)
+        if slopes.numel() != heads:
+            raise ValueError("slopes has an entry per head of q")
     if not (0 <= window < 1 << 31 and 0 <= longest < 1 << 32 and 0 <= page < 1 << 32):
         raise LCError(ERR_ARG, "lc_cache_attend")
     if workspace is None:
         workspace = alloc_attend_workspace(cache, sequences)
-    elif workspace.get_device() != index:
-        raise ValueError("workspace is on another device")
-    i32 = torch.int32
-    how = _attend(table.data_ptr(), table.stride(0), width, page, _whole(begin, "begin", i32, index), 0 if first is None else _whole(first, "first", i32, index),
-                  sequences, longest, heads, window, dim ** -0.5 if scale is None else scale, cap,
-                  0 if slopes is None else _whole(slopes, "slopes", torch.float32, index), 0 if prefix is None else _whole(prefix, "prefix", i32, index))
+    elif workspace.dtype != torch.uint8 or workspace.get_device() != index:
+        raise ValueError("workspace must be uint8 on the cache's device")
+    how = _attend(table.data_ptr(), table_strides[0], width, page, at, first_at, sequences, longest, heads, window, dim ** -0.5 if scale is None else scale, cap,
+                  slopes_at, prefix_at)
     _call("lc_cache_attend", index, cache._at, _one_plane(q.data_ptr(), strides[0], strides[1]), _one_plane(out.data_ptr(), strides2[0], strides2[1]), kind, rows,
-          how, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _status(status, index))
+          how, workspace.data_ptr(), workspace.numel(), None if status is None else _whole(status, "status", i32, index))
     return out

@@ -25,7 +25,8 @@ struct AttendArgs {
   uint32_t sequences, rows, shortest, longest;  // a kernel takes the sequences of shortest ... longest rows
   uint32_t most;                                // no sequence of the call has more rows
   uint32_t shared, window;
-  uint32_t near;  // slot * heads + head is below 2^32
+  uint32_t near;   // slot * heads + head is below 2^32
+  uint32_t whole;  // few rows: blocks are dealt out whole, not by their tiles, and nothing is joined
   float scale, cap;
   int32_t* status;
   float* parts;                 // partial results of the CTAs' first and last blocks

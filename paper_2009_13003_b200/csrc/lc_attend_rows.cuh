@@ -4,11 +4,11 @@
 //   out_i   = sum over the p that i sees of exp(t(i, p)) v_p / sum of exp(t(i, p)), or 0 if it sees none
 //
 // in one pass over the keys, with a running maximum and sum of each query (a block of keys whose scores exceed the maximum so far scales
-// what there is down by exp of the difference). Work is (sequence, block of queries of one head of the cache, tile of 64 keys); all tiles of a call
+// what there is down by exp of the difference). Work is (sequence, block of queries of one head of the cache, tile of 128 or 64 keys); all tiles of a call
 // are dealt out evenly, so that one long sequence keeps all SMs busy like many short ones. A CTA's first and last block may be shared with
 // its neighbours: those go to the workspace as sums with their maxima, and a second launch joins them in a fixed order.
 //
-// A warp holds 16 keys of a tile and multiplies codes, not values: keys are the rows of the product (m16n8k16), 8 queries its columns, and
+// A warp holds 32 or 16 keys of a tile and multiplies codes, not values: keys are the rows of the product (m16n8k16), 8 queries its columns, and
 // the values' product is transposed the same way, so that a code becomes an operand once for 8 ... 32 queries. The codes become
 // bf16 numbers by a mask and one fused multiplication for two of them, exactly: in a bf16 number's lowest 8 bits a whole number N stands
 // for N * 2^-133 (subnormals, and the first binade above, in the same steps). Queries of more than 8 bits enter as the bf16 parts that they
@@ -108,11 +108,13 @@ struct Shape {
   static constexpr uint32_t kPart = kColumns * (NB * 32 + 2);  // floats of a partial result
 };
 
-// How the tiles of a call are dealt out: `share` of them to each CTA, one behind the other.
-__device__ __forceinline__ uint64_t share_of(uint64_t tiles, uint32_t ctas) {
+// How the tiles of a call are dealt out: `share` of them to each CTA, one behind the other. (Or, if sequences are so short that joining costs more than it
+// gains, whole blocks: kWholeRoom.)
+__device__ __forceinline__ uint64_t share_of(uint64_t tiles, uint32_t ctas, bool whole) {
   const uint64_t share = (tiles + ctas - 1) / ctas;
-  return share < 2 ? 2 : share;
+  return share < 2 && !whole ? 2 : share;
 }
+constexpr uint64_t kWholeRoom = 512;
 
 // kWide: 4 bits, groups of 64 values or more: a word of eight values may be dealt to products of 64 rows.
 template <int kBits, int NB, int NT, int kParts, bool kWide>
@@ -248,7 +250,7 @@ struct Kernel {
     unsigned long long all = 0;
     for (uint32_t s = threadIdx.x; s < A.sequences; s += kThreads) {
       const Sequence q = sequence_of<kTile>(A, s, blockIdx.x == 0);
-      all += (unsigned long long)blocks_of(A, q, S::kColumns) * A.heads * q.tiles;
+      all += (unsigned long long)blocks_of(A, q, S::kColumns) * A.heads * (A.whole ? q.tiles > 0 : q.tiles);
     }
 #pragma unroll
     for (int d = 16; d; d >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, d);
@@ -257,7 +259,7 @@ struct Kernel {
     all = 0;
 #pragma unroll
     for (uint32_t w = 0; w < kWarps; ++w) all += scan[w];
-    const unsigned long long share = share_of(all, gridDim.x), from = blockIdx.x * share, to = min(from + share, all);
+    const unsigned long long share = share_of(all, gridDim.x, A.whole), from = blockIdx.x * share, to = min(from + share, all);
     if (blockIdx.x == 0 || from < all) {
       unsigned long long base = 0;
       for (uint32_t s0 = 0; s0 < A.sequences; s0 += kThreads) {
@@ -265,7 +267,7 @@ struct Kernel {
         unsigned long long mine = 0;
         if (s < A.sequences) {
           const Sequence q = sequence_of<kTile>(A, s, false);
-          mine = (unsigned long long)blocks_of(A, q, S::kColumns) * A.heads * q.tiles;
+          mine = (unsigned long long)blocks_of(A, q, S::kColumns) * A.heads * (A.whole ? q.tiles > 0 : q.tiles);
         }
         unsigned long long upto = mine;
 #pragma unroll
@@ -298,12 +300,12 @@ struct Kernel {
     Sequence q = sequence_of<kTile>(A, s, false);
     uint64_t rest = from - found_base;
     uint32_t blocks = blocks_of(A, q, S::kColumns);
-    uint32_t item = (uint32_t)(rest / q.tiles), j0 = (uint32_t)(rest - (uint64_t)item * q.tiles);  // item: block * heads + head
+    uint32_t item = A.whole ? (uint32_t)rest : (uint32_t)(rest / q.tiles), j0 = A.whole ? 0 : (uint32_t)(rest - (uint64_t)item * q.tiles);  // item: block * heads + head
     uint8_t* ring = smem + S::kQueries + warp * S::kStages * S::kStage;
     float* const red = reinterpret_cast<float*>(smem + S::kQueries);
 
     for (unsigned long long at = from; at < to;) {
-      const uint32_t j1 = (uint32_t)min((unsigned long long)q.tiles, j0 + (to - at));
+      const uint32_t j1 = A.whole ? q.tiles : (uint32_t)min((unsigned long long)q.tiles, j0 + (to - at));
       const uint32_t block = item / A.heads, head = item - block * A.heads;
       load_queries(A, q, head, block, smem);
       // the columns of this thread: positions, slopes; the block's first and last position
@@ -634,7 +636,7 @@ struct Kernel {
         part_out[S::kColumns * (NB * 32 + 1) + threadIdx.x] = sum;
       }
 
-      at += j1 - j0;
+      at += A.whole ? 1 : j1 - j0;
       j0 = 0;
       if (at < to && ++item == blocks * A.heads) {
         item = 0;
@@ -665,7 +667,7 @@ __global__ void __launch_bounds__(256 * NT) join_kernel(AttendArgs A, uint32_t c
   constexpr uint32_t kColumns = 8 * NT, kPart = kColumns * (NB * 32 + 2);
   wait_previous();
   const uint32_t lane = threadIdx.x & 31, column = threadIdx.x >> 5;
-  const unsigned long long all = A.flat[A.sequences], share = share_of(all, ctas), border = (blockIdx.x + 1) * share;
+  const unsigned long long all = A.flat[A.sequences], share = share_of(all, ctas, false), border = (blockIdx.x + 1) * share;
   if (border >= all) return;
   uint32_t lo = 0, count = A.sequences;  // the last sequence that begins at or ahead of the border, among `count`
   while (count > 1) {
@@ -725,7 +727,8 @@ __global__ void __launch_bounds__(256 * NT) join_kernel(AttendArgs A, uint32_t c
 }
 
 template <int kBits, int NB, int NT, int kParts, bool kWide>
-cudaError_t launch(const AttendArgs& a, bool overlap, cudaStream_t cs) {
+cudaError_t launch(const AttendArgs& args, bool overlap, cudaStream_t cs) {
+  AttendArgs a = args;
   using S = Shape<kBits, NB, NT, kParts>;
   constexpr int per_sm = kPerSm<kBits, NB, NT, kParts>;
   static int sms[kMaxDevices] = {};  // by device ordinal: 0 not looked at yet
@@ -744,13 +747,14 @@ cudaError_t launch(const AttendArgs& a, bool overlap, cudaStream_t cs) {
     sms[dev] = n;
   }
   // no more CTAs than there can be work for
-  const uint64_t blocks = (uint64_t)a.rows * a.shared / S::kColumns + (a.rows < a.sequences ? a.rows : a.sequences);
-  const uint64_t tiles = blocks * a.heads * ((a.room + S::kTile - 1) / S::kTile + 1);
+  const uint64_t blocks = ((uint64_t)a.rows * a.shared / S::kColumns + (a.rows < a.sequences ? a.rows : a.sequences)) * a.heads;
   uint64_t ctas = (uint64_t)sms[dev] * fit[dev];
   if (ctas > kMaxParts) ctas = kMaxParts;
-  if (ctas > (tiles + 1) / 2) ctas = (tiles + 1) / 2;
+  const uint64_t most = args.room <= kWholeRoom ? blocks : (blocks * ((a.room + S::kTile - 1) / S::kTile + 1) + 1) / 2;
+  if (ctas > most) ctas = most;
+  a.whole = args.room <= kWholeRoom;
   cudaError_t e = launch_kernel(overlap, kernel, (unsigned)ctas, kThreads, S::kWhole, cs, a);
-  if (e == cudaSuccess && ctas > 1) e = launch_kernel(true, join_kernel<NB, NT, typename Query<kParts>::T>, (unsigned)ctas - 1, 256 * NT, 0, cs, a, (uint32_t)ctas);
+  if (e == cudaSuccess && ctas > 1 && !a.whole) e = launch_kernel(true, join_kernel<NB, NT, typename Query<kParts>::T>, (unsigned)ctas - 1, 256 * NT, 0, cs, a, (uint32_t)ctas);
   return e;
 }
 

@@ -6,8 +6,8 @@ namespace {
 
 constexpr uint32_t kPlanThreads = 512, kPlanCtas = 8;  // CTAs: a portable cluster
 constexpr uint32_t kPlanHere = 4096;                   // rows whose slots the first launch writes itself
-constexpr uint32_t kSearch = 1024;                     // sequences whose beginnings fit into shared memory
-constexpr uint32_t kSlotThreads = 256;
+constexpr uint32_t kSearch = 4096;                     // sequences whose beginnings fit into shared memory
+constexpr uint32_t kSlotThreads = 256, kSlotRows = 4;  // rows of a thread
 
 struct PlanArgs {
   int32_t* table;
@@ -61,6 +61,28 @@ __device__ __forceinline__ void write_slot(const PlanArgs& A, const int32_t* beg
     else if (A.status) set_status(A.status, LC_ERR_INDEX);
   }
   A.slots[row] = slot;
+}
+
+// f(lane of the sequence, page of it) for n pages of each lane's sequence, a page a lane: sequences of a few pages and of many take their turns side by side.
+template <class F>
+__device__ __forceinline__ void for_pages(uint32_t n, F f) {
+  const uint32_t lane = threadIdx.x & 31;
+  uint32_t upto = n;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+    if (lane >= (uint32_t)d) upto += x;
+  }
+  const uint32_t all = __shfl_sync(0xFFFFFFFFu, upto, 31);
+#pragma unroll 4
+  for (uint32_t base = 0; base < all; base += 32) {
+    uint32_t owner = 0;  // the first lane whose pages end behind this one
+#pragma unroll
+    for (uint32_t step = 16; step; step >>= 1)
+      if (__shfl_sync(0xFFFFFFFFu, upto, owner + step - 1) <= base + lane) owner += step;
+    const uint32_t before = __shfl_sync(0xFFFFFFFFu, upto - n, owner);
+    f(owner, base + lane - before, base + lane < all);
+  }
 }
 
 // One cluster. Every thread takes a strip of neighbouring sequences; the threads' sums are added up within the CTA, the CTAs' read from each
@@ -147,12 +169,12 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs A) {
       A.first[s] = first;
       A.held_after[s] = first + (int32_t)x.rows;
     }
-    for (uint32_t left = __ballot_sync(0xFFFFFFFFu, x.gives > 0); left; left &= left - 1) {
-      const int from_lane = __ffs(left) - 1;
-      const uint32_t seq = __shfl_sync(0xFFFFFFFFu, s, from_lane), n = __shfl_sync(0xFFFFFFFFu, (uint32_t)x.gives, from_lane);
-      const uint32_t behind = (uint32_t)count + __shfl_sync(0xFFFFFFFFu, (uint32_t)ahead.gives, from_lane);
-      for (uint32_t i = lane; i < n; i += 32) A.spare[behind + i] = A.table[seq * A.table_stride + i];
-    }
+    const uint32_t behind = (uint32_t)count + (uint32_t)ahead.gives;
+    if (__any_sync(0xFFFFFFFFu, x.gives > 0))
+      for_pages((uint32_t)x.gives, [&](uint32_t owner, uint32_t i, bool is) {
+        const uint32_t seq = __shfl_sync(0xFFFFFFFFu, s, owner), to_list = __shfl_sync(0xFFFFFFFFu, behind, owner);
+        if (is) A.spare[to_list + i] = A.table[seq * A.table_stride + i];
+      });
     ahead = ahead + x;
   }
   cluster_meet();
@@ -166,12 +188,11 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs A) {
         has = pages_of(A.by_page, first);
         n = pages_of(A.by_page, after) - has;
       }
-      for (uint32_t left = __ballot_sync(0xFFFFFFFFu, n > 0); left; left &= left - 1) {
-        const int from_lane = __ffs(left) - 1;
-        const uint32_t seq = __shfl_sync(0xFFFFFFFFu, s, from_lane), m = __shfl_sync(0xFFFFFFFFu, n, from_lane), j = __shfl_sync(0xFFFFFFFFu, has, from_lane);
-        const uint32_t last = top - 1 - __shfl_sync(0xFFFFFFFFu, wants, from_lane);
-        for (uint32_t i = lane; i < m; i += 32) A.table[seq * A.table_stride + j + i] = A.spare[last - i];
-      }
+      if (__any_sync(0xFFFFFFFFu, n > 0))
+        for_pages(n, [&](uint32_t owner, uint32_t i, bool is) {
+          const uint32_t seq = __shfl_sync(0xFFFFFFFFu, s, owner), j = __shfl_sync(0xFFFFFFFFu, has, owner), last = top - 1 - __shfl_sync(0xFFFFFFFFu, wants, owner);
+          if (is) A.table[seq * A.table_stride + j + i] = A.spare[last - i];
+        });
       wants += n;
     }
   }
@@ -194,8 +215,11 @@ __global__ void __launch_bounds__(kSlotThreads) slots_kernel(PlanArgs A) {
     for (uint32_t i = threadIdx.x; i <= A.sequences; i += kSlotThreads) begins[i] = A.begin[i];
     __syncthreads();
   }
-  const uint64_t row = (uint64_t)blockIdx.x * kSlotThreads + threadIdx.x;
-  if (row < A.rows) write_slot(A, here ? begins : A.begin, (uint32_t)row);
+#pragma unroll
+  for (uint32_t k = 0; k < kSlotRows; ++k) {
+    const uint64_t row = ((uint64_t)blockIdx.x * kSlotRows + k) * kSlotThreads + threadIdx.x;
+    if (row < A.rows) write_slot(A, here ? begins : A.begin, (uint32_t)row);
+  }
 }
 
 }  // namespace
@@ -245,7 +269,7 @@ extern "C" int lc_cache_plan(const lc_pages* pages, const int32_t* tokens, uint3
   cfg.attrs = at;
   cfg.numAttrs = 1;
   if (cudaLaunchKernelEx(&cfg, plan_kernel, a) != cudaSuccess) return LC_ERR_CUDA;
-  if (rows > kPlanHere && launch_kernel(true, slots_kernel, (unsigned)((rows + kSlotThreads - 1) / kSlotThreads), kSlotThreads, 0, cs, a) != cudaSuccess)
+  if (rows > kPlanHere && launch_kernel(true, slots_kernel, (unsigned)((rows + kSlotThreads * kSlotRows - 1) / (kSlotThreads * kSlotRows)), kSlotThreads, 0, cs, a) != cudaSuccess)
     return LC_ERR_CUDA;
   return LC_OK;
 }
