@@ -824,14 +824,19 @@ def alloc_pages(sequences, width, pages, page, device) -> Pages:
                  torch.full((1,), pages, dtype=torch.int32, device=device), page)
 
 
-class Plan(NamedTuple):
-    """A step of a batch (lc_cache_plan): ``begin`` [sequences + 1], ``first`` [sequences], ``slots`` [rows], and the books after it."""
+class Plan:
+    """A step of a batch (lc_cache_plan): ``begin`` [sequences + 1], ``first`` [sequences] int32, ``slots`` [rows] int64, and the books after it, ``held``
+    [sequences] and ``count`` [1] int32, tensors of one CUDA device."""
 
-    begin: torch.Tensor
-    first: torch.Tensor
-    slots: torch.Tensor
-    held: torch.Tensor
-    count: torch.Tensor
+    def __init__(self, begin, first, slots, held, count):
+        index = begin.get_device()
+        pointers = [_whole(t, name, torch.int64 if name == "slots" else torch.int32, index)
+                    for t, name in ((begin, "begin"), (first, "first"), (slots, "slots"), (held, "held"), (count, "count"))]
+        self.sequences = first.numel()
+        if index < 0 or begin.numel() != self.sequences + 1 or held.numel() != self.sequences or count.numel() != 1:
+            raise ValueError("first and held have an entry per sequence, begin one more, count one, on a CUDA device")
+        self.begin, self.first, self.slots, self.held, self.count = begin, first, slots, held, count
+        self._index, self._to = index, (slots.numel(), *pointers)
 
 
 def alloc_plan(pages, rows, in_place=True) -> Plan:
@@ -850,13 +855,9 @@ def cache_plan(pages, tokens, rows=None, plan=None, status=None) -> Plan:
             raise ValueError("rows or a plan is needed")
         plan = alloc_plan(pages, rows)
     index, sequences = pages._index, pages.sequences
-    begin, first, slots, held, count = plan
-    if tokens.numel() != sequences or begin.numel() != sequences + 1 or first.numel() != sequences or held.numel() != sequences or count.numel() != 1:
-        raise ValueError("tokens, first and held have an entry per sequence, begin one more, count one")
-    i32 = torch.int32
-    _call("lc_cache_plan", index, pages._at, _whole(tokens, "tokens", i32, index), sequences, slots.numel(), _whole(begin, "begin", i32, index),
-          _whole(first, "first", i32, index), _whole(slots, "slots", torch.int64, index), _whole(held, "held", i32, index), _whole(count, "count", i32, index),
-          _status(status, index))
+    if tokens.numel() != sequences or plan.sequences != sequences or plan._index != index:
+        raise ValueError("tokens and the plan have as many sequences as the pages, on one device")
+    _call("lc_cache_plan", index, pages._at, _whole(tokens, "tokens", torch.int32, index), sequences, *plan._to, _status(status, index))
     return plan
 
 

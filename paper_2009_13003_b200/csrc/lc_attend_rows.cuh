@@ -317,6 +317,7 @@ struct Kernel {
         position[c] = q.first + token;
         slope[c] = A.slopes ? A.slopes[head * A.shared + h] * kLog2e : 0.0f;
       }
+      const int used = NT == 1 ? 1 : (int)min((uint32_t)NT, (q.rows * A.shared - block * S::kColumns + 7) / 8);  // eights of columns that hold queries
       const uint32_t low = q.first + A.by_shared.div(block * S::kColumns);
       const uint32_t high = q.first + min(A.by_shared.div(block * S::kColumns + S::kColumns - 1), q.rows - 1);
       // of the tiles j0 ... j1 - 1, those that some query of the block sees: some of the prefix's and some behind
@@ -413,6 +414,7 @@ struct Kernel {
           const bool begins = (b & (A.per_group - 1)) == 0, ends = ((b + 1) & (A.per_group - 1)) == 0 || (uint32_t)b + 1 == words;
 #pragma unroll
           for (int c = 0; c < NT; ++c) {
+            if (c >= used) break;
             if (begins) {
 #pragma unroll
               for (int x = 0; x < M; ++x) part[x][c][0] = part[x][c][1] = part[x][c][2] = part[x][c][3] = 0.0f;
@@ -433,6 +435,7 @@ struct Kernel {
               const float sa = bf16_float(*key_scales[x][0]++), sb = bf16_float(*key_scales[x][1]++);
 #pragma unroll
               for (int c = 0; c < NT; ++c) {
+                if (c >= used) break;
                 score[x][c][0] = fmaf(part[x][c][0], sa, score[x][c][0]);
                 score[x][c][1] = fmaf(part[x][c][1], sa, score[x][c][1]);
                 score[x][c][2] = fmaf(part[x][c][2], sb, score[x][c][2]);
@@ -449,6 +452,7 @@ struct Kernel {
         float top[NT][2];
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
+          if (c >= used) break;
 #pragma unroll
           for (int x = 0; x < M; ++x)
 #pragma unroll
@@ -485,7 +489,8 @@ struct Kernel {
         }
         if (__any_sync(0xFFFFFFFFu, higher)) {
 #pragma unroll
-          for (int c = 0; c < NT; ++c)
+          for (int c = 0; c < NT; ++c) {
+            if (c >= used) break;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               // by its own scores alone, so that a query's bits do not depend on those beside it
@@ -497,9 +502,11 @@ struct Kernel {
 #pragma unroll
                 for (int x = 0; x < 2; ++x) o[b][x][c][h] *= down, o[b][x][c][h + 2] *= down;
             }
+          }
         }
 #pragma unroll
-        for (int c = 0; c < NT; ++c)
+        for (int c = 0; c < NT; ++c) {
+          if (c >= used) break;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const float base = m[c][h] == -INFINITY ? 0.0f : m[c][h];
@@ -510,6 +517,7 @@ struct Kernel {
               l[c][h] += score[x][c][h] + score[x][c][h + 2];
             }
           }
+        }
 
         // ---- probabilities, with the values' scales, times codes
         uint32_t prob[M][NT][kParts][2];
@@ -525,6 +533,7 @@ struct Kernel {
               const float sa = bf16_float(*value_scales[x][0]++), sb = bf16_float(*value_scales[x][1]++);
 #pragma unroll
               for (int c = 0; c < NT; ++c) {
+                if (c >= used) break;
                 float p[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) p[e] = score[x][c][e] * (e < 2 ? sa : sb);
@@ -562,12 +571,14 @@ struct Kernel {
               }
             }
 #pragma unroll
-            for (int c = 0; c < NT; ++c)
+            for (int c = 0; c < NT; ++c) {
+              if (c >= used) break;
 #pragma unroll
               for (int k = 0; k < kParts; ++k) {
                 mma_bf16(o[b][0][c], a0, prob[x][c][k][0], prob[x][c][k][1]);
                 mma_bf16(o[b][1][c], a1, prob[x][c][k][0], prob[x][c][k][1]);
               }
+            }
           }
         }
       }

@@ -24,7 +24,12 @@ struct PlanArgs {
   FastDiv by_page;
 };
 
+// The CTAs of the cluster meet, and see what the others wrote ahead of it. One alone needs less.
 __device__ __forceinline__ void cluster_meet() {
+  if (gridDim.x == 1) {
+    __syncthreads();
+    return;
+  }
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -45,8 +50,8 @@ __device__ __forceinline__ Ask ask(const PlanArgs& A, int32_t held, int32_t toke
   return Ask{(uint64_t)tokens, pages_of(A.by_page, held + tokens) - pages_of(A.by_page, held), 0};
 }
 
-// The slot of a row. begins: where the sequences begin, in shared memory where that fits.
-__device__ __forceinline__ void write_slot(const PlanArgs& A, const int32_t* begins, uint32_t row) {
+// The slot of a row. begins, firsts: where the sequences begin, and at which position, in shared memory where that fits.
+__device__ __forceinline__ void write_slot(const PlanArgs& A, const int32_t* begins, const int32_t* firsts, uint32_t row) {
   uint32_t lo = 0, hi = A.sequences;
   while (lo < hi) {
     const uint32_t mid = (lo + hi) / 2;
@@ -55,7 +60,7 @@ __device__ __forceinline__ void write_slot(const PlanArgs& A, const int32_t* beg
   }
   int64_t slot = -1;
   if (lo < A.sequences) {
-    const uint32_t at = (uint32_t)A.first[lo] + (row - (uint32_t)begins[lo]), page = A.by_page.div(at);
+    const uint32_t at = (uint32_t)firsts[lo] + (row - (uint32_t)begins[lo]), page = A.by_page.div(at);
     const int32_t number = A.table[lo * A.table_stride + page];
     if (number >= 0 && (uint32_t)number < A.pages) slot = (int64_t)number * A.by_page.d + (at - page * A.by_page.d);
     else if (A.status) set_status(A.status, LC_ERR_INDEX);
@@ -93,7 +98,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs A) {
   __shared__ Ask warps[kPlanThreads / 32];
   __shared__ Ask mine;
   __shared__ uint32_t faults;
-  __shared__ int32_t begins[kSearch + 1];
+  __shared__ int32_t begins[kPlanThreads + 1], firsts[kPlanThreads];  // of one CTA alone
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, all = gridDim.x * kPlanThreads, me = blockIdx.x * kPlanThreads + threadIdx.x;
   const uint32_t strip = (A.sequences + all - 1) / all;
   const uint32_t from = (uint32_t)min((uint64_t)me * strip, (uint64_t)A.sequences), to = (uint32_t)min((uint64_t)from + strip, (uint64_t)A.sequences);
@@ -104,14 +109,12 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs A) {
   const int32_t count = *A.count;
   Ask sum = {0, 0, 0};
   uint32_t bad = 0;  // 1: the books are wrong, 2: no room
+  int32_t held = 0, tokens = 0, first = 0, after = 0;  // of a strip of one sequence all the way
   for (uint32_t s = from; s < to; ++s) {
-    const int32_t held = A.held[s], tokens = A.tokens[s];
+    held = A.held[s], tokens = A.tokens[s];
     if (held < 0 || (uint64_t)held > A.room) bad |= 1;
     else if (tokens > 0 && (uint64_t)held + (uint64_t)tokens > A.room) bad |= 2;
-    else {
-      int32_t first;
-      sum = sum + ask(A, held, tokens, first);
-    }
+    else sum = sum + ask(A, held, tokens, first);
   }
   if (bad) atomicOr(&faults, bad);
   Ask ahead = sum;  // of this thread's strip and those before it in the warp
@@ -148,11 +151,12 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs A) {
   if (count < 0 || (uint64_t)count + whole.gives > A.pages) fault |= 1;
   else if (whole.wants > (uint64_t)count + whole.gives || whole.rows > A.rows) fault |= 2;
   const uint32_t top = (uint32_t)count + (uint32_t)whole.gives;  // pages in the list once all are back
-  const bool ok = fault == 0;
+  const bool ok = fault == 0, here = gridDim.x == 1 && strip <= 1;
   if (me == 0) {
     if (!ok && A.status) set_status(A.status, fault & 1 ? LC_ERR_INDEX : LC_ERR_CAPACITY);
     *A.count_after = ok ? (int32_t)(top - (uint32_t)whole.wants) : count;
     A.begin[A.sequences] = ok ? (int32_t)whole.rows : 0;
+    if (here) begins[A.sequences] = ok ? (int32_t)whole.rows : 0;
   }
 
   // a warp's sequences: books by its lanes, pages of one sequence after the other by all of them
@@ -162,12 +166,15 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs A) {
     const bool there = s < to;
     Ask x = {0, 0, 0};
     if (there) {
-      const int32_t held = A.held[s], tokens = A.tokens[s];
-      int32_t first = held;
+      if (strip > 1) held = A.held[s], tokens = A.tokens[s];
+      first = held;
       if (ok) x = ask(A, held, tokens, first);
-      A.begin[s] = ok ? (int32_t)ahead.rows : 0;
+      after = first + (int32_t)x.rows;
+      const int32_t begin = ok ? (int32_t)ahead.rows : 0;
+      A.begin[s] = begin;
       A.first[s] = first;
-      A.held_after[s] = first + (int32_t)x.rows;
+      A.held_after[s] = after;
+      if (here) begins[s] = begin, firsts[s] = first;
     }
     const uint32_t behind = (uint32_t)count + (uint32_t)ahead.gives;
     if (__any_sync(0xFFFFFFFFu, x.gives > 0))
@@ -184,7 +191,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs A) {
       const uint32_t s = from + k;
       uint32_t has = 0, n = 0;
       if (s < to) {
-        const int32_t first = A.first[s], after = A.held_after[s];
+        if (strip > 1) first = A.first[s], after = A.held_after[s];
         has = pages_of(A.by_page, first);
         n = pages_of(A.by_page, after) - has;
       }
@@ -198,12 +205,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs A) {
   }
   if (A.rows > kPlanHere) return;
   cluster_meet();
-  const bool here = A.sequences <= kSearch;
-  if (here) {
-    for (uint32_t i = threadIdx.x; i <= A.sequences; i += kPlanThreads) begins[i] = A.begin[i];
-    __syncthreads();
-  }
-  for (uint32_t row = me; row < A.rows; row += all) write_slot(A, here ? begins : A.begin, row);
+  for (uint32_t row = me; row < A.rows; row += all) write_slot(A, here ? begins : A.begin, here ? firsts : A.first, row);
 }
 
 // The slots of a larger batch, a second launch over all SMs.
@@ -218,7 +220,7 @@ __global__ void __launch_bounds__(kSlotThreads) slots_kernel(PlanArgs A) {
 #pragma unroll
   for (uint32_t k = 0; k < kSlotRows; ++k) {
     const uint64_t row = ((uint64_t)blockIdx.x * kSlotRows + k) * kSlotThreads + threadIdx.x;
-    if (row < A.rows) write_slot(A, here ? begins : A.begin, (uint32_t)row);
+    if (row < A.rows) write_slot(A, here ? begins : A.begin, A.first, (uint32_t)row);
   }
 }
 
