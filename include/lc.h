@@ -486,7 +486,7 @@ int lc_cache_plan(const lc_pages* pages, const int32_t* tokens, uint32_t sequenc
  * table, table_stride, width, page, begin, first, sequences   as for lc_cache_read_pages.
  * longest    no sequence has more rows than that; 0: not known. A smaller bound may choose a faster kernel.
  * slopes     DEVICE fp32, one per head of q, or NULL.     prefix   DEVICE, one per sequence, or NULL for 0.
- * scale      finite; cap finite, 0 for none. window below 2^31, 0 for none. heads <= 65536, a multiple of the cache's; rows * heads < 2^30.
+ * scale      at most 1e30 in magnitude; cap at most 1e30, 0 for none. window below 2^31, 0 for none. heads <= 65536, a multiple of the cache's; rows * heads < 2^30.
  * status     as for lc_cache_read_pages: LC_ERR_INDEX if a sequence has rows or positions that are not there (begin outside of q, more rows than
  *            `longest`, positions below 0 or beyond its row of the table: its rows are left as they are), or a page that the cache does not
  *            have (its keys and values count as zeros).

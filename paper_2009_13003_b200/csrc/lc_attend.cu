@@ -9,6 +9,8 @@ uint64_t flat_bytes(uint64_t sequences) { return (8 * (sequences + 1) + 255) / 2
 // Queries of a sequence for one head of the cache up to which the kernel for few rows takes it.
 constexpr uint32_t kFewQueries = 16;
 
+constexpr float kLargest = 1e30f;  // of scale and cap: what is made of them stays in fp32's range
+
 // A cache that can be attended to, whatever the number of its slots.
 bool shape_ok(const lc_cache* cache) {
   if (!cache || cache->planes != 2 || cache->dim > kAttendDim) return false;
@@ -36,7 +38,7 @@ int lc_cache_attend(const lc_cache* cache, const lc_rows* q, const lc_rows* out,
   if (how->page < 1 || how->page >= (1u << 31) || how->sequences >= (1u << 31) || how->table_stride >= (1ull << 32) ||
       (how->sequences > 1 && how->table_stride < how->width) || how->window >= (1u << 31))
     return LC_ERR_ARG;
-  if (!(how->scale - how->scale == 0.0f) || !(how->cap >= 0.0f) || !(how->cap - how->cap == 0.0f)) return LC_ERR_ARG;  // finite, cap not negative
+  if (!(how->scale >= -kLargest && how->scale <= kLargest) || !(how->cap >= 0.0f && how->cap <= kLargest)) return LC_ERR_ARG;
   if (rows == 0 || how->sequences == 0) return LC_OK;
   const lc_rows* both[2] = {q, out};
   for (const lc_rows* r : both)
@@ -85,7 +87,7 @@ int lc_cache_attend(const lc_cache* cache, const lc_rows* q, const lc_rows* out,
   a.window = how->window;
   a.near = cache->slots < 0xFFFFFFFFull / cache->heads;
   a.scale = how->scale;
-  a.cap = how->cap;
+  a.cap = how->cap > 0.0f && how->cap < 1.0f / kLargest ? 1.0f / kLargest : how->cap;  // below that scores are 0 all the same
   a.status = status;
   a.flat = static_cast<unsigned long long*>(workspace);
   a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + 2 * flat_bytes(how->sequences));

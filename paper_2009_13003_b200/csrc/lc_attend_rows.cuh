@@ -243,7 +243,7 @@ struct Kernel {
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const uint32_t words = (A.dim + 31) / 32;  // blocks of 32 values that are there
     const uint32_t value_blocks = kWide ? (words + 1) & ~1u : words;
-    const float factor = kUnit * A.scale * kLog2e, cap_in = 2.0f * factor / A.cap, cap_out = A.cap * kLog2e;
+    const float factor = kUnit * A.scale * kLog2e, cap_in = 2.0f / A.cap, cap_out = A.cap * kLog2e;
     begin_next();
 
     // all tiles of the call, and where this CTA's begin
@@ -461,7 +461,7 @@ struct Kernel {
               float y = score[x][c][e];
               if (A.cap > 0.0f) {
                 // cap * tanh(z / cap), z = score * scale
-                const float u = exp2_fast(y * cap_in);
+                const float u = exp2_fast(y * factor * cap_in);
                 y = fmaf(-2.0f * cap_out, reciprocal(1.0f + u), cap_out);
               } else {
                 y *= factor;

@@ -3,13 +3,14 @@
 // A CTA takes blocks of 256 queries of one head of the cache (its tokens, times the heads that share it) as two tiles of 128, and goes through the keys
 // 128 at a time with a running maximum and sum of each query. Its warps have one task each: four read the keys' codes and four the values', turn them into
 // numbers of the queries' type and store them as operands (both in one layout, rows of 64 values with the 128-byte swizzle: keys are read along a row, values across);
+// two warps look up where the next tiles' keys lie, and their scales;
 // a thread for each tile issues its products; a warpgroup for each tile takes the scores out of tensor memory, a query a thread, and puts the probabilities back
 // there, over the scores, as the first operand of the product with the values. Scores go to the warps 64 keys at a time: while one half of a tile is with
 // them, the products of the other half, and of the other tile, run.
 // The sums of the values stay in tensor memory; they are scaled down only where a score exceeds the maximum so far by more than a factor of 2^kSlack.
 //
 // What a code stands for is rounded to the type once. bf16: code / 64 is exact (see lc_attend_rows.cuh) and times the scale rounded; the 64 comes in
-// with the scores' factor, so that nothing overflows. fp16: keys in units of a power of two of their tile, so that no magnitude of them is out of the
+// with the scores' factor, so that nothing overflows. fp16: keys in units of a power of two of 16 neighbours, so that no magnitude of them is out of the
 // type; values as lc_cache_read gives them, but numbers beyond the type as its largest. A value of NaN enters as 0, or rows that do not see it would
 // get 0 * NaN; rows that do get their NaN at the end.
 //
@@ -21,12 +22,11 @@ namespace lc {
 namespace {
 
 constexpr uint32_t kRows = 128, kKeys = 128, kHalf = 64;  // of a tile of queries, of keys, of the keys that are between products and warps at a time
-constexpr uint32_t kSoftmaxWarps = 8, kReadWarps = 4;   // kReadWarps each for keys and for values, then the warp that issues
+constexpr uint32_t kSoftmaxWarps = 8, kReadWarps = 4;   // kReadWarps each for keys and for values, then two that issue and two that look up
 constexpr uint32_t kThreads = 32 * (kSoftmaxWarps + 2 * kReadWarps + 4), kReaders = 32 * kReadWarps;
 // Registers of a thread: as launched, and what each warpgroup then has (together no more than before).
 constexpr uint32_t kRegsAtLaunch = 96, kRegsSoftmax = 152, kRegsReader = 64, kRegsIssue = 48;
 static_assert(2 * kRegsSoftmax + 2 * kRegsReader + kRegsIssue <= 5 * kRegsAtLaunch && kThreads == 5 * 128, "registers of five warpgroups");
-static_assert(kReaders == kKeys && kHalf == 64, "a reader looks up a key; a half of a tile is that of two warps");
 constexpr uint32_t kStages = 3;                         // halves of a tile of keys, and of values, as operands
 constexpr uint32_t kAhead = 3;                          // halves whose codes are on their way
 constexpr uint32_t kFound = 4;                          // tiles whose keys have been looked up
@@ -517,7 +517,7 @@ struct Kernel {
     __syncthreads();
     order_after();
     const uint32_t tensor = S.tensor;
-    const float scale = fmaxf(fabsf(A.scale), 1e-30f) * (kBf16 ? 64.0f : 1.0f);  // 0: times -Inf, a key that is not seen, would be no number
+    const float scale = fabsf(A.scale) * (kBf16 ? 64.0f : 1.0f);
     volatile uint32_t* dead = &S.dead;
     Walk walk(A, S.found, from - S.found_base, from, to);
     uint32_t done = 0;  // tiles of keys so far: what the barriers' phases go by
@@ -529,145 +529,152 @@ struct Kernel {
         const Sequence& q = walk.q;
         const Tiles& tiles = walk.tiles;
         const uint32_t block = walk.block, head = walk.head, j0 = walk.j0, n = walk.n, s = walk.s;
-        {
-          // ---- scores to probabilities: a query a thread
-          const uint32_t t = warp / 4, row = threadIdx.x % kRows, r = block * kTileRows + t * kRows + row, token = A.by_shared.div(r), in_group = r - token * A.shared;
-          const uint32_t lanes = tensor + ((warp & 3) * 32 << 16), scores = lanes + L::kScoresAt + t * kKeys, sums = lanes + L::kSumsAt + t * DP;
-          const uint32_t position = q.first + min(token, q.rows - 1);
-          const float slope = kBias ? A.slopes[head * A.shared + in_group] * kLog2e : 0.0f;
-          const float cap_out = A.cap * kLog2e;
-          // positions of this warp's first and last query
-          const uint32_t low = __shfl_sync(0xFFFFFFFFu, position, 0), high = __shfl_sync(0xFFFFFFFFu, position, 31);
-          float m = -INFINITY;
-          Two l = two(0.0f, 0.0f);
-          uint32_t broken = 0;  // groups whose value is no number for this query
-          load_queries(A, q, block * kTileRows + t * kRows, head, row, queries + t * L::kQueries);
-          order_for_products();
-          order_before();  // the sums of the block before are read
-          barrier_arrive(shared_address(&S.queries[t]));
-          good = false;  // all tiles are through
-          for (uint32_t i = 0; i < 2 * n; ++i) {
-            const uint32_t number = done + i / 2, half = i & 1, key = tiles.key(j0 + i / 2) + half * kHalf, at = scores + half * kHalf;
-            if (!warp_wait(shared_address(&S.scores[t][half]), number & 1, dead)) break;
-            order_after();
-            float y[kHalf];
-            tensor_load(at, y);
-            float factor[kHalf / 16];  // of 16 keys each
+        // ---- scores to probabilities: a query a thread
+        const uint32_t t = warp / 4, row = threadIdx.x % kRows, r = block * kTileRows + t * kRows + row, token = A.by_shared.div(r), in_group = r - token * A.shared;
+        const uint32_t lanes = tensor + ((warp & 3) * 32 << 16), scores = lanes + L::kScoresAt + t * kKeys, sums = lanes + L::kSumsAt + t * DP;
+        const uint32_t position = q.first + min(token, q.rows - 1);
+        const float slope = kBias ? A.slopes[head * A.shared + in_group] * kLog2e : 0.0f;
+        const float cap_out = A.cap * kLog2e;
+        // positions of this warp's first and last query
+        const uint32_t low = __shfl_sync(0xFFFFFFFFu, position, 0), high = __shfl_sync(0xFFFFFFFFu, position, 31);
+        float m = -INFINITY;
+        Two l = two(0.0f, 0.0f);
+        uint32_t broken = 0;  // groups whose value is no number for this query
+        load_queries(A, q, block * kTileRows + t * kRows, head, row, queries + t * L::kQueries);
+        order_for_products();
+        order_before();  // the sums of the block before are read
+        barrier_arrive(shared_address(&S.queries[t]));
+        good = false;  // all tiles are through
+        for (uint32_t i = 0; i < 2 * n; ++i) {
+          const uint32_t number = done + i / 2, half = i & 1, key = tiles.key(j0 + i / 2) + half * kHalf, at = scores + half * kHalf;
+          if (!warp_wait(shared_address(&S.scores[t][half]), number & 1, dead)) break;
+          order_after();
+          float y[kHalf];
+          tensor_load(at, y);
+          float factor[kHalf / 16];  // of 16 keys each; not 0, or a key that is not seen, -Inf, times that would be no number
 #pragma unroll
-            for (uint32_t c = 0; c < kHalf / 16; ++c) factor[c] = scale * kLog2e * (kBf16 ? 1.0f : S.units[number % kMemo][half * 4 + c]);
-            const bool full = key + kHalf - 1 <= low && (A.window == 0 || high - key < A.window);
-            tensor_loaded(y);
-            if constexpr (kCap || kBias) {
-              const float cap_in = kCap ? 2.0f / A.cap : 0.0f, away = (float)(int32_t)(position - key);
+          for (uint32_t c = 0; c < kHalf / 16; ++c) factor[c] = fmaxf(scale * kLog2e * (kBf16 ? 1.0f : S.units[number % kMemo][half * 4 + c]), 1e-37f);
+          const bool full = key + kHalf - 1 <= low && (A.window == 0 || high - key < A.window);
+          tensor_loaded(y);
+          if constexpr (kCap || kBias) {
+            const float cap_in = kCap ? 2.0f / A.cap : 0.0f, away = (float)(int32_t)(position - key);
 #pragma unroll
-              for (uint32_t e = 0; e < kHalf; ++e) {
-                y[e] = kCap ? fmaf(-2.0f * cap_out, reciprocal(1.0f + exp2_fast(y[e] * factor[e / 16] * cap_in)), cap_out) : y[e] * factor[e / 16];
-                if constexpr (kBias) y[e] = fmaf(-slope, fabsf(away - (float)e), y[e]);
-              }
+            for (uint32_t e = 0; e < kHalf; ++e) {
+              y[e] = kCap ? fmaf(-2.0f * cap_out, reciprocal(1.0f + exp2_fast(y[e] * factor[e / 16] * cap_in)), cap_out) : y[e] * factor[e / 16];
+              if constexpr (kBias) y[e] = fmaf(-slope, fabsf(away - (float)e), y[e]);
             }
-            if (!full) {
-              // of these keys a query sees those from `begin` on and ahead of `end`, and those ahead of `prefix`
-              const int32_t end = (int32_t)(position - key) + 1, begin = A.window ? end - (int32_t)A.window : 0, prefix = (int32_t)(q.prefix - key);
-#pragma unroll
-              for (uint32_t c = 0; c < kHalf; c += 32) {
-                const uint32_t seen = (bits_below(end - (int32_t)c) & ~bits_below(begin - (int32_t)c)) | bits_below(prefix - (int32_t)c);
-#pragma unroll
-                for (uint32_t e = 0; e < 32; ++e) y[c + e] = seen >> e & 1 ? y[c + e] : -INFINITY;
-              }
-            }
-            float top = -INFINITY;
-#pragma unroll
-            for (uint32_t c = 0; c < kHalf; c += 16) {
-              float x = fmaxf(y[c], y[c + 1]);
-#pragma unroll
-              for (uint32_t e = 2; e < 16; e += 2) x = max_of(x, y[c + e], y[c + e + 1]);
-              top = fmaxf(top, kCap || kBias ? x : x * factor[c / 16]);  // grows with the product
-            }
-            const bool rises = top > m + kSlack;
-            if (__any_sync(0xFFFFFFFFu, rises)) {
-              const float now = rises ? top : m, down = rises ? exp2_fast(m - now) : 1.0f;
-              if (i > 0) {
-                // the product before (the one before that has ended, or these scores would not be there)
-                if (!warp_wait(shared_address(&S.sums[t][1 - half]), (done + (i - 1) / 2) & 1, dead)) break;
-                order_after();
-#pragma unroll 1
-                for (uint32_t d = 0; d < DP; d += 16) scale_sums(sums + d, down);
-              }
-              m = now;
-              l = mul_two(l, two(down, down));
-            }
-            const float base = (m == -INFINITY ? 0.0f : m) - kLift;
-            uint32_t p[kHalf / 2];
-#pragma unroll
-            for (uint32_t e = 0; e < kHalf; e += 2) {
-              if constexpr (!kCap && !kBias) split_two(fma_two(two(y[e], y[e + 1]), two(factor[e / 16], factor[e / 16]), two(-base, -base)), y[e], y[e + 1]);
-              else split_two(add_two(two(y[e], y[e + 1]), two(-base, -base)), y[e], y[e + 1]);
-              y[e] = exp2_fast(y[e]), y[e + 1] = exp2_fast(y[e + 1]);
-              l = add_two(l, two(y[e], y[e + 1]));
-              p[e / 2] = rounded<kBf16>(y[e], y[e + 1]);
-            }
-            tensor_store(at, p);
-            tensor_stored();
-            order_before();
-            barrier_arrive(shared_address(&S.weights[t][half]));
-            good = i + 1 == 2 * n;
           }
-          for (uint32_t h = 0; h < 2; ++h) good = good && warp_wait(shared_address(&S.sums[t][h]), (done + n - 1) & 1, dead);
-          if (good) {
-            order_after();
-            if (S.broken) {  // some value was no number: which of this block's are, and this query sees
-              for (uint32_t k = 0; k < n * kKeys; ++k) {
-                const uint32_t at_key = tiles.key(j0 + k / kKeys) + k % kKeys;
-                const bool visible = (at_key <= position && (A.window == 0 || position - at_key < A.window)) || at_key < q.prefix;
-                const uint32_t place = place_of_key(A, q, head, at_key, page_of(A, q, s, at_key));
-                if (place == kNone || !visible) continue;
-                for (uint32_t g = 0; g < A.groups; ++g)
-                  if ((A.scales[A.plane_scales + (uint64_t)place * A.groups + g] & 0x7F80u) == 0x7F80u) broken |= 1u << g;
-              }
+          if (!full) {
+            // of these keys a query sees those from `begin` on and ahead of `end`, and those ahead of `prefix`
+            const int32_t end = (int32_t)(position - key) + 1, begin = A.window ? end - (int32_t)A.window : 0, prefix = (int32_t)(q.prefix - key);
+#pragma unroll
+            for (uint32_t c = 0; c < kHalf; c += 32) {
+              const uint32_t seen = (bits_below(end - (int32_t)c) & ~bits_below(begin - (int32_t)c)) | bits_below(prefix - (int32_t)c);
+#pragma unroll
+              for (uint32_t e = 0; e < 32; ++e) y[c + e] = seen >> e & 1 ? y[c + e] : -INFINITY;
             }
-            const bool whole = j0 == 0 && n == tiles.count, there = token < q.rows;
-            float* part = A.parts + (2ull * blockIdx.x + (walk.first ? 0 : 1)) * (kTilePartBytes / 4);
-            T* out = static_cast<T*>(A.out) + (uint64_t)(q.row + min(token, q.rows - 1)) * A.out_row + (uint64_t)(head * A.shared + in_group) * A.out_head;
-            const bool aligned = ((reinterpret_cast<uintptr_t>(A.out) / 2 | A.out_row | A.out_head) & 7) == 0;
-            float sum, other;
-            split_two(l, sum, other);
-            sum += other;
-            const float over = whole ? (kBf16 ? 64.0f : 1.0f) / sum : 1.0f;
-            const uint32_t shift = 5 + (A.per_group > 1) + (A.per_group > 2);  // values of a group
+          }
+          float top = -INFINITY;
+#pragma unroll
+          for (uint32_t c = 0; c < kHalf; c += 16) {
+            float x = fmaxf(y[c], y[c + 1]);
+#pragma unroll
+            for (uint32_t e = 2; e < 16; e += 2) x = max_of(x, y[c + e], y[c + e + 1]);
+            top = fmaxf(top, kCap || kBias ? x : __fmul_rn(x, factor[c / 16]));  // grows with the product
+          }
+          const bool rises = top > m + kSlack;
+          if (__any_sync(0xFFFFFFFFu, rises)) {
+            const float now = rises ? top : m, down = rises ? exp2_fast(m - now) : 1.0f;
+            if (i > 0) {
+              // the product before (the one before that has ended, or these scores would not be there)
+              if (!warp_wait(shared_address(&S.sums[t][1 - half]), (done + (i - 1) / 2) & 1, dead)) break;
+              order_after();
 #pragma unroll 1
-            for (uint32_t c = 0; c < A.dim; c += 32) {
-              float x[32];
-              tensor_load(sums + c, x);
-              tensor_loaded(x);
+              for (uint32_t d = 0; d < DP; d += 16) scale_sums(sums + d, down);
+            }
+            m = now;
+            l = mul_two(l, two(down, down));
+          }
+          const float base = (m == -INFINITY ? 0.0f : m) - kLift;
+          if (kCap || kBias || fabsf(m) > 0x1p20f) {
+            // Of large scores the product is rounded like the maximum was, which then weighs 1: fused, what rounding took from that is 2^-24 of it and no small
+            // exponent.
 #pragma unroll
-              for (uint32_t e = 0; e < 32; ++e) x[e] *= over;
-              if (broken >> (c >> shift) & 1) {
+            for (uint32_t e = 0; e < kHalf; ++e) y[e] = (kCap || kBias ? y[e] : __fmul_rn(y[e], factor[e / 16])) - base;
+          } else {
 #pragma unroll
-                for (uint32_t e = 0; e < 32; ++e) x[e] = __uint_as_float(0x7FFFFFFFu);
-              }
-              if (!there) continue;
-              if (whole) {
+            for (uint32_t e = 0; e < kHalf; e += 2) split_two(fma_two(two(y[e], y[e + 1]), two(factor[e / 16], factor[e / 16]), two(-base, -base)), y[e], y[e + 1]);
+          }
+          uint32_t p[kHalf / 2];
 #pragma unroll
-                for (uint32_t e = 0; e < 32; e += 8) {
-                  const uint32_t w[4] = {rounded<kBf16>(x[e], x[e + 1]), rounded<kBf16>(x[e + 2], x[e + 3]), rounded<kBf16>(x[e + 4], x[e + 5]), rounded<kBf16>(x[e + 6], x[e + 7])};
-                  if (aligned && c + e + 8 <= A.dim) {
-                    *reinterpret_cast<uint4*>(out + c + e) = make_uint4(w[0], w[1], w[2], w[3]);
-                  } else {
+          for (uint32_t e = 0; e < kHalf; e += 2) {
+            y[e] = exp2_fast(y[e]), y[e + 1] = exp2_fast(y[e + 1]);
+            l = add_two(l, two(y[e], y[e + 1]));
+            p[e / 2] = rounded<kBf16>(y[e], y[e + 1]);
+          }
+          __syncwarp();
+          tensor_store(at, p);
+          tensor_stored();
+          order_before();
+          barrier_arrive(shared_address(&S.weights[t][half]));
+          good = i + 1 == 2 * n;
+        }
+        for (uint32_t h = 0; h < 2; ++h) good = good && warp_wait(shared_address(&S.sums[t][h]), (done + n - 1) & 1, dead);
+        if (good) {
+          order_after();
+          if (S.broken) {  // some value was no number: which of this block's are, and this query sees
+            for (uint32_t k = 0; k < n * kKeys; ++k) {
+              const uint32_t at_key = tiles.key(j0 + k / kKeys) + k % kKeys;
+              const bool visible = (at_key <= position && (A.window == 0 || position - at_key < A.window)) || at_key < q.prefix;
+              const uint32_t place = place_of_key(A, q, head, at_key, page_of(A, q, s, at_key));
+              if (place == kNone || !visible) continue;
+              for (uint32_t g = 0; g < A.groups; ++g)
+                if ((A.scales[A.plane_scales + (uint64_t)place * A.groups + g] & 0x7F80u) == 0x7F80u) broken |= 1u << g;
+            }
+            __syncwarp();
+          }
+          const bool whole = j0 == 0 && n == tiles.count, there = token < q.rows;
+          float* part = A.parts + (2ull * blockIdx.x + (walk.first ? 0 : 1)) * (kTilePartBytes / 4);
+          T* out = static_cast<T*>(A.out) + (uint64_t)(q.row + min(token, q.rows - 1)) * A.out_row + (uint64_t)(head * A.shared + in_group) * A.out_head;
+          const bool aligned = ((reinterpret_cast<uintptr_t>(A.out) / 2 | A.out_row | A.out_head) & 7) == 0;
+          float sum, other;
+          split_two(l, sum, other);
+          sum += other;
+          const float over = whole ? (kBf16 ? 64.0f : 1.0f) / sum : 1.0f;
+          const uint32_t shift = 5 + (A.per_group > 1) + (A.per_group > 2);  // values of a group
+#pragma unroll 1
+          for (uint32_t c = 0; c < A.dim; c += 32) {
+            float x[32];
+            tensor_load(sums + c, x);
+            tensor_loaded(x);
 #pragma unroll
-                    for (uint32_t k = 0; k < 8; ++k)
-                      if (c + e + k < A.dim) reinterpret_cast<unsigned short*>(out)[c + e + k] = (unsigned short)(w[k / 2] >> (16 * (k & 1)));
-                  }
+            for (uint32_t e = 0; e < 32; ++e) x[e] *= over;
+            if (broken >> (c >> shift) & 1) {
+#pragma unroll
+              for (uint32_t e = 0; e < 32; ++e) x[e] = __uint_as_float(0x7FFFFFFFu);
+            }
+            if (there && whole) {
+#pragma unroll
+              for (uint32_t e = 0; e < 32; e += 8) {
+                const uint32_t w[4] = {rounded<kBf16>(x[e], x[e + 1]), rounded<kBf16>(x[e + 2], x[e + 3]), rounded<kBf16>(x[e + 4], x[e + 5]), rounded<kBf16>(x[e + 6], x[e + 7])};
+                if (aligned && c + e + 8 <= A.dim) {
+                  *reinterpret_cast<uint4*>(out + c + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                } else {
+#pragma unroll
+                  for (uint32_t k = 0; k < 8; ++k)
+                    if (c + e + k < A.dim) reinterpret_cast<unsigned short*>(out)[c + e + k] = (unsigned short)(w[k / 2] >> (16 * (k & 1)));
                 }
-              } else {
-#pragma unroll
-                for (uint32_t e = 0; e < 32; e += 4)
-                  *reinterpret_cast<float4*>(part + ((c + e) / 4 * kTileRows + t * kRows + row) * 4) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
               }
+            } else if (there) {
+#pragma unroll
+              for (uint32_t e = 0; e < 32; e += 4)
+                *reinterpret_cast<float4*>(part + ((c + e) / 4 * kTileRows + t * kRows + row) * 4) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
             }
-            if (!whole) {
-              part[kTileRows * kTileDim + t * kRows + row] = m;
-              part[kTileRows * (kTileDim + 1) + t * kRows + row] = sum;
-            }
+            __syncwarp();
+          }
+          if (!whole) {
+            part[kTileRows * kTileDim + t * kRows + row] = m;
+            part[kTileRows * (kTileDim + 1) + t * kRows + row] = sum;
           }
         }
         done += n;

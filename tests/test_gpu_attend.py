@@ -104,6 +104,26 @@ def test_chunks(lc, kind, bits, group, dim, counts, page):
     case.check(lc, case.call(lc))
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+@pytest.mark.parametrize("bits,group", [(4, 32), (4, 128), (8, 32), (8, 64)])
+@pytest.mark.parametrize("heads,shared,dim", [(1, 1, 1), (3, 2, 49), (2, 4, 64), (1, 7, 80), (2, 3, 100), (1, 300, 40)])
+def test_chunks_of_any_dim(lc, kind, bits, group, heads, shared, dim):
+    """Rows that do not end on whole pieces, heads that outnumber a block's queries."""
+    counts = [3] if shared > 100 else [190, 21, 64]
+    case = Case(lc, kind, bits, group, heads, shared, dim, 16, [140, 0, 400][: len(counts)], counts, seed=dim)
+    case.check(lc, case.call(lc))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+def test_long_chunks(lc, kind):
+    """Chunks behind long sequences: blocks that several CTAs share, and whole ones."""
+    case = Case(lc, kind, 8, 128, 2, 4, 128, 64, [9000, 300, 5000], [70, 700, 1], seed=2)
+    a = case.call(lc)
+    case.check(lc, a)
+    assert torch.equal(a, case.call(lc, workspace=torch.full_like(lc.alloc_attend_workspace(case.cache, 3), 255)))
+    case.check(lc, case.call(lc, window=1000, cap=20.0), window=1000, cap=20.0)
+
+
 @pytest.mark.parametrize("kind", list(TYPES))
 @pytest.mark.parametrize("counts", [[1, 1, 1], [4, 6, 1], [150, 70, 9]])
 @pytest.mark.parametrize("options", ["cap", "slopes", "window", "window 1", "prefix", "prefix window", "all", "scale"])
@@ -247,6 +267,72 @@ def test_bad_places(lc):
         case.first.copy_(first), case.begin.copy_(begin)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("counts", [[1], [200]])
+def test_scales_and_caps_at_their_ends(lc, kind, counts):
+    """A scale of 0, as small and as large as may be; a cap that leaves nothing of the scores."""
+    case = Case(lc, kind, 8, 64, 1, 2, 64, 16, [90], counts, seed=7)
+    for kw in (dict(scale=0.0), dict(scale=-1e-30), dict(cap=1e-38), dict(cap=1e-3), dict(scale=0.0, window=17)):
+        case.check(lc, case.call(lc, **kw), **dict(kw, cap=kw.get("cap", 0.0)))
+    # one key has it all: the largest score's
+    got = case.call(lc, scale=1e30)
+    assert bool(got[: counts[0]].isfinite().all())
+
+
+def at_once(lc, cases, streams, graphs):
+    outs = [torch.full(c.q.shape, 7.0, dtype=c.kind, device=DEV) for c in cases]
+    works = [lc.alloc_attend_workspace(c.cache, len(c.counts)) for c in cases]
+    run = lambda i: lc.cache_attend(cases[i].cache, cases[i].q, cases[i].table, cases[i].page, cases[i].begin, outs[i], first=cases[i].first, workspace=works[i])
+    torch.cuda.synchronize()
+    made = []
+    for i, stream in enumerate(streams):
+        with torch.cuda.stream(stream):
+            run(i)
+            if graphs:
+                stream.synchronize()
+                made.append(torch.cuda.CUDAGraph())
+                with torch.cuda.graph(made[-1], stream=stream):
+                    run(i)
+    torch.cuda.synchronize()
+    for turn in range(5):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                outs[i].fill_(7.0)
+                made[i].replay() if graphs else run(i)
+    torch.cuda.synchronize()
+    return outs
+
+
+@pytest.mark.parametrize("graphs", [False, True])
+def test_two_at_once(lc, graphs):
+    """Two calls on two streams, eagerly and as graphs, each with its workspace, give what they give alone: long chunks beside each other, and beside
+    single tokens."""
+    cases = [Case(lc, "bf16", 8, 64, 4, 4, 64, 16, [3000, 20], [500, 300], seed=1), Case(lc, "fp16", 4, 32, 4, 2, 64, 16, [100, 2000], [800, 1], seed=2),
+             Case(lc, "bf16", 4, 64, 8, 4, 128, 64, [5000] * 9, [1] * 9, seed=3)]
+    alone = [c.call(lc) for c in cases]
+    outs = at_once(lc, cases, [torch.cuda.Stream() for _ in cases], graphs)
+    for a, b in zip(alone, outs):
+        assert torch.equal(a, b)
+
+
+def test_a_captured_step_goes_by_its_buffers(lc):
+    """One graph for a batch of fixed size: lengths, pages and queries change between replays."""
+    case = Case(lc, "bf16", 8, 64, 2, 4, 64, 16, [200, 60, 300], [40, 1, 3], seed=9, rows_behind=0)
+    out, status, work = torch.full(case.q.shape, 7.0, dtype=case.kind, device=DEV), lc.alloc_status(DEV), lc.alloc_attend_workspace(case.cache, 3)
+    call = lambda: lc.cache_attend(case.cache, case.q, case.table, 16, case.begin, out, first=case.first, workspace=work, status=status)
+    call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for firsts, counts in (([200, 60, 300], [40, 1, 3]), ([0, 61, 303], [0, 1, 1]), ([190, 0, 280], [1, 20, 23]), ([100, 50, 250], [1, 1, 1])):
+        case.firsts, case.counts = firsts, counts
+        case.first.copy_(torch.tensor(firsts)), case.begin.copy_(torch.tensor([0] + np.cumsum(counts).tolist()))
+        case.q.copy_(torch.randn(case.q.shape, device=DEV)), out.fill_(7.0)
+        graph.replay()
+        case.status = status
+        case.check(lc, out)
+
+
 def test_nothing_to_do(lc):
     cache = lc.alloc_cache(32, 2, 64, 8, 64, DEV)
     none = torch.zeros(0, 4, 64, dtype=torch.bfloat16, device=DEV)
@@ -267,10 +353,10 @@ def test_refuses(lc):
     for bad in (dict(q=case.q[:, :3]), dict(q=case.q[..., :63]), dict(q=case.q.double()), dict(cache=one), dict(q=case.q.cpu()), dict(table=case.table.long()),
                 dict(begin=case.begin[:1]), dict(first=case.first.long()), dict(prefix=case.begin), dict(slopes=torch.ones(3, device=DEV)),
                 dict(slopes=torch.ones(4, device=DEV).double()), dict(out=case.q.float()), dict(status=torch.zeros(1, device=DEV)),
-                dict(q=case.q.clone().requires_grad_()), dict(workspace=torch.zeros(1 << 26, dtype=torch.uint8))):
+                dict(q=case.q.clone().requires_grad_()), dict(workspace=torch.zeros(1 << 27, dtype=torch.uint8)), dict(workspace=torch.zeros(1 << 24, device=DEV))):
         with pytest.raises(ValueError):
             call(**bad)
-    for bad in (dict(page=0), dict(window=-1), dict(longest=-1), dict(cap=-1.0), dict(cap=math.inf), dict(scale=math.nan), dict(cache=wide, q=torch.zeros(3, 4, 264, dtype=torch.bfloat16, device=DEV)),
+    for bad in (dict(page=0), dict(window=-1), dict(longest=-1), dict(cap=-1.0), dict(cap=math.inf), dict(cap=2e30), dict(scale=math.nan), dict(scale=-2e30), dict(cache=wide, q=torch.zeros(3, 4, 264, dtype=torch.bfloat16, device=DEV)),
                 dict(workspace=torch.zeros(1024, dtype=torch.uint8, device=DEV)), dict(out=case.q[:1].clone().expand(5, 4, 64))):
         with pytest.raises(lc.LCError):
             call(**bad)
