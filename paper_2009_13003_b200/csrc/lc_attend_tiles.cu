@@ -2,17 +2,19 @@
 //
 // A CTA takes blocks of 256 queries of one head of the cache (its tokens, times the heads that share it) as two tiles of 128, and goes through the keys
 // 128 at a time with a running maximum and sum of each query. Its warps have one task each: four read the keys' codes and four the values', turn them into
-// numbers of the queries' type and store them as operands (both in one layout, rows of 64 values with the 128-byte swizzle: keys are read along a row, values across);
+// numbers and store them as operands (both in one layout, rows of 64 values with the 128-byte swizzle: keys are read along a row, values across);
 // two warps look up where the next tiles' keys lie, and their scales;
 // a thread for each tile issues its products; a warpgroup for each tile takes the scores out of tensor memory, a query a thread, and puts the probabilities back
 // there, over the scores, as the first operand of the product with the values. Scores go to the warps 64 keys at a time: while one half of a tile is with
 // them, the products of the other half, and of the other tile, run.
 // The sums of the values stay in tensor memory; they are scaled down only where a score exceeds the maximum so far by more than a factor of 2^kSlack.
 //
-// What a code stands for is rounded to the type once. bf16: code / 64 is exact (see lc_attend_rows.cuh) and times the scale rounded; the 64 comes in
-// with the scores' factor, so that nothing overflows. fp16: keys in units of a power of two of 16 neighbours, so that no magnitude of them is out of the
-// type; values as lc_cache_read gives them, but numbers beyond the type as its largest. A value of NaN enters as 0, or rows that do not see it would
-// get 0 * NaN; rows that do get their NaN at the end.
+// All products are of fp16 numbers, 11 bits, also for bf16 queries: a query's row is multiplied by the power of two that takes its largest value to [1, 2) (what
+// that loses lies 2^-25 below it), keys are in units of the power of two in the largest scale of 16 neighbours, values in units of that of the block's
+// values so far; where it rises the sums are scaled down. So no magnitude of them is out of the type, and what a code stands for is rounded once, to 11 bits or to
+// 2^-25 of the unit. Probabilities are held 2^7 times as large, up to 2^(7 + kSlack): next to its smallest numbers the type has few bits. (With keys, values and
+// probabilities of bf16, 2 x 1024 rows behind 16384 keys took as long, and the error was 0.0049 of the result, of which the result's own rounding is 0.0017.)
+// A value of NaN enters as 0, or rows that do not see it would get 0 * NaN; rows that do get their NaN at the end.
 //
 // Blocks differ in how many keys they see. Each weighs about as many as it does and a block's own cost; a CTA gets an equal share of the weight, and
 // of a block that it shares with its neighbours the tiles in proportion. Those parts are joined by a second launch, in a fixed order.
@@ -30,7 +32,7 @@ static_assert(2 * kRegsSoftmax + 2 * kRegsReader + kRegsIssue <= 5 * kRegsAtLaun
 constexpr uint32_t kStages = 3;                         // halves of a tile of keys, and of values, as operands
 constexpr uint32_t kAhead = 3;                          // halves whose codes are on their way
 constexpr uint32_t kFound = 4;                          // tiles whose keys have been looked up
-constexpr uint32_t kMemo = 8;                           // tiles whose units are kept: scores of a tile are done before the keys of the seventh behind it are looked up
+constexpr uint32_t kMemo = 8;                           // tiles whose units are kept: the scores of a tile are done before the keys of the seventh behind it are looked up
 constexpr float kSlack = 8.0f;
 constexpr long long kWaitCycles = 4ll << 30;            // how long a barrier is waited for before the kernel gives up: some two seconds
 constexpr uint32_t kBlockCost = 320;                    // what a block costs beyond its keys, in keys
@@ -54,6 +56,12 @@ __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, vola
 }
 // The same for a warp as a whole: its threads go on together or not at all.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* dead) { return __all_sync(0xFFFFFFFFu, barrier_wait(bar, parity, dead)); }
+// Whether all of a warpgroup's threads say so: they go on together or not at all.
+__device__ __forceinline__ bool together(uint32_t barrier, bool good) {
+  uint32_t all;
+  asm volatile("{ .reg .pred p, r; setp.ne.b32 p, %3, 0; barrier.cta.red.and.pred r, %1, %2, p; selp.u32 %0, 1, 0, r; }" : "=r"(all) : "r"(barrier), "n"(kRows), "r"((uint32_t)good) : "memory");
+  return all;
+}
 __device__ __forceinline__ void order_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void order_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void commit_to(uint32_t bar) {
@@ -79,10 +87,8 @@ __device__ __forceinline__ bool one_lane() {
   asm volatile("{ .reg .pred p; elect.sync _|p, 0xFFFFFFFF; selp.u32 %0, 1, 0, p; }" : "=r"(yes));
   return yes;
 }
-// The product's shape and types: fp32 sums, m = 128.
-__device__ __forceinline__ uint32_t product_kind(bool bf16, uint32_t n, bool across) {
-  return 1u << 4 | (uint32_t)bf16 << 7 | (uint32_t)bf16 << 10 | (uint32_t)across << 16 | (n >> 3) << 17 | (kRows >> 4) << 24;
-}
+// The product's shape and types: fp16 operands, fp32 sums, m = 128.
+__device__ __forceinline__ uint32_t product_kind(uint32_t n, bool across) { return 1u << 4 | (uint32_t)across << 16 | (n >> 3) << 17 | (kRows >> 4) << 24; }
 
 // 16, 32 or 64 columns of the 32 lanes of a warp, a lane a thread. tensor_loaded: the numbers are there; they go through it, so that nothing that uses them
 // is moved ahead of it. The load of 16 waits itself.
@@ -267,9 +273,11 @@ struct Shared {
   unsigned long long full_k[kStages], empty_k[kStages], full_v[kStages], empty_v[kStages], found_full[2][kFound], found_empty[2][kFound], queries[2], scores[2][2], weights[2][2], sums[2][2];  // barriers
   unsigned long long scan[kThreads / 32], found_base;
   uint32_t found, tensor, dead, broken;  // broken: a scale of the values so far was no number
-  uint2 scales[2][kFound][kKeys];          // for the readers of keys and of values: a key's scales, two in a word
+  uint2 scales[2][kFound][kKeys];          // for the readers of keys and of values: a key's scales in fp16, two in a word
   uint32_t places[2][kFound][kKeys];       // slot * heads + head, which is below 2^32 in this kernel; kNone
-  float units[kMemo][kKeys / 16];          // fp16: the power of two that 16 keys are in units of, from the largest of their scales
+  float units[kMemo][kKeys / 16];          // the powers of two that 16 keys each are in units of
+  float value_units[kMemo];                // that a tile's values are in units of
+  float query_units[kTileRows];
 };
 
 // kCap, kBias: scores are capped, lowered by distance.
@@ -277,19 +285,33 @@ template <int kBits, uint32_t DP, bool kBf16, bool kCap, bool kBias>
 struct Kernel {
   using L = Layout<kBits, DP>;
   using T = typename TypeOf<kBf16 ? LC_TYPE_BF16 : LC_TYPE_F16>::T;
-  // fp16 weights are held 2^7 times as large, up to 2^(7 + kSlack): next to its smallest numbers the type has few bits
-  static constexpr float kLift = kBf16 ? 0.0f : 7.0f;
+  static constexpr float kLift = 7.0f;
   static constexpr uint32_t kParts = L::kRow / 16, kUnits = kParts / 2;  // pieces of 16 bytes of a row's codes, at most; of half a tile that a reader takes
 
   // A tile of a block's queries as an operand, by the warpgroup that takes its scores. A negative scale goes to their signs. All of a thread's loads are on their
   // way at once.
-  static __device__ __forceinline__ void load_queries(const AttendArgs& A, const Sequence& q, uint32_t first, uint32_t head, uint32_t thread, uint8_t* to) {
+  static __device__ __forceinline__ void load_queries(const AttendArgs& A, const Sequence& q, uint32_t first, uint32_t head, uint32_t thread, uint8_t* to, float* units) {
     const uint32_t flip = A.scale < 0.0f ? 0x80008000u : 0u, c = thread % (DP / 8);
     constexpr uint32_t kRowsAtOnce = kRows / (DP / 8);  // rows that the threads take together
     const unsigned short* const from = static_cast<const unsigned short*>(A.q) + (uint64_t)(head * A.shared) * A.q_head + c * 8;
     auto row_at = [&](uint32_t i) { return i * kRowsAtOnce + thread / (DP / 8); };
     auto put = [&](uint32_t row, uint4 x) {
-      *reinterpret_cast<uint4*>(to + (c / 8) * (kRows * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = make_uint4(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
+      uint32_t w[4] = {x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip};
+      if constexpr (kBf16) {
+        // the row's largest exponent, over the lanes that hold it
+        uint32_t most = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) most = __vmaxu2(most, w[e] & 0x7F807F80u);
+        most = max(most & 0xFFFFu, most >> 16) >> 7;
+#pragma unroll
+        for (uint32_t d = DP / 16; d; d >>= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
+        most = most == 255 ? 127 : min(max(most, 1u), 253u);  // of Inf and NaN: as they are
+        const float down = __uint_as_float((254 - most) << 23);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = rounded<false>(__uint_as_float(w[e] << 16) * down, __uint_as_float(w[e] & 0xFFFF0000u) * down);
+        if (c == 0) units[row] = __uint_as_float(most << 23);
+      }
+      *reinterpret_cast<uint4*>(to + (c / 8) * (kRows * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
     };
     if (A.dim % 8 == 0 && ((reinterpret_cast<uintptr_t>(A.q) / 2 | A.q_row | A.q_head) & 7) == 0) {
       uint4 x[DP / 8];
@@ -363,38 +385,33 @@ struct Kernel {
     }
   }
   static __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-  // Four pairs of numbers from eight codes. scale: of bf16 two of it, of fp16 a float's bits.
+  // Four pairs of fp16 numbers from eight codes; scale: twice. In the lowest bits of 1024 a whole number is itself, or 16 times as large, and one exact operation
+  // for two of them brings them to where they belong.
   static __device__ __forceinline__ uint4 numbers(uint32_t a, uint32_t b, uint32_t scale) {
     uint32_t r[4];
-    if constexpr (kBf16) {
-      constexpr uint32_t kLow = 0x7F007F00u, kHigh = 0x7D007D00u, minus = kBits == 4 ? 0xBE00BE00u : 0xC000C000u;  // 2^127, 2^123; -2^-3, -2
-      uint32_t x[4], times[4] = {kLow, kLow, kLow, kLow};
-      if constexpr (kBits == 4) {
-        x[0] = a & 0x000F000Fu, x[1] = a & 0x00F000F0u, x[2] = a >> 8 & 0x000F000Fu, x[3] = a >> 8 & 0x00F000F0u;
-        times[1] = times[3] = kHigh;
-      } else {
-        x[0] = __byte_perm(a, 0, 0x4140), x[1] = __byte_perm(a, 0, 0x4342), x[2] = __byte_perm(b, 0, 0x4140), x[3] = __byte_perm(b, 0, 0x4342);
-      }
+    if constexpr (kBits == 4) {
+      const uint32_t x[4] = {(a & 0x000F000Fu) | 0x64006400u, (a & 0x00F000F0u) | 0x64006400u, (a >> 8 & 0x000F000Fu) | 0x64006400u, (a >> 8 & 0x00F000F0u) | 0x64006400u};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r[e]) : "r"(x[e]), "r"(times[e]), "r"(minus));
-        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r[e]) : "r"(r[e]), "r"(scale));
+        if (e % 2 == 0) asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r[e]) : "r"(x[e]), "r"(0xE408E408u));              // - 1032
+        else asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r[e]) : "r"(x[e]), "r"(0x2C002C00u), "r"(0xD480D480u));  // / 16 - 72
       }
     } else {
-      float v[8];
-      values_in_row<kBits, 8>(make_uint2(a, b), __uint_as_float(scale), v);
+      const uint32_t x[4] = {__byte_perm(a, 0x64646464u, 0x4140), __byte_perm(a, 0x64646464u, 0x4342), __byte_perm(b, 0x64646464u, 0x4140), __byte_perm(b, 0x64646464u, 0x4342)};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r[e]) : "f"(v[2 * e + 1]), "f"(v[2 * e]));
+      for (int e = 0; e < 4; ++e) asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r[e]) : "r"(x[e]), "r"(0xE480E480u));  // - 1152
     }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r[e]) : "r"(r[e]), "r"(scale));
     return make_uint4(r[0], r[1], r[2], r[3]);
   }
-  // A half's pieces as operands. scales: of its keys, down: what they are multiplied by (fp16).
-  static __device__ __forceinline__ void store_numbers(const AttendArgs& A, const uint2* scales, float down, uint32_t slot, const Reader& r, uint32_t operand) {
+  // A half's pieces as operands. scales: of its keys.
+  static __device__ __forceinline__ void store_numbers(const uint2* scales, uint32_t slot, const Reader& r, uint32_t operand) {
     if (r.left == 0) return;
     const uint32_t* pairs = reinterpret_cast<const uint32_t*>(scales + r.key) + r.group / 2;
 #pragma unroll
     for (uint32_t i = 0; i < kUnits; ++i) {
-      const uint32_t x = pairs[i * kStep * 2], scale = kBf16 ? __byte_perm(x, 0, r.group & 1 ? 0x3232 : 0x1010) : __float_as_uint(__uint_as_float(r.group & 1 ? x & 0xFFFF0000u : x << 16) * down);
+      const uint32_t scale = __byte_perm(pairs[i * kStep * 2], 0, r.group & 1 ? 0x3232 : 0x1010);
       uint32_t w[4];
       asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(r.copies + slot * L::kCodes + i * (kReaders * 16)) : "memory");
 #pragma unroll
@@ -517,7 +534,6 @@ struct Kernel {
     __syncthreads();
     order_after();
     const uint32_t tensor = S.tensor;
-    const float scale = fabsf(A.scale) * (kBf16 ? 64.0f : 1.0f);
     volatile uint32_t* dead = &S.dead;
     Walk walk(A, S.found, from - S.found_base, from, to);
     uint32_t done = 0;  // tiles of keys so far: what the barriers' phases go by
@@ -540,7 +556,13 @@ struct Kernel {
         float m = -INFINITY;
         Two l = two(0.0f, 0.0f);
         uint32_t broken = 0;  // groups whose value is no number for this query
-        load_queries(A, q, block * kTileRows + t * kRows, head, row, queries + t * L::kQueries);
+        load_queries(A, q, block * kTileRows + t * kRows, head, row, queries + t * L::kQueries, S.query_units + t * kRows);
+        float own = fabsf(A.scale) * kLog2e;  // what the row's scores are multiplied by
+        if constexpr (kBf16) {
+          asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + t), "n"(kRows) : "memory");
+          own *= S.query_units[t * kRows + row];
+        }
+        float value_unit = 1.0f;  // of the sums
         order_for_products();
         order_before();  // the sums of the block before are read
         barrier_arrive(shared_address(&S.queries[t]));
@@ -551,9 +573,10 @@ struct Kernel {
           order_after();
           float y[kHalf];
           tensor_load(at, y);
+          const float tile_unit = S.value_units[number % kMemo];
           float factor[kHalf / 16];  // of 16 keys each; not 0, or a key that is not seen, -Inf, times that would be no number
 #pragma unroll
-          for (uint32_t c = 0; c < kHalf / 16; ++c) factor[c] = fmaxf(scale * kLog2e * (kBf16 ? 1.0f : S.units[number % kMemo][half * 4 + c]), 1e-37f);
+          for (uint32_t c = 0; c < kHalf / 16; ++c) factor[c] = fmaxf(own * S.units[number % kMemo][half * 4 + c], 1e-37f);
           const bool full = key + kHalf - 1 <= low && (A.window == 0 || high - key < A.window);
           tensor_loaded(y);
           if constexpr (kCap || kBias) {
@@ -583,14 +606,15 @@ struct Kernel {
             top = fmaxf(top, kCap || kBias ? x : __fmul_rn(x, factor[c / 16]));  // grows with the product
           }
           const bool rises = top > m + kSlack;
-          if (__any_sync(0xFFFFFFFFu, rises)) {
-            const float now = rises ? top : m, down = rises ? exp2_fast(m - now) : 1.0f;
+          if (__any_sync(0xFFFFFFFFu, rises) || tile_unit != value_unit) {
+            const float now = rises ? top : m, down = rises ? exp2_fast(m - now) : 1.0f, sums_down = down * (value_unit / tile_unit);
+            value_unit = tile_unit;
             if (i > 0) {
               // the product before (the one before that has ended, or these scores would not be there)
               if (!warp_wait(shared_address(&S.sums[t][1 - half]), (done + (i - 1) / 2) & 1, dead)) break;
               order_after();
 #pragma unroll 1
-              for (uint32_t d = 0; d < DP; d += 16) scale_sums(sums + d, down);
+              for (uint32_t d = 0; d < DP; d += 16) scale_sums(sums + d, sums_down);
             }
             m = now;
             l = mul_two(l, two(down, down));
@@ -610,7 +634,7 @@ struct Kernel {
           for (uint32_t e = 0; e < kHalf; e += 2) {
             y[e] = exp2_fast(y[e]), y[e + 1] = exp2_fast(y[e + 1]);
             l = add_two(l, two(y[e], y[e + 1]));
-            p[e / 2] = rounded<kBf16>(y[e], y[e + 1]);
+            p[e / 2] = rounded<false>(y[e], y[e + 1]);
           }
           __syncwarp();
           tensor_store(at, p);
@@ -640,7 +664,7 @@ struct Kernel {
           float sum, other;
           split_two(l, sum, other);
           sum += other;
-          const float over = whole ? (kBf16 ? 64.0f : 1.0f) / sum : 1.0f;
+          const float over = whole ? value_unit / sum : value_unit;
           const uint32_t shift = 5 + (A.per_group > 1) + (A.per_group > 2);  // values of a group
 #pragma unroll 1
           for (uint32_t c = 0; c < A.dim; c += 32) {
@@ -678,6 +702,7 @@ struct Kernel {
           }
         }
         done += n;
+        good = together(1 + t, good);
       }
     } else if (warp < kSoftmaxWarps + 2 * kReadWarps) {
       // ---- codes to operands
@@ -713,9 +738,7 @@ struct Kernel {
           if (turn > 0) good = warp_wait(shared_address(&empty[stage]), (turn - 1) & 1, dead);
           if (!good) break;
           asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
-          float down = 1.0f;
-          if (!kBf16 && !set) down = 1.0f / S.units[(done + i / 2) % kMemo][(i & 1) * 4 + mine];
-          store_numbers(A, S.scales[set][(done + i / 2) % kFound] + (i & 1) * kHalf, down, slot, R, operands + stage * L::kOperand);
+          store_numbers(S.scales[set][(done + i / 2) % kFound] + (i & 1) * kHalf, slot, R, operands + stage * L::kOperand);
           order_for_products();
           barrier_arrive(shared_address(&full[stage]));
           if (i + kAhead < 2 * n) {
@@ -740,7 +763,7 @@ struct Kernel {
         // ---- the products, a warp for each tile of queries: the warp as a whole goes through the keys, with numbers that the compiler knows to be the same for all
         // lanes; one lane issues
         const uint32_t all_lanes = 0xFFFFFFFFu, at_tensor = __shfl_sync(all_lanes, tensor, 0), t = __shfl_sync(all_lanes, warp, 0) - (kSoftmaxWarps + 2 * kReadWarps);
-        const uint32_t steps = (A.dim + 15) / 16, scores_kind = product_kind(kBf16, kHalf, false), sums_kind = product_kind(kBf16, steps * 16, true);
+        const uint32_t steps = (A.dim + 15) / 16, scores_kind = product_kind(kHalf, false), sums_kind = product_kind(steps * 16, true);
         const uint32_t query_at = operand_at(shared_address(queries) + t * L::kQueries, 16), key_at = operand_at(shared_address(keys), 16), value_at = operand_at(shared_address(values), kHalf * 128);
         const uint32_t scores_at = at_tensor + L::kScoresAt + t * kKeys, sums_at = at_tensor + L::kSumsAt + t * DP;
         auto multiply_keys = [&](uint32_t half, uint32_t stage) {
@@ -790,6 +813,7 @@ struct Kernel {
         // ---- where keys lie, and their scales: a warp for the readers of keys, one for those of values
         const uint32_t set = warp - (kSoftmaxWarps + 2 * kReadWarps + 2);
         const unsigned short* const scales = A.scales + (set ? A.plane_scales : 0);
+        uint32_t value_unit = 0;  // the upper half of a float
         bool good = true;
         while (good && walk.next(A)) {
           for (uint32_t i = 0; i < walk.n; ++i) {
@@ -808,22 +832,41 @@ struct Kernel {
 #pragma unroll
               for (uint32_t g = 0; g < 4; ++g)
                 if (place[k] != kNone && g < A.groups) all_scales[k][g] = __ldg(scales + (uint64_t)place[k] * A.groups + g);
+            // the largest exponents, of 16 keys or of the tile, among scales that are numbers; values that are not count as 0
+            uint32_t unit[kKeys / 32];
 #pragma unroll
             for (uint32_t k = 0; k < kKeys / 32; ++k) {
-              uint32_t (&y)[4] = all_scales[k];
-              if (set) {  // scales that are no numbers
+              unit[k] = 0;
 #pragma unroll
-                for (uint32_t g = 0; g < 4; ++g)
-                  if ((y[g] & 0x7F80u) == 0x7F80u) y[g] = 0, S.broken = 1;
-              } else if constexpr (!kBf16) {
-                uint32_t most = 0;
-#pragma unroll
-                for (uint32_t g = 0; g < 4; ++g) most = max(most, (y[g] & 0x7F80u) == 0x7F80u ? 0u : y[g] & 0x7F80u);
-#pragma unroll
-                for (int d = 8; d; d >>= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
-                if (lane % 16 == 0) S.units[x % kMemo][2 * k + lane / 16] = most ? __uint_as_float(min(max(most << 16, 0x01000000u), 0x7E000000u)) : 1.0f;
+              for (uint32_t g = 0; g < 4; ++g) {
+                const bool number = (all_scales[k][g] & 0x7F80u) != 0x7F80u;
+                if (set && !number) all_scales[k][g] = 0, S.broken = 1;
+                unit[k] = max(unit[k], number ? all_scales[k][g] & 0x7F80u : 0u);
               }
-              S.scales[set][slot][lane + 32 * k] = make_uint2(y[0] | y[1] << 16, y[2] | y[3] << 16);
+            }
+            if (set) {
+              uint32_t most = max(max(unit[0], unit[1]), max(unit[2], unit[3]));
+              most = min(max(__reduce_max_sync(0xFFFFFFFFu, most), 0x0100u), 0x7E00u);
+              value_unit = i == 0 ? most : max(value_unit, most);
+              if (lane == 0) S.value_units[x % kMemo] = __uint_as_float(value_unit << 16);
+#pragma unroll
+              for (uint32_t k = 0; k < kKeys / 32; ++k) unit[k] = value_unit;
+            } else {
+#pragma unroll
+              for (uint32_t k = 0; k < kKeys / 32; ++k) {
+#pragma unroll
+                for (int d = 8; d; d >>= 1) unit[k] = max(unit[k], __shfl_xor_sync(0xFFFFFFFFu, unit[k], d));
+                unit[k] = min(max(unit[k], 0x0100u), 0x7E00u);
+                if (lane % 16 == 0) S.units[x % kMemo][2 * k + lane / 16] = __uint_as_float(unit[k] << 16);
+              }
+            }
+#pragma unroll
+            for (uint32_t k = 0; k < kKeys / 32; ++k) {
+              const float down = __uint_as_float((0x7F00u - unit[k]) << 16);
+              float y[4];
+#pragma unroll
+              for (uint32_t g = 0; g < 4; ++g) y[g] = __uint_as_float(all_scales[k][g] << 16) * down;
+              S.scales[set][slot][lane + 32 * k] = make_uint2(rounded<false>(y[0], y[1]), rounded<false>(y[2], y[3]));
               S.places[set][slot][lane + 32 * k] = place[k];
             }
             __syncwarp();
@@ -903,7 +946,7 @@ __global__ void __launch_bounds__(kTileRows) join_tiles_kernel(AttendArgs A, uin
   }
   if (parts == 0) return;  // one CTA has had them all
   T* out = static_cast<T*>(A.out) + (uint64_t)(q.row + token) * A.out_row + (uint64_t)(P.head * A.shared + (r - token * A.shared)) * A.out_head + d0;
-  const float over = (kBf16 ? 64.0f : 1.0f) / sum;
+  const float over = 1.0f / sum;
   if (d0 + 16 <= A.dim && (reinterpret_cast<uintptr_t>(out) & 15) == 0) {
 #pragma unroll
     for (uint32_t e = 0; e < 16; e += 8)

@@ -42,13 +42,14 @@ def bound(kind, out, size, products, bias, plain, dim, cap=0.0):
     rounded to the type move a score by u * sum |q k|, sums in fp32 by (dim + 32) 2^-24 of that, a bias by 2^-22 of its size (keys that it lowers
     by 20 or more do not count: they weigh e^-20 together with their error); the cap halves none of this and its own function is good to cap * 2^-20; exp
     is good to 2^-20. A score that is off by d moves its weight by d of itself, and so does the sum that divides: 2 d. Probabilities and values
-    rounded to the type: 2 u of the mean of |v|; the result's own rounding: u of itself. A probability of fp16 that is small has fewer bits: held 2^7 times as large beside a largest one of 1 or more, it is
-    on a grid of 2^-24 at worst, so off by 2^-25 / 2^7 of the largest, and so of their sum: 2^-32 for every |v| that is seen."""
+    rounded to the type: 2 u of the mean of |v|; the result's own rounding: u of itself. A small probability that is held in fp16 (of bf16 rows too) has fewer bits: 2^7 times as large beside a largest one of 1 or
+    more, it is on a grid of 2^-24 at worst, so off by 2^-25 / 2^7 of the largest, and so of their sum: 2^-32 for every |v| that is seen. Values in fp16 are in units of a power of two near their block's largest scale
+    and keep its 11 bits, no fewer than their rows' type, while no scale is 2^14 times as small; so they have no term of their own here."""
     u = HALF_STEP[kind]
     given = 0.0 if kind == torch.float32 else u
     d = (given + (dim + 32) * 2.0 ** -24) * products + 2.0 ** -22 * bias + cap * 2.0 ** -20 + 2.0 ** -20
     d = torch.expm1(d)[..., None]  # for scores that are off by much
-    return (2 * max(given, 2.0 ** -22) + 2 * d) * size * 1.01 + u * out.abs() * 1.01 + (2.0 ** -24 + 2.0 ** -32 * plain) * (kind == torch.float16) + 1e-30
+    return (2 * max(given, 2.0 ** -22) + 2 * d) * size * 1.01 + u * out.abs() * 1.01 + 2.0 ** -24 * (kind == torch.float16) + 2.0 ** -32 * plain * (kind != torch.float32) + 1e-30
 
 
 def plan(table, held, spare, count, tokens, page, rows):
