@@ -13,7 +13,7 @@
 // that loses lies 2^-25 below it), keys are in units of the power of two in the largest scale of 16 neighbours, values in units of that of the block's
 // values so far; where it rises the sums are scaled down. So no magnitude of them is out of the type, and what a code stands for is rounded once, to 11 bits or to
 // 2^-25 of the unit. Probabilities are held 2^7 times as large, up to 2^(7 + kSlack): next to its smallest numbers the type has few bits. (With keys, values and
-// probabilities of bf16, 2 x 1024 rows behind 16384 keys took as long, and the error was 0.0049 of the result, of which the result's own rounding is 0.0017.)
+// probabilities of bf16, 2 x 1024 rows behind up to 16384 keys took 602 us instead of 636, and the error was 0.0049 of the result instead of 0.0017, the result's own rounding.)
 // A value of NaN enters as 0, or rows that do not see it would get 0 * NaN; rows that do get their NaN at the end.
 //
 // Blocks differ in how many keys they see. Each weighs about as many as it does and a block's own cost; a CTA gets an equal share of the weight, and
