@@ -570,6 +570,10 @@ struct Kernel {
         for (uint32_t i = 0; i < 2 * n; ++i) {
           const uint32_t number = done + i / 2, half = i & 1, key = tiles.key(j0 + i / 2) + half * kHalf, at = scores + half * kHalf;
           if (!warp_wait(shared_address(&S.scores[t][half]), number & 1, dead)) break;
+          // What is looked up of a tile's values (their unit) comes another way than its scores. Behind a block's first tile it is there: scores of a half wait for the
+          // values of the second half ahead of it, which are stored once the tile after theirs has been looked up. For the first tile its values are waited for; they
+          // are not replaced before this warp's probabilities have met them.
+          if (i == 0 && !warp_wait(shared_address(&S.full_v[2 * done % kStages]), 2 * done / kStages & 1, dead)) break;
           order_after();
           float y[kHalf];
           tensor_load(at, y);
