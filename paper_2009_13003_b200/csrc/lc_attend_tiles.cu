@@ -32,7 +32,7 @@ static_assert(2 * kRegsSoftmax + 2 * kRegsReader + kRegsIssue <= 5 * kRegsAtLaun
 constexpr uint32_t kStages = 3;                         // halves of a tile of keys, and of values, as operands
 constexpr uint32_t kAhead = 3;                          // halves whose codes are on their way
 constexpr uint32_t kFound = 4;                          // tiles whose keys have been looked up
-constexpr uint32_t kMemo = 8;                           // tiles whose units are kept: the scores of a tile are done before the keys of the seventh behind it are looked up
+constexpr uint32_t kMemo = 8;                           // tiles whose units are kept: the scores of a tile are done before the keys of the seventh behind it are looked up (blocks have a tile or more)
 constexpr float kSlack = 8.0f;
 constexpr long long kWaitCycles = 4ll << 30;            // how long a barrier is waited for before the kernel gives up: some two seconds
 constexpr uint32_t kBlockCost = 320;                    // what a block costs beyond its keys, in keys
@@ -272,12 +272,13 @@ constexpr uint32_t kNone = ~0u;  // a key without a place
 struct Shared {
   unsigned long long full_k[kStages], empty_k[kStages], full_v[kStages], empty_v[kStages], found_full[2][kFound], found_empty[2][kFound], queries[2], scores[2][2], weights[2][2], sums[2][2];  // barriers
   unsigned long long scan[kThreads / 32], found_base;
-  uint32_t found, tensor, dead, broken;  // broken: a scale of the values so far was no number
+  uint32_t found, tensor, dead;
   uint2 scales[2][kFound][kKeys];          // for the readers of keys and of values: a key's scales in fp16, two in a word
   uint32_t places[2][kFound][kKeys];       // slot * heads + head, which is below 2^32 in this kernel; kNone
   float units[kMemo][kKeys / 16];          // the powers of two that 16 keys each are in units of
   float value_units[kMemo];                // that a tile's values are in units of
   float query_units[kTileRows];
+  uint32_t broken[kMemo][kTileRows / 8];   // for the queries of a block, four bits each: groups of which they see a value that is no number
 };
 
 // kCap, kBias: scores are capped, lowered by distance.
@@ -437,6 +438,25 @@ struct Kernel {
     return (uint32_t)slot * A.heads + head;
   }
 
+  // Notes which queries of the walk's block see values of a tile that are no numbers, and in which groups. broken: of a lane's keys first + lane + 32 k, four bits
+  // each.
+  static __device__ __forceinline__ void note_broken(const AttendArgs& A, const Walk& walk, uint32_t broken, uint32_t first, uint32_t lane, uint32_t* noted) {
+#pragma unroll 1
+    for (uint32_t k = 0; k < kKeys / 32; ++k) {
+      const uint32_t groups = broken >> (4 * k) & 15;
+#pragma unroll 1
+      for (uint32_t those = __ballot_sync(0xFFFFFFFFu, groups); those; those &= those - 1) {
+        const uint32_t owner = __ffs(those) - 1, its = __shfl_sync(0xFFFFFFFFu, groups, owner), key = first + 32 * k + owner;
+#pragma unroll 1
+        for (uint32_t row = lane; row < kTileRows; row += 32) {
+          const uint32_t position = walk.q.first + min(A.by_shared.div(walk.block * kTileRows + row), walk.q.rows - 1);
+          if ((key <= position && (A.window == 0 || position - key < A.window)) || key < walk.q.prefix) atomicOr(noted + row / 8, its << (row % 8 * 4));
+        }
+        __syncwarp();
+      }
+    }
+  }
+
   static __device__ __forceinline__ void run(const AttendArgs& A) {
     extern __shared__ uint8_t raw[];
     __shared__ Shared S;
@@ -448,7 +468,7 @@ struct Kernel {
     begin_next();
 
     if (threadIdx.x == 0) {
-      S.dead = S.broken = 0;
+      S.dead = 0;
       for (uint32_t i = 0; i < kStages; ++i) {
         barrier_init(shared_address(&S.full_k[i]), kReaders);
         barrier_init(shared_address(&S.empty_k[i]), 2);
@@ -469,6 +489,8 @@ struct Kernel {
       }
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+
+    if (threadIdx.x < kMemo * (kTileRows / 8)) S.broken[threadIdx.x / (kTileRows / 8)][threadIdx.x % (kTileRows / 8)] = 0;
 
     // this CTA's share of the weight
     unsigned long long all = 0;
@@ -541,10 +563,10 @@ struct Kernel {
     if (warp < kSoftmaxWarps) {
       asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
       bool good = true;
-      while (good && walk.next(A)) {
+      for (uint32_t blocks = 0; good && walk.next(A); ++blocks) {
         const Sequence& q = walk.q;
         const Tiles& tiles = walk.tiles;
-        const uint32_t block = walk.block, head = walk.head, j0 = walk.j0, n = walk.n, s = walk.s;
+        const uint32_t block = walk.block, head = walk.head, j0 = walk.j0, n = walk.n;
         // ---- scores to probabilities: a query a thread
         const uint32_t t = warp / 4, row = threadIdx.x % kRows, r = block * kTileRows + t * kRows + row, token = A.by_shared.div(r), in_group = r - token * A.shared;
         const uint32_t lanes = tensor + ((warp & 3) * 32 << 16), scores = lanes + L::kScoresAt + t * kKeys, sums = lanes + L::kSumsAt + t * DP;
@@ -555,7 +577,6 @@ struct Kernel {
         const uint32_t low = __shfl_sync(0xFFFFFFFFu, position, 0), high = __shfl_sync(0xFFFFFFFFu, position, 31);
         float m = -INFINITY;
         Two l = two(0.0f, 0.0f);
-        uint32_t broken = 0;  // groups whose value is no number for this query
         load_queries(A, q, block * kTileRows + t * kRows, head, row, queries + t * L::kQueries, S.query_units + t * kRows);
         float own = fabsf(A.scale) * kLog2e;  // what the row's scores are multiplied by
         if constexpr (kBf16) {
@@ -650,17 +671,11 @@ struct Kernel {
         for (uint32_t h = 0; h < 2; ++h) good = good && warp_wait(shared_address(&S.sums[t][h]), (done + n - 1) & 1, dead);
         if (good) {
           order_after();
-          if (S.broken) {  // some value was no number: which of this block's are, and this query sees
-            for (uint32_t k = 0; k < n * kKeys; ++k) {
-              const uint32_t at_key = tiles.key(j0 + k / kKeys) + k % kKeys;
-              const bool visible = (at_key <= position && (A.window == 0 || position - at_key < A.window)) || at_key < q.prefix;
-              const uint32_t place = place_of_key(A, q, head, at_key, page_of(A, q, s, at_key));
-              if (place == kNone || !visible) continue;
-              for (uint32_t g = 0; g < A.groups; ++g)
-                if ((A.scales[A.plane_scales + (uint64_t)place * A.groups + g] & 0x7F80u) == 0x7F80u) broken |= 1u << g;
-            }
-            __syncwarp();
-          }
+          // noted by the warp that looks up values, ahead of those that the sums have waited for
+          uint32_t* const noted = &S.broken[blocks % kMemo][(t * kRows + row) / 8];
+          const uint32_t broken = *noted >> (row % 8 * 4) & 15;
+          __syncwarp();
+          if (row % 8 == 0) *noted = 0;
           const bool whole = j0 == 0 && n == tiles.count, there = token < q.rows;
           float* part = A.parts + (2ull * blockIdx.x + (walk.first ? 0 : 1)) * (kTilePartBytes / 4);
           T* out = static_cast<T*>(A.out) + (uint64_t)(q.row + min(token, q.rows - 1)) * A.out_row + (uint64_t)(head * A.shared + in_group) * A.out_head;
@@ -819,7 +834,7 @@ struct Kernel {
         const unsigned short* const scales = A.scales + (set ? A.plane_scales : 0);
         uint32_t value_unit = 0;  // the upper half of a float
         bool good = true;
-        while (good && walk.next(A)) {
+        for (uint32_t blocks = 0; good && walk.next(A); ++blocks) {
           for (uint32_t i = 0; i < walk.n; ++i) {
             const uint32_t x = done + i, slot = x % kFound;
             if (x >= kFound) good = warp_wait(shared_address(&S.found_empty[set][slot]), (x / kFound - 1) & 1, dead);
@@ -837,19 +852,30 @@ struct Kernel {
               for (uint32_t g = 0; g < 4; ++g)
                 if (place[k] != kNone && g < A.groups) all_scales[k][g] = __ldg(scales + (uint64_t)place[k] * A.groups + g);
             // the largest exponents, of 16 keys or of the tile, among scales that are numbers; values that are not count as 0
-            uint32_t unit[kKeys / 32];
+            constexpr uint32_t kExponent = 0x7F80u;
+            uint32_t unit[kKeys / 32], most = 0;
 #pragma unroll
             for (uint32_t k = 0; k < kKeys / 32; ++k) {
-              unit[k] = 0;
+              unit[k] = max(max(all_scales[k][0] & kExponent, all_scales[k][1] & kExponent), max(all_scales[k][2] & kExponent, all_scales[k][3] & kExponent));
+              most = max(most, unit[k]);
+            }
+            if (__any_sync(0xFFFFFFFFu, most == kExponent)) {  // some are no numbers
+              uint32_t broken = 0;  // four bits for each key's groups
+              most = 0;
 #pragma unroll
-              for (uint32_t g = 0; g < 4; ++g) {
-                const bool number = (all_scales[k][g] & 0x7F80u) != 0x7F80u;
-                if (set && !number) all_scales[k][g] = 0, S.broken = 1;
-                unit[k] = max(unit[k], number ? all_scales[k][g] & 0x7F80u : 0u);
+              for (uint32_t k = 0; k < kKeys / 32; ++k) {
+                unit[k] = 0;
+#pragma unroll
+                for (uint32_t g = 0; g < 4; ++g) {
+                  const bool number = (all_scales[k][g] & kExponent) != kExponent;
+                  if (set && !number) all_scales[k][g] = 0, broken |= 1u << (4 * k + g);
+                  unit[k] = max(unit[k], number ? all_scales[k][g] & kExponent : 0u);
+                }
+                most = max(most, unit[k]);
               }
+              if (set) note_broken(A, walk, broken, key - lane, lane, S.broken[blocks % kMemo]);
             }
             if (set) {
-              uint32_t most = max(max(unit[0], unit[1]), max(unit[2], unit[3]));
               most = min(max(__reduce_max_sync(0xFFFFFFFFu, most), 0x0100u), 0x7E00u);
               value_unit = i == 0 ? most : max(value_unit, most);
               if (lane == 0) S.value_units[x % kMemo] = __uint_as_float(value_unit << 16);

@@ -43,3 +43,15 @@ def test_later_tiles_units_are_written_ahead_of_their_scores(parts):
     assert int(re.search(r"constexpr uint32_t kAhead = (\d+);", text).group(1)) == 3  # found((i + 3) / 2) at odd i is the tile behind half i's
     lookup = parts["lookup"]
     assert lookup.index("S.value_units[") < lookup.index("barrier_arrive(shared_address(&S.found_full[set][slot]))")
+
+
+def test_the_warps_of_the_scores_look_nothing_up(parts):
+    # Which queries see values that are no numbers is noted by the warp that looks those up. (A walk through a block's keys by every thread of the scores, behind one
+    # such value, can take longer than the other warps wait for.) The notes are read once the sums are there, and no way that a warp takes as a whole hangs on them.
+    text = parts["scores"]
+    assert not re.search(r"\b(page_of|place_of_key)\(|A\.scales|A\.table", text)
+    read = [m.start() for m in re.finditer(r"S\.broken", text)]
+    assert len(read) == 1 and read[0] > text.index("warp_wait(shared_address(&S.sums[t][h]), (done + n - 1) & 1, dead)")
+    assert not re.search(r"if \([^)]*S\.broken", text)
+    lookup = parts["lookup"]
+    assert lookup.index("note_broken(") < lookup.index("barrier_arrive(shared_address(&S.found_full[set][slot]))")
