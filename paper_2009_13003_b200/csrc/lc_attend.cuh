@@ -85,6 +85,28 @@ __device__ __forceinline__ float reciprocal(float x) {
 }
 constexpr float kLog2e = 1.4426950408889634f;
 
+// Scores and the cap in units of base 2: cap * tanh(z / cap) of z. Where x = z / cap is small, the series x - x^3 / 3 + 2 x^5 / 15 - 17 x^7 / 315 + 62 x^9 / 2835 (what it
+// leaves out is below 2^-26 of x), elsewhere cap - 2 cap / (1 + e^2x), which is off by some 2^-22 of the cap: everywhere by no more than 2^-20 of the result.
+// (That form alone would lose small scores in the rounding of a large cap.)
+struct Cap {
+  float in, out;  // 2 x log2(e) = z * in; out: the cap
+  static constexpr float kSmall = 0.72f;  // of |2 x log2(e)|: |x| < 0.2496
+  __device__ __forceinline__ explicit Cap(float cap) : in(2.0f / cap), out(cap * kLog2e) {}
+  // The series in a^2, a = 2 x log2(e), i.e. x^2 = (ln(2) / 2)^2 a^2: what follows its leading 1, over a^2.
+  static constexpr float kUnit = 0.1201132535f, k1 = -kUnit / 3, k2 = 2 * kUnit * kUnit / 15, k3 = -17 * kUnit * kUnit * kUnit / 315, k4 = 62 * kUnit * kUnit * kUnit * kUnit / 2835;
+  __device__ __forceinline__ float operator()(float z) const {
+    const float a = z * in, b = a * a, series = b * fmaf(fmaf(fmaf(k4, b, k3), b, k2), b, k1);
+    return fabsf(a) < kSmall ? fmaf(z, series, z) : large(z);
+  }
+  __device__ __forceinline__ float large(float z) const { return fmaf(-2.0f * out, reciprocal(1.0f + exp2_fast(z * in)), out); }
+  // Two of them that are known to be small.
+  __device__ __forceinline__ Two small(Two z) const {
+    const Two a = mul_two(z, two(in, in)), b = mul_two(a, a);
+    const Two series = mul_two(b, fma_two(fma_two(fma_two(two(k4, k4), b, two(k3, k3)), b, two(k2, k2)), b, two(k1, k1)));
+    return fma_two(z, series, z);
+  }
+};
+
 constexpr uint64_t kPartBytes = 4ull * (kMaxColumns * 128 + 2 * kMaxColumns);  // of a partial result: 32 queries of 128 values, or 16 of 256
 
 constexpr uint32_t kTileCtas = 160;     // CTAs of the kernel for many rows, at most: one on each SM

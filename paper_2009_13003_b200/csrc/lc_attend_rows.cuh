@@ -243,7 +243,8 @@ struct Kernel {
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const uint32_t words = (A.dim + 31) / 32;  // blocks of 32 values that are there
     const uint32_t value_blocks = kWide ? (words + 1) & ~1u : words;
-    const float factor = kUnit * A.scale * kLog2e, cap_in = 2.0f / A.cap, cap_out = A.cap * kLog2e;
+    const float factor = kUnit * A.scale * kLog2e;
+    const Cap cap(A.cap);
     begin_next();
 
     // all tiles of the call, and where this CTA's begin
@@ -458,14 +459,8 @@ struct Kernel {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const uint32_t at_key = key + row + 16 * x + 8 * (e / 2), p = position[2 * c + (e & 1)];
-              float y = score[x][c][e];
-              if (A.cap > 0.0f) {
-                // cap * tanh(z / cap), z = score * scale
-                const float u = exp2_fast(y * factor * cap_in);
-                y = fmaf(-2.0f * cap_out, reciprocal(1.0f + u), cap_out);
-              } else {
-                y *= factor;
-              }
+              float y = score[x][c][e] * factor;
+              if (A.cap > 0.0f) y = cap(y);
               if (A.slopes) y = fmaf(-slope[2 * c + (e & 1)], fabsf((float)(int32_t)(p - at_key)), y);
               if (!full) {
                 const bool visible = (at_key <= p && (A.window == 0 || p - at_key < A.window)) || at_key < q.prefix;

@@ -35,6 +35,9 @@ constexpr uint32_t kFound = 4;                          // tiles whose keys have
 constexpr uint32_t kMemo = 8;                           // tiles whose units are kept: the scores of a tile are done before the keys of the seventh behind it are looked up (blocks have a tile or more)
 constexpr float kSlack = 8.0f;
 constexpr long long kWaitCycles = 4ll << 30;            // how long a barrier is waited for before the kernel gives up: some two seconds
+// Up to this cap the form for large scores is taken for all of them: it is off by 2^-22 of the cap, which moves a weight by no more than 2^-16, and they have 11 bits here. (2 x
+// 1024 rows behind up to 16384 keys, cap 3: 1031 us; with both forms and a choice for each score 1577. Where scores are far below their cap: the series alone, 890.)
+constexpr float kPlainCap = 64.0f;
 constexpr uint32_t kBlockCost = 320;                    // what a block costs beyond its keys, in keys
 
 // ---- barriers and tensor memory -----------------------------------------------------------------------------------
@@ -572,7 +575,7 @@ struct Kernel {
         const uint32_t lanes = tensor + ((warp & 3) * 32 << 16), scores = lanes + L::kScoresAt + t * kKeys, sums = lanes + L::kSumsAt + t * DP;
         const uint32_t position = q.first + min(token, q.rows - 1);
         const float slope = kBias ? A.slopes[head * A.shared + in_group] * kLog2e : 0.0f;
-        const float cap_out = A.cap * kLog2e;
+        const Cap cap(kCap ? A.cap : 1.0f);
         // positions of this warp's first and last query
         const uint32_t low = __shfl_sync(0xFFFFFFFFu, position, 0), high = __shfl_sync(0xFFFFFFFFu, position, 31);
         float m = -INFINITY;
@@ -605,11 +608,29 @@ struct Kernel {
           const bool full = key + kHalf - 1 <= low && (A.window == 0 || high - key < A.window);
           tensor_loaded(y);
           if constexpr (kCap || kBias) {
-            const float cap_in = kCap ? 2.0f / A.cap : 0.0f, away = (float)(int32_t)(position - key);
 #pragma unroll
-            for (uint32_t e = 0; e < kHalf; ++e) {
-              y[e] = kCap ? fmaf(-2.0f * cap_out, reciprocal(1.0f + exp2_fast(y[e] * factor[e / 16] * cap_in)), cap_out) : y[e] * factor[e / 16];
-              if constexpr (kBias) y[e] = fmaf(-slope, fabsf(away - (float)e), y[e]);
+            for (uint32_t e = 0; e < kHalf; ++e) y[e] *= factor[e / 16];
+            if constexpr (kCap) {
+              if (A.cap <= kPlainCap) {
+#pragma unroll
+                for (uint32_t e = 0; e < kHalf; ++e) y[e] = cap.large(y[e]);
+              } else {
+                float most = 0.0f;
+#pragma unroll
+                for (uint32_t e = 0; e < kHalf; ++e) most = fmaxf(most, fabsf(y[e]));
+                if (__all_sync(0xFFFFFFFFu, most * cap.in < Cap::kSmall)) {  // the same numbers as below
+#pragma unroll
+                  for (uint32_t e = 0; e < kHalf; e += 2) split_two(cap.small(two(y[e], y[e + 1])), y[e], y[e + 1]);
+                } else {
+#pragma unroll
+                  for (uint32_t e = 0; e < kHalf; ++e) y[e] = cap(y[e]);
+                }
+              }
+            }
+            if constexpr (kBias) {
+              const float away = (float)(int32_t)(position - key);
+#pragma unroll
+              for (uint32_t e = 0; e < kHalf; ++e) y[e] = fmaf(-slope, fabsf(away - (float)e), y[e]);
             }
           }
           if (!full) {
