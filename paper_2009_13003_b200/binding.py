@@ -913,8 +913,8 @@ def cache_attend(cache, q, table, page, begin, out=None, first=None, scale=None,
         raise LCError(ERR_ARG, "lc_cache_attend")
     if workspace is None:
         workspace = alloc_attend_workspace(cache, sequences)
-    elif workspace.dtype != torch.uint8 or workspace.get_device() != index:
-        raise ValueError("workspace must be uint8 on the cache's device")
+    else:
+        _whole(workspace, "workspace", torch.uint8, index)
     how = _attend(table.data_ptr(), table_strides[0], width, page, at, first_at, sequences, longest, heads, window, dim ** -0.5 if scale is None else scale, cap,
                   slopes_at, prefix_at)
     _call("lc_cache_attend", index, cache._at, _one_plane(q.data_ptr(), strides[0], strides[1]), _one_plane(out.data_ptr(), strides2[0], strides2[1]), kind, rows,
