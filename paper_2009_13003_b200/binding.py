@@ -742,6 +742,12 @@ def _whole(t, name, dtype, index):
     return t.data_ptr()
 
 
+def _fits(page, what):
+    """Refuses what would not arrive as it is in 32 bits; the library looks at the rest."""
+    if not 0 <= page < 1 << 32:
+        raise LCError(ERR_ARG, what)
+
+
 def _status(status, index):
     return None if status is None else _whole(status, "status", torch.int32, index)
 
@@ -791,6 +797,7 @@ def cache_read_pages(cache, table, page, begin, outs, first=None, status=None):
     at = _whole(begin, "begin", torch.int32, index)
     if begin.numel() != sequences + 1 or (first is not None and first.numel() != sequences):
         raise ValueError("begin has an entry per sequence and one more, first one per sequence")
+    _fits(page, "lc_cache_read_pages")
     _call("lc_cache_read_pages", index, cache._at, out, kind, rows, table.data_ptr(), table.stride(0), width, page, at,
           None if first is None else _whole(first, "first", torch.int32, index), sequences, _status(status, index))
     return outs
@@ -811,6 +818,7 @@ class Pages:
             _whole(t, name, torch.int32, index)
         if held.shape != table.shape[:1] or spare.dim() != 1 or count.numel() != 1:
             raise ValueError("held has an entry per sequence, spare one per page, count one")
+        _fits(page, "lc_cache_plan")
         self.table, self.held, self.spare, self.count, self.page = table, held, spare, count, page
         self.sequences, self.device, self._index = table.shape[0], table.device, index
         self._c = LCPages(table.data_ptr(), table.stride(0), held.data_ptr(), spare.data_ptr(), count.data_ptr(), table.shape[1], page, spare.numel())
@@ -909,7 +917,8 @@ def cache_attend(cache, q, table, page, begin, out=None, first=None, scale=None,
         slopes_at = _whole(slopes, "slopes", torch.float32, index)
         if slopes.numel() != heads:
             raise ValueError("slopes has an entry per head of q")
-    if not (0 <= window < 1 << 31 and 0 <= longest < 1 << 32 and 0 <= page < 1 << 32):
+    _fits(page, "lc_cache_attend")
+    if not (0 <= window < 1 << 31 and 0 <= longest < 1 << 32):
         raise LCError(ERR_ARG, "lc_cache_attend")
     if workspace is None:
         workspace = alloc_attend_workspace(cache, sequences)

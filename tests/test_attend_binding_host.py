@@ -42,3 +42,17 @@ def test_a_workspace_has_its_bytes_one_behind_the_other(reached):
         with pytest.raises(ValueError):
             attend(workspace=bad)
     assert reached == ["lc_cache_attend"]
+
+
+@pytest.mark.parametrize("page", [-1, (1 << 32) + 16, 1 << 32])
+def test_a_page_that_does_not_fit_into_32_bits_is_not_another_one(reached, page):
+    ints = lambda *shape: on(torch.zeros(shape, dtype=torch.int32))
+    with pytest.raises(binding.LCError):
+        binding.Pages(ints(3, 4), ints(3), ints(12), ints(1), page)
+    with pytest.raises(binding.LCError):
+        attend(page=page)
+    codes = on(torch.zeros(1, 32, 1, 64, dtype=torch.uint8))
+    cache = binding.Cache(codes, on(torch.zeros(1, 32, 1, 1, dtype=torch.bfloat16)), 64, 8, 64)
+    with pytest.raises(binding.LCError):
+        binding.cache_read_pages(cache, ints(1, 2), page, ints(2), [on(torch.zeros(2, 1, 64))])
+    assert reached == []
