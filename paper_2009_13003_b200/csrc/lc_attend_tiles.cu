@@ -11,8 +11,10 @@
 //
 // All products are of fp16 numbers, 11 bits, also for bf16 queries: a query's row is multiplied by the power of two that takes its largest value to [1, 2) (what
 // that loses lies 2^-25 below it), keys are in units of the power of two in the largest scale of 16 neighbours, values in units of that of the block's
-// values so far; where it rises the sums are scaled down. So no magnitude of them is out of the type, and what a code stands for is rounded once, to 11 bits or to
-// 2^-25 of the unit. Probabilities are held 2^7 times as large, up to 2^(7 + kSlack): next to its smallest numbers the type has few bits. (With keys, values and
+// values so far; where it rises the sums are scaled down. So no magnitude of them is out of the type, and what a code stands for is rounded once, to 11 bits. Where scales
+// differ by more than 2^14 that would not hold, and a key that a row does not see would take bits from those that it sees: there each key has a unit of its own, and what that lacks goes
+// to its score and, for its values, to its probability. (Such tiles go through a loop of their own; looking for them costs 2 %: chunks 639 -> 646 us, a prompt 888 -> 902.)
+// Probabilities are held 2^7 times as large, up to 2^(7 + kSlack): next to its smallest numbers the type has few bits. (With keys, values and
 // probabilities of bf16, 2 x 1024 rows behind up to 16384 keys took 602 us instead of 636, and the error was 0.0049 of the result instead of 0.0017, the result's own rounding.)
 // A value of NaN enters as 0, or rows that do not see it would get 0 * NaN; rows that do get their NaN at the end.
 //
@@ -27,7 +29,7 @@ constexpr uint32_t kRows = 128, kKeys = 128, kHalf = 64;  // of a tile of querie
 constexpr uint32_t kSoftmaxWarps = 8, kReadWarps = 4;   // kReadWarps each for keys and for values, then two that issue and two that look up
 constexpr uint32_t kThreads = 32 * (kSoftmaxWarps + 2 * kReadWarps + 4), kReaders = 32 * kReadWarps;
 // Registers of a thread: as launched, and what each warpgroup then has (together no more than before).
-constexpr uint32_t kRegsAtLaunch = 96, kRegsSoftmax = 152, kRegsReader = 64, kRegsIssue = 48;
+constexpr uint32_t kRegsAtLaunch = 96, kRegsSoftmax = 144, kRegsReader = 64, kRegsIssue = 64;
 static_assert(2 * kRegsSoftmax + 2 * kRegsReader + kRegsIssue <= 5 * kRegsAtLaunch && kThreads == 5 * 128, "registers of five warpgroups");
 constexpr uint32_t kStages = 3;                         // halves of a tile of keys, and of values, as operands
 constexpr uint32_t kAhead = 3;                          // halves whose codes are on their way
@@ -123,6 +125,10 @@ __device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t (&x)[16
 }
 __device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t (&x)[32]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]), "r"(x[9]), "r"(x[10]), "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15]), "r"(x[16]), "r"(x[17]), "r"(x[18]), "r"(x[19]), "r"(x[20]), "r"(x[21]), "r"(x[22]), "r"(x[23]), "r"(x[24]), "r"(x[25]), "r"(x[26]), "r"(x[27]), "r"(x[28]), "r"(x[29]), "r"(x[30]), "r"(x[31]), "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t (&x)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(at)
                : "memory");
 }
 __device__ __forceinline__ void tensor_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -278,8 +284,10 @@ struct Shared {
   uint32_t found, tensor, dead;
   uint2 scales[2][kFound][kKeys];          // for the readers of keys and of values: a key's scales in fp16, two in a word
   uint32_t places[2][kFound][kKeys];       // slot * heads + head, which is below 2^32 in this kernel; kNone
-  float units[kMemo][kKeys / 16];          // the powers of two that 16 keys each are in units of
-  float value_units[kMemo];                // that a tile's values are in units of
+  // The powers of two that 16 keys each are in units of, and that a tile's values are in units of; below 0 where each key, or each key's values, is in units of a power
+  // of its own, whose exponents (of fp32) then stand beside.
+  float units[kMemo][kKeys / 16], value_units[kMemo];
+  alignas(16) uint8_t exponents[2][kMemo][kKeys];
   float query_units[kTileRows];
   uint32_t broken[kMemo][kTileRows / 8];   // for the queries of a block, four bits each: groups of which they see a value that is no number
 };
@@ -586,12 +594,15 @@ struct Kernel {
           asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + t), "n"(kRows) : "memory");
           own *= S.query_units[t * kRows + row];
         }
-        float value_unit = 1.0f;  // of the sums
+        float value_unit = 1.0f;  // of the sums; by_exponent: its exponent as it stands in fp32, then no whole number
+        bool by_exponent = false;
         order_for_products();
         order_before();  // the sums of the block before are read
         barrier_arrive(shared_address(&S.queries[t]));
         good = false;  // all tiles are through
-        for (uint32_t i = 0; i < 2 * n; ++i) {
+        uint32_t i = 0;
+        bool apart = false;
+        for (; i < 2 * n; ++i) {
           const uint32_t number = done + i / 2, half = i & 1, key = tiles.key(j0 + i / 2) + half * kHalf, at = scores + half * kHalf;
           if (!warp_wait(shared_address(&S.scores[t][half]), number & 1, dead)) break;
           // What is looked up of a tile's values (their unit) comes another way than its scores. Behind a block's first tile it is there: scores of a half wait for the
@@ -601,7 +612,12 @@ struct Kernel {
           order_after();
           float y[kHalf];
           tensor_load(at, y);
-          const float tile_unit = S.value_units[number % kMemo];
+          const float tile_unit = S.value_units[number % kMemo], first_unit = S.units[number % kMemo][half * 4];
+          if (fminf(tile_unit, first_unit) < 0.0f) {
+            tensor_loaded(y);
+            apart = true;
+            break;
+          }
           float factor[kHalf / 16];  // of 16 keys each; not 0, or a key that is not seen, -Inf, times that would be no number
 #pragma unroll
           for (uint32_t c = 0; c < kHalf / 16; ++c) factor[c] = fmaxf(own * S.units[number % kMemo][half * 4 + c], 1e-37f);
@@ -689,6 +705,80 @@ struct Kernel {
           barrier_arrive(shared_address(&S.weights[t][half]));
           good = i + 1 == 2 * n;
         }
+        // From the first tile on whose keys, or their values, have units of their own (see the warps that look them up): the same with fewer registers, 16 scores at a time, each
+        // read as often as it is needed. A value's power of two goes to its probability: with m and e_k the base and the exponents, sums are of 2^(y_k - m + e_k - d), and in units
+        // of 2^d, where d grows with the largest that the query has seen. (A loop of its own: as a way through the one above it took that 6 % of its time.)
+        if (apart) {
+          for (; i < 2 * n; ++i) {
+            const uint32_t number = done + i / 2, half = i & 1, key = tiles.key(j0 + i / 2) + half * kHalf, at = scores + half * kHalf, memo = number % kMemo;
+            if (!warp_wait(shared_address(&S.scores[t][half]), number & 1, dead)) break;
+            order_after();
+            const float tile_unit = S.value_units[memo];
+            const bool keys_apart = S.units[memo][0] < 0.0f, values_apart = tile_unit < 0.0f;
+            auto scores_of = [&](uint32_t c, float (&y)[16]) {  // 16 of them from c on
+              uint32_t x[16];
+              tensor_load(at + c, x);
+              const int32_t end = (int32_t)(position - key - c) + 1, begin = A.window ? end - (int32_t)A.window : 0, prefix = (int32_t)(q.prefix - key - c);
+              const uint32_t seen = (bits_below(end) & ~bits_below(begin)) | bits_below(prefix);
+              const float away = (float)(int32_t)(position - key - c);
+#pragma unroll
+              for (uint32_t e = 0; e < 16; ++e) {
+                const float unit = keys_apart ? __uint_as_float((uint32_t)S.exponents[0][memo][half * kHalf + c + e] << 23) : S.units[memo][half * 4 + c / 16];
+                y[e] = __fmul_rn(__uint_as_float(x[e]), own * unit);
+                if constexpr (kCap) y[e] = A.cap <= kPlainCap ? cap.large(y[e]) : cap(y[e]);
+                if constexpr (kBias) y[e] = fmaf(-slope, fabsf(away - (float)e), y[e]);
+                if (!(seen >> e & 1)) y[e] = -INFINITY;
+              }
+            };
+            auto exponent_of = [&](uint32_t k) { return (float)(values_apart ? (uint32_t)S.exponents[1][memo][half * kHalf + k] : __float_as_uint(tile_unit) >> 23); };
+            float y[16], now = m;
+#pragma unroll 1
+            for (uint32_t c = 0; c < kHalf; c += 16) {
+              scores_of(c, y);
+#pragma unroll
+              for (uint32_t e = 0; e < 16; ++e) now = fmaxf(now, y[e]);
+            }
+            const float base = now == -INFINITY ? 0.0f : now, down = m == now ? 1.0f : exp2_fast(m - now);
+            const float before = m == -INFINITY ? -1e4f : (by_exponent ? value_unit : (float)(__float_as_uint(value_unit) >> 23)) + (m - now);
+            float d = values_apart ? before : exponent_of(0);
+            if (values_apart) {
+#pragma unroll 1
+              for (uint32_t c = 0; c < kHalf; c += 16) {
+                scores_of(c, y);
+#pragma unroll
+                for (uint32_t e = 0; e < 16; ++e) d = fmaxf(d, y[e] - base + exponent_of(c + e));
+              }
+            }
+            const float sums_down = exp2_fast(before - d);
+            if (i > 0 && __any_sync(0xFFFFFFFFu, sums_down != 1.0f)) {
+              if (!warp_wait(shared_address(&S.sums[t][1 - half]), (done + (i - 1) / 2) & 1, dead)) break;
+              order_after();
+#pragma unroll 1
+              for (uint32_t c = 0; c < DP; c += 16) scale_sums(sums + c, sums_down);
+            }
+            m = now;
+            l = mul_two(l, two(down, down));
+            by_exponent = values_apart;
+            value_unit = values_apart ? d : tile_unit;
+#pragma unroll 1
+            for (uint32_t c = 0; c < kHalf; c += 16) {
+              scores_of(c, y);
+              uint32_t p[8];
+#pragma unroll
+              for (uint32_t e = 0; e < 16; e += 2) {
+                y[e] -= base, y[e + 1] -= base;
+                l = add_two(l, two(exp2_fast(y[e] + kLift), exp2_fast(y[e + 1] + kLift)));
+                p[e / 2] = rounded<false>(exp2_fast(y[e] + (exponent_of(c + e) - d + kLift)), exp2_fast(y[e + 1] + (exponent_of(c + e + 1) - d + kLift)));
+              }
+              __syncwarp();
+              tensor_store(at + c / 2, p);  // over scores that have been read
+            }
+            tensor_stored();
+            order_before();
+            barrier_arrive(shared_address(&S.weights[t][half]));
+            good = i + 1 == 2 * n;
+          }
+        }
         for (uint32_t h = 0; h < 2; ++h) good = good && warp_wait(shared_address(&S.sums[t][h]), (done + n - 1) & 1, dead);
         if (good) {
           order_after();
@@ -704,6 +794,7 @@ struct Kernel {
           float sum, other;
           split_two(l, sum, other);
           sum += other;
+          if (by_exponent) value_unit = exp2_fast(value_unit - 127.0f);
           const float over = whole ? value_unit / sum : value_unit;
           const uint32_t shift = 5 + (A.per_group > 1) + (A.per_group > 2);  // values of a group
 #pragma unroll 1
@@ -853,8 +944,8 @@ struct Kernel {
         // ---- where keys lie, and their scales: a warp for the readers of keys, one for those of values
         const uint32_t set = warp - (kSoftmaxWarps + 2 * kReadWarps + 2);
         const unsigned short* const scales = A.scales + (set ? A.plane_scales : 0);
-        uint32_t value_unit = 0;  // the upper half of a float
-        bool good = true;
+        uint32_t value_unit = 0;  // the upper half of a float, 0 while there are only zeros
+        bool good = true, apart = false;
         for (uint32_t blocks = 0; good && walk.next(A); ++blocks) {
           for (uint32_t i = 0; i < walk.n; ++i) {
             const uint32_t x = done + i, slot = x % kFound;
@@ -872,51 +963,77 @@ struct Kernel {
 #pragma unroll
               for (uint32_t g = 0; g < 4; ++g)
                 if (place[k] != kNone && g < A.groups) all_scales[k][g] = __ldg(scales + (uint64_t)place[k] * A.groups + g);
-            // the largest exponents, of 16 keys or of the tile, among scales that are numbers; values that are not count as 0
+            // the largest exponents, of a key, and of 16 keys or of the tile, among scales that are numbers; values that are not count as 0
             constexpr uint32_t kExponent = 0x7F80u;
-            uint32_t unit[kKeys / 32], most = 0;
+            const bool more = A.groups > 2;
+            uint32_t own[kKeys / 32], several[kKeys / 32], most = 0, least = ~0u;  // least: of the scales less 1, so that a 0 does not count
 #pragma unroll
             for (uint32_t k = 0; k < kKeys / 32; ++k) {
-              unit[k] = max(max(all_scales[k][0] & kExponent, all_scales[k][1] & kExponent), max(all_scales[k][2] & kExponent, all_scales[k][3] & kExponent));
-              most = max(most, unit[k]);
+              own[k] = max(all_scales[k][0], all_scales[k][1]);
+              least = min(least, min(all_scales[k][0] - 1, all_scales[k][1] - 1));
+              if (more) {
+                own[k] = max(own[k], max(all_scales[k][2], all_scales[k][3]));
+                least = min(least, min(all_scales[k][2] - 1, all_scales[k][3] - 1));
+              }
+              most = max(most, own[k]);
             }
-            if (__any_sync(0xFFFFFFFFu, most == kExponent)) {  // some are no numbers
+            if (__any_sync(0xFFFFFFFFu, most >= kExponent)) {  // some are no numbers, or below 0
               uint32_t broken = 0;  // four bits for each key's groups
               most = 0;
 #pragma unroll
               for (uint32_t k = 0; k < kKeys / 32; ++k) {
-                unit[k] = 0;
+                own[k] = 0;
 #pragma unroll
                 for (uint32_t g = 0; g < 4; ++g) {
                   const bool number = (all_scales[k][g] & kExponent) != kExponent;
                   if (set && !number) all_scales[k][g] = 0, broken |= 1u << (4 * k + g);
-                  unit[k] = max(unit[k], number ? all_scales[k][g] & kExponent : 0u);
+                  own[k] = max(own[k], number ? all_scales[k][g] & kExponent : 0u);
                 }
-                most = max(most, unit[k]);
+                most = max(most, own[k]);
               }
               if (set) note_broken(A, walk, broken, key - lane, lane, S.broken[blocks % kMemo]);
             }
+            auto in_range = [](uint32_t x) { return min(max(x & kExponent, 0x0100u), 0x7E00u); };
+            // A unit for several keys will do while every scale is above 2^-14 of it: in fp16 it keeps its bits then, and its products with codes 11 (and sums do not lose
+            // theirs where the unit rises). Else each key has its own, or what one row sees would cost another row bits of what it sees.
+            constexpr uint32_t kTogether = 14 << 7;
             if (set) {
-              most = min(max(__reduce_max_sync(0xFFFFFFFFu, most), 0x0100u), 0x7E00u);
+              most = __reduce_max_sync(0xFFFFFFFFu, most) & kExponent;
+              apart = i > 0 && (apart || (value_unit > 0 && most > value_unit + kTogether));  // for the rest of the block
               value_unit = i == 0 ? most : max(value_unit, most);
-              if (lane == 0) S.value_units[x % kMemo] = __uint_as_float(value_unit << 16);
+              most = in_range(value_unit);
 #pragma unroll
-              for (uint32_t k = 0; k < kKeys / 32; ++k) unit[k] = value_unit;
+              for (uint32_t k = 0; k < kKeys / 32; ++k) several[k] = most;
             } else {
+              apart = false;
+              uint32_t two[2] = {own[0] | own[1] << 16, own[2] | own[3] << 16};
+#pragma unroll
+              for (int d = 8; d; d >>= 1) two[0] = __vmaxu2(two[0], __shfl_xor_sync(0xFFFFFFFFu, two[0], d)), two[1] = __vmaxu2(two[1], __shfl_xor_sync(0xFFFFFFFFu, two[1], d));
+#pragma unroll
+              for (uint32_t k = 0; k < kKeys / 32; ++k) several[k] = in_range(two[k / 2] >> (16 * (k & 1)));
+              most = max(max(several[0], several[1]), max(several[2], several[3]));
+            }
+            apart = __any_sync(0xFFFFFFFFu, apart || (least < kExponent && least + kTogether < most));
+            if (apart) {
 #pragma unroll
               for (uint32_t k = 0; k < kKeys / 32; ++k) {
-#pragma unroll
-                for (int d = 8; d; d >>= 1) unit[k] = max(unit[k], __shfl_xor_sync(0xFFFFFFFFu, unit[k], d));
-                unit[k] = min(max(unit[k], 0x0100u), 0x7E00u);
-                if (lane % 16 == 0) S.units[x % kMemo][2 * k + lane / 16] = __uint_as_float(unit[k] << 16);
+                several[k] = in_range(own[k]);
+                S.exponents[set][x % kMemo][lane + 32 * k] = (uint8_t)(several[k] >> 7);
               }
+            }
+            if (set) {
+              if (lane == 0) S.value_units[x % kMemo] = apart ? -1.0f : __uint_as_float(most << 16);
+            } else if (lane % 16 == 0) {
+#pragma unroll
+              for (uint32_t k = 0; k < kKeys / 32; ++k) S.units[x % kMemo][2 * k + lane / 16] = apart ? -1.0f : __uint_as_float(several[k] << 16);
             }
 #pragma unroll
             for (uint32_t k = 0; k < kKeys / 32; ++k) {
-              const float down = __uint_as_float((0x7F00u - unit[k]) << 16);
-              float y[4];
+              const float down = __uint_as_float((0x7F00u - several[k]) << 16);
+              float y[4] = {};
 #pragma unroll
-              for (uint32_t g = 0; g < 4; ++g) y[g] = __uint_as_float(all_scales[k][g] << 16) * down;
+              for (uint32_t g = 0; g < 4; ++g)
+                if (g < 2 || more) y[g] = __uint_as_float(all_scales[k][g] << 16) * down;
               S.scales[set][slot][lane + 32 * k] = make_uint2(rounded<false>(y[0], y[1]), rounded<false>(y[2], y[3]));
               S.places[set][slot][lane + 32 * k] = place[k];
             }

@@ -12,7 +12,9 @@ A score is off by what its key's rounding and its sums in fp32 do. With u = 2^-1
 
 Weights and values, relative to sum p |v|: weights have 11 bits where `many`, else what the rows' type has twice over (bf16 8 bits, fp16 16, fp32 24); values of 8-bit codes 11 where
 `many`. Sums over n keys in fp32, 16 at a time: n 2^-27 of sum p |v|, and n 2^-25 of the output for the sum that divides. Small weights in fp16, 2^7 times as large as the largest is at least, are on a grid
-of 2^-24: off by 2^-32 for every |v| that is seen. The result's own rounding comes last.
+of 2^-24: off by 2^-32 for every |v| that is seen. (`apart`: where scales differ by 2^14 and more, weights take the power of two that a key's values have beside the row's
+largest weighted ones, so that 2^-32 is of those: with codes of at most c, and a scale's power of two in half a scale at least, off by 2^-31 of max_k p_k |v_k| for every key.)
+A key that may move its own weight by e^20 makes a row's bound infinite. The result's own rounding comes last.
 
 Where all those roundings are independent of each other the mean square is known too: a number rounded to half a step h of itself at most is off by h^2 / 3 in the mean at most. (A score in fp32
 is summed 16 products at a time, those of fp32 queries in three parts, and each of these 3 dim / 16 sums is off by 2^-23 of sum |q k| at most. Of fp32 rows that is the most of it.)
@@ -33,7 +35,7 @@ HALF_STEP = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11, torch.float32
 U = 2.0 ** -11
 
 
-def attend(kind, bits, many, q, k, v, positions, scale, cap=0.0, slopes=None, window=0, prefix=0):
+def attend(kind, bits, many, q, k, v, positions, scale, cap=0.0, slopes=None, window=0, prefix=0, apart=False):
     """One sequence (as in attend_reference.attend): out, how far off it may be, and its mean square."""
     n, heads, dim = q.shape
     length, shared = k.shape[0], heads // k.shape[1]
@@ -59,7 +61,9 @@ def attend(kind, bits, many, q, k, v, positions, scale, cap=0.0, slopes=None, wi
         if slopes is not None:
             t = t - slopes[h].double() * away.abs()
             d = d + 2.0 ** -22 * slopes[h].double().abs() * away.abs()
-        d = (d + 2.0 ** -22 * t.abs()).clamp(max=20.0)
+        d = d + 2.0 ** -22 * t.abs()
+        wild = (seen & (d > 20.0)).any(-1)
+        d = d.clamp(max=20.0)
         t = t.masked_fill(~seen, -torch.inf)
         p = torch.where(seen, torch.exp(t - t.amax(-1, keepdim=True)), 0.0)
         p = p / p.sum(-1, keepdim=True)
@@ -70,6 +74,9 @@ def attend(kind, bits, many, q, k, v, positions, scale, cap=0.0, slopes=None, wi
         off += (weight + key + length * 2.0 ** -27 + 2.0 ** -20) * size + length * 2.0 ** -25 * o.abs()
         if many:
             off += 2.0 ** -32 * seen.double() @ vv.abs()
+        if many and apart:
+            off += 2.0 ** -31 * (p * vv.abs().amax(-1)).amax(-1, keepdim=True) * seen.sum(-1, keepdim=True)
+        off = off.masked_fill(wild[:, None], torch.inf)
         allowed[:, h] = 1.01 * (off + HALF_STEP[kind] * (o.abs() + off)) + (2.0 ** -24 if kind == torch.float16 else 1e-30)
         spread = p ** 2 * ((key * scale) ** 2 / 3 * (qq ** 2 @ (kk ** 2).T) + steps * (2.0 ** -23 * products) ** 2)
         square[:, h] = spread @ vv ** 2 - 2 * o * (spread @ vv) + o ** 2 * spread.sum(-1, keepdim=True)

@@ -20,7 +20,7 @@ def test_a_tiles_units_are_read_behind_the_wait_for_its_values(parts):
     # The warps that look up values write them ahead of found_full, which the readers of values wait for ahead of full_v. A block's first scores depend on its
     # keys alone, so the warps of the scores wait for full_v themselves.
     text = parts["scores"]
-    loop = text.index("for (uint32_t i = 0; i < 2 * n; ++i) {")
+    loop = text.index("; i < 2 * n; ++i) {")
     scores, read = text.index("warp_wait(shared_address(&S.scores[t][half])", loop), text.index("S.value_units[", loop)
     wait = re.search(r"if \(i == 0 && !warp_wait\(shared_address\(&S\.full_v\[2 \* done % kStages\]\), 2 \* done / kStages & 1, dead\)\) break;", text[scores:read])
     assert wait

@@ -30,7 +30,7 @@ class Close(Case):
     def call(self, lc, **kw):  # noqa: F811
         return super().call(lc, scale=self.scale, **kw)
 
-    def check(self, lc, got, mean=True, prefix=None, **kw):  # noqa: F811
+    def check(self, lc, got, mean=True, apart=False, prefix=None, **kw):  # noqa: F811
         held, cache = values(self.cache), self.cache
         off2, allowed2 = 0.0, 0.0
         for s, (first, n) in enumerate(zip(self.firsts, self.counts)):
@@ -39,10 +39,11 @@ class Close(Case):
             mine, place, shared = slice(int(self.begin[s]), int(self.begin[s]) + n), self.places(s), self.q.shape[1] // cache.heads
             many = self.kind != torch.float32 and cache.dim <= 128 and n > 16 // shared
             out, allowed, square = bounds.attend(self.kind, cache.bits, many, self.q[mine].double(), held[0][place], held[1][place], first + torch.arange(n, device=DEV), self.scale,
-                                                 prefix=0 if prefix is None else int(prefix[s]), **kw)
+                                                 prefix=0 if prefix is None else int(prefix[s]), apart=apart, **kw)
             off = (got[mine].double() - out).abs()
             if self.kind == torch.float16:  # what is beyond the type's numbers may be Inf
                 off = torch.where(out.abs() + allowed < 65504.0, off, 0.0)
+            off = torch.where(allowed.isinf(), 0.0, off)
             assert bool((off <= allowed).all()), (s, float((off / allowed).max()), int((off > allowed).sum()), off.numel())
             off2, allowed2 = off2 + float((off ** 2).sum()), allowed2 + float(square.sum())
         assert lc.last_status(self.status) == lc.OK
