@@ -14,7 +14,7 @@
 // for N * 2^-133 (subnormals, and the first binade above, in the same steps). Queries of more than 8 bits enter as the bf16 parts that they
 // are the sum of: fp16 two, fp32 three. A group's scale meets the key's sums in fp32, and the value's scale the probability ahead of its
 // rounding to as many parts; so nothing of the cache is rounded, and a scale's magnitude, NaN in a key that a query does not
-// see, or a type's range cost nothing. Probabilities of bf16 queries have 8 bits, of fp16 16, of fp32 24; sums are fp32.
+// see, or a type's range cost nothing (up to sums of values beyond fp32's range). Probabilities of bf16 queries have 8 bits, of fp16 16, of fp32 24; sums are fp32.
 #pragma once
 
 #include "lc_attend.cuh"
@@ -629,7 +629,7 @@ struct Kernel {
           float sum = 0.0f;
 #pragma unroll
           for (uint32_t w = 0; w < kWarps; ++w) sum += sums[w][column];
-          from_float(v * kUnit / sum, static_cast<T*>(A.out)[(uint64_t)(q.row + token) * A.out_row + (uint64_t)(head * A.shared + (r - token * A.shared)) * A.out_head + d]);
+          from_float(v * (kUnit / sum), static_cast<T*>(A.out)[(uint64_t)(q.row + token) * A.out_row + (uint64_t)(head * A.shared + (r - token * A.shared)) * A.out_head + d]);
         } else {
           part_out[x] = v;
         }

@@ -795,7 +795,7 @@ struct Kernel {
           split_two(l, sum, other);
           sum += other;
           if (by_exponent) value_unit = exp2_fast(value_unit - 127.0f);
-          const float over = whole ? value_unit / sum : value_unit;
+          const float over = sum == 0.0f ? 0.0f : value_unit / sum;  // a part is a mean too, that of the keys that it has: its sums in fp32 may be beyond the type
           const uint32_t shift = 5 + (A.per_group > 1) + (A.per_group > 2);  // values of a group
 #pragma unroll 1
           for (uint32_t c = 0; c < A.dim; c += 32) {
@@ -1092,7 +1092,7 @@ __global__ void __launch_bounds__(kTileRows) join_tiles_kernel(AttendArgs A, uin
     const uint32_t j0 = from > begin ? tile_at(from - begin, tiles.count, P.weight) : 0, j1 = to < end ? tile_at(to - begin, tiles.count, P.weight) : tiles.count;
     return j0 == j1 || (j0 == 0 && j1 == tiles.count) ? nullptr : A.parts + (2ull * cta + (begin <= from ? 0 : 1)) * (kTilePartBytes / 4);
   };
-  float most = -INFINITY, sum = 0.0f, v[16] = {};
+  float most = -INFINITY, sum = 0.0f, v[16] = {};  // v: the mean over the parts so far
   uint32_t parts = 0;
   const uint32_t d0 = blockIdx.y * 16;
   for (uint32_t c = first; c <= last; ++c) {
@@ -1102,28 +1102,27 @@ __global__ void __launch_bounds__(kTileRows) join_tiles_kernel(AttendArgs A, uin
     float4 x[4];
 #pragma unroll
     for (uint32_t e = 0; e < 4; ++e) x[e] = d0 + 4 * e < A.dim ? *reinterpret_cast<const float4*>(p + ((d0 / 4 + e) * kTileRows + threadIdx.x) * 4) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    const float old = most == now ? 1.0f : exp2_fast(most - now), here = m == now ? 1.0f : exp2_fast(m - now);
-    sum = sum * old + l * here;
+    const float old = most == now ? sum : sum * exp2_fast(most - now), added = m == now ? l : l * exp2_fast(m - now);
+    sum = old + added;
+    const float over = sum == 0.0f ? 0.0f : 1.0f / sum, keeps = old * over, here = added * over;
 #pragma unroll
     for (uint32_t e = 0; e < 4; ++e) {
-      v[4 * e] = v[4 * e] * old + x[e].x * here, v[4 * e + 1] = v[4 * e + 1] * old + x[e].y * here;
-      v[4 * e + 2] = v[4 * e + 2] * old + x[e].z * here, v[4 * e + 3] = v[4 * e + 3] * old + x[e].w * here;
+      v[4 * e] = v[4 * e] * keeps + x[e].x * here, v[4 * e + 1] = v[4 * e + 1] * keeps + x[e].y * here;
+      v[4 * e + 2] = v[4 * e + 2] * keeps + x[e].z * here, v[4 * e + 3] = v[4 * e + 3] * keeps + x[e].w * here;
     }
     most = now;
     ++parts;
   }
   if (parts == 0) return;  // one CTA has had them all
   T* out = static_cast<T*>(A.out) + (uint64_t)(q.row + token) * A.out_row + (uint64_t)(P.head * A.shared + (r - token * A.shared)) * A.out_head + d0;
-  const float over = 1.0f / sum;
   if (d0 + 16 <= A.dim && (reinterpret_cast<uintptr_t>(out) & 15) == 0) {
 #pragma unroll
     for (uint32_t e = 0; e < 16; e += 8)
-      *reinterpret_cast<uint4*>(out + e) = make_uint4(rounded<kBf16>(v[e] * over, v[e + 1] * over), rounded<kBf16>(v[e + 2] * over, v[e + 3] * over),
-                                                      rounded<kBf16>(v[e + 4] * over, v[e + 5] * over), rounded<kBf16>(v[e + 6] * over, v[e + 7] * over));
+      *reinterpret_cast<uint4*>(out + e) = make_uint4(rounded<kBf16>(v[e], v[e + 1]), rounded<kBf16>(v[e + 2], v[e + 3]), rounded<kBf16>(v[e + 4], v[e + 5]), rounded<kBf16>(v[e + 6], v[e + 7]));
   } else {
 #pragma unroll
     for (uint32_t e = 0; e < 16; ++e)
-      if (d0 + e < A.dim) from_float(v[e] * over, out[e]);
+      if (d0 + e < A.dim) from_float(v[e], out[e]);
   }
 }
 
