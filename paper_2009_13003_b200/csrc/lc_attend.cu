@@ -6,7 +6,9 @@ namespace {
 
 uint64_t flat_bytes(uint64_t sequences) { return (8 * (sequences + 1) + 255) / 256 * 256; }
 
-// Queries of a sequence for one head of the cache up to which the kernel for few rows takes it.
+// Queries of a sequence for one head of the cache up to which the kernel for few rows takes it. The other one multiplies blocks of 256, full or not. 24 sequences of up to 8192
+// keys, 8 heads in 8 bits (in 4), 20, 32, 64 queries for each, few rows / many, us: dim 128 301 / 212, 332 / 212, 634 / 212 (255 / 210, 292 / 210, 559 / 208); dim 64 156 / 198, 173 / 196,
+// 315 / 194 (151 / 197, 169 / 195, 309 / 194). One limit for both dims: that of dim 128.
 constexpr uint32_t kFewQueries = 16;
 
 constexpr float kLargest = 1e30f;  // of scale and cap: what is made of them stays in fp32's range

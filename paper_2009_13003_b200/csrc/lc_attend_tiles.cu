@@ -292,6 +292,8 @@ struct Shared {
   uint32_t broken[kMemo][kTileRows / 8];   // for the queries of a block, four bits each: groups of which they see a value that is no number
 };
 
+static_assert(sizeof(Shared) + Layout<8, 128>::kWhole <= 232448, "a CTA's shared memory");
+
 // kCap, kBias: scores are capped, lowered by distance.
 template <int kBits, uint32_t DP, bool kBf16, bool kCap, bool kBias>
 struct Kernel {
