@@ -870,7 +870,7 @@ def cache_plan(pages, tokens, rows=None, plan=None, status=None) -> Plan:
 
 
 def alloc_attend_workspace(cache, sequences) -> torch.Tensor:
-    """A workspace for cache_attend of up to ``sequences`` sequences."""
+    """A workspace for cache_attend of up to ``sequences`` sequences: some 62 MB, whatever their lengths. A program keeps one for each of its streams."""
     size = int(lib().lc_cache_attend_bytes(cache._c, sequences))
     if size == 0:
         raise LCError(ERR_ARG, "lc_cache_attend_bytes")

@@ -15,7 +15,7 @@
 // differ by more than 2^14 that would not hold, and a key that a row does not see would take bits from those that it sees: there each key has a unit of its own, and what that lacks goes
 // to its score and, for its values, to its probability. (Such tiles go through a loop of their own; looking for them costs 2 %: chunks 639 -> 646 us, a prompt 888 -> 902.)
 // Probabilities are held 2^7 times as large, up to 2^(7 + kSlack): next to its smallest numbers the type has few bits. (With keys, values and
-// probabilities of bf16, 2 x 1024 rows behind up to 16384 keys took 602 us instead of 636, and the error was 0.0049 of the result instead of 0.0017, the result's own rounding.)
+// probabilities of bf16, 2 x 1024 rows behind up to 16384 keys took 602 us instead of 638, and the error was 0.0049 of the result instead of 0.0017, the result's own rounding.)
 // A value of NaN enters as 0, or rows that do not see it would get 0 * NaN; rows that do get their NaN at the end.
 //
 // Blocks differ in how many keys they see. Each weighs about as many as it does and a block's own cost; a CTA gets an equal share of the weight, and
@@ -40,7 +40,7 @@ constexpr long long kWaitCycles = 4ll << 30;            // how long a barrier is
 // Up to this cap the form for large scores is taken for all of them: it is off by 2^-22 of the cap, which moves a weight by no more than 2^-16, and they have 11 bits here. (2 x
 // 1024 rows behind up to 16384 keys, cap 3: 1031 us; with both forms and a choice for each score 1577. Where scores are far below their cap: the series alone, 890.)
 constexpr float kPlainCap = 64.0f;
-constexpr uint32_t kBlockCost = 320;                    // what a block costs beyond its keys, in keys
+constexpr uint32_t kBlockCost = 320;                    // what a block costs beyond its keys, in keys: fitted to a prompt of 8192 (with 192 its first CTA took twice as long as the others)
 
 // ---- barriers and tensor memory -----------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
