@@ -797,7 +797,8 @@ struct Kernel {
           split_two(l, sum, other);
           sum += other;
           if (by_exponent) value_unit = exp2_fast(value_unit - 127.0f);
-          const float over = sum == 0.0f ? 0.0f : value_unit / sum;  // a part is a mean too, that of the keys that it has: its sums in fp32 may be beyond the type
+          // A part is a mean too, that of the keys that it has: its sums may be beyond fp32. (Its queries may see none of them. Of a whole block's a sum is 0 only if all scores are -Inf.)
+          const float over = !whole && sum == 0.0f ? 0.0f : value_unit / sum;
           const uint32_t shift = 5 + (A.per_group > 1) + (A.per_group > 2);  // values of a group
 #pragma unroll 1
           for (uint32_t c = 0; c < A.dim; c += 32) {
@@ -1116,6 +1117,10 @@ __global__ void __launch_bounds__(kTileRows) join_tiles_kernel(AttendArgs A, uin
     ++parts;
   }
   if (parts == 0) return;  // one CTA has had them all
+  if (sum == 0.0f) {  // all scores are -Inf
+#pragma unroll
+    for (uint32_t e = 0; e < 16; ++e) v[e] = __uint_as_float(0x7FFFFFFFu);
+  }
   T* out = static_cast<T*>(A.out) + (uint64_t)(q.row + token) * A.out_row + (uint64_t)(P.head * A.shared + (r - token * A.shared)) * A.out_head + d0;
   if (d0 + 16 <= A.dim && (reinterpret_cast<uintptr_t>(out) & 15) == 0) {
 #pragma unroll

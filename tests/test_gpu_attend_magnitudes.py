@@ -52,3 +52,17 @@ def test_the_largest_score_has_it_all(lc, kind, counts, dim, scale):  # noqa: F8
             told += int(clear.sum())
     assert told >= sum(counts)  # an eighth of them
     assert lc.last_status(case.status) == lc.OK
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("firsts,counts", [([60], [1]), ([300], [200]), ([9000], [130])])
+def test_scores_that_are_all_minus_infinity(lc, kind, firsts, counts):  # noqa: F811
+    """0 / 0 in the formula, and no number here, by either kernel, in blocks that one CTA has and in those that several share."""
+    case = Close(lc, kind, 8, 64, 1, 4, 64, 16, firsts, counts, seed=1)
+    ones = torch.ones(case.cache.slots, 1, 64, device=DEV)
+    lc.cache_write(case.cache, ones, values(case.cache)[1].float(), torch.arange(case.cache.slots, device=DEV))
+    case.cache.scales[0] *= 2.0 ** 100
+    case.q.fill_(-1.0)
+    case.scale = 1e25
+    n = counts[0]
+    assert bool(case.call(lc)[:n].isnan().all())
