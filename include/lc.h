@@ -493,10 +493,11 @@ int lc_cache_plan(const lc_pages* pages, const int32_t* tokens, uint32_t sequenc
  * workspace  DEVICE, 256-byte aligned, lc_cache_attend_bytes (0 on bad arguments; the number of slots does not matter); two calls that overlap in time
  *            need two. scales of the cache are on 4 bytes here.
  * Scores, sums and what they are divided by are fp32 (values beyond 2^120 may sum to Inf, and a row may be no number where scale times its query times a key of its
- * sequence is beyond fp32); a cap moves a score by 2^-20 of itself or less (rows of bf16 and fp16, caps up to 64: by 2^-16 or less). Rows of bf16 and of fp16 round probabilities to 8 and 11 bits or more (some: those below 2^-21 of a row's largest to multiples of 2^-31 of it, and so, where
- * scales differ by 2^14 and more, products of probabilities and values), and may round keys and values to 11 bits, or to 2^-25 of the largest of their position and head where
- * that is less; bf16 queries to 2^-25 of that of their row. fp32 rounds none of these. What a row does not see takes no bits from it, however large it is, and an Inf or NaN
- * there changes none. A step that does not end (LC_ERR_TIMEOUT) shows in the status word. The same inputs give the same bits.
+ * sequence is beyond fp32); a cap moves a score by 2^-20 of itself or less (rows of bf16 and fp16, caps up to 64: by 2^-16 or less). Rows of bf16 and of fp16 round
+ * probabilities to 8 and 11 bits or more (some: those below 2^-21 of a row's largest to multiples of 2^-31 of it, and so, where scales differ by 2^14 and more,
+ * products of probabilities and values), and may round keys and values to 11 bits, or to 2^-25 of the largest of their position and head where that is less; bf16
+ * queries to 2^-25 of that of their row. fp32 rounds none of these. What a row does not see takes no bits from it, however large it is, and an Inf or NaN there changes
+ * none. A step that does not end (LC_ERR_TIMEOUT) shows in the status word. The same inputs give the same bits.
  */
 typedef struct lc_attend {
   const int32_t* table;
